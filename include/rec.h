@@ -61,7 +61,8 @@ typedef enum {
     REC_ERR_INDEX_RANGE = 5, /* device: a row id outside [0, rows)               */
     REC_ERR_OVERFLOW = 6,    /* a count does not fit the 32-bit index math       */
     REC_ERR_DEVICE = 7,      /* a HIP call failed                                */
-    REC_ERR_CAPACITY = 8     /* rec_forward_static(): call exceeds the static scratch */
+    REC_ERR_CAPACITY = 8,    /* rec_forward_static(): call exceeds the static scratch */
+    REC_ERR_VALUE = 9        /* device: a NaN or an infinity on its way into a cache (rec_history.h) */
 } rec_status;
 
 typedef enum { REC_F32 = 0, REC_F16 = 1 } rec_dtype;

@@ -1,7 +1,7 @@
-"""ctypes binding of the C boundary declared in include/rec.h.
+"""ctypes binding of the C boundary declared in include/rec.h and include/rec_history.h.
 
-Argument marshalling only: every step of the forward pass runs in the HIP
-library.  PyTorch supplies device memory and the stream.  Importing this
+Argument marshalling only: every step of the forward pass, and of attention over
+user histories, runs in the HIP library.  PyTorch supplies device memory and the stream.  Importing this
 module raises if the library has not been built; there is no fallback.
 """
 from __future__ import annotations
@@ -28,9 +28,12 @@ _F32, _I32 = torch.float32, torch.int32
 REC_OK = 0
 REC_ERR_ARG, REC_ERR_SHAPE, REC_ERR_STATE, REC_ERR_LENGTHS = 1, 2, 3, 4
 REC_ERR_INDEX_RANGE, REC_ERR_OVERFLOW, REC_ERR_DEVICE, REC_ERR_CAPACITY = 5, 6, 7, 8
+REC_ERR_VALUE = 9
 REC_STATIC_SCRATCH_BYTES = 64 << 20
 REC_STATIC_MAX_TABLES = 64
-REC_F32, REC_F16 = 0, 1
+REC_F32, REC_F16, REC_BF16 = 0, 1, 2
+REC_MX4, REC_MX8 = 0, 1
+REC_FAULT_LENGTH, REC_FAULT_SLOT, REC_FAULT_PAGE, REC_FAULT_VALUE, REC_FAULT_WORDS = 0, 1, 2, 3, 4
 REC_BOTTOM, REC_TOP = 0, 1          # REC_TOP + k: tower k of the Predict-FC
 REC_INTERACT_DOT, REC_INTERACT_CONCAT = 0, 1
 REC_MAX_TOWERS = 8
@@ -51,7 +54,9 @@ EXPORTS = ("rec_create", "rec_destroy", "rec_workspace_bytes", "rec_bind_workspa
            "rec_load_tables", "rec_load_hot_rows", "rec_mlp_packed_bytes", "rec_load_mlp", "rec_forward", "rec_forward_static", "rec_check",
            "rec_debug_get", "rec_set_option", "rec_set_dense_stream", "rec_set_pool_streams", "rec_drain", "rec_set_profiling", "rec_stage_ms", "rec_stage_shared", "rec_status_string",
            "rec_synth_fill_table", "rec_probe_mfma", "rec_probe_scan", "rec_probe_fc_form", "rec_probe_plan",
-           "rec_probe_plan_joined", "rec_probe_plan_pooling", "rec_probe_dense_copy")
+           "rec_probe_plan_joined", "rec_probe_plan_pooling", "rec_probe_dense_copy",
+           "rec_history_bytes", "rec_history_write", "rec_history_read", "rec_history_attend_workspace_bytes",
+           "rec_history_attend", "rec_window_attend", "rec_history_check")
 
 
 class rec_config(C.Structure):
@@ -61,6 +66,30 @@ class rec_config(C.Structure):
                 ("bottom_widths", C.POINTER(C.c_int32)), ("n_top", C.c_int32),
                 ("top_widths", C.POINTER(C.c_int32)), ("max_batch", C.c_int32),
                 ("max_nnz", C.c_int64), ("interaction", C.c_int32), ("num_towers", C.c_int32)]
+
+
+class rec_history(C.Structure):
+    _fields_ = [("dev_pages", C.c_void_p), ("num_pages", C.c_int64), ("page_tokens", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("format", C.c_int32), ("dev_fault", C.c_void_p)]
+
+
+class rec_rows(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class rec_query(C.Structure):
+    _fields_ = [("dev_q", C.c_void_p), ("dev_out", C.c_void_p), ("batch_stride", C.c_int64),
+                ("query_stride", C.c_int64), ("head_stride", C.c_int64), ("dtype", C.c_int32), ("batch", C.c_int32),
+                ("queries", C.c_int32), ("heads", C.c_int32), ("dev_pages_of", C.c_void_p), ("table_stride", C.c_int64),
+                ("table_width", C.c_int32), ("dev_lengths", C.c_void_p), ("scale", C.c_float), ("window", C.c_int32),
+                ("sinks", C.c_int32), ("candidates", C.c_int32)]
+
+
+class rec_window(C.Structure):
+    _fields_ = [("q", rec_rows), ("k", rec_rows), ("v", rec_rows), ("dev_out", C.c_void_p), ("dtype", C.c_int32),
+                ("batch", C.c_int32), ("tokens", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dev_offsets", C.c_void_p), ("scale", C.c_float), ("window", C.c_int32),
+                ("sinks", C.c_int32), ("dev_fault", C.c_void_p)]
 
 
 _vp = C.c_void_p
@@ -122,6 +151,21 @@ _lib.rec_probe_dense_copy.restype = C.c_int
 _lib.rec_probe_dense_copy.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
 _lib.rec_probe_fc_form.restype = C.c_int
 _lib.rec_probe_fc_form.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_uint32, C.c_int32, C.POINTER(C.c_int32)]
+
+_lib.rec_history_bytes.restype = C.c_size_t
+_lib.rec_history_bytes.argtypes = [C.POINTER(rec_history)]
+_lib.rec_history_write.restype = C.c_int
+_lib.rec_history_write.argtypes = [C.POINTER(rec_history), C.POINTER(rec_rows), C.POINTER(rec_rows), C.c_int32, _vp, C.c_int64, _vp]
+_lib.rec_history_read.restype = C.c_int
+_lib.rec_history_read.argtypes = [C.POINTER(rec_history), _vp, C.c_int64, C.c_int32, _vp, _vp, _vp]
+_lib.rec_history_attend_workspace_bytes.restype = C.c_size_t
+_lib.rec_history_attend_workspace_bytes.argtypes = [C.POINTER(rec_history), C.POINTER(rec_query)]
+_lib.rec_history_attend.restype = C.c_int
+_lib.rec_history_attend.argtypes = [C.POINTER(rec_history), C.POINTER(rec_query), _vp, C.c_size_t, _vp]
+_lib.rec_window_attend.restype = C.c_int
+_lib.rec_window_attend.argtypes = [C.POINTER(rec_window), _vp]
+_lib.rec_history_check.restype = C.c_int
+_lib.rec_history_check.argtypes = [_vp, _vp, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
 
 
 class RecError(RuntimeError):
@@ -304,6 +348,39 @@ def rec_probe_dense_copy(rows: int, columns: int, pad: int, left: int = -1) -> T
     deal = (C.c_int32 * 3)()
     st = _lib.rec_probe_dense_copy(int(rows), int(columns), int(pad), int(left), deal)
     return st, *deal
+
+
+# User histories: same names, structures by reference.
+def rec_history_bytes(h: rec_history) -> int:
+    return int(_lib.rec_history_bytes(C.byref(h)))
+
+
+def rec_history_write(h: rec_history, k: rec_rows, v: rec_rows, dtype: int, dev_slots, tokens: int) -> int:
+    return _lib.rec_history_write(C.byref(h), C.byref(k), C.byref(v), int(dtype), _ptr(dev_slots), int(tokens), _stream())
+
+
+def rec_history_read(h: rec_history, dev_slots, tokens: int, dtype: int, dev_k, dev_v) -> int:
+    return _lib.rec_history_read(C.byref(h), _ptr(dev_slots), int(tokens), int(dtype), _ptr(dev_k), _ptr(dev_v), _stream())
+
+
+def rec_history_attend_workspace_bytes(h: rec_history, q: rec_query) -> int:
+    return int(_lib.rec_history_attend_workspace_bytes(C.byref(h), C.byref(q)))
+
+
+def rec_history_attend(h: rec_history, q: rec_query, workspace=None) -> int:
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _lib.rec_history_attend(C.byref(h), C.byref(q), _ptr(workspace), nbytes, _stream())
+
+
+def rec_window_attend(w: rec_window) -> int:
+    return _lib.rec_window_attend(C.byref(w), _stream())
+
+
+def rec_history_check(dev_fault: torch.Tensor) -> Tuple[int, int, int]:
+    """(status, position, REC_FAULT_* word); the last two -1 without a fault."""
+    pos, word = C.c_int64(-1), C.c_int32(-1)
+    st = _lib.rec_history_check(_ptr(dev_fault), _stream(), C.byref(pos), C.byref(word))
+    return st, pos.value, word.value
 
 
 class RecModel:
@@ -501,3 +578,147 @@ class CapturedForward:
 
     def replay(self) -> None:
         self.graph.replay()
+
+
+_DTYPE_CODES = {torch.float32: REC_F32, torch.float16: REC_F16, torch.bfloat16: REC_BF16}
+_ATTEND_CODES = {torch.float16: REC_F16, torch.bfloat16: REC_BF16}
+_FORMATS = {"mx4": REC_MX4, "mx8": REC_MX8}
+
+
+def _faults(device) -> torch.Tensor:
+    return torch.full((REC_FAULT_WORDS,), -1, dtype=torch.int64, device=device)
+
+
+def _check_int32(call: str, name: str, t: torch.Tensor, shape, device) -> None:
+    if t.dtype is not _I32 or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{call}: {name} must be a contiguous int32 tensor of shape {tuple(shape)} on {device}")
+
+
+class HistoryCache:
+    """Keys and values of user histories in 4 or 8 bits a number (include/rec_history.h), and
+    attention over them.
+
+    The pages are one uint8 tensor, the cache's own or the caller's (`pages`, of
+    [num_pages, kv_heads, page_tokens / 16, bytes of a group]); which page holds what is the
+    caller's bookkeeping.  Calls go to the current stream and only enqueue."""
+
+    def __init__(self, num_pages: int, page_tokens: int, kv_heads: int, head_dim: int, fmt: str = "mx4",
+                 device: str = "cuda:0", pages: Optional[torch.Tensor] = None):
+        if fmt not in _FORMATS:
+            raise ValueError(f"HistoryCache: format must be one of {sorted(_FORMATS)}, not {fmt!r}")
+        self.page_tokens, self.kv_heads, self.head_dim, self.fmt = page_tokens, kv_heads, head_dim, fmt
+        self._h = rec_history(None, num_pages, page_tokens, kv_heads, head_dim, _FORMATS[fmt], None)
+        nbytes = rec_history_bytes(self._h)
+        if nbytes == 0:
+            raise RecError(REC_ERR_SHAPE, "HistoryCache")
+        if pages is None:
+            if not torch.cuda.is_available():
+                raise RuntimeError("no GPU visible: a history cache has no CPU path")
+            shape = (num_pages, kv_heads, page_tokens // 16, nbytes // (num_pages * kv_heads * (page_tokens // 16)))
+            pages = torch.empty(shape, dtype=torch.uint8, device=device)
+        elif not (pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous() and pages.numel() == nbytes):
+            raise ValueError(f"HistoryCache: pages must be a contiguous uint8 device tensor of {nbytes} bytes")
+        self.pages, self.device = pages, pages.device
+        self.fault = _faults(self.device)
+        self._h.dev_pages, self._h.dev_fault = pages.data_ptr(), self.fault.data_ptr()
+        self._k, self._v, self._q = rec_rows(), rec_rows(), rec_query()
+
+    def _ok(self, st: int, where: str) -> None:
+        if st != REC_OK:
+            raise RecError(st, where)
+
+    def _slots(self, call: str, slots: torch.Tensor) -> int:
+        if slots.dtype is not torch.int64 or slots.device != self.device or slots.dim() != 1 or not slots.is_contiguous():
+            raise ValueError(f"{call}: slots must be a contiguous int64 vector on {self.device}")
+        return slots.shape[0]
+
+    def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+        """k, v: [tokens, kv_heads, head_dim] (any token and head strides), fp32, fp16 or bf16;
+        slots: int64 [tokens], page * page_tokens + place, -1 for a row to leave out."""
+        n = self._slots("rec_history_write", slots)
+        shape = (n, self.kv_heads, self.head_dim)
+        for t, r in ((k, self._k), (v, self._v)):
+            if t.shape != shape or t.dtype not in _DTYPE_CODES or t.dtype is not k.dtype or t.device != self.device or t.stride(2) != 1:
+                raise ValueError(f"rec_history_write: k and v must be {shape} on {self.device}, of one floating type, rows contiguous")
+            r.dev, (r.token_stride, r.head_stride, _) = t.data_ptr(), t.stride()
+        st = rec_history_write(self._h, self._k, self._v, _DTYPE_CODES[k.dtype], slots, n)
+        if st:
+            self._ok(st, "rec_history_write")
+
+    def read(self, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Keys and values of `slots` as [tokens, kv_heads, head_dim]; zeros for slot -1."""
+        n = self._slots("rec_history_read", slots)
+        if dtype not in _DTYPE_CODES:
+            raise ValueError(f"rec_history_read: unsupported type {dtype}")
+        shape = (n, self.kv_heads, self.head_dim)
+        k, v = torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device)
+        st = rec_history_read(self._h, slots, n, _DTYPE_CODES[dtype], k, v)
+        if st:
+            self._ok(st, "rec_history_read")
+        return k, v
+
+    def attend(self, q: torch.Tensor, pages_of: torch.Tensor, lengths: torch.Tensor, scale: Optional[float] = None,
+               window: int = 0, sinks: int = 0, candidates: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """q: [batch, queries, heads, head_dim] or, one query each, [batch, heads, head_dim], fp16 or bf16
+        (any strides but the last); pages_of: int32 [batch, width], a history's pages in order; lengths:
+        int32 [batch].  scale: 1 / sqrt(head_dim) if None.  Returns attention outputs of q's shape, contiguous."""
+        q4 = q if q.dim() == 4 else q.unsqueeze(1)
+        batch, queries, heads, dim = q4.shape
+        if dim != self.head_dim or q.dtype not in _ATTEND_CODES or q.device != self.device or q4.stride(3) != 1:
+            raise ValueError(f"rec_history_attend: q must be fp16 or bf16 [batch, queries, heads, {self.head_dim}] on "
+                             f"{self.device}, rows contiguous")
+        if pages_of.dim() != 2 or pages_of.dtype is not _I32 or pages_of.device != self.device or pages_of.shape[0] != batch \
+                or pages_of.stride(1) != 1:
+            raise ValueError(f"rec_history_attend: pages_of must be int32 [{batch}, width] on {self.device}, rows contiguous")
+        _check_int32("rec_history_attend", "lengths", lengths, (batch,), self.device)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        elif out.shape != q.shape or out.dtype is not q.dtype or out.device != self.device or not out.is_contiguous():
+            raise ValueError("rec_history_attend: out must be contiguous and of q's shape, type and device")
+        r = self._q
+        r.dev_q, r.dev_out = q.data_ptr(), out.data_ptr()
+        r.batch_stride, r.query_stride, r.head_stride, _ = q4.stride()
+        r.dtype, r.batch, r.queries, r.heads = _ATTEND_CODES[q.dtype], batch, queries, heads
+        r.dev_pages_of, r.table_stride, r.table_width = pages_of.data_ptr(), pages_of.stride(0), pages_of.shape[1]
+        r.dev_lengths, r.scale = lengths.data_ptr(), dim ** -0.5 if scale is None else scale
+        r.window, r.sinks, r.candidates = window, sinks, bool(candidates)
+        need = rec_history_attend_workspace_bytes(self._h, r)
+        workspace = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        st = rec_history_attend(self._h, r, workspace)
+        if st:
+            self._ok(st, "rec_history_attend")
+        return out
+
+    def check(self) -> Tuple[int, int, int]:
+        """Waits; (status, position, REC_FAULT_* word) of the first fault since the last check."""
+        return rec_history_check(self.fault)
+
+
+def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, scale: Optional[float] = None,
+                  window: int = 0, sinks: int = 0, fault: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Whole histories attend to themselves (rec_window_attend()).  q: [tokens, heads, head_dim], k and v:
+    [tokens, kv_heads, head_dim], fp16 or bf16, any token and head strides; offsets: int32 [batch + 1].
+    fault: int64 [REC_FAULT_WORDS], all -1, for rec_history_check(), or None."""
+    device = q.device
+    tokens, heads, dim = q.shape
+    for t in (q, k, v):
+        if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != dim or t.dtype is not q.dtype or t.dtype not in _ATTEND_CODES \
+                or t.device != device or not t.is_cuda or t.stride(2) != 1:
+            raise ValueError("rec_window_attend: q, k and v must be device tensors [tokens, heads, head_dim] of one type, fp16 or "
+                             "bf16, rows contiguous")
+    if k.shape != v.shape:
+        raise ValueError("rec_window_attend: k and v must have the same shape")
+    if offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("rec_window_attend: offsets must have batch + 1 entries")
+    _check_int32("rec_window_attend", "offsets", offsets, offsets.shape, device)
+    if fault is not None and (fault.dtype is not torch.int64 or fault.device != device or fault.numel() < REC_FAULT_WORDS):
+        raise ValueError(f"rec_window_attend: fault must be int64 [{REC_FAULT_WORDS}] on {device}")
+    out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=device)
+    w = rec_window(rec_rows(q.data_ptr(), q.stride(0), q.stride(1)), rec_rows(k.data_ptr(), k.stride(0), k.stride(1)),
+                   rec_rows(v.data_ptr(), v.stride(0), v.stride(1)), out.data_ptr(), _ATTEND_CODES[q.dtype],
+                   offsets.shape[0] - 1, tokens, heads, k.shape[1], dim, offsets.data_ptr(),
+                   dim ** -0.5 if scale is None else scale, window, sinks, _ptr(fault))
+    st = rec_window_attend(w)
+    if st != REC_OK:
+        raise RecError(st, "rec_window_attend")
+    return out

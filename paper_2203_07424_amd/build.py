@@ -12,7 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librec_mi355x.so")
 
-SOURCES = ["scan.hip", "pool.hip", "pool_hot.hip", "gemm.hip", "gemm_big.hip", "gemm_split.hip", "mlp_chain.hip", "tail.hip", "front.hip", "lookup.hip", "interact.hip", "synth_fill.hip", "probe.hip", "rec_api.hip"]
+SOURCES = ["scan.hip", "pool.hip", "pool_hot.hip", "gemm.hip", "gemm_big.hip", "gemm_split.hip", "mlp_chain.hip", "tail.hip", "front.hip", "lookup.hip", "interact.hip", "synth_fill.hip", "probe.hip", "rec_api.hip",
+           "history_cache.hip", "history_attend.hip", "window_attend.hip", "history_api.hip"]
 
 # The packed-fp32 target feature is switched off for all device code.  A wave starts
 # with the first 16 words of its kernel's arguments in registers instead of loading
@@ -41,7 +42,7 @@ def _compile(src: str, force: bool, sanitize: bool = False) -> str:
     o = os.path.join(OBJ_SAN if sanitize else OBJ, src + ".o")
     deps = [s, *(os.path.join(CSRC, h) for h in sorted(os.listdir(CSRC)) if h.endswith(".h")),
             os.path.join(ROOT, "include", "rec.h"),
-            os.path.join(ROOT, "include", "rec_synth.h"), os.path.join(ROOT, "include", "rec_probe.h"),
+            os.path.join(ROOT, "include", "rec_synth.h"), os.path.join(ROOT, "include", "rec_probe.h"), os.path.join(ROOT, "include", "rec_history.h"),
             os.path.abspath(__file__)]
     if not force and os.path.exists(o) and all(os.path.getmtime(o) >= os.path.getmtime(d) for d in deps):
         return o

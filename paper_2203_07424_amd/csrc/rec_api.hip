@@ -895,6 +895,7 @@ const char *rec_status_string(int status)
     case REC_ERR_OVERFLOW: return "count exceeds 32-bit index range";
     case REC_ERR_DEVICE: return "HIP call failed";
     case REC_ERR_CAPACITY: return "call needs more scratch than the static array holds";
+    case REC_ERR_VALUE: return "NaN or infinity in a row to be stored";
     }
     return "unknown status";
 }

@@ -1,0 +1,467 @@
+"""User histories on the device: the compressed cache and attention, against 64-bit oracles."""
+import numpy as np
+import pytest
+import torch
+
+import history_oracle as O
+
+pytestmark = pytest.mark.gpu
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2203_07424_amd import binding
+    return binding
+
+
+@pytest.fixture(autouse=True)
+def say(request):
+    print(request.node.name, flush=True)
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def new_cache(b, pages, page_tokens, kv, d, fmt, fill=255):
+    """A cache whose unwritten places hold `fill` (255: NaN scales, NaN codes)."""
+    c = b.HistoryCache(pages, page_tokens, kv, d, fmt)
+    c.pages.fill_(fill)
+    return c
+
+
+def stored(c, fmt, d, page_tokens, slots, heads):
+    """Oracle's reading of the pages' bytes: K, V float64 [n, heads, d]."""
+    raw = c.pages.cpu().numpy()
+    rows = [[O.row_of(raw, fmt, d, page_tokens, s, h) for h in range(heads)] for s in slots]
+    return tuple(np.array([[r[i] for r in per] for per in rows]) for i in range(2))
+
+
+# ------------------------------------------------------------------ write and read
+def tricky(n, kv, d, dtype, seed):
+    """Values on and next to rounding ties, powers of two, zeros, wide ranges inside a block."""
+    g = gen(seed)
+    x = torch.randn(n, kv, d, generator=g)
+    kind = torch.arange(n) % 6
+    x[kind == 1] *= torch.exp2(torch.randint(-20, 12, (int((kind == 1).sum()), kv, d), generator=g).float())
+    x[kind == 2] = torch.randint(-64, 65, (int((kind == 2).sum()), kv, d), generator=g).float() / 8      # ties
+    x[kind == 3] = 0.0
+    x[kind == 4] *= 1000.0
+    x[kind == 5] *= 1e-5
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("d,kv,page_tokens,dtype", [(32, 1, 16, F32), (64, 3, 32, BF), (128, 2, 256, HF), (64, 1, 64, F32), (32, 5, 128, BF), (128, 1, 16, F32)])
+def test_written_rows_have_the_nearest_values(b, fmt, d, kv, page_tokens, dtype):
+    n, pages = 61, 8
+    c = new_cache(b, pages, page_tokens, kv, d, fmt)
+    k, v = tricky(n, kv, d, dtype, 1), tricky(n, kv, d, dtype, 2)
+    slots = torch.randperm(pages * page_tokens, generator=gen(3))[:n]
+    before = c.pages.clone()
+    c.write(k.cuda(), v.cuda(), slots.cuda())
+    assert c.check() == (b.REC_OK, -1, -1)
+    got_k, got_v = stored(c, fmt, d, page_tokens, slots.tolist(), kv)
+    for x, got in ((k, got_k), (v, got_v)):
+        codes, scales = O.quantise(x.double().numpy().reshape(-1, 32), fmt)
+        want = O.values(codes, fmt) * O.scale_values(scales)[:, None]
+        assert np.array_equal(got.reshape(-1, 32), want)
+    # nothing else was touched: writing the same rows again over other bytes leaves those
+    c.pages.fill_(0xA5)
+    c.write(k.cuda(), v.cuda(), slots.cuda())
+    changed_once, changed_twice = (before != 0xA5), (c.pages != 0xA5)
+    per = n * kv * (d * (17 if fmt == "mx4" else 33) // 16)
+    assert int(changed_twice.sum()) <= per and changed_once.all()
+    for out in (F32, BF, HF):
+        rk, rv = c.read(slots.cuda(), out)
+        for r, got in ((rk, got_k), (rv, got_v)):
+            want = torch.from_numpy(got).to(out)         # exact, or the rounding of the type
+            assert torch.equal(r.cpu(), want)
+
+
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("start,n,page_tokens", [(0, 64, 32), (0, 80, 16), (5, 70, 32), (16, 37, 64), (31, 100, 256), (0, 1, 16), (15, 2, 16)])
+def test_runs_of_consecutive_slots(b, fmt, start, n, page_tokens):
+    """Whole groups and parts of groups, with pages in any order; read back over the same runs and others."""
+    d, kv = 64, 2
+    per = -(-(start + n) // page_tokens)
+    c = new_cache(b, per + 3, page_tokens, kv, d, fmt)
+    order = torch.randperm(per + 3, generator=gen(n))[:per]
+    at = torch.arange(start, start + n)
+    slots = order[at // page_tokens] * page_tokens + at % page_tokens
+    k, v = tricky(n, kv, d, BF, 5), tricky(n, kv, d, BF, 6)
+    c.write(k.cuda(), v.cuda(), slots.cuda())
+    want_k, want_v = (O.values(*(lambda cs: (cs[0], fmt))(O.quantise(x.double().numpy().reshape(-1, 32), fmt)))
+                      * O.scale_values(O.quantise(x.double().numpy().reshape(-1, 32), fmt)[1])[:, None] for x in (k, v))
+    got_k, got_v = stored(c, fmt, d, page_tokens, slots.tolist(), kv)
+    assert np.array_equal(got_k.reshape(-1, 32), want_k) and np.array_equal(got_v.reshape(-1, 32), want_v)
+    for pick in (slice(None), slice(1, None), slice(None, None, 2)):
+        rk, rv = c.read(slots[pick].contiguous().cuda(), F32)
+        assert torch.equal(rk.cpu().double(), torch.from_numpy(got_k[pick])) and torch.equal(rv.cpu().double(), torch.from_numpy(got_v[pick]))
+
+
+def test_strided_rows_and_padding_slots(b):
+    d, kv, n = 64, 2, 40
+    whole = torch.randn(n, 9, d, generator=gen(9)).to(BF).cuda()
+    k, v = whole[:, 2:4], whole[:, 5:9:2]
+    slots = torch.arange(n)
+    slots[::7] = -1
+    c, e = new_cache(b, 3, 16, kv, d, "mx4"), new_cache(b, 3, 16, kv, d, "mx4")
+    c.write(k, v, slots.cuda())
+    e.write(k.contiguous(), v.contiguous(), slots.cuda())
+    assert torch.equal(c.pages, e.pages) and c.check()[0] == b.REC_OK
+    rk, rv = c.read(slots.cuda(), F32)
+    assert not rk[::7].any() and not rv[::7].any() and bool(rk[1:7].any())
+
+
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+def test_ends_of_the_range(b, fmt):
+    """The largest and smallest fp32, and blocks with NaN and infinities."""
+    d, n = 32, 8
+    x = torch.zeros(n, 1, d)
+    x[0, 0, :4] = torch.tensor([3.4028234e38, -3.4e38, 1e38, 1.0])
+    x[1, 0, :3] = torch.tensor([1e-38, -1e-40, 1e-45])
+    x[2, 0, 5] = float("nan")
+    x[3, 0, 31] = float("inf")
+    x[4, 0, 0] = float("-inf")
+    x[5] = -0.0
+    x[6, 0, :3] = torch.tensor([2.0 ** -108, 2.0 ** -111, 2.0 ** -112])
+    x[7, 0, :2] = torch.tensor([1.75, -1.8125]) * 2.0 ** 126
+    c = new_cache(b, 1, 16, 1, d, fmt, fill=0)
+    c.write(x.cuda(), x.flip(0).contiguous().cuda(), torch.arange(n).cuda())
+    assert c.check() == (b.REC_ERR_VALUE, 2, b.REC_FAULT_VALUE)
+    assert c.check() == (b.REC_OK, -1, -1)
+    rk, rv = c.read(torch.arange(n).cuda(), F32)
+    codes, scales = O.quantise(x.double().numpy().reshape(-1, 32), fmt)
+    want = torch.from_numpy(O.values(codes, fmt) * O.scale_values(scales)[:, None]).view(n, 1, d)
+    assert torch.equal(torch.nan_to_num(rk.cpu().double(), nan=7.0), torch.nan_to_num(want, nan=7.0))
+    assert torch.equal(torch.nan_to_num(rv.cpu().double(), nan=7.0), torch.nan_to_num(want.flip(0), nan=7.0))
+    assert bool(torch.isfinite(rk[0]).all()) and bool(rk[2:5].isnan().all())
+
+
+def test_slots_outside_the_cache_are_reported_and_left_out(b):
+    c = new_cache(b, 2, 16, 2, 32, "mx8", fill=0)
+    k = torch.randn(6, 2, 32, generator=gen(1)).cuda()
+    slots = torch.tensor([3, 32, -2, -1, 2 ** 40, 31]).cuda()
+    c.write(k, k, slots)
+    assert c.check() == (b.REC_ERR_INDEX_RANGE, 1, b.REC_FAULT_SLOT)
+    rk, rv = c.read(slots, F32)
+    assert c.check() == (b.REC_ERR_INDEX_RANGE, 1, b.REC_FAULT_SLOT)
+    assert not rk[1:5].any() and not rv[1:5].any() and bool(rk[0].any()) and bool(rk[5].any())
+    assert int((c.pages != 0).sum()) <= 2 * 2 * 66
+
+
+def test_empty_calls(b):
+    c = new_cache(b, 2, 16, 2, 32, "mx4")
+    none = torch.empty(0, 2, 32, dtype=BF, device="cuda")
+    c.write(none, none, torch.empty(0, dtype=torch.int64, device="cuda"))
+    k, v = c.read(torch.empty(0, dtype=torch.int64, device="cuda"))
+    assert k.shape == (0, 2, 32)
+    out = c.attend(torch.empty(0, 4, 32, dtype=BF, device="cuda"), torch.empty(0, 3, dtype=torch.int32, device="cuda"),
+                   torch.empty(0, dtype=torch.int32, device="cuda"))
+    assert out.shape == (0, 4, 32)
+    x = torch.empty(0, 2, 64, dtype=HF, device="cuda")
+    assert b.attend_window(x, x, x, torch.zeros(3, dtype=torch.int32, device="cuda")).shape == (0, 2, 64)
+
+
+# ------------------------------------------------------------------- attention, cached
+class Histories:
+    """Random histories in a cache whose other places hold NaN."""
+
+    def __init__(self, b, lengths, kv, d, fmt, page_tokens, seed=0, width=None, spread=0.5):
+        self.lengths, self.kv, self.d, self.fmt, self.page_tokens = lengths, kv, d, fmt, page_tokens
+        used = [-(-n // page_tokens) for n in lengths]
+        total = sum(used) + 2
+        g = gen(seed)
+        order = torch.randperm(total, generator=g).tolist()
+        width = width or max(1, max(used))
+        table = torch.full((len(lengths), width), -1, dtype=torch.int32)
+        slots = []
+        for i, (n, u) in enumerate(zip(lengths, used)):
+            mine = [order.pop() for _ in range(u)]
+            table[i, :u] = torch.tensor(mine, dtype=torch.int32)
+            slots += [mine[j // page_tokens] * page_tokens + j % page_tokens for j in range(n)]
+        self.slots = torch.tensor(slots, dtype=torch.int64)
+        self.cache = new_cache(b, total, page_tokens, kv, d, fmt)
+        k = torch.randn(len(slots), kv, d, generator=g) * torch.exp(spread * torch.randn(d, generator=g))
+        v = torch.randn(len(slots), kv, d, generator=g)
+        self.cache.write(k.cuda(), v.cuda(), self.slots.cuda())
+        self.k, self.v = (x.double().cpu().numpy() for x in self.cache.read(self.slots.cuda(), F32))
+        self.table, self.len_t = table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda()
+        self.ends = np.cumsum([0] + list(lengths))
+
+    def expect(self, q, scale, window, sinks, candidates, hidden=None):
+        """hidden: {history: set of its keys that nobody sees}."""
+        bq = q.double().cpu().numpy()
+        nb, nq, heads, d = bq.shape
+        out, off = np.zeros_like(bq), np.zeros_like(bq)
+        per = heads // self.kv
+        for i, n in enumerate(self.lengths):
+            at = [n - 1 if candidates else n - nq + x for x in range(nq)]
+            for h in range(heads):
+                k, v = (x[self.ends[i]:self.ends[i + 1], h // per] for x in (self.k, self.v))
+                out[i, :, h], off[i, :, h] = O.attend_rows(bq[i, :, h], k, v, at, scale, window, sinks, q.dtype,
+                                                           (hidden or {}).get(i, ()))
+        return out, off
+
+
+LENGTHS = [1, 0, 15, 16, 17, 31, 33, 64, 65, 127, 129, 200]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("d,kv,per,page_tokens", [(32, 2, 1, 16), (64, 1, 4, 32), (128, 2, 2, 64), (64, 3, 5, 16), (32, 1, 17, 128), (128, 1, 40, 256)])
+def test_one_query_each(b, dtype, fmt, d, kv, per, page_tokens):
+    s = Histories(b, LENGTHS, kv, d, fmt, page_tokens)
+    q = torch.randn(len(LENGTHS), 1, kv * per, d, generator=gen(7)).to(dtype).cuda()
+    for window, sinks in ((0, 0), (1, 0), (20, 3), (64, 64), (7, 100)):
+        want, off = s.expect(q, d ** -0.5, window, sinks, False)
+        O.assert_close(s.cache.attend(q, s.table, s.len_t, window=window, sinks=sinks), want, off, (window, sinks))
+    O.assert_close(s.cache.attend(q[:, 0], s.table, s.len_t), *s.expect(q, d ** -0.5, 0, 0, False))
+    assert s.cache.check()[0] == b.REC_OK
+
+
+@pytest.mark.parametrize("candidates", [False, True])
+@pytest.mark.parametrize("d,kv,per,queries,fmt,dtype", [(64, 2, 2, 3, "mx4", BF), (32, 1, 4, 9, "mx8", HF), (128, 1, 1, 33, "mx4", HF), (64, 1, 3, 70, "mx8", BF)])
+def test_several_queries(b, candidates, d, kv, per, queries, fmt, dtype):
+    """More queries than events leave rows that see nothing."""
+    s = Histories(b, [1, 0, 40, 77, 150], kv, d, fmt, 32, seed=2)
+    q = torch.randn(5, queries, kv * per, d, generator=gen(8)).to(dtype).cuda()
+    for window, sinks in ((0, 0), (10, 2), (33, 0)):
+        want, off = s.expect(q, 0.2, window, sinks, candidates)
+        O.assert_close(s.cache.attend(q, s.table, s.len_t, scale=0.2, window=window, sinks=sinks, candidates=candidates), want, off, (window, sinks))
+
+
+@pytest.mark.parametrize("lengths,window,sinks", [([5000], 0, 0), ([4999, 1, 700], 0, 0), ([5000, 3000], 2500, 5), ([4100], 4000, 4), ([6000], 100, 300)])
+@pytest.mark.parametrize("fmt,d,kv,per,dtype", [("mx4", 64, 1, 2, BF), ("mx8", 128, 2, 1, HF), ("mx4", 32, 2, 3, HF)])
+def test_long_histories(b, lengths, window, sinks, fmt, d, kv, per, dtype):
+    s = Histories(b, lengths, kv, d, fmt, 64, seed=3, width=-(-8192 // 64))
+    q = torch.randn(len(lengths), 1, kv * per, d, generator=gen(4)).to(dtype).cuda()
+    want, off = s.expect(q, d ** -0.5, window, sinks, False)
+    O.assert_close(s.cache.attend(q, s.table, s.len_t, window=window, sinks=sinks), want, off)
+
+
+def test_weights_on_few_keys(b):
+    """Large scores: softmax next to a selection, with the best key first, last or in the middle."""
+    s = Histories(b, [300, 300, 300], 1, 64, "mx8", 32, seed=5)
+    q = torch.randn(3, 1, 2, 64, generator=gen(6)).to(BF).cuda() * 6
+    for scale in (1.0, 0.0, -0.5):
+        want, off = s.expect(q, scale, 0, 0, False)
+        O.assert_close(s.cache.attend(q, s.table, s.len_t, scale=scale), want, off, scale)
+
+
+def test_query_and_table_strides(b):
+    s = Histories(b, [50, 90, 33], 2, 64, "mx4", 32, seed=6, width=5)
+    wide = torch.randn(3, 2, 11, 64, generator=gen(3)).to(BF).cuda()
+    q = wide[:, :, 3:7]
+    table = torch.full((3, 9), 12345, dtype=torch.int32, device="cuda")
+    table[:, 2:7] = s.table
+    got = s.cache.attend(q, table[:, 2:7], s.len_t)
+    assert torch.equal(got, s.cache.attend(q.contiguous(), s.table, s.len_t))
+    O.assert_close(got, *s.expect(q, 0.125, 0, 0, False))
+    turned = wide[:, :, 3:7].transpose(0, 1).contiguous().transpose(0, 1)
+    assert torch.equal(got, s.cache.attend(turned, s.table, s.len_t))
+
+
+def test_bad_lengths_and_pages_are_reported(b):
+    s = Histories(b, [40, 64, 30, 60], 1, 32, "mx4", 16, seed=8, width=4)
+    q = torch.randn(4, 1, 2, 32, generator=gen(2)).to(BF).cuda()
+    lengths = s.len_t.clone()
+    lengths[1], lengths[2] = 65, -3
+    got = s.cache.attend(q, s.table, lengths)
+    assert s.cache.check() == (b.REC_ERR_LENGTHS, 1, b.REC_FAULT_LENGTH)
+    want, off = s.expect(q, 32 ** -0.5, 0, 0, False)
+    want[2] = 0
+    O.assert_close(got, want, off)
+    table = s.table.clone()
+    table[0, 1], table[3, 0], table[3, 2] = 2 ** 31 - 1, -1, 10 ** 6
+    got = s.cache.attend(q, table, s.len_t)
+    assert s.cache.check() == (b.REC_ERR_INDEX_RANGE, 0 * 4 + 1, b.REC_FAULT_PAGE)
+    O.assert_close(got, *s.expect(q, 32 ** -0.5, 0, 0, False, {0: set(range(16, 32)), 3: set(range(0, 16)) | set(range(32, 48))}))
+    table[:] = -7                                    # a history without a valid page
+    assert not s.cache.attend(q, table, s.len_t).any()
+    assert s.cache.check()[0] == b.REC_ERR_INDEX_RANGE
+    got = s.cache.attend(q, table[:, :0], s.len_t)   # no pages at all
+    assert not got.any() and s.cache.check() == (b.REC_ERR_LENGTHS, 0, b.REC_FAULT_LENGTH)
+
+
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+def test_what_a_query_does_not_see_has_no_part(b, fmt):
+    """NaN keys and values outside the window, and behind a query's own position."""
+    d, n, nq, window, sinks = 64, 150, 8, 40, 2
+    s = Histories(b, [n], 1, d, fmt, 32, seed=9)
+    q = torch.randn(1, nq, 2, d, generator=gen(5)).to(BF).cuda()
+    nan = torch.full((1, 1, d), float("nan"), device="cuda")
+    for bad in (2, 57, 102, 109, 110, 140, 146, 149):
+        s = Histories(b, [n], 1, d, fmt, 32, seed=9)
+        s.cache.write(nan, nan, s.slots[bad:bad + 1].cuda())
+        s.cache.check()
+        s.k[bad], s.v[bad] = np.nan, np.nan
+        want, off = s.expect(q, 0.125, window, sinks, False)
+        touched = [i for i in range(nq) if O.sees(n - nq + i, bad, window, sinks)]
+        assert np.isnan(want[0, touched]).all() and not np.isnan(np.delete(want[0], touched, 0)).any()
+        O.assert_close(s.cache.attend(q, s.table, s.len_t, window=window, sinks=sinks), want, off, bad)
+
+
+def test_nan_and_infinite_queries(b):
+    s = Histories(b, [70, 70, 70], 1, 64, "mx4", 32, seed=10)
+    q = torch.randn(3, 1, 3, 64, generator=gen(1)).to(HF)
+    q[0, 0, 1, 5], q[1, 0, 0, 63], q[2, 0, 2, 0] = float("nan"), float("inf"), float("-inf")
+    got = s.cache.attend(q.cuda(), s.table, s.len_t)
+    assert got[0, 0, 1].isnan().all() and got[1, 0, 0].isnan().all() and got[2, 0, 2].isnan().all()
+    bad = torch.zeros(3, 1, 3, dtype=torch.bool)
+    bad[0, 0, 1] = bad[1, 0, 0] = bad[2, 0, 2] = True
+    want, off = s.expect(torch.where(bad[..., None], torch.zeros((), dtype=HF), q), 0.125, 0, 0, False)
+    want[bad.numpy()] = np.nan
+    O.assert_close(got, want, off)
+
+
+def test_queries_of_wide_range(b):
+    """Elements of a query from its type's largest to its smallest."""
+    s = Histories(b, [70, 33], 1, 64, "mx8", 32, seed=11)
+    for dtype, top in ((HF, 3.0e4), (BF, 1.0e30)):
+        q = torch.randn(2, 1, 2, 64, generator=gen(1)) * torch.exp(-4 * torch.rand(2, 1, 2, 64, generator=gen(2)))
+        q = (q * top).to(dtype).cuda()
+        want, off = s.expect(q, 0.5 / top, 0, 0, False)
+        O.assert_close(s.cache.attend(q, s.table, s.len_t, scale=0.5 / top), want, off)
+        q = (q.float() / top * (2.0 ** -14 if dtype == HF else 1e-30)).to(dtype)
+        want, off = s.expect(q, 0.5, 0, 0, False)
+        O.assert_close(s.cache.attend(q, s.table, s.len_t, scale=0.5), want, off)
+
+
+# --------------------------------------------------------------- whole histories
+def whole(lengths, heads, kv, d, dtype, seed, fused=True):
+    g = gen(seed)
+    total = sum(lengths)
+    if fused:
+        x = torch.randn(total, heads + 2 * kv, d, generator=g).to(dtype).cuda()
+        q, k, v = x[:, :heads], x[:, heads:heads + kv], x[:, heads + kv:]
+    else:
+        q, k, v = (torch.randn(total, n, d, generator=g).to(dtype).cuda() for n in (heads, kv, kv))
+    return q, k, v, torch.tensor(np.cumsum([0] + list(lengths)), dtype=torch.int32).cuda()
+
+
+def expect_whole(q, k, v, lengths, scale, window, sinks):
+    qn, kn, vn = (x.double().cpu().numpy() for x in (q, k, v))
+    out, off, at = np.zeros_like(qn), np.zeros_like(qn), 0
+    per = qn.shape[1] // kn.shape[1]
+    for n in lengths:
+        for h in range(qn.shape[1]):
+            part = slice(at, at + n)
+            out[part, h], off[part, h] = O.attend_rows(qn[part, h], kn[part, h // per], vn[part, h // per], range(n), scale, window, sinks, q.dtype)
+        at += n
+    return out, off
+
+
+RAGGED = [1, 17, 0, 64, 65, 2, 130, 0, 0, 31, 1]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+@pytest.mark.parametrize("d,heads,kv", [(32, 2, 2), (64, 6, 2), (128, 3, 1), (64, 1, 1)])
+def test_whole_histories(b, dtype, d, heads, kv):
+    q, k, v, offsets = whole(RAGGED, heads, kv, d, dtype, 20)
+    fault = b._faults("cuda:0")
+    for window, sinks in ((0, 0), (1, 0), (16, 2), (40, 0), (100, 500), (7, 70)):
+        want, off = expect_whole(q, k, v, RAGGED, d ** -0.5, window, sinks)
+        O.assert_close(b.attend_window(q, k, v, offsets, window=window, sinks=sinks, fault=fault), want, off, (window, sinks))
+    assert b.rec_history_check(fault) == (b.REC_OK, -1, -1)
+
+
+@pytest.mark.parametrize("d,n,window,sinks", [(64, 700, 0, 0), (128, 523, 129, 4), (32, 1000, 256, 16), (64, 641, 64, 128)])
+def test_longer_whole_histories(b, d, n, window, sinks):
+    lengths = [n, 3, n // 2 + 1]
+    q, k, v, offsets = whole(lengths, 2, 1, d, BF, 21, fused=False)
+    O.assert_close(b.attend_window(q, k, v, offsets, scale=0.3, window=window, sinks=sinks), *expect_whole(q, k, v, lengths, 0.3, window, sinks))
+
+
+def test_many_short_whole_histories(b):
+    lengths = [int(x) for x in torch.randint(0, 5, (700,), generator=gen(1))]
+    q, k, v, offsets = whole(lengths, 2, 2, 32, HF, 22)
+    O.assert_close(b.attend_window(q, k, v, offsets), *expect_whole(q, k, v, lengths, 32 ** -0.5, 0, 0))
+
+
+def test_whole_histories_ignore_what_they_do_not_see(b):
+    """NaN and infinities in later events, in events behind the window, and in the neighbours' histories."""
+    lengths, window, sinks, d = [70, 150, 40], 30, 2, 64
+    for where, what in ((70 + 149, "nan"), (70 + 100, "nan"), (70 + 60, "inf"), (69, "nan"), (220, "inf"), (70, "nan"), (70 + 64, "inf")):
+        q, k, v, offsets = whole(lengths, 2, 1, d, BF, 23)
+        v[where] = float(what)
+        k[where] = float("nan")
+        want, off = expect_whole(q, k, v, lengths, 0.125, window, sinks)
+        assert np.isnan(want).any() and not np.isnan(want).all()
+        O.assert_close(b.attend_window(q, k, v, offsets, window=window, sinks=sinks), want, off, (where, what))
+
+
+def test_infinite_values_that_are_seen(b):
+    """An infinite value alone gives an infinity, not NaN, to the rows that see it, in its column."""
+    lengths, d = [90], 32
+    q, k, v, offsets = whole(lengths, 1, 1, d, BF, 24)
+    v[40, 0, 3] = float("inf")
+    want, off = expect_whole(q, k, v, lengths, 32 ** -0.5, 0, 0)
+    got = b.attend_window(q, k, v, offsets).double().cpu().numpy()
+    assert np.array_equal(np.isposinf(got), np.isposinf(want)) and np.isposinf(want).sum() == 50
+    fine = np.isfinite(want)
+    assert (np.abs(got[fine] - want[fine]) <= off[fine]).all()
+
+
+@pytest.mark.parametrize("offsets", [[0, 30, 20, 50], [0, 10, 60, 50], [-5, 10, 20, 50], [5, 10, 20, 50], [0, 10, 20, 49], [0, 10, 20, 5000], [50, 0, 50, 0]])
+def test_offsets_that_are_none(b, offsets):
+    """Reported, and nothing outside the buffers is touched (guard rows around the output's neighbours stay)."""
+    q, k, v, _ = whole([50], 2, 2, 32, BF, 25)
+    fault = b._faults("cuda:0")
+    out = b.attend_window(q, k, v, torch.tensor(offsets, dtype=torch.int32).cuda(), fault=fault)
+    torch.cuda.synchronize()
+    st, at, word = b.rec_history_check(fault)
+    assert st == b.REC_ERR_LENGTHS and word == b.REC_FAULT_LENGTH and 0 <= at < 3 and out.shape == (50, 2, 32)
+
+
+# -------------------------------------------------------------- streams and graphs
+def test_another_stream(b):
+    s = Histories(b, [300, 20], 1, 64, "mx4", 32, seed=12)
+    q = torch.randn(2, 1, 2, 64, generator=gen(1)).to(BF).cuda()
+    want = s.cache.attend(q, s.table, s.len_t)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        got = s.cache.attend(q, s.table, s.len_t)
+    stream.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_a_captured_step_replays(b):
+    """One event arrives, is written and queried: recorded once, replayed on new contents."""
+    lengths = [700, 5, 64]
+    s = Histories(b, lengths, 2, 64, "mx4", 32, seed=13, width=30)
+    q = torch.randn(3, 1, 4, 64, generator=gen(1)).to(BF).cuda()
+    k, v = (torch.randn(3, 2, 64, generator=gen(i)).to(BF).cuda() for i in (2, 3))
+    slots = torch.stack([s.slots[s.ends[i + 1] - 1] for i in range(3)]).cuda()     # their last places
+    out = torch.empty_like(q)
+
+    def step():
+        s.cache.write(k, v, slots)
+        s.cache.attend(q, s.table, s.len_t, out=out, window=500, sinks=4)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        for x in (q, k, v):
+            x.copy_(torch.randn(x.shape, generator=gen(100 + i)).to(BF))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, pages = out.clone(), s.cache.pages.clone()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(pages, s.cache.pages)
+
+
+def test_same_inputs_same_bits(b):
+    s = Histories(b, [5000, 40, 900], 2, 128, "mx4", 64, seed=14)
+    q = torch.randn(3, 1, 8, 128, generator=gen(1)).to(BF).cuda()
+    first = s.cache.attend(q, s.table, s.len_t)
+    for _ in range(3):
+        assert torch.equal(first, s.cache.attend(q, s.table, s.len_t))
