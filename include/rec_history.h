@@ -110,8 +110,8 @@ typedef struct {
  *   k, v     [tokens][kv_heads][head_dim] of dtype (REC_F32, REC_F16, REC_BF16)
  * Device faults: REC_FAULT_SLOT (the row is left out), REC_FAULT_VALUE.
  * A slot that is named twice in one call holds one of its rows or a mixture.
- * REC_ERR_ARG: null, misaligned, bad enum, tokens < 0 or >= 2^31; REC_ERR_SHAPE: a shape
- * that rec_history_bytes() refuses.
+ * REC_ERR_ARG: null, misaligned, bad enum, tokens < 0; REC_ERR_SHAPE: a shape that
+ * rec_history_bytes() refuses; REC_ERR_OVERFLOW: tokens * kv_heads >= 2^31.
  */
 REC_API rec_status rec_history_write(const rec_history *h, const rec_rows *k, const rec_rows *v,
                                      int32_t dtype, const int64_t *dev_slots, int64_t tokens, void *stream);
@@ -163,7 +163,8 @@ REC_API size_t rec_history_attend_workspace_bytes(const rec_history *h, const re
  * free for other use once the call's work is done; what it holds before does not matter.
  * REC_ERR_ARG: null, misaligned, bad enum, negative counts, a workspace too small;
  * REC_ERR_SHAPE: heads no multiple of kv_heads, or a shape that rec_history_bytes()
- * refuses; REC_ERR_OVERFLOW: batch * queries * heads or table_width * page_tokens >= 2^31. */
+ * refuses; REC_ERR_OVERFLOW: batch * queries * heads >= 2^31, or table_width * page_tokens
+ * > 2^31 - 1024. */
 REC_API rec_status rec_history_attend(const rec_history *h, const rec_query *q, void *dev_workspace,
                                       size_t workspace_bytes, void *stream);
 
@@ -178,7 +179,7 @@ REC_API rec_status rec_history_attend(const rec_history *h, const rec_query *q, 
  *   dev_fault     as in rec_history; may be null
  * Device faults: REC_FAULT_LENGTH (offsets that decrease, or do not run from 0 to tokens,
  * are brought into that range; rows of no history are not written).
- * REC_ERR_ARG, REC_ERR_SHAPE and REC_ERR_OVERFLOW (tokens >= 2^31) as above.
+ * REC_ERR_ARG, REC_ERR_SHAPE as above; REC_ERR_OVERFLOW: tokens * heads >= 2^31.
  */
 typedef struct {
     rec_rows q, k, v;

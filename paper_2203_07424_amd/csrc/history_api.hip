@@ -5,6 +5,9 @@ namespace {
 
 using rec::hist::Cache;
 
+// Of a history: the kernels count a little past the last one in 32 bits.
+constexpr int64_t MOST_TOKENS = (1ll << 31) - 1024;
+
 bool head_dim_fits(int d) { return d == 32 || d == 64 || d == 128; }
 
 bool shape_fits(const rec_history *h)
@@ -50,7 +53,7 @@ rec_status check_query(const rec_history *h, const rec_query *q)
         q->window < 0 || q->sinks < 0 || (q->candidates != 0 && q->candidates != 1))
         return REC_ERR_ARG;
     if (q->heads % h->kv_heads) return REC_ERR_SHAPE;
-    if ((int64_t)q->table_width * h->page_tokens >= 1ll << 31 || (int64_t)q->queries * q->heads >= 1ll << 31 ||
+    if ((int64_t)q->table_width * h->page_tokens > MOST_TOKENS || (int64_t)q->queries * q->heads >= 1ll << 31 ||
         (int64_t)q->queries * q->heads * q->batch >= 1ll << 31)
         return REC_ERR_OVERFLOW;
     return REC_OK;

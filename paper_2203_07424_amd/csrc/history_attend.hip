@@ -1,118 +1,644 @@
-// Attention over cached histories: a wave a query row, a lane a key.
+// Attention over cached histories.
+//
+// A wave has 16 query rows of one kv head (its heads of every query, one after the
+// other) and walks over 64 keys at a time.  Scores come transposed, S^T = K Q^T, on
+// the block-scaled matrix instructions (16 x 16 x 128): they take the cache's codes and
+// scale bytes as they lie in memory, so keys cost no vector instruction at all.  A
+// query enters as two (fp16: three) E4M3 terms, each the rounding of what the terms before
+// left, which hold it to 2^-22 of the largest of 32 elements; for head_dim 32 and 64 the
+// terms share an instruction's 128 columns and the keys are repeated.
+//
+// Key 4 r + x of a tile is row r of its x-th product, so that a lane's scores (column c =
+// query row, lane group g) are those of the 16 neighbouring tokens 16 g ..., which is
+// what it also loads of the values: one row of a group, 16 tokens of two columns.
+// Weights therefore go from scores straight into the operand of O^T += V^T P^T
+// (16 x 16 x 32 bf16), with no exchange between lanes.  Values become bf16 exactly: the
+// scaled conversions look at a scale's exponent bits only, so one shift puts a scale
+// byte in place.  A product with ones sums the weights as they were rounded.
+//
+// The running maximum moves only when a tile's exceeds it by 2^8: weights stay below 2^8,
+// and the accumulators are rescaled a few times a history instead of every tile.
+//
+// Few pairs of history and head are divided: among the waves of a block, which meet in
+// LDS, and, where that leaves compute units idle, among blocks, whose parts
+// combine_kernel joins.
+#include <algorithm>
+
 #include "history.h"
 
 namespace rec {
 namespace hist {
 namespace {
 
-template <int FMT, int D, bool BF>
-__global__ __launch_bounds__(64) void attend_kernel(Cache c, rec_query q)
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int ROWS = 16;       // query rows of a wave
+constexpr int TILE = 64;       // keys
+constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
+constexpr int CUS = 256;
+
+struct AttendArgs {
+    Cache c;
+    rec_query q;
+    int per;        // query heads of a kv head
+    int rows;       // queries * per
+    int row_tiles;  // of ROWS
+    int splits;
+    float *part_o;   // [splits][batch * queries * heads][D]
+    f32x2 *part_ml;  // [splits][batch * queries * heads]
+};
+
+__device__ inline float neg_inf() { return -__builtin_inff(); }
+
+// Terms of eight query elements x in units of 2^-4k of `scale`; x becomes what is left.
+__device__ inline u32x2 term_of(float (&x)[8], float scale)
 {
-    __shared__ float qs[D], ps[64];
+    u32x2 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        s16x2 w = {0, 0};
+        const float most = 448.0f * scale;
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = __builtin_amdgcn_fmed3f(x[4 * i + j], -most, most);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, y[0], y[1], scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, y[2], y[3], scale, true);
+        const unsigned bits = __builtin_bit_cast(unsigned, w);
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bits, scale, false);
+        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bits, scale, true);
+        x[4 * i] -= a[0];
+        x[4 * i + 1] -= a[1];
+        x[4 * i + 2] -= b[0];
+        x[4 * i + 3] -= b[1];
+        r[i] = bits;
+    }
+    return r;
+}
+
+// A wave's query rows as operands.  Column k of a product is byte k % 16 of half k / 64 of
+// lane group k / 16 % 4; its scale is byte 0 of lane group k / 32.
+template <int D, bool BF>
+struct Query {
+    static constexpr int TERMS = BF ? 2 : 3;
+    static constexpr int STEPS = D == 128 ? TERMS : D == 64 && TERMS == 3 ? 2 : 1;
+    i32x8 b[STEPS];
+    int scale[STEPS];
+
+    // `row`: this lane's row (lane % 16) or null; `flip`: its sign changes.
+    __device__ inline void load(const void *row, bool flip, int g)
+    {
+        using T = std::conditional_t<BF, __bf16, _Float16>;
+        typedef T tx8 __attribute__((ext_vector_type(8)));
+        constexpr int PARTS = D == 128 ? 2 : 1;  // 16 elements of this lane each
+        float x[PARTS][2][8];
+        unsigned most[PARTS];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const int first = 64 * p + 16 * (D == 32 ? g & 1 : g);
+            most[p] = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                tx8 v = {};
+                if (row) v = *reinterpret_cast<const tx8 *>(static_cast<const T *>(row) + first + 8 * h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float f = (float)v[i];
+                    x[p][h][i] = flip ? -f : f;
+                    most[p] = max(most[p], __builtin_bit_cast(unsigned, f) & 0x7fffffffu);
+                }
+            }
+            most[p] = max(most[p], (unsigned)__shfl_xor((int)most[p], 16));  // 32 elements: lane groups 2 j and 2 j + 1
+        }
+        unsigned byte[PARTS];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            // The exponent that E4M3 blocks of the cache have; 255 where the query is not finite.
+            const int e = (int)(most[p] >> 23) - 127 - 8 + ((most[p] & 0x7fffffu) > 0x680000u ? 1 : 0);
+            byte[p] = most[p] >= 0x7f800000u ? 255u : (unsigned)(min(max(e, -110), 119) + 127);
+        }
+        u32x4 term[TERMS][PARTS];
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                const float s = __builtin_bit_cast(float, (byte[p] - 4 * t) << 23);
+                const u32x2 lo = term_of(x[p][0], s), hi = term_of(x[p][1], s);
+                term[t][p] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+            }
+        // The scale of block j of 32 elements is with lane groups 2 j and 2 j + 1 of its part.
+        const int lane = threadIdx.x & 63;
+        if constexpr (D == 128) {
+            const unsigned a = (unsigned)__shfl((int)byte[0], (g & 1) * 32 + (lane & 15)), z = (unsigned)__shfl((int)byte[1], (g & 1) * 32 + (lane & 15));
+            const unsigned mine = g < 2 ? a : z;
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) {
+                set(t, term[t][0], term[t][1]);
+                scale[t] = mine == 255u ? 255 : (int)(mine - 4 * t);
+            }
+        } else if constexpr (D == 64) {
+            const unsigned mine = (unsigned)__shfl((int)byte[0], (g & 1) * 32 + (lane & 15));
+            set(0, term[0][0], term[1][0]);
+            scale[0] = mine == 255u ? 255 : (int)(mine - 4 * (g >> 1));
+            if constexpr (TERMS == 3) {
+                set(1, term[2][0], u32x4{0u, 0u, 0u, 0u});
+                scale[1] = mine == 255u ? 255 : (int)(mine - 8);
+            }
+        } else {
+            const u32x4 none = {0u, 0u, 0u, 0u};
+            set(0, g < 2 ? term[0][0] : term[1][0], TERMS == 3 && g < 2 ? term[TERMS - 1][0] : none);
+            scale[0] = byte[0] == 255u ? 255 : (int)(byte[0] - 4 * min(g, TERMS - 1));
+        }
+    }
+    __device__ inline void set(int s, u32x4 lo, u32x4 hi)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            b[s][i] = (int)lo[i];
+            b[s][4 + i] = (int)hi[i];
+        }
+    }
+};
+
+// Codes and scales of 64 keys and values, as this lane needs them.
+template <int FMT, int D>
+struct Tile {
+    static constexpr int WIDE = FMT == REC_MX8 ? 2 : 1;
+    static constexpr int KW = FMT == REC_MX8 && D == 128 ? 2 : 1;
+    static constexpr int SW = D / BLOCK;
+    u32x4 k[4][KW];
+    unsigned ks[SW];
+    u32x4 v[D / BLOCK][WIDE], vs[D / BLOCK];
+
+    // kg: the group of this lane's keys.
+    __device__ inline void load_keys(const unsigned char *kg, int c, int g)
+    {
+        constexpr int CB = code_bytes<FMT>(D);
+        const int part = FMT == REC_MX4 ? (D == 32 ? 0 : D == 64 ? 16 * (g & 1) : 16 * g) : (D == 32 ? 16 * (g & 1) : 16 * g);
+        const unsigned char *kp = kg + 4 * (c & 3) * CB + part;
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int w = 0; w < KW; ++w) k[x][w] = *reinterpret_cast<const u32x4 *>(kp + x * CB + 64 * w);
+        const unsigned char *sp = kg + 2 * GROUP * CB + 4 * (c & 3) * SW;
+        if constexpr (SW == 1) {
+            ks[0] = *reinterpret_cast<const unsigned *>(sp);
+        } else if constexpr (SW == 2) {
+            const u32x2 s = *reinterpret_cast<const u32x2 *>(sp);
+            ks[0] = s[0];
+            ks[1] = s[1];
+        } else {
+            const u32x4 s = *reinterpret_cast<const u32x4 *>(sp);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) ks[x] = s[x];
+        }
+    }
+    // vg: the group of its values.
+    __device__ inline void load_values(const unsigned char *vg, int c)
+    {
+        constexpr int CB = code_bytes<FMT>(D);
+        const unsigned char *vp = vg + GROUP * CB + c * GROUP * WIDE, *vsp = vg + 2 * GROUP * CB + GROUP * SW;
+#pragma unroll
+        for (int b = 0; b < D / BLOCK; ++b) {
+#pragma unroll
+            for (int w = 0; w < WIDE; ++w) v[b][w] = *reinterpret_cast<const u32x4 *>(vp + b * GROUP * GROUP * WIDE + 16 * w);
+            vs[b] = *reinterpret_cast<const u32x4 *>(vsp + b * GROUP);
+        }
+    }
+};
+
+// Scores of the x-th product.
+template <int FMT, int D, bool BF, int X>
+__device__ inline f32x4 scores(const Tile<FMT, D> &t, const Query<D, BF> &q, int g)
+{
+    i32x8 a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = (int)t.k[X][0][i];
+        a[4 + i] = (int)t.k[X][Tile<FMT, D>::KW - 1][i];
+    }
+    // Byte of the scale word; the block's byte moves there where it depends on the lane.
+    constexpr int AT = D == 32 ? X : D == 64 ? 2 * (X & 1) : 0;
+    const int s = (int)(D == 32 ? t.ks[0] : D == 64 ? t.ks[(X >> 1) % Tile<FMT, D>::SW] >> (8 * (g & 1)) : t.ks[X % Tile<FMT, D>::SW] >> (8 * g));
+    f32x4 r = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < Query<D, BF>::STEPS; ++i)
+        r = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.b[i], r, FMT == REC_MX4 ? 4 : 0, 0, AT, s, 0, q.scale[i]);
+    return r;
+}
+
+// The values of token T of a lane's 16 in columns j and j + 16 of block b, in bf16.
+template <int FMT, int D, int T>
+__device__ inline unsigned value_pair(const Tile<FMT, D> &t, int b)
+{
+    constexpr int at = 8 * (T & 3);
+    const unsigned word = t.vs[b][T >> 2];
+    const float s = __builtin_bit_cast(float, at < 23 ? word << (23 - at) : word >> (at - 23));
+    bf16x2 r;
+    if constexpr (FMT == REC_MX4) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[b][0][T >> 2], s, T & 3);
+    else r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(t.v[b][T >> 3][(T >> 1) & 3], s, (T & 1) != 0);
+    return __builtin_bit_cast(unsigned, r);
+}
+
+// Operands of eight tokens, 8 H ..., for the two column tiles of block b.
+template <int FMT, int D, int H>
+__device__ inline void value_operands(const Tile<FMT, D> &t, int b, u32x4 &lo, u32x4 &hi)
+{
+    const unsigned a[8] = {value_pair<FMT, D, 8 * H>(t, b),     value_pair<FMT, D, 8 * H + 1>(t, b), value_pair<FMT, D, 8 * H + 2>(t, b),
+                           value_pair<FMT, D, 8 * H + 3>(t, b), value_pair<FMT, D, 8 * H + 4>(t, b), value_pair<FMT, D, 8 * H + 5>(t, b),
+                           value_pair<FMT, D, 8 * H + 6>(t, b), value_pair<FMT, D, 8 * H + 7>(t, b)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        lo[i] = __builtin_amdgcn_perm(a[2 * i + 1], a[2 * i], 0x05040100u);
+        hi[i] = __builtin_amdgcn_perm(a[2 * i + 1], a[2 * i], 0x07060302u);
+    }
+}
+
+__device__ inline f32x4 product(u32x4 a, u32x4 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+__device__ inline unsigned pack(float a, float b)
+{
+    const bf16x2 r = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(unsigned, r);
+}
+
+// What a wave carries: for query row lane % 16, columns 16 i + 4 (lane / 16) ... + 3.
+template <int D>
+struct Sums {
+    f32x4 o[D / 16], l;
+    float m;
+};
+
+// Tokens of a lane's 16 that count as zero whatever their bytes are: 0 * NaN would reach the
+// rows that do not see a value.  Those are the ones that no row sees (bit t of `used` clear) and,
+// a block at a time, those whose block is NaN.  Returns the blocks (bit b) of which row c,
+// which sees the tokens in `seen`, sees a NaN.
+template <int FMT, int D>
+__device__ inline unsigned clear_values(Tile<FMT, D> &t, unsigned used, unsigned seen)
+{
+    unsigned nan = 0;
+#pragma unroll
+    for (int b = 0; b < D / BLOCK; ++b) {
+        unsigned bad = 0;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const unsigned shift = 8 * (x & 3);
+            if ((t.vs[b][x >> 2] >> shift & 255u) == 255u || !(used >> x & 1u)) {
+                bad |= 1u << x;
+                t.vs[b][x >> 2] &= ~(255u << shift);
+                if constexpr (FMT == REC_MX4) t.v[b][0][x >> 2] &= ~(255u << shift);
+                else t.v[b][x >> 3][(x >> 1) & 3] &= ~(0xffffu << (16 * (x & 1)));
+            }
+        }
+        if (bad & seen) nan |= 1u << b;
+    }
+    nan |= (unsigned)__shfl_xor((int)nan, 16);
+    return nan | (unsigned)__shfl_xor((int)nan, 32);
+}
+
+// Where a wave's row goes.
+__device__ inline long long out_row(const AttendArgs &a, int b, int kv, int row)
+{
+    const int i = row / a.per;
+    return ((long long)b * a.q.queries + i) * a.q.heads + kv * a.per + (row - i * a.per);
+}
+
+template <int FMT, int D, bool BF, int W>
+__global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend_kernel(AttendArgs a)
+{
     using T = std::conditional_t<BF, __bf16, _Float16>;
-    const int lane = threadIdx.x;
-    const unsigned row = blockIdx.x;
-    const int head = (int)(row % (unsigned)q.heads), i = (int)(row / (unsigned)q.heads % (unsigned)q.queries);
-    const int b = (int)(row / (unsigned)q.heads / (unsigned)q.queries), kv = head / (q.heads / c.kv_heads);
-    const T *src = static_cast<const T *>(q.dev_q) + b * q.batch_stride + i * q.query_stride + head * q.head_stride;
-    for (int x = lane; x < D; x += 64) qs[x] = (float)src[x];
-    __syncthreads();
-    int len = q.dev_lengths[b];
-    const int most = q.table_width << c.page_shift;
-    if (len < 0 || len > most) {
-        if (lane == 0) report(c.fault, REC_FAULT_LENGTH, b);
-        len = len < 0 ? 0 : most;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    unsigned at = blockIdx.x;
+    const int split = (int)(at % (unsigned)a.splits);
+    at /= (unsigned)a.splits;
+    const int row_tile = (int)(at % (unsigned)a.row_tiles);
+    at /= (unsigned)a.row_tiles;
+    const int kv = (int)(at % (unsigned)a.c.kv_heads), b = (int)(at / (unsigned)a.c.kv_heads);
+
+    const int shift = a.c.page_shift, most_tokens = a.q.table_width << shift;
+    int len = a.q.dev_lengths[b];
+    if (len < 0 || len > most_tokens) {
+        if (threadIdx.x == 0 && kv == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)b);
+        len = len < 0 ? 0 : most_tokens;
     }
-    const int pos = q.candidates ? len - 1 : len - q.queries + i;
-    float m = -__builtin_inff(), l = 0.0f, o[(D + 63) / 64] = {};
-    bool any = false;
-    for (int t0 = 0; t0 <= pos; t0 += 64) {
-        const int j = t0 + lane;
-        bool seen = j <= pos && (q.window == 0 || pos - j < q.window || j < q.sinks);
-        long long page = -1;
-        if (j < len) {
-            const int col = j >> c.page_shift;
-            page = q.dev_pages_of[b * q.table_stride + col];
-            if (page < 0 || page >= c.num_pages) {
-                if (seen) report(c.fault, REC_FAULT_PAGE, (unsigned long long)b * q.table_width + col);
-                page = -1;
-                seen = false;
-            }
-        }
-        const int at = j & ((1 << c.page_shift) - 1), t = at & 15;
-        float x = -__builtin_inff();
-        if (seen) {
-            const unsigned char *g = group_of<FMT>(c, D, page, at, kv);
-            const unsigned char *sc = g + 2 * GROUP * code_bytes<FMT>(D) + t * (D / BLOCK);
-            float sum = 0.0f;
-            for (int blk = 0; blk < D / BLOCK; ++blk) {
-                float part = 0.0f;
-                for (int e = 0; e < BLOCK; e += 2) {
-                    const int el = blk * BLOCK + e;
-                    const unsigned w = FMT == REC_MX4 ? g[t * code_bytes<FMT>(D) + el / 2]
-                                                      : *reinterpret_cast<const unsigned short *>(g + t * code_bytes<FMT>(D) + el);
-                    const f32x2 two = two_values<FMT, 0>(w);
-                    part += qs[el] * two[0] + qs[el + 1] * two[1];
+    // Positions of this wave's rows: of its first, its last, and this lane's.
+    const int first_row = row_tile * ROWS, last_row = min(first_row + ROWS, a.rows) - 1, row = min(first_row + c, last_row);
+    const bool together = a.q.candidates != 0;
+    const int before = len - (together ? 1 : a.q.queries);
+    const int p_lo = before + (together ? 0 : first_row / a.per), p_hi = before + (together ? 0 : last_row / a.per);
+    const int pos = before + (together ? 0 : row / a.per);
+    const int window = a.q.window == 0 ? 0x7fffffff : a.q.window, sinks = a.q.sinks;
+
+    // Tiles that some row sees something of: [0, n_sink) and [n_from, n_to).
+    int n_from = 0, n_sink = 0, n_to = 0;
+    if (p_hi >= 0) {
+        n_to = p_hi / TILE + 1;
+        n_from = max(max(p_lo, 0) - window + 1, 0) / TILE;
+        n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from);
+    }
+    const int tiles = n_sink + n_to - n_from, each = (tiles + a.splits - 1) / a.splits;
+    const int begin = min(split * each, tiles), end = min(begin + each, tiles);
+
+    Sums<D> sum;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) sum.o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    sum.l = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    sum.m = neg_inf();
+
+    if (begin + wave < end) {
+        const long long row_bytes = 2ll * (b * a.q.batch_stride + (row / a.per) * a.q.query_stride + (kv * a.per + row % a.per) * a.q.head_stride);
+        Query<D, BF> q;
+        q.load(first_row + c <= last_row ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr, a.q.scale < 0.0f, g);
+        const float factor = __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
+        const int32_t *table = a.q.dev_pages_of + b * a.q.table_stride;
+        const int groups = 1 << (shift - 4);
+
+        // Tile n of the walk starts at this key.
+        auto key_of = [&](int n) { return (n < n_sink ? n : n_from + n - n_sink) * TILE; };
+        // The page of a group's first token, or -1.
+        auto page_of = [&](int token) {
+            int page = -1;
+            if (token < len) page = table[token >> shift];
+            return page;
+        };
+        auto group_at = [&](int page, int token) {
+            const bool ok = page >= 0 && page < a.c.num_pages;
+            const long long index = ok ? ((long long)page * a.c.kv_heads + kv) * groups + ((token >> 4) & (groups - 1)) : 0;
+            return a.c.pages + index * group_bytes<FMT>(D);
+        };
+
+        int n = begin + wave, key = key_of(n);
+        int k_page = page_of(key + 16 * (c >> 2)), v_page = page_of(key + 16 * g);
+        Tile<FMT, D> tile;
+        tile.load_keys(group_at(k_page, key + 16 * (c >> 2)), c, g);
+        tile.load_values(group_at(v_page, key + 16 * g), c);
+        k_page = n + W < end ? page_of(key_of(n + W) + 16 * (c >> 2)) : -1;
+        int v_next = n + W < end ? page_of(key_of(n + W) + 16 * g) : -1;
+        for (;; n += W) {
+            const bool more = n + W < end;
+            const int key_next = more ? key_of(n + W) : 0;
+            f32x4 s[4] = {scores<FMT, D, BF, 0>(tile, q, g), scores<FMT, D, BF, 1>(tile, q, g), scores<FMT, D, BF, 2>(tile, q, g),
+                          scores<FMT, D, BF, 3>(tile, q, g)};
+            // The next tile's keys and values take the place of this one's as soon as that is used.
+            if (more) tile.load_keys(group_at(k_page, key_next + 16 * (c >> 2)), c, g);
+
+            // Groups come with their page or not at all.
+            const bool there = v_page >= 0 && v_page < a.c.num_pages;
+            const bool whole = key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there);
+            unsigned seen = 0xffffu, nan = 0;  // bit t: row c sees token t of group g; bit b: and a NaN in block b
+            if (!whole) {
+                const int first = key + 16 * g, from = max(p_lo, 0) - window;
+                unsigned used = 0;  // bit t: some row sees token t
+                seen = 0;
+#pragma unroll
+                for (int t = 0; t < 16; ++t) {
+                    const int j = first + t;
+                    if (j <= pos && (pos - j < window || j < sinks)) seen |= 1u << t;
+                    if (j <= p_hi && (j > from || j < sinks)) used |= 1u << t;
                 }
-                sum += part * scale_of(sc[blk]);
+                if (!there) {
+                    if (used && c == 0)
+                        report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)b * (unsigned)a.q.table_width + (unsigned)(first >> shift));
+                    seen = used = 0;
+                }
+                nan = clear_values<FMT, D>(tile, used, seen);
+#pragma unroll
+                for (int t = 0; t < 16; ++t)
+                    if (!(seen >> t & 1u)) s[t & 3][t >> 2] = neg_inf();
             }
-            x = sum * q.scale;
-        }
-        float mt = x;
-        for (int s = 32; s; s >>= 1) mt = fmaxf(mt, __shfl_xor(mt, s));
-        const float mn = fmaxf(m, mt), ref = mn == -__builtin_inff() ? 0.0f : mn;
-        const float p = seen ? __expf(x - ref) : 0.0f, alpha = __expf(m - ref);
-        m = mn;
-        float sum = p;
-        for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
-        l = l * alpha + sum;
-        ps[lane] = p;
-        const unsigned long long who = __ballot(seen);
-        any |= who != 0;
-        for (int x2 = 0; x2 < (D + 63) / 64; ++x2) {
-            const int el = x2 * 64 + lane;
-            float acc = o[x2] * alpha;
-            for (int s = 0; s < 64; ++s) {
-                if (!(who >> s & 1)) continue;
-                const long long pg = __shfl(page, s);
-                const int a2 = (t0 + s) & ((1 << c.page_shift) - 1), tt = a2 & 15;
-                if (el < D) {
-                    const unsigned char *g = group_of<FMT>(c, D, pg, a2, kv);
-                    const int code = ((el >> 5) * 16 + (el & 15)) * GROUP + tt;
-                    const unsigned char *vp = g + GROUP * code_bytes<FMT>(D);
-                    const unsigned w = FMT == REC_MX4 ? vp[code] : *reinterpret_cast<const unsigned short *>(vp + 2 * code);
-                    const f32x2 two = two_values<FMT, 0>(w);
-                    const float sc = scale_of(g[2 * GROUP * code_bytes<FMT>(D) + GROUP * (D / BLOCK) + (el >> 5) * GROUP + tt]);
-                    acc += ps[s] * (el & 16 ? two[1] : two[0]) * sc;
+
+            float most = neg_inf();
+#pragma unroll
+            for (int t = 0; t < 16; ++t) most = fmaxf(most, s[t & 3][t >> 2]);
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            most = most == neg_inf() ? most : most * factor;
+            if (__any(most > sum.m + SLACK)) {
+                const float m = fmaxf(sum.m, most);
+                const float down = sum.m == m ? 1.0f : __builtin_amdgcn_exp2f(sum.m - m);
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) sum.o[i] *= down;
+                sum.l *= down;
+                sum.m = m;
+            }
+            float p[16];
+#pragma unroll
+            for (int t = 0; t < 16; ++t) p[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t & 3][t >> 2], factor, -sum.m));
+            if (!whole)
+#pragma unroll
+                for (int t = 0; t < 16; ++t) p[t] = seen >> t & 1u ? p[t] : 0.0f;
+
+            // Weights as bf16, for fp16 results with what that rounding left out beside them.
+            constexpr int TERMS = BF ? 1 : 2;
+            u32x4 w[TERMS][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[0][h][i] = pack(p[8 * h + 2 * i], p[8 * h + 2 * i + 1]);
+                    if constexpr (TERMS == 2) {
+                        const unsigned word = w[0][h][i];
+                        w[1][h][i] = pack(p[8 * h + 2 * i] - __builtin_bit_cast(float, word << 16),
+                                          p[8 * h + 2 * i + 1] - __builtin_bit_cast(float, word & 0xffff0000u));
+                    }
+                }
+            const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) sum.l = product(ones, w[k][h], sum.l);
+#pragma unroll
+            for (int i = 0; i < D / BLOCK; ++i) {
+                u32x4 lo, hi;
+                value_operands<FMT, D, 0>(tile, i, lo, hi);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) {
+                    sum.o[2 * i] = product(lo, w[k][0], sum.o[2 * i]);
+                    sum.o[2 * i + 1] = product(hi, w[k][0], sum.o[2 * i + 1]);
+                }
+                value_operands<FMT, D, 1>(tile, i, lo, hi);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) {
+                    sum.o[2 * i] = product(lo, w[k][1], sum.o[2 * i]);
+                    sum.o[2 * i + 1] = product(hi, w[k][1], sum.o[2 * i + 1]);
                 }
             }
-            o[x2] = acc;
+            if (nan)
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    if (nan >> (i / 2) & 1u) sum.o[i] += __builtin_nanf("");
+            if (!more) break;
+            tile.load_values(group_at(v_next, key_next + 16 * g), c);
+            key = key_next;
+            v_page = v_next;
+            if (n + 2 * W < end) {
+                k_page = page_of(key_of(n + 2 * W) + 16 * (c >> 2));
+                v_next = page_of(key_of(n + 2 * W) + 16 * g);
+            }
         }
+    }
+
+    const long long out = out_row(a, b, kv, row);
+    const bool real = first_row + c <= last_row;
+    const long long all_rows = (long long)a.q.batch * a.q.queries * a.q.heads;
+    if constexpr (W == 1) {
+        const float l = sum.l[0];
+        if (a.splits > 1) {
+            if (real && g == 0) a.part_ml[split * all_rows + out] = f32x2{sum.m, l};
+            if (real)
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    *reinterpret_cast<f32x4 *>(a.part_o + (split * all_rows + out) * D + 16 * i + 4 * g) = sum.o[i];
+        } else if (real) {
+            const float by = l == 0.0f ? 0.0f : 1.0f / l;
+            typedef T tx4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                *reinterpret_cast<tx4 *>(static_cast<T *>(a.q.dev_out) + out * D + 16 * i + 4 * g) = __builtin_convertvector(sum.o[i] * by, tx4);
+        }
+    } else {
+        // Rows of all waves in LDS; a thread then joins eight columns of a row.
+        constexpr int LD = D + 4;
+        __shared__ float o_of[W][ROWS][LD];
+        __shared__ f32x2 ml_of[W][ROWS];
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(&o_of[wave][c][16 * i + 4 * g]) = sum.o[i];
+        if (g == 0) ml_of[wave][c] = f32x2{sum.m, sum.l[0]};
         __syncthreads();
+        for (int i = threadIdx.x; i < ROWS * D / 8; i += 64 * W) {
+            const int r = i / (D / 8), col = i % (D / 8) * 8;
+            if (first_row + r > last_row) break;
+            float m = neg_inf();
+#pragma unroll
+            for (int w = 0; w < W; ++w) m = fmaxf(m, ml_of[w][r][0]);
+            float l = 0.0f;
+            f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const f32x2 ml = ml_of[w][r];
+                const float by = ml[0] == neg_inf() && ml[1] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml[0] - m);
+                l += ml[1] * by;
+                x += *reinterpret_cast<const f32x4 *>(&o_of[w][r][col]) * by;
+                y += *reinterpret_cast<const f32x4 *>(&o_of[w][r][col + 4]) * by;
+            }
+            const long long to = out_row(a, b, kv, first_row + r);
+            if (a.splits > 1) {
+                float *p = a.part_o + (split * all_rows + to) * D + col;
+                *reinterpret_cast<f32x4 *>(p) = x;
+                *reinterpret_cast<f32x4 *>(p + 4) = y;
+                if (col == 0) a.part_ml[split * all_rows + to] = f32x2{m, l};
+            } else {
+                typedef T tx8 __attribute__((ext_vector_type(8)));
+                const float by = l == 0.0f ? 0.0f : 1.0f / l;
+                x *= by;
+                y *= by;
+                const f32x8 z = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                *reinterpret_cast<tx8 *>(static_cast<T *>(a.q.dev_out) + to * D + col) = __builtin_convertvector(z, tx8);
+            }
+        }
     }
-    T *out = static_cast<T *>(q.dev_out) + (long long)row * D;
-    for (int x2 = 0; x2 < (D + 63) / 64; ++x2)
-        if (x2 * 64 + lane < D) out[x2 * 64 + lane] = (T)(any ? o[x2] / l : 0.0f);
+}
+
+// Joins the parts of a row: four columns a thread, always in the same order.
+template <int D, bool BF>
+__global__ __launch_bounds__(256) void combine_kernel(const float *part_o, const f32x2 *part_ml, int splits, long long rows, void *out)
+{
+    using T = std::conditional_t<BF, __bf16, _Float16>;
+    typedef T tx4 __attribute__((ext_vector_type(4)));
+    constexpr int EACH = D / 4;
+    const long long row = (long long)blockIdx.x * (256 / EACH) + threadIdx.x / EACH;
+    if (row >= rows) return;
+    const int col = threadIdx.x % EACH * 4;
+    float m = neg_inf();
+    for (int s = 0; s < splits; ++s) m = fmaxf(m, part_ml[s * rows + row][0]);
+    float l = 0.0f;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < splits; ++s) {
+        const f32x2 ml = part_ml[s * rows + row];
+        const float by = ml[0] == neg_inf() && ml[1] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml[0] - m);
+        l += ml[1] * by;
+        x += *reinterpret_cast<const f32x4 *>(part_o + (s * rows + row) * D + col) * by;
+    }
+    x *= l == 0.0f ? 0.0f : 1.0f / l;
+    *reinterpret_cast<tx4 *>(static_cast<T *>(out) + row * D + col) = __builtin_convertvector(x, tx4);
+}
+
+struct Plan {
+    int waves, splits, row_tiles, per;
+    long long rows;  // of the whole call
+};
+
+Plan plan_of(const Cache &c, const rec_query &q)
+{
+    Plan p;
+    p.per = q.heads / c.kv_heads;
+    p.rows = (long long)q.batch * q.queries * q.heads;
+    const long long rows = (long long)q.queries * p.per;
+    p.row_tiles = (int)((rows + ROWS - 1) / ROWS);
+    const long long pairs = (long long)q.batch * c.kv_heads * p.row_tiles;
+    // Most tiles that a wave's rows can see something of.
+    long long tiles = (((long long)q.table_width << c.page_shift) + TILE - 1) / TILE;
+    if (q.window) {
+        const long long apart = q.candidates ? 0 : std::min<long long>(q.queries - 1, (ROWS - 1) / p.per + 1);
+        tiles = std::min(tiles, (q.window + apart + TILE - 2) / TILE + 1 + (q.sinks + TILE - 1ll) / TILE);
+    }
+    p.waves = tiles >= 4 && pairs < 16 * CUS ? 4 : tiles >= 2 && pairs < 32 * CUS ? 2 : 1;
+    p.splits = 1;
+    if (pairs * p.waves < 12 * CUS && tiles > 2 * p.waves)
+        p.splits = (int)std::max(1ll, std::min({(tiles + 2 * p.waves - 1) / (2 * p.waves), (16 * CUS + pairs * p.waves - 1) / (pairs * p.waves), 64ll}));
+    return p;
+}
+
+template <int FMT, int D, bool BF>
+hipError_t attend_as(const AttendArgs &a, const Plan &p, hipStream_t s)
+{
+    const dim3 grid((unsigned)((long long)a.q.batch * a.c.kv_heads * p.row_tiles * p.splits));
+    if (p.waves == 4) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 4>), grid, dim3(256), 0, s, a);
+    else if (p.waves == 2) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 2>), grid, dim3(128), 0, s, a);
+    else hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1>), grid, dim3(64), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int each = 256 / (D / 4);
+    hipLaunchKernelGGL((combine_kernel<D, BF>), dim3((unsigned)((p.rows + each - 1) / each)), dim3(256), 0, s, a.part_o, a.part_ml, p.splits,
+                       p.rows, a.q.dev_out);
+    return hipGetLastError();
 }
 
 template <int FMT, int D>
-hipError_t attend_as(const Cache &c, const rec_query &q, hipStream_t s)
+hipError_t attend_of(const AttendArgs &a, const Plan &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)((long long)q.batch * q.queries * q.heads));
-    if (q.dtype == REC_BF16) hipLaunchKernelGGL((attend_kernel<FMT, D, true>), grid, dim3(64), 0, s, c, q);
-    else hipLaunchKernelGGL((attend_kernel<FMT, D, false>), grid, dim3(64), 0, s, c, q);
-    return hipGetLastError();
+    return a.q.dtype == REC_BF16 ? attend_as<FMT, D, true>(a, p, s) : attend_as<FMT, D, false>(a, p, s);
 }
 
 }  // namespace
 
-size_t attend_workspace(const Cache &, int, int, const rec_query &) { return 0; }
-
-hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *, hipStream_t s)
+size_t attend_workspace(const Cache &c, int, int d, const rec_query &q)
 {
+    if (q.batch == 0 || q.queries == 0) return 0;
+    const Plan p = plan_of(c, q);
+    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)p.rows * ((size_t)d * sizeof(float) + sizeof(f32x2));
+}
+
+hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *workspace, hipStream_t s)
+{
+    const Plan p = plan_of(c, q);
+    AttendArgs a;
+    a.c = c;
+    a.q = q;
+    a.per = p.per;
+    a.rows = (int)((long long)q.queries * p.per);
+    a.row_tiles = p.row_tiles;
+    a.splits = p.splits;
+    a.part_o = static_cast<float *>(workspace);
+    a.part_ml = reinterpret_cast<f32x2 *>(a.part_o + (p.splits > 1 ? p.splits * p.rows * d : 0));
     if (format == REC_MX4)
-        return d == 32 ? attend_as<REC_MX4, 32>(c, q, s) : d == 64 ? attend_as<REC_MX4, 64>(c, q, s) : attend_as<REC_MX4, 128>(c, q, s);
-    return d == 32 ? attend_as<REC_MX8, 32>(c, q, s) : d == 64 ? attend_as<REC_MX8, 64>(c, q, s) : attend_as<REC_MX8, 128>(c, q, s);
+        return d == 32 ? attend_of<REC_MX4, 32>(a, p, s) : d == 64 ? attend_of<REC_MX4, 64>(a, p, s) : attend_of<REC_MX4, 128>(a, p, s);
+    return d == 32 ? attend_of<REC_MX8, 32>(a, p, s) : d == 64 ? attend_of<REC_MX8, 64>(a, p, s) : attend_of<REC_MX8, 128>(a, p, s);
 }
 
 }  // namespace hist

@@ -286,6 +286,23 @@ def test_bad_lengths_and_pages_are_reported(b):
     assert not got.any() and s.cache.check() == (b.REC_ERR_LENGTHS, 0, b.REC_FAULT_LENGTH)
 
 
+@pytest.mark.parametrize("fmt,fill", [("mx8", 127), ("mx8", 126), ("mx4", 254)])
+def test_places_that_were_never_written(b, fmt, fill):
+    """Bytes that are NaN or huge numbers under finite scales, behind a history's end and before its window."""
+    lengths = [1, 50, 64, 90, 100]
+    s = Histories(b, lengths, 1, 64, fmt, 32, seed=15)
+    written = s.cache.read(s.slots.cuda(), F32)
+    s.cache.pages.fill_(fill)
+    s.cache.write(*written, s.slots.cuda())
+    q = torch.randn(5, 3, 2, 64, generator=gen(5)).to(BF).cuda()
+    for window, sinks in ((0, 0), (9, 1)):
+        table = s.table.clone()
+        if window:
+            table[3, 1], table[4, 1] = -1, s.cache.pages.shape[0] - 1   # freed, and given to nobody yet
+        O.assert_close(s.cache.attend(q, table, s.len_t, window=window, sinks=sinks), *s.expect(q, 0.125, window, sinks, False), (window, sinks))
+        assert s.cache.check()[0] == b.REC_OK
+
+
 @pytest.mark.parametrize("fmt", ["mx4", "mx8"])
 def test_what_a_query_does_not_see_has_no_part(b, fmt):
     """NaN keys and values outside the window, and behind a query's own position."""
