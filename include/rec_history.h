@@ -164,7 +164,7 @@ REC_API size_t rec_history_attend_workspace_bytes(const rec_history *h, const re
  * REC_ERR_ARG: null, misaligned, bad enum, negative counts, a workspace too small;
  * REC_ERR_SHAPE: heads no multiple of kv_heads, or a shape that rec_history_bytes()
  * refuses; REC_ERR_OVERFLOW: batch * queries * heads >= 2^31, or table_width * page_tokens
- * > 2^31 - 1024. */
+ * > 2^31 - 1024, or more threads than a launch can have (2^32). */
 REC_API rec_status rec_history_attend(const rec_history *h, const rec_query *q, void *dev_workspace,
                                       size_t workspace_bytes, void *stream);
 
@@ -179,7 +179,9 @@ REC_API rec_status rec_history_attend(const rec_history *h, const rec_query *q, 
  *   dev_fault     as in rec_history; may be null
  * Device faults: REC_FAULT_LENGTH (offsets that decrease, or do not run from 0 to tokens,
  * are brought into that range; rows of no history are not written).
- * REC_ERR_ARG, REC_ERR_SHAPE as above; REC_ERR_OVERFLOW: tokens * heads >= 2^31.
+ * REC_ERR_ARG, REC_ERR_SHAPE as above; REC_ERR_OVERFLOW: tokens * heads >= 2^31, more
+ * than 2^24 workgroups (tokens * heads / 128 + batch * kv_heads), a token stride of k or v that is
+ * negative or >= 2^23 elements.
  */
 typedef struct {
     rec_rows q, k, v;

@@ -62,8 +62,10 @@ hipError_t launch_write(const Cache &c, int format, int d, const rec_rows &k, co
                         const int64_t *slots, long long tokens, hipStream_t s);
 hipError_t launch_read(const Cache &c, int format, int d, const int64_t *slots, long long tokens, int dtype,
                        void *k, void *v, hipStream_t s);
+long long attend_threads(const Cache &c, const rec_query &q);
 size_t attend_workspace(const Cache &c, int format, int d, const rec_query &q);
 hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *workspace, hipStream_t s);
+long long window_blocks(const rec_window &w);  // of 256 threads
 hipError_t launch_window(const rec_window &w, hipStream_t s);
 hipError_t launch_clear_faults(unsigned long long *fault, hipStream_t s);
 

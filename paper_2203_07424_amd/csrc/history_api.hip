@@ -8,6 +8,9 @@ using rec::hist::Cache;
 // Of a history: the kernels count a little past the last one in 32 bits.
 constexpr int64_t MOST_TOKENS = (1ll << 31) - 1024;
 
+// What a launch counts its threads in.
+constexpr int64_t MOST_THREADS = (1ll << 32) - 1;
+
 bool head_dim_fits(int d) { return d == 32 || d == 64 || d == 128; }
 
 bool shape_fits(const rec_history *h)
@@ -56,13 +59,16 @@ rec_status check_query(const rec_history *h, const rec_query *q)
     if ((int64_t)q->table_width * h->page_tokens > MOST_TOKENS || (int64_t)q->queries * q->heads >= 1ll << 31 ||
         (int64_t)q->queries * q->heads * q->batch >= 1ll << 31)
         return REC_ERR_OVERFLOW;
-    return REC_OK;
+    return rec::hist::attend_threads(cache_of(h), *q) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
 }
 
 bool rows_fit(const rec_rows &r, int size)
 {
     return aligned(r.dev) && stride_fits(r.token_stride, size) && stride_fits(r.head_stride, size);
 }
+
+// Tiles of 64 rows are addressed from their first one in 31 bits.
+bool tiles_fit(const rec_rows &r) { return r.token_stride >= 0 && r.token_stride < 1ll << 23; }
 
 rec_status status_of(hipError_t e) { return e == hipSuccess ? REC_OK : REC_ERR_DEVICE; }
 
@@ -129,7 +135,8 @@ rec_status rec_window_attend(const rec_window *w, void *stream)
         w->window < 0 || w->sinks < 0)
         return REC_ERR_ARG;
     if (!head_dim_fits(w->head_dim) || w->heads % w->kv_heads) return REC_ERR_SHAPE;
-    if (w->tokens >= 1ll << 31 || w->tokens * w->heads >= 1ll << 31) return REC_ERR_OVERFLOW;
+    if (w->tokens > MOST_TOKENS || w->tokens * w->heads >= 1ll << 31) return REC_ERR_OVERFLOW;
+    if (rec::hist::window_blocks(*w) * 256 > MOST_THREADS || !tiles_fit(w->k) || !tiles_fit(w->v)) return REC_ERR_OVERFLOW;
     if (w->tokens == 0 || w->batch == 0) return REC_OK;
     if (!rows_fit(w->q, 2) || !rows_fit(w->k, 2) || !rows_fit(w->v, 2) || !aligned(w->dev_out) || !w->dev_offsets) return REC_ERR_ARG;
     return status_of(rec::hist::launch_window(*w, static_cast<hipStream_t>(stream)));

@@ -617,6 +617,12 @@ hipError_t attend_of(const AttendArgs &a, const Plan &p, hipStream_t s)
 
 }  // namespace
 
+long long attend_threads(const Cache &c, const rec_query &q)
+{
+    const Plan p = plan_of(c, q);
+    return (long long)q.batch * c.kv_heads * p.row_tiles * p.splits * 64 * p.waves;
+}
+
 size_t attend_workspace(const Cache &c, int, int d, const rec_query &q)
 {
     if (q.batch == 0 || q.queries == 0) return 0;

@@ -1,91 +1,351 @@
-// Attention of whole histories to themselves: a wave a query row, a lane a key.
+// Attention of whole, ragged histories to themselves, over a window and a few first events.
+//
+// A block has 128 query rows of one history and kv head (the heads that share it, token
+// after token, so that a block spans few positions) and walks over tiles of 64 keys that
+// some of them sees.  Keys and values pass through two buffers in LDS: while a tile is
+// computed the next one is on its way into registers.  A wave has 32 rows.
+//
+// Scores come transposed, S^T = K Q^T (32 x 32 x 16), so that a lane holds 16 scores of
+// one row for each half of a tile, and those, exponentiated and narrowed, are the operand of
+// O^T += V^T P^T as they stand: k of that product is a key in the order of the registers.
+// V^T comes out of LDS by transposing reads (4 keys of a column each), which give just the
+// four neighbouring keys that a lane's four neighbouring scores belong to.
+//
+// LDS rows have no padding; the 16-byte pieces of a row are exchanged by the low bits of its
+// number instead, so that 8 rows read at one column lie in different banks.
+//
+// The running maximum moves only when a tile's exceeds it by 2^8.  Masks are looked at in
+// tiles that some row of the wave sees partly, and a masked weight is 0.  Since 0 * NaN is NaN,
+// a row whose result is NaN is computed again, key by key, from the keys it sees (redo_row()).
+#include <algorithm>
+
 #include "history.h"
 
 namespace rec {
 namespace hist {
 namespace {
 
-template <int D, bool BF>
-__global__ __launch_bounds__(64) void window_kernel(rec_window w)
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr int WAVES = 4, THREADS = 64 * WAVES;
+constexpr int WAVE_ROWS = 32, BLOCK_ROWS = WAVE_ROWS * WAVES;
+constexpr int TILE = 64;       // keys
+constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
+
+struct WindowArgs {
+    rec_window w;
+    int per;    // query heads of a kv head
+    int tiles;  // of BLOCK_ROWS, more than there can be
+};
+
+__device__ inline float neg_inf() { return -__builtin_inff(); }
+
+template <bool BF>
+__device__ inline f32x16 product(u32x4 a, u32x4 b, f32x16 c)
 {
-    __shared__ float qs[D], ps[64];
-    using T = std::conditional_t<BF, __bf16, _Float16>;
-    const int lane = threadIdx.x;
-    const unsigned row = blockIdx.x;
-    const int head = (int)(row % (unsigned)w.heads), token = (int)(row / (unsigned)w.heads), kv = head / (w.heads / w.kv_heads);
-    int lo = 0, hi = w.batch;  // the last history that starts at or before the token
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (w.dev_offsets[mid] <= token) lo = mid;
-        else hi = mid;
-    }
-    const int start = w.dev_offsets[lo], end = w.dev_offsets[lo + 1];
-    if (start < 0 || start > token || end <= token) return;
-    const int pos = token - start;
-    const T *src = static_cast<const T *>(w.q.dev) + token * w.q.token_stride + head * w.q.head_stride;
-    const T *k = static_cast<const T *>(w.k.dev) + start * w.k.token_stride + kv * w.k.head_stride;
-    const T *v = static_cast<const T *>(w.v.dev) + start * w.v.token_stride + kv * w.v.head_stride;
-    for (int x = lane; x < D; x += 64) qs[x] = (float)src[x];
-    __syncthreads();
-    float m = -__builtin_inff(), l = 0.0f, o[(D + 63) / 64] = {};
-    for (int t0 = 0; t0 <= pos; t0 += 64) {
-        const int j = t0 + lane;
-        const bool seen = j <= pos && (w.window == 0 || pos - j < w.window || j < w.sinks);
-        float x = -__builtin_inff();
-        if (seen) {
-            float sum = 0.0f;
-            for (int e = 0; e < D; ++e) sum += qs[e] * (float)k[j * w.k.token_stride + e];
-            x = sum * w.scale;
-        }
-        float mt = x;
-        for (int s = 32; s; s >>= 1) mt = fmaxf(mt, __shfl_xor(mt, s));
-        const float mn = fmaxf(m, mt), ref = mn == -__builtin_inff() ? 0.0f : mn;
-        const float p = seen ? __expf(x - ref) : 0.0f, alpha = __expf(m - ref);
-        m = mn;
-        float sum = p;
-        for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
-        l = l * alpha + sum;
-        ps[lane] = p;
-        const unsigned long long who = __ballot(seen);
-        for (int x2 = 0; x2 < (D + 63) / 64; ++x2) {
-            const int el = x2 * 64 + lane;
-            float acc = o[x2] * alpha;
-            for (int s = 0; s < 64; ++s)
-                if ((who >> s & 1) && el < D) acc += ps[s] * (float)v[(t0 + s) * w.v.token_stride + el];
-            o[x2] = acc;
-        }
-        __syncthreads();
-    }
-    T *out = static_cast<T *>(w.dev_out) + (long long)row * D;
-    for (int x2 = 0; x2 < (D + 63) / 64; ++x2)
-        if (x2 * 64 + lane < D) out[x2 * 64 + lane] = (T)(o[x2] / l);
+    if constexpr (BF) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// Offsets run from 0 to tokens and never decrease.
-__global__ __launch_bounds__(256) void check_offsets_kernel(const int32_t *offsets, int batch, long long tokens, unsigned long long *fault)
+template <bool BF>
+__device__ inline unsigned pack(float a, float b)
 {
-    for (long long b = (long long)blockIdx.x * 256 + threadIdx.x; b < batch; b += 256ll * gridDim.x)
-        if (offsets[b] > offsets[b + 1] || (b == 0 && offsets[0] != 0) || (b == batch - 1 && offsets[batch] != tokens))
-            report(fault, REC_FAULT_LENGTH, (unsigned long long)b);
+    if constexpr (BF) {
+        const bf16x2 r = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(unsigned, r);
+    } else {
+        const f16x2 r = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(unsigned, r);
+    }
+}
+
+// s + the two numbers of w.
+template <bool BF>
+__device__ inline float add_pair(unsigned w, float s)
+{
+    if constexpr (BF) {
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), ones, s, false);
+    } else {
+        const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), ones, s, false);
+    }
+}
+
+// Where a 16-byte piece of a row is among the row's.
+template <int D>
+__device__ inline int place(int row, int piece)
+{
+    return D == 32 ? piece ^ ((row >> 1) & 3) : piece ^ (row & 7);
+}
+
+__device__ inline bool sees(int pos, int j, int window, int sinks) { return j <= pos && (pos - j < window || j < sinks); }
+
+// A history's share of the grid starts at this tile: every history has room for its rows'
+// tiles between its own start and the next one's, whatever the lengths.
+__device__ inline long long first_tile(long long offset, int per, int b) { return offset * per / BLOCK_ROWS + b; }
+
+// One row by a wave, from nothing but what it sees.
+template <int D, typename T>
+__device__ void redo_row(const T *q, const T *k, long long k_stride, const T *v, long long v_stride, int pos, float factor, int window,
+                         int sinks, T *out, int lane)
+{
+    constexpr int EACH = (D + 63) / 64;
+    float m = neg_inf(), l = 0.0f, o[EACH] = {};
+    for (int t0 = 0; t0 <= pos; t0 += 64) {
+        const int j = t0 + lane;
+        const bool seen = sees(pos, j, window, sinks);
+        float x = neg_inf();
+        if (seen) {
+            x = 0.0f;
+            for (int e = 0; e < D; ++e) x += (float)q[e] * (float)k[j * k_stride + e];
+            x *= factor;
+        }
+        const unsigned long long who = __ballot(seen);
+        if (!who) continue;
+        float most = x;
+        for (int s = 32; s; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+        const float next = fmaxf(m, most);
+        const float p = seen ? __builtin_amdgcn_exp2f(x - next) : 0.0f;
+        const float down = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+        m = next;
+        float sum = p;
+        for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
+        l = l * down + sum;
+        for (int i = 0; i < EACH; ++i) o[i] *= down;
+        for (int s = 0; s < 64; ++s) {
+            if (!(who >> s & 1)) continue;
+            const float ps = __shfl(p, s);
+            for (int i = 0; i < EACH; ++i)
+                if (64 * i + lane < D) o[i] += ps * (float)v[(t0 + s) * v_stride + 64 * i + lane];
+        }
+    }
+    for (int i = 0; i < EACH; ++i)
+        if (64 * i + lane < D) out[64 * i + lane] = (T)(o[i] / l);
+}
+
+template <int D, bool BF>
+__global__ __launch_bounds__(THREADS, 2) void window_kernel(WindowArgs a)
+{
+    using T = std::conditional_t<BF, __bf16, _Float16>;
+    constexpr int ROW_BYTES = 2 * D, PIECES = D / 8, LOADS = TILE * PIECES / THREADS;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][TILE * ROW_BYTES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, half = lane >> 5;
+    const rec_window &w = a.w;
+    const int kv = (int)(blockIdx.x % (unsigned)w.kv_heads);
+    // Late rows see most: they start first.
+    const long long x = a.tiles - 1 - (long long)(blockIdx.x / (unsigned)w.kv_heads);
+
+    if (w.dev_fault && blockIdx.x == 0)
+        for (int b = threadIdx.x; b < w.batch; b += THREADS)
+            if (w.dev_offsets[b] > w.dev_offsets[b + 1] || (b == 0 && w.dev_offsets[0] != 0) || (b == w.batch - 1 && w.dev_offsets[b + 1] != w.tokens))
+                report(reinterpret_cast<unsigned long long *>(w.dev_fault), REC_FAULT_LENGTH, (unsigned long long)b);
+
+    // The last history whose tiles start at or before this one, 64 candidates a step.
+    auto offset_of = [&](int b) { return (int)min(max((long long)w.dev_offsets[b], 0ll), (long long)w.tokens); };
+    int b = 0;
+    for (int n = w.batch; n > 1;) {
+        const int step = (n + 63) / 64, at = b + lane * step;
+        const bool ok = lane * step < n && first_tile(offset_of(at), a.per, at) <= x;
+        const int count = max(__popcll(__ballot(ok)), 1);
+        b += (count - 1) * step;
+        n = min(step, n - (count - 1) * step);
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    const int start = offset_of(b), len = max(offset_of(b + 1) - start, 0);
+    const long long first_row = (x - first_tile(start, a.per, b)) * BLOCK_ROWS, all_rows = (long long)len * a.per;
+    if (first_row < 0 || first_row >= all_rows) return;
+
+    const int window = w.window == 0 ? 0x7fffffff : w.window, sinks = w.sinks;
+    auto pos_of = [&](long long row) { return (int)((unsigned)min(row, all_rows - 1) / (unsigned)a.per); };
+    const int p_lo = pos_of(first_row), p_hi = pos_of(first_row + BLOCK_ROWS - 1);
+    const long long wave_row = first_row + wave * WAVE_ROWS;
+    const bool busy = wave_row < all_rows;
+    const int w_lo = pos_of(wave_row), w_hi = pos_of(wave_row + WAVE_ROWS - 1), pos = pos_of(wave_row + c);
+    const int my_head = kv * a.per + (int)(min(wave_row + c, all_rows - 1) - (long long)pos * a.per);
+    const T *k_base = static_cast<const T *>(w.k.dev) + (long long)start * w.k.token_stride + (long long)kv * w.k.head_stride;
+    const T *v_base = static_cast<const T *>(w.v.dev) + (long long)start * w.v.token_stride + (long long)kv * w.v.head_stride;
+    const T *q_row = static_cast<const T *>(w.q.dev) + (long long)(start + pos) * w.q.token_stride + (long long)my_head * w.q.head_stride;
+
+    u32x4 q[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        q[i] = *reinterpret_cast<const u32x4 *>(q_row + 16 * i + 8 * half);
+        if (w.scale < 0.0f) q[i] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+    }
+    const float factor = __builtin_fabsf(w.scale) * 1.44269504088896341f;
+
+    const int n_to = p_hi / TILE + 1, n_from = max(p_lo - window + 1, 0) / TILE;
+    const int n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from), count = n_sink + n_to - n_from;
+    auto key_of = [&](int n) { return (n < n_sink ? n : n_from + n - n_sink) * TILE; };
+
+    // A thread's pieces of a tile: rows behind the history's end come as zeros.
+    u32x4 in_k[LOADS], in_v[LOADS];
+    auto fetch = [&](int key) {
+        const int rows = min(TILE, len - key);
+        const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(k_base + key * w.k.token_stride), 0,
+                                                          (int)(2 * (rows - 1) * w.k.token_stride + ROW_BYTES), 0x00020000);
+        const auto rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(v_base + key * w.v.token_stride), 0,
+                                                          (int)(2 * (rows - 1) * w.v.token_stride + ROW_BYTES), 0x00020000);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int n = i * THREADS + threadIdx.x, row = n / PIECES, piece = n % PIECES;
+            // A zero stride has all rows in the first one's place.
+            in_k[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, row * (int)w.k.token_stride * 2 + piece * 16, 0, 0);
+            in_v[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, row * (int)w.v.token_stride * 2 + piece * 16, 0, 0);
+        }
+    };
+    auto stage = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int n = i * THREADS + threadIdx.x, row = n / PIECES, piece = n % PIECES;
+            const int at = row * ROW_BYTES + 16 * place<D>(row, piece);
+            *reinterpret_cast<u32x4 *>(&lds[buffer][0][at]) = in_k[i];
+            *reinterpret_cast<u32x4 *>(&lds[buffer][1][at]) = in_v[i];
+        }
+    };
+
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
+    float m = neg_inf(), l = 0.0f;
+
+    fetch(key_of(0));
+    stage(0);
+    __syncthreads();
+    for (int n = 0; n < count; ++n) {
+        const int key = key_of(n);
+        if (n + 1 < count) fetch(key_of(n + 1));
+        // Something in it for this wave.
+        if (busy && key <= w_hi && (key + TILE > w_lo - window + 1 || key < sinks)) {
+            const unsigned char *kt = lds[n & 1][0], *vt = lds[n & 1][1];
+            f32x16 s[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const u32x4 kk = *reinterpret_cast<const u32x4 *>(kt + (32 * u + c) * ROW_BYTES + 16 * place<D>(c, 2 * i + half));
+                    s[u] = product<BF>(kk, q[i], s[u]);
+                }
+            }
+            const bool whole = key + TILE - 1 <= w_lo && (key > w_hi - window || key + TILE <= sinks);
+            if (!whole)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!sees(pos, key + 32 * u + 8 * (r >> 2) + 4 * half + (r & 3), window, sinks)) s[u][r] = neg_inf();
+            float most = neg_inf();
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, s[u][r]);
+            most = fmaxf(most, __shfl_xor(most, 32));
+            most = most == neg_inf() ? most : most * factor;
+            if (__any(most > m + SLACK)) {
+                const float next = fmaxf(m, most);
+                const float down = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) o[i] *= down;
+                l *= down;
+                m = next;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], factor, -m));
+            if (!whole)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!sees(pos, key + 32 * u + 8 * (r >> 2) + 4 * half + (r & 3), window, sinks)) s[u][r] = 0.0f;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    u32x4 p;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[i] = pack<BF>(s[u][8 * t + 2 * i], s[u][8 * t + 2 * i + 1]);
+                        l = add_pair<BF>(p[i], l);
+                    }
+                    const int row = 32 * u + 16 * t + 4 * half + ((lane & 15) >> 2);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const int piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+                        const unsigned char *at = vt + row * ROW_BYTES + 16 * place<D>(row, piece) + 8 * (lane & 1);
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * ROW_BYTES));
+                        const u32x2 lo2 = __builtin_bit_cast(u32x2, lo), hi2 = __builtin_bit_cast(u32x2, hi);
+                        o[i] = product<BF>(u32x4{lo2[0], lo2[1], hi2[0], hi2[1]}, p, o[i]);
+                    }
+                }
+        }
+        if (n + 1 < count) {
+            stage((n + 1) & 1);
+            __syncthreads();
+        }
+    }
+    if (!busy) return;
+
+    l += __shfl_xor(l, 32);
+    const float by = 1.0f / l;
+    bool bad = false;
+    const bool real = wave_row + c < all_rows;
+    T *out = static_cast<T *>(w.dev_out) + ((long long)(start + pos) * w.heads + my_head) * D;
+    typedef T tx4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 y = f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]} * by;
+            bad |= y[0] != y[0] || y[1] != y[1] || y[2] != y[2] || y[3] != y[3];
+            if (real) *reinterpret_cast<tx4 *>(out + 32 * i + 8 * (r >> 2) + 4 * half) = __builtin_convertvector(y, tx4);
+        }
+    unsigned long long again = __ballot(bad && real);
+    again |= again >> 32;
+    for (unsigned rows = (unsigned)again; rows; rows &= rows - 1) {
+        const int r = __builtin_ctz(rows), p = pos_of(wave_row + r), head = kv * a.per + (int)(wave_row + r - (long long)p * a.per);
+        redo_row<D, T>(static_cast<const T *>(w.q.dev) + (long long)(start + p) * w.q.token_stride + (long long)head * w.q.head_stride, k_base,
+                       w.k.token_stride, v_base, w.v.token_stride, p, w.scale * 1.44269504088896341f, window, sinks,
+                       static_cast<T *>(w.dev_out) + ((long long)(start + p) * w.heads + head) * D, lane);
+    }
 }
 
 template <int D>
-hipError_t window_as(const rec_window &w, hipStream_t s)
+hipError_t window_as(const WindowArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(w.tokens * w.heads));
-    if (w.dtype == REC_BF16) hipLaunchKernelGGL((window_kernel<D, true>), grid, dim3(64), 0, s, w);
-    else hipLaunchKernelGGL((window_kernel<D, false>), grid, dim3(64), 0, s, w);
-    if (w.dev_fault)
-        hipLaunchKernelGGL(check_offsets_kernel, dim3(1), dim3(256), 0, s, w.dev_offsets, w.batch, (long long)w.tokens,
-                           reinterpret_cast<unsigned long long *>(w.dev_fault));
+    const dim3 grid((unsigned)a.tiles * (unsigned)a.w.kv_heads);
+    if (a.w.dtype == REC_BF16) hipLaunchKernelGGL((window_kernel<D, true>), grid, dim3(THREADS), 0, s, a);
+    else hipLaunchKernelGGL((window_kernel<D, false>), grid, dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
+long long window_blocks(const rec_window &w)
+{
+    return (w.tokens * (w.heads / w.kv_heads) / BLOCK_ROWS + w.batch) * w.kv_heads;
+}
+
 hipError_t launch_window(const rec_window &w, hipStream_t s)
 {
-    return w.head_dim == 32 ? window_as<32>(w, s) : w.head_dim == 64 ? window_as<64>(w, s) : window_as<128>(w, s);
+    WindowArgs a;
+    a.w = w;
+    a.per = w.heads / w.kv_heads;
+    a.tiles = (int)(window_blocks(w) / w.kv_heads);
+    return w.head_dim == 32 ? window_as<32>(a, s) : w.head_dim == 64 ? window_as<64>(a, s) : window_as<128>(a, s);
 }
 
 }  // namespace hist
