@@ -44,7 +44,7 @@ rec_status check_rows(const rec_history *h, int32_t dtype, const int64_t *dev_sl
     if (!shape_fits(h)) return REC_ERR_SHAPE;
     if (!aligned(h->dev_pages) || (dtype != REC_F32 && dtype != REC_F16 && dtype != REC_BF16) || tokens < 0) return REC_ERR_ARG;
     if (tokens && (!dev_slots || (reinterpret_cast<uintptr_t>(dev_slots) & 7u))) return REC_ERR_ARG;
-    if (tokens >= 1ll << 31 || tokens * h->kv_heads >= 1ll << 31) return REC_ERR_OVERFLOW;
+    if (tokens >= 1ll << 30 || tokens * h->kv_heads >= 1ll << 30) return REC_ERR_OVERFLOW;
     return REC_OK;
 }
 

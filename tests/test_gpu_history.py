@@ -101,6 +101,35 @@ def test_runs_of_consecutive_slots(b, fmt, start, n, page_tokens):
         assert torch.equal(rk.cpu().double(), torch.from_numpy(got_k[pick])) and torch.equal(rv.cpu().double(), torch.from_numpy(got_v[pick]))
 
 
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("d,kv,dtype", [(32, 3, F32), (64, 1, HF), (128, 2, BF)])
+def test_lists_of_many_runs(b, fmt, d, kv, dtype):
+    """Histories one after the other in the list, from 1 to 70 events, padded in between: groups start anywhere in it."""
+    g = gen(31)
+    slots, page = [], 0
+    for n in torch.randint(1, 71, (40,), generator=g).tolist():
+        first = int(torch.randint(0, 20, (1,), generator=g))
+        slots += list(range(page * 32 + first, page * 32 + first + n)) + [-1] * int(torch.randint(0, 3, (1,), generator=g))
+        page += -(-(first + n) // 32)
+    slots = torch.tensor(slots)
+    c = new_cache(b, page, 32, kv, d, fmt)
+    k, v = tricky(len(slots), kv, d, dtype, 7), tricky(len(slots), kv, d, dtype, 8)
+    c.write(k.cuda(), v.cuda(), slots.cuda())
+    assert c.check()[0] == b.REC_OK
+    e = new_cache(b, page, 32, kv, d, fmt)
+    for i in torch.randperm(len(slots), generator=g).split(9):      # the same rows in no order: one by one
+        e.write(k[i].cuda(), v[i].cuda(), slots[i].cuda())
+    assert torch.equal(c.pages, e.pages)
+    there = slots >= 0
+    got_k, got_v = stored(c, fmt, d, 32, slots[there].tolist(), kv)
+    for x, got in ((k, got_k), (v, got_v)):
+        codes, scales = O.quantise(x[there].double().numpy().reshape(-1, 32), fmt)
+        assert np.array_equal(got.reshape(-1, 32), O.values(codes, fmt) * O.scale_values(scales)[:, None])
+    rk, rv = c.read(slots.cuda(), F32)
+    for r, got in ((rk, got_k), (rv, got_v)):
+        assert torch.equal(r[there].cpu().double(), torch.from_numpy(got)) and not r[~there].any()
+
+
 def test_strided_rows_and_padding_slots(b):
     d, kv, n = 64, 2, 40
     whole = torch.randn(n, 9, d, generator=gen(9)).to(BF).cuda()
