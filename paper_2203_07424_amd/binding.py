@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, Optional, Sequence, Tuple
 
 import torch  # loads the HIP runtime the library binds to
@@ -152,20 +153,24 @@ _lib.rec_probe_dense_copy.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32
 _lib.rec_probe_fc_form.restype = C.c_int
 _lib.rec_probe_fc_form.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_uint32, C.c_int32, C.POINTER(C.c_int32)]
 
+# Structures go in by address: a ctypes structure by reference, or one packed into bytes.
 _lib.rec_history_bytes.restype = C.c_size_t
-_lib.rec_history_bytes.argtypes = [C.POINTER(rec_history)]
+_lib.rec_history_bytes.argtypes = [_vp]
 _lib.rec_history_write.restype = C.c_int
-_lib.rec_history_write.argtypes = [C.POINTER(rec_history), C.POINTER(rec_rows), C.POINTER(rec_rows), C.c_int32, _vp, C.c_int64, _vp]
+_lib.rec_history_write.argtypes = [_vp, _vp, _vp, C.c_int32, _vp, C.c_int64, _vp]
 _lib.rec_history_read.restype = C.c_int
-_lib.rec_history_read.argtypes = [C.POINTER(rec_history), _vp, C.c_int64, C.c_int32, _vp, _vp, _vp]
+_lib.rec_history_read.argtypes = [_vp, _vp, C.c_int64, C.c_int32, _vp, _vp, _vp]
 _lib.rec_history_attend_workspace_bytes.restype = C.c_size_t
-_lib.rec_history_attend_workspace_bytes.argtypes = [C.POINTER(rec_history), C.POINTER(rec_query)]
+_lib.rec_history_attend_workspace_bytes.argtypes = [_vp, _vp]
 _lib.rec_history_attend.restype = C.c_int
-_lib.rec_history_attend.argtypes = [C.POINTER(rec_history), C.POINTER(rec_query), _vp, C.c_size_t, _vp]
+_lib.rec_history_attend.argtypes = [_vp, _vp, _vp, C.c_size_t, _vp]
 _lib.rec_window_attend.restype = C.c_int
-_lib.rec_window_attend.argtypes = [C.POINTER(rec_window), _vp]
+_lib.rec_window_attend.argtypes = [_vp, _vp]
 _lib.rec_history_check.restype = C.c_int
 _lib.rec_history_check.argtypes = [_vp, _vp, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
+# The same layouts for one packing call, a quarter of the time of setting a structure's fields.
+_ROWS, _QUERY, _WINDOW = struct.Struct("@Pqq"), struct.Struct("@PPqqqiiiiPqiPfiii"), struct.Struct("@PqqPqqPqqPiiqiiiPfiiP")
+assert (_ROWS.size, _QUERY.size, _WINDOW.size) == (C.sizeof(rec_rows), C.sizeof(rec_query), C.sizeof(rec_window))
 
 
 class RecError(RuntimeError):
@@ -583,15 +588,18 @@ class CapturedForward:
 _DTYPE_CODES = {torch.float32: REC_F32, torch.float16: REC_F16, torch.bfloat16: REC_BF16}
 _ATTEND_CODES = {torch.float16: REC_F16, torch.bfloat16: REC_BF16}
 _FORMATS = {"mx4": REC_MX4, "mx8": REC_MX8}
+_I64 = torch.int64
 
 
 def _faults(device) -> torch.Tensor:
     return torch.full((REC_FAULT_WORDS,), -1, dtype=torch.int64, device=device)
 
 
-def _check_int32(call: str, name: str, t: torch.Tensor, shape, device) -> None:
-    if t.dtype is not _I32 or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{call}: {name} must be a contiguous int32 tensor of shape {tuple(shape)} on {device}")
+def _stream_on(index: int, call: str) -> int:
+    """The current stream of device `index`, which has to be the current device: kernels start there."""
+    if torch._C._cuda_getDevice() != index:
+        raise ValueError(f"{call}: the tensors are on cuda:{index}, the current device is another")
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 class HistoryCache:
@@ -618,41 +626,52 @@ class HistoryCache:
             pages = torch.empty(shape, dtype=torch.uint8, device=device)
         elif not (pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous() and pages.numel() == nbytes):
             raise ValueError(f"HistoryCache: pages must be a contiguous uint8 device tensor of {nbytes} bytes")
-        self.pages, self.device = pages, pages.device
+        self.pages, self.device, self._index = pages, pages.device, pages.get_device()
         self.fault = _faults(self.device)
         self._h.dev_pages, self._h.dev_fault = pages.data_ptr(), self.fault.data_ptr()
-        self._k, self._v, self._q = rec_rows(), rec_rows(), rec_query()
+        self._ref = C.byref(self._h)
+        self._workspaces: dict = {}      # bytes by the shapes that decide them
 
     def _ok(self, st: int, where: str) -> None:
         if st != REC_OK:
             raise RecError(st, where)
 
     def _slots(self, call: str, slots: torch.Tensor) -> int:
-        if slots.dtype is not torch.int64 or slots.device != self.device or slots.dim() != 1 or not slots.is_contiguous():
+        if slots.dtype is not _I64 or slots.get_device() != self._index or slots.dim() != 1 or not slots.is_contiguous():
             raise ValueError(f"{call}: slots must be a contiguous int64 vector on {self.device}")
         return slots.shape[0]
+
+    def _rows(self, t: torch.Tensor, shape, dtype) -> bytes:
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index:
+            raise ValueError(f"rec_history_write: k and v must be {tuple(shape)} on {self.device}, both of one type")
+        token, head, column = t.stride()
+        if column != 1:
+            raise ValueError("rec_history_write: rows of k and v must be contiguous")
+        return _ROWS.pack(t.data_ptr(), token, head)
 
     def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
         """k, v: [tokens, kv_heads, head_dim] (any token and head strides), fp32, fp16 or bf16;
         slots: int64 [tokens], page * page_tokens + place, -1 for a row to leave out."""
         n = self._slots("rec_history_write", slots)
+        code = _DTYPE_CODES.get(k.dtype)
+        if code is None:
+            raise ValueError(f"rec_history_write: unsupported type {k.dtype}")
         shape = (n, self.kv_heads, self.head_dim)
-        for t, r in ((k, self._k), (v, self._v)):
-            if t.shape != shape or t.dtype not in _DTYPE_CODES or t.dtype is not k.dtype or t.device != self.device or t.stride(2) != 1:
-                raise ValueError(f"rec_history_write: k and v must be {shape} on {self.device}, of one floating type, rows contiguous")
-            r.dev, (r.token_stride, r.head_stride, _) = t.data_ptr(), t.stride()
-        st = rec_history_write(self._h, self._k, self._v, _DTYPE_CODES[k.dtype], slots, n)
+        st = _lib.rec_history_write(self._ref, self._rows(k, shape, k.dtype), self._rows(v, shape, k.dtype), code, slots.data_ptr(), n,
+                                    _stream_on(self._index, "rec_history_write"))
         if st:
             self._ok(st, "rec_history_write")
 
     def read(self, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16) -> Tuple[torch.Tensor, torch.Tensor]:
         """Keys and values of `slots` as [tokens, kv_heads, head_dim]; zeros for slot -1."""
         n = self._slots("rec_history_read", slots)
-        if dtype not in _DTYPE_CODES:
+        code = _DTYPE_CODES.get(dtype)
+        if code is None:
             raise ValueError(f"rec_history_read: unsupported type {dtype}")
-        shape = (n, self.kv_heads, self.head_dim)
-        k, v = torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device)
-        st = rec_history_read(self._h, slots, n, _DTYPE_CODES[dtype], k, v)
+        k = torch.empty((n, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
+        st = _lib.rec_history_read(self._ref, slots.data_ptr(), n, code, k.data_ptr(), v.data_ptr(),
+                                   _stream_on(self._index, "rec_history_read"))
         if st:
             self._ok(st, "rec_history_read")
         return k, v
@@ -662,29 +681,41 @@ class HistoryCache:
         """q: [batch, queries, heads, head_dim] or, one query each, [batch, heads, head_dim], fp16 or bf16
         (any strides but the last); pages_of: int32 [batch, width], a history's pages in order; lengths:
         int32 [batch].  scale: 1 / sqrt(head_dim) if None.  Returns attention outputs of q's shape, contiguous."""
-        q4 = q if q.dim() == 4 else q.unsqueeze(1)
-        batch, queries, heads, dim = q4.shape
-        if dim != self.head_dim or q.dtype not in _ATTEND_CODES or q.device != self.device or q4.stride(3) != 1:
-            raise ValueError(f"rec_history_attend: q must be fp16 or bf16 [batch, queries, heads, {self.head_dim}] on "
+        index, code = self._index, _ATTEND_CODES.get(q.dtype)
+        if q.dim() == 4:
+            batch, queries, heads, dim = q.shape
+            by_batch, by_query, by_head, by_column = q.stride()
+        elif q.dim() == 3:
+            (batch, heads, dim), queries = q.shape, 1
+            (by_batch, by_head, by_column), by_query = q.stride(), 0
+        else:
+            code = None
+        if code is None or dim != self.head_dim or q.get_device() != index or by_column != 1:
+            raise ValueError(f"rec_history_attend: q must be fp16 or bf16 [batch, (queries,) heads, {self.head_dim}] on "
                              f"{self.device}, rows contiguous")
-        if pages_of.dim() != 2 or pages_of.dtype is not _I32 or pages_of.device != self.device or pages_of.shape[0] != batch \
-                or pages_of.stride(1) != 1:
+        if pages_of.dim() != 2 or pages_of.dtype is not _I32 or pages_of.get_device() != index or pages_of.shape[0] != batch \
+                or (pages_of.stride(1) != 1 and pages_of.shape[1] > 1):
             raise ValueError(f"rec_history_attend: pages_of must be int32 [{batch}, width] on {self.device}, rows contiguous")
-        _check_int32("rec_history_attend", "lengths", lengths, (batch,), self.device)
+        if lengths.dtype is not _I32 or lengths.get_device() != index or lengths.shape != (batch,) or not lengths.is_contiguous():
+            raise ValueError(f"rec_history_attend: lengths must be a contiguous int32 [{batch}] on {self.device}")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-        elif out.shape != q.shape or out.dtype is not q.dtype or out.device != self.device or not out.is_contiguous():
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != index or not out.is_contiguous():
             raise ValueError("rec_history_attend: out must be contiguous and of q's shape, type and device")
-        r = self._q
-        r.dev_q, r.dev_out = q.data_ptr(), out.data_ptr()
-        r.batch_stride, r.query_stride, r.head_stride, _ = q4.stride()
-        r.dtype, r.batch, r.queries, r.heads = _ATTEND_CODES[q.dtype], batch, queries, heads
-        r.dev_pages_of, r.table_stride, r.table_width = pages_of.data_ptr(), pages_of.stride(0), pages_of.shape[1]
-        r.dev_lengths, r.scale = lengths.data_ptr(), dim ** -0.5 if scale is None else scale
-        r.window, r.sinks, r.candidates = window, sinks, bool(candidates)
-        need = rec_history_attend_workspace_bytes(self._h, r)
+        width = pages_of.shape[1]
+        query = _QUERY.pack(q.data_ptr(), out.data_ptr(), by_batch, by_query, by_head, code, batch, queries, heads, pages_of.data_ptr(),
+                            pages_of.stride(0), width, lengths.data_ptr(), dim ** -0.5 if scale is None else scale, window, sinks,
+                            1 if candidates else 0)
+        shapes = (batch, queries, heads, width, window, sinks, candidates, code)
+        need = self._workspaces.get(shapes)
+        if need is None:
+            need = _lib.rec_history_attend_workspace_bytes(self._ref, query)
+            if len(self._workspaces) >= 1024:
+                self._workspaces.clear()
+            self._workspaces[shapes] = need
         workspace = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        st = rec_history_attend(self._h, r, workspace)
+        st = _lib.rec_history_attend(self._ref, query, workspace.data_ptr() if need else None, need,
+                                     _stream_on(index, "rec_history_attend"))
         if st:
             self._ok(st, "rec_history_attend")
         return out
@@ -699,26 +730,24 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: to
     """Whole histories attend to themselves (rec_window_attend()).  q: [tokens, heads, head_dim], k and v:
     [tokens, kv_heads, head_dim], fp16 or bf16, any token and head strides; offsets: int32 [batch + 1].
     fault: int64 [REC_FAULT_WORDS], all -1, for rec_history_check(), or None."""
-    device = q.device
+    code, index = _ATTEND_CODES.get(q.dtype), q.get_device()
+    if code is None or index < 0 or q.dim() != 3 or k.dim() != 3 or k.shape != v.shape:
+        raise ValueError("rec_window_attend: q must be [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim] on a device, "
+                         "fp16 or bf16")
     tokens, heads, dim = q.shape
-    for t in (q, k, v):
-        if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != dim or t.dtype is not q.dtype or t.dtype not in _ATTEND_CODES \
-                or t.device != device or not t.is_cuda or t.stride(2) != 1:
-            raise ValueError("rec_window_attend: q, k and v must be device tensors [tokens, heads, head_dim] of one type, fp16 or "
-                             "bf16, rows contiguous")
-    if k.shape != v.shape:
-        raise ValueError("rec_window_attend: k and v must have the same shape")
-    if offsets.dim() != 1 or offsets.shape[0] < 1:
-        raise ValueError("rec_window_attend: offsets must have batch + 1 entries")
-    _check_int32("rec_window_attend", "offsets", offsets, offsets.shape, device)
-    if fault is not None and (fault.dtype is not torch.int64 or fault.device != device or fault.numel() < REC_FAULT_WORDS):
-        raise ValueError(f"rec_window_attend: fault must be int64 [{REC_FAULT_WORDS}] on {device}")
-    out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=device)
-    w = rec_window(rec_rows(q.data_ptr(), q.stride(0), q.stride(1)), rec_rows(k.data_ptr(), k.stride(0), k.stride(1)),
-                   rec_rows(v.data_ptr(), v.stride(0), v.stride(1)), out.data_ptr(), _ATTEND_CODES[q.dtype],
-                   offsets.shape[0] - 1, tokens, heads, k.shape[1], dim, offsets.data_ptr(),
-                   dim ** -0.5 if scale is None else scale, window, sinks, _ptr(fault))
-    st = rec_window_attend(w)
-    if st != REC_OK:
+    (q_token, q_head, q_column), (k_token, k_head, k_column), (v_token, v_head, v_column) = q.stride(), k.stride(), v.stride()
+    if k.shape[0] != tokens or k.shape[2] != dim or k.dtype is not q.dtype or v.dtype is not q.dtype or k.get_device() != index \
+            or v.get_device() != index or not q_column == k_column == v_column == 1:
+        raise ValueError("rec_window_attend: q, k and v must agree in tokens, head_dim, type and device, rows contiguous")
+    if offsets.dtype is not _I32 or offsets.get_device() != index or offsets.dim() != 1 or offsets.shape[0] < 1 or not offsets.is_contiguous():
+        raise ValueError(f"rec_window_attend: offsets must be a contiguous int32 [batch + 1] on {q.device}")
+    if fault is not None and (fault.dtype is not _I64 or fault.get_device() != index or fault.numel() < REC_FAULT_WORDS):
+        raise ValueError(f"rec_window_attend: fault must be int64 [{REC_FAULT_WORDS}] on {q.device}")
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    st = _lib.rec_window_attend(
+        _WINDOW.pack(q.data_ptr(), q_token, q_head, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, out.data_ptr(), code,
+                     offsets.shape[0] - 1, tokens, heads, k.shape[1], dim, offsets.data_ptr(), dim ** -0.5 if scale is None else scale,
+                     window, sinks, fault.data_ptr() if fault is not None else 0), _stream_on(index, "rec_window_attend"))
+    if st:
         raise RecError(st, "rec_window_attend")
     return out
