@@ -11,8 +11,9 @@
 // V^T comes out of LDS by transposing reads (4 keys of a column each), which give just the
 // four neighbouring keys that a lane's four neighbouring scores belong to.
 //
-// LDS rows have no padding; the 16-byte pieces of a row are exchanged by the low bits of its
-// number instead, so that 8 rows read at one column lie in different banks.
+// LDS rows have no padding; the 16-byte pieces of a row are exchanged by bits of its number
+// instead, so that what 16 lanes (keys) or 32 (values) read at once lies in 256 different bytes of
+// the 64 banks.
 //
 // The running maximum moves only when a tile's exceeds it by 2^8.  Masks are looked at in
 // tiles that some row of the wave sees partly, and a masked weight is 0.  Since 0 * NaN is NaN,
@@ -78,14 +79,24 @@ __device__ inline float add_pair(unsigned w, float s)
     }
 }
 
-// Where a 16-byte piece of a row is among the row's.
+// Where a 16-byte piece of a key's row is among the row's: 16 neighbouring rows are read at
+// one piece.
 template <int D>
-__device__ inline int place(int row, int piece)
+__device__ inline int key_place(int row, int piece)
 {
-    return D == 32 ? piece ^ ((row >> 1) & 3) : piece ^ (row & 7);
+    return piece ^ (D == 32 ? (row >> 2) & 3 : D == 64 ? (row >> 1) & 7 : row & 15);
+}
+// Of a value's: four neighbouring rows (from a multiple of four) are read at four pieces (the same).
+template <int D>
+__device__ inline int value_place(int row, int piece)
+{
+    return piece ^ (D == 32 ? 0 : D == 64 ? (row & 2) << 1 : (row & 3) << 2);
 }
 
 __device__ inline bool sees(int pos, int j, int window, int sinks) { return j <= pos && (pos - j < window || j < sinks); }
+
+// Bits [0, n) of 64, for any n.
+__device__ inline unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
 // A history's share of the grid starts at this tile: every history has room for its rows'
 // tiles between its own start and the next one's, whatever the lengths.
@@ -131,7 +142,7 @@ __device__ void redo_row(const T *q, const T *k, long long k_stride, const T *v,
 }
 
 template <int D, bool BF>
-__global__ __launch_bounds__(THREADS, 2) void window_kernel(WindowArgs a)
+__global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(WindowArgs a)
 {
     using T = std::conditional_t<BF, __bf16, _Float16>;
     constexpr int ROW_BYTES = 2 * D, PIECES = D / 8, LOADS = TILE * PIECES / THREADS;
@@ -149,16 +160,21 @@ __global__ __launch_bounds__(THREADS, 2) void window_kernel(WindowArgs a)
 
     // The last history whose tiles start at or before this one, 64 candidates a step.
     auto offset_of = [&](int b) { return (int)min(max((long long)w.dev_offsets[b], 0ll), (long long)w.tokens); };
-    int b = 0;
-    for (int n = w.batch; n > 1;) {
-        const int step = (n + 63) / 64, at = b + lane * step;
-        const bool ok = lane * step < n && first_tile(offset_of(at), a.per, at) <= x;
-        const int count = max(__popcll(__ballot(ok)), 1);
-        b += (count - 1) * step;
-        n = min(step, n - (count - 1) * step);
+    int b = 0, start = 0, stop = 0;
+    for (int n = w.batch;;) {
+        const int step = (n + 62) / 63, at = min(b + lane * step, w.batch), mine = offset_of(at);
+        const bool ok = lane * step < n && first_tile(mine, a.per, at) <= x;
+        const int last = max(__popcll(__ballot(ok)), 1) - 1;
+        b += last * step;
+        if (step == 1) {  // the next lane has where it ends
+            start = __builtin_amdgcn_readlane(mine, last);
+            stop = __builtin_amdgcn_readlane(mine, last + 1);
+            break;
+        }
+        n = min(step, n - last * step);
     }
     b = __builtin_amdgcn_readfirstlane(b);
-    const int start = offset_of(b), len = max(offset_of(b + 1) - start, 0);
+    const int len = max(stop - start, 0);
     const long long first_row = (x - first_tile(start, a.per, b)) * BLOCK_ROWS, all_rows = (long long)len * a.per;
     if (first_row < 0 || first_row >= all_rows) return;
 
@@ -178,8 +194,10 @@ __global__ __launch_bounds__(THREADS, 2) void window_kernel(WindowArgs a)
     for (int i = 0; i < D / 16; ++i) {
         q[i] = *reinterpret_cast<const u32x4 *>(q_row + 16 * i + 8 * half);
         if (w.scale < 0.0f) q[i] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+        if (w.scale == 0.0f) q[i] = u32x4{0u, 0u, 0u, 0u};
     }
-    const float factor = __builtin_fabsf(w.scale) * 1.44269504088896341f;
+    // Positive, so that masked scores stay at -inf.
+    const float factor = w.scale == 0.0f ? 1.0f : __builtin_fabsf(w.scale) * 1.44269504088896341f;
 
     const int n_to = p_hi / TILE + 1, n_from = max(p_lo - window + 1, 0) / TILE;
     const int n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from), count = n_sink + n_to - n_from;
@@ -205,9 +223,8 @@ __global__ __launch_bounds__(THREADS, 2) void window_kernel(WindowArgs a)
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int n = i * THREADS + threadIdx.x, row = n / PIECES, piece = n % PIECES;
-            const int at = row * ROW_BYTES + 16 * place<D>(row, piece);
-            *reinterpret_cast<u32x4 *>(&lds[buffer][0][at]) = in_k[i];
-            *reinterpret_cast<u32x4 *>(&lds[buffer][1][at]) = in_v[i];
+            *reinterpret_cast<u32x4 *>(&lds[buffer][0][row * ROW_BYTES + 16 * key_place<D>(row, piece)]) = in_k[i];
+            *reinterpret_cast<u32x4 *>(&lds[buffer][1][row * ROW_BYTES + 16 * value_place<D>(row, piece)]) = in_v[i];
         }
     };
 
@@ -234,17 +251,24 @@ __global__ __launch_bounds__(THREADS, 2) void window_kernel(WindowArgs a)
                 for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    const u32x4 kk = *reinterpret_cast<const u32x4 *>(kt + (32 * u + c) * ROW_BYTES + 16 * place<D>(c, 2 * i + half));
+                    const u32x4 kk = *reinterpret_cast<const u32x4 *>(kt + (32 * u + c) * ROW_BYTES + 16 * key_place<D>(c, 2 * i + half));
                     s[u] = product<BF>(kk, q[i], s[u]);
                 }
             }
             const bool whole = key + TILE - 1 <= w_lo && (key > w_hi - window || key + TILE <= sinks);
-            if (!whole)
+            if (!whole) {
+                // Bit j: this lane's row sees key + 4 half + j.
+                const int ahead = pos - key - 4 * half;
+                const unsigned long long upto = below(ahead + 1), inside = ~below(ahead - window + 1) | below(sinks - key - 4 * half);
+                const unsigned long long seen = upto & inside;
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < 2; ++u) {
+                    const unsigned bits = (unsigned)(seen >> (32 * u));
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (!sees(pos, key + 32 * u + 8 * (r >> 2) + 4 * half + (r & 3), window, sinks)) s[u][r] = neg_inf();
+                        if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) s[u][r] = neg_inf();
+                }
+            }
             float most = neg_inf();
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -260,16 +284,11 @@ __global__ __launch_bounds__(THREADS, 2) void window_kernel(WindowArgs a)
                 l *= down;
                 m = next;
             }
+            const float by = m == neg_inf() ? 0.0f : m;  // a row that sees nothing yet has weights of 2^(-inf)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], factor, -m));
-            if (!whole)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (!sees(pos, key + 32 * u + 8 * (r >> 2) + 4 * half + (r & 3), window, sinks)) s[u][r] = 0.0f;
+                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], factor, -by));
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -284,7 +303,7 @@ __global__ __launch_bounds__(THREADS, 2) void window_kernel(WindowArgs a)
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) {
                         const int piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                        const unsigned char *at = vt + row * ROW_BYTES + 16 * place<D>(row, piece) + 8 * (lane & 1);
+                        const unsigned char *at = vt + row * ROW_BYTES + 16 * value_place<D>(row, piece) + 8 * (lane & 1);
                         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
                         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * ROW_BYTES));
                         const u32x2 lo2 = __builtin_bit_cast(u32x2, lo), hi2 = __builtin_bit_cast(u32x2, hi);
