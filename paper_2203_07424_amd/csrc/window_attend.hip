@@ -95,6 +95,14 @@ __device__ inline int value_place(int row, int piece)
 
 __device__ inline bool sees(int pos, int j, int window, int sinks) { return j <= pos && (pos - j < window || j < sinks); }
 
+// The larger of lanes l and l ^ 32.
+__device__ inline float larger_half(float x)
+{
+    const unsigned bits = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+
 // Bits [0, n) of 64, for any n.
 __device__ inline unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
@@ -147,7 +155,7 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
     using T = std::conditional_t<BF, __bf16, _Float16>;
     constexpr int ROW_BYTES = 2 * D, PIECES = D / 8, LOADS = TILE * PIECES / THREADS;
     __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][TILE * ROW_BYTES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, half = lane >> 5;
     const rec_window &w = a.w;
     const int kv = (int)(blockIdx.x % (unsigned)w.kv_heads);
     // Late rows see most: they start first.
@@ -246,15 +254,12 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
             const unsigned char *kt = lds[n & 1][0], *vt = lds[n & 1][1];
             f32x16 s[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
+                for (int u = 0; u < 2; ++u) {
                     const u32x4 kk = *reinterpret_cast<const u32x4 *>(kt + (32 * u + c) * ROW_BYTES + 16 * key_place<D>(c, 2 * i + half));
-                    s[u] = product<BF>(kk, q[i], s[u]);
+                    s[u] = product<BF>(kk, q[i], i == 0 ? f32x16{} : s[u]);
                 }
-            }
             const bool whole = key + TILE - 1 <= w_lo && (key > w_hi - window || key + TILE <= sinks);
             if (!whole) {
                 // Bit j: this lane's row sees key + 4 half + j.
@@ -274,7 +279,7 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[u][r]);
-            most = fmaxf(most, __shfl_xor(most, 32));
+            most = larger_half(most);
             most = most == neg_inf() ? most : most * factor;
             if (__any(most > m + SLACK)) {
                 const float next = fmaxf(m, most);
