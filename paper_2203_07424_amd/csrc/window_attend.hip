@@ -2,8 +2,8 @@
 //
 // A block has 128 query rows of one history and kv head (the heads that share it, token
 // after token, so that a block spans few positions) and walks over tiles of 64 keys that
-// some of them sees.  Keys and values pass through two buffers in LDS: while a tile is
-// computed the next one is on its way into registers.  A wave has 32 rows.
+// some of them sees.  Keys and values have two buffers in LDS: while a tile is computed the
+// next one is on its way there.  A wave has 32 rows.
 //
 // Scores come transposed, S^T = K Q^T (32 x 32 x 16), so that a lane holds 16 scores of
 // one row for each half of a tile, and those, exponentiated and narrowed, are the operand of
@@ -33,6 +33,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
 constexpr int WAVE_ROWS = 32, BLOCK_ROWS = WAVE_ROWS * WAVES;
@@ -101,6 +102,12 @@ __device__ inline float larger_half(float x)
     const unsigned bits = __builtin_bit_cast(unsigned, x);
     const auto r = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
     return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+
+// 1024 bytes of a buffer to LDS, 16 a lane from where each says.
+__device__ inline void to_lds(__amdgpu_buffer_rsrc_t from, int offset, void *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)to, 16, offset, 0, 0, 0);
 }
 
 // Bits [0, n) of 64, for any n.
@@ -211,9 +218,16 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
     const int n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from), count = n_sink + n_to - n_from;
     auto key_of = [&](int n) { return (n < n_sink ? n : n_from + n - n_sink) * TILE; };
 
-    // A thread's pieces of a tile: rows behind the history's end come as zeros.
-    u32x4 in_k[LOADS], in_v[LOADS];
-    auto fetch = [&](int key) {
+    // A tile goes straight to LDS, 1024 bytes an instruction in the order of the lanes: a lane
+    // fetches the piece whose place is its own.  Rows behind the history's end come as zeros.
+    int k_offset[LOADS], v_offset[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int n = i * THREADS + threadIdx.x, row = n / PIECES, at = n % PIECES;
+        k_offset[i] = row * (int)w.k.token_stride * 2 + 16 * key_place<D>(row, at);
+        v_offset[i] = row * (int)w.v.token_stride * 2 + 16 * value_place<D>(row, at);
+    }
+    auto fetch = [&](int key, int buffer) {
         const int rows = min(TILE, len - key);
         const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(k_base + key * w.k.token_stride), 0,
                                                           (int)(2 * (rows - 1) * w.k.token_stride + ROW_BYTES), 0x00020000);
@@ -221,18 +235,9 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
                                                           (int)(2 * (rows - 1) * w.v.token_stride + ROW_BYTES), 0x00020000);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int n = i * THREADS + threadIdx.x, row = n / PIECES, piece = n % PIECES;
-            // A zero stride has all rows in the first one's place.
-            in_k[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, row * (int)w.k.token_stride * 2 + piece * 16, 0, 0);
-            in_v[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, row * (int)w.v.token_stride * 2 + piece * 16, 0, 0);
-        }
-    };
-    auto stage = [&](int buffer) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int n = i * THREADS + threadIdx.x, row = n / PIECES, piece = n % PIECES;
-            *reinterpret_cast<u32x4 *>(&lds[buffer][0][row * ROW_BYTES + 16 * key_place<D>(row, piece)]) = in_k[i];
-            *reinterpret_cast<u32x4 *>(&lds[buffer][1][row * ROW_BYTES + 16 * value_place<D>(row, piece)]) = in_v[i];
+            const int to = 16 * (i * THREADS + 64 * wave);
+            to_lds(rk, k_offset[i], &lds[buffer][0][to]);
+            to_lds(rv, v_offset[i], &lds[buffer][1][to]);
         }
     };
 
@@ -243,12 +248,15 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
         for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
     float m = neg_inf(), l = 0.0f;
 
-    fetch(key_of(0));
-    stage(0);
-    __syncthreads();
+    fetch(key_of(0), 0);
     for (int n = 0; n < count; ++n) {
         const int key = key_of(n);
-        if (n + 1 < count) fetch(key_of(n + 1));
+        // This wave's part of tile n has arrived and its reads of the other buffer are done; then
+        // so are all waves'.
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (n + 1 < count) fetch(key_of(n + 1), (n + 1) & 1);
         // Something in it for this wave.
         if (busy && key <= w_hi && (key + TILE > w_lo - window + 1 || key < sinks)) {
             const unsigned char *kt = lds[n & 1][0], *vt = lds[n & 1][1];
@@ -315,10 +323,6 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
                         o[i] = product<BF>(u32x4{lo2[0], lo2[1], hi2[0], hi2[1]}, p, o[i]);
                     }
                 }
-        }
-        if (n + 1 < count) {
-            stage((n + 1) & 1);
-            __syncthreads();
         }
     }
     if (!busy) return;
