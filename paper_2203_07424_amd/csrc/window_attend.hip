@@ -37,7 +37,6 @@ typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
 constexpr int WAVE_ROWS = 32, BLOCK_ROWS = WAVE_ROWS * WAVES;
-constexpr int TILE = 64;       // keys
 constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
 
 struct WindowArgs {
@@ -157,9 +156,10 @@ __device__ void redo_row(const T *q, const T *k, long long k_stride, const T *v,
 }
 
 template <int D, bool BF>
-__global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(WindowArgs a)
+__global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(WindowArgs a)
 {
     using T = std::conditional_t<BF, __bf16, _Float16>;
+    constexpr int TILE = D == 128 ? 32 : 64, PARTS = TILE / 32;  // keys
     constexpr int ROW_BYTES = 2 * D, PIECES = D / 8, LOADS = TILE * PIECES / THREADS;
     __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][TILE * ROW_BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, half = lane >> 5;
@@ -260,14 +260,16 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
         // Something in it for this wave.
         if (busy && key <= w_hi && (key + TILE > w_lo - window + 1 || key < sinks)) {
             const unsigned char *kt = lds[n & 1][0], *vt = lds[n & 1][1];
-            f32x16 s[2];
+            f32x16 s[PARTS];
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < PARTS; ++u) {
                     const u32x4 kk = *reinterpret_cast<const u32x4 *>(kt + (32 * u + c) * ROW_BYTES + 16 * key_place<D>(c, 2 * i + half));
                     s[u] = product<BF>(kk, q[i], i == 0 ? f32x16{} : s[u]);
                 }
+            __builtin_amdgcn_s_setprio(0);
             const bool whole = key + TILE - 1 <= w_lo && (key > w_hi - window || key + TILE <= sinks);
             if (!whole) {
                 // Bit j: this lane's row sees key + 4 half + j.
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
                 const unsigned long long upto = below(ahead + 1), inside = ~below(ahead - window + 1) | below(sinks - key - 4 * half);
                 const unsigned long long seen = upto & inside;
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < PARTS; ++u) {
                     const unsigned bits = (unsigned)(seen >> (32 * u));
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
             }
             float most = neg_inf();
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < PARTS; ++u)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[u][r]);
             most = larger_half(most);
@@ -299,11 +301,11 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 2 : 3) void window_kernel(Windo
             }
             const float by = m == neg_inf() ? 0.0f : m;  // a row that sees nothing yet has weights of 2^(-inf)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < PARTS; ++u)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], factor, -by));
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < PARTS; ++u)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     u32x4 p;
