@@ -1,8 +1,8 @@
 // Attention of whole, ragged histories to themselves, over a window and a few first events.
 //
 // A block has 128 query rows of one history and kv head (the heads that share it, token
-// after token, so that a block spans few positions) and walks over tiles of 64 keys that
-// some of them sees.  Keys and values have two buffers in LDS: while a tile is computed the
+// after token, so that a block spans few positions) and walks over tiles of 32 (head_dim 32: 64)
+// keys that some of them sees.  Keys and values have two buffers in LDS: while a tile is computed the
 // next one is on its way there.  A wave has 32 rows.
 //
 // Scores come transposed, S^T = K Q^T (32 x 32 x 16), so that a lane holds 16 scores of
@@ -159,7 +159,7 @@ template <int D, bool BF>
 __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(WindowArgs a)
 {
     using T = std::conditional_t<BF, __bf16, _Float16>;
-    constexpr int TILE = D == 128 ? 32 : 64, PARTS = TILE / 32;  // keys
+    constexpr int TILE = D == 32 ? 64 : 32, PARTS = TILE / 32;  // keys; every thread fetches 16 bytes of them at least
     constexpr int ROW_BYTES = 2 * D, PIECES = D / 8, LOADS = TILE * PIECES / THREADS;
     __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][TILE * ROW_BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, half = lane >> 5;
@@ -261,7 +261,6 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
         if (busy && key <= w_hi && (key + TILE > w_lo - window + 1 || key < sinks)) {
             const unsigned char *kt = lds[n & 1][0], *vt = lds[n & 1][1];
             f32x16 s[PARTS];
-            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -269,7 +268,6 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
                     const u32x4 kk = *reinterpret_cast<const u32x4 *>(kt + (32 * u + c) * ROW_BYTES + 16 * key_place<D>(c, 2 * i + half));
                     s[u] = product<BF>(kk, q[i], i == 0 ? f32x16{} : s[u]);
                 }
-            __builtin_amdgcn_s_setprio(0);
             const bool whole = key + TILE - 1 <= w_lo && (key > w_hi - window || key + TILE <= sinks);
             if (!whole) {
                 // Bit j: this lane's row sees key + 4 half + j.
