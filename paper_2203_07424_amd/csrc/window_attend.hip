@@ -17,7 +17,7 @@
 //
 // The running maximum moves only when a tile's exceeds it by 2^8.  Masks are looked at in
 // tiles that some row of the wave sees partly, and a masked weight is 0.  Since 0 * NaN is NaN,
-// a row whose result is NaN is computed again, key by key, from the keys it sees (redo_row()).
+// a row whose result is not finite is computed again, key by key, from the keys it sees (redo_row()).
 #include <algorithm>
 
 #include "history.h"
@@ -41,8 +41,9 @@ constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
 
 struct WindowArgs {
     rec_window w;
-    int per;    // query heads of a kv head
-    int tiles;  // of BLOCK_ROWS, more than there can be
+    int per;  // query heads of a kv head
+    unsigned magic, shift;  // row / per = row * magic >> shift, in 64 bits, for rows below 2^31
+    int tiles;              // of BLOCK_ROWS, more than there can be
 };
 
 __device__ inline float neg_inf() { return -__builtin_inff(); }
@@ -66,16 +67,16 @@ __device__ inline unsigned pack(float a, float b)
     }
 }
 
-// s + the two numbers of w.
+// s + the two numbers of w times `by`.
 template <bool BF>
-__device__ inline float add_pair(unsigned w, float s)
+__device__ inline float add_pair(unsigned w, float s, float by = 1.0f)
 {
     if constexpr (BF) {
-        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), ones, s, false);
+        const bf16x2 both = {(__bf16)by, (__bf16)by};
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), both, s, false);
     } else {
-        const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
-        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), ones, s, false);
+        const f16x2 both = {(_Float16)by, (_Float16)by};
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), both, s, false);
     }
 }
 
@@ -109,12 +110,13 @@ __device__ inline void to_lds(__amdgpu_buffer_rsrc_t from, int offset, void *to)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)to, 16, offset, 0, 0, 0);
 }
 
-// Bits [0, n) of 64, for any n.
-__device__ inline unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
+// Bits [0, n) of the 28 that a lane's scores of 32 keys take, for any n.
+__device__ inline unsigned below(int n) { return (1u << min(max(n, 0), 28)) - 1u; }
 
 // A history's share of the grid starts at this tile: every history has room for its rows'
-// tiles between its own start and the next one's, whatever the lengths.
-__device__ inline long long first_tile(long long offset, int per, int b) { return offset * per / BLOCK_ROWS + b; }
+// tiles between its own start and the next one's, whatever the lengths.  Rows and tiles of a call
+// fit 31 bits (launch_window()'s callers see to that).
+__device__ inline int first_tile(int offset, int per, int b) { return (int)((unsigned)offset * (unsigned)per / BLOCK_ROWS) + b; }
 
 // One row by a wave, from nothing but what it sees.
 template <int D, typename T>
@@ -166,40 +168,51 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
     const rec_window &w = a.w;
     const int kv = (int)(blockIdx.x % (unsigned)w.kv_heads);
     // Late rows see most: they start first.
-    const long long x = a.tiles - 1 - (long long)(blockIdx.x / (unsigned)w.kv_heads);
+    const int x = a.tiles - 1 - (int)(blockIdx.x / (unsigned)w.kv_heads);
 
     if (w.dev_fault && blockIdx.x == 0)
         for (int b = threadIdx.x; b < w.batch; b += THREADS)
             if (w.dev_offsets[b] > w.dev_offsets[b + 1] || (b == 0 && w.dev_offsets[0] != 0) || (b == w.batch - 1 && w.dev_offsets[b + 1] != w.tokens))
                 report(reinterpret_cast<unsigned long long *>(w.dev_fault), REC_FAULT_LENGTH, (unsigned long long)b);
 
-    // The last history whose tiles start at or before this one, 64 candidates a step.
-    auto offset_of = [&](int b) { return (int)min(max((long long)w.dev_offsets[b], 0ll), (long long)w.tokens); };
+    // The last history whose tiles start at or before this one.  A lane looks at up to four
+    // candidates a step, so that up to 252 histories take one trip to memory.
+    const int tokens = (int)w.tokens;
     int b = 0, start = 0, stop = 0;
     for (int n = w.batch;;) {
-        const int step = (n + 62) / 63, at = min(b + lane * step, w.batch), mine = offset_of(at);
-        const bool ok = lane * step < n && first_tile(mine, a.per, at) <= x;
-        const int last = max(__popcll(__ballot(ok)), 1) - 1;
+        const int step = (n + 251) / 252;
+        int mine[4] = {}, last = -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (64 * i * step <= n) mine[i] = min(max(w.dev_offsets[min(b + (64 * i + lane) * step, w.batch)], 0), tokens);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (64 * i * step < n) {
+                const int at = (64 * i + lane) * step;
+                last += __popcll(__ballot(at < n && first_tile(mine[i], a.per, b + at) <= x));
+            }
+        last = max(last, 0);
         b += last * step;
-        if (step == 1) {  // the next lane has where it ends
-            start = __builtin_amdgcn_readlane(mine, last);
-            stop = __builtin_amdgcn_readlane(mine, last + 1);
+        if (step == 1) {  // the next candidate has where it ends
+            auto of = [&](int i) { return __builtin_amdgcn_readlane(i < 64 ? mine[0] : i < 128 ? mine[1] : i < 192 ? mine[2] : mine[3], i & 63); };
+            start = of(last);
+            stop = of(last + 1);
             break;
         }
         n = min(step, n - last * step);
     }
     b = __builtin_amdgcn_readfirstlane(b);
     const int len = max(stop - start, 0);
-    const long long first_row = (x - first_tile(start, a.per, b)) * BLOCK_ROWS, all_rows = (long long)len * a.per;
+    const int first_row = (x - first_tile(start, a.per, b)) * BLOCK_ROWS, all_rows = len * a.per;
     if (first_row < 0 || first_row >= all_rows) return;
 
     const int window = w.window == 0 ? 0x7fffffff : w.window, sinks = w.sinks;
-    auto pos_of = [&](long long row) { return (int)((unsigned)min(row, all_rows - 1) / (unsigned)a.per); };
+    auto pos_of = [&](int row) { return (int)((unsigned long long)(unsigned)min(row, all_rows - 1) * a.magic >> a.shift); };
     const int p_lo = pos_of(first_row), p_hi = pos_of(first_row + BLOCK_ROWS - 1);
-    const long long wave_row = first_row + wave * WAVE_ROWS;
+    const int wave_row = first_row + wave * WAVE_ROWS;
     const bool busy = wave_row < all_rows;
     const int w_lo = pos_of(wave_row), w_hi = pos_of(wave_row + WAVE_ROWS - 1), pos = pos_of(wave_row + c);
-    const int my_head = kv * a.per + (int)(min(wave_row + c, all_rows - 1) - (long long)pos * a.per);
+    const int my_head = kv * a.per + min(wave_row + c, all_rows - 1) - pos * a.per;
     const T *k_base = static_cast<const T *>(w.k.dev) + (long long)start * w.k.token_stride + (long long)kv * w.k.head_stride;
     const T *v_base = static_cast<const T *>(w.v.dev) + (long long)start * w.v.token_stride + (long long)kv * w.v.head_stride;
     const T *q_row = static_cast<const T *>(w.q.dev) + (long long)(start + pos) * w.q.token_stride + (long long)my_head * w.q.head_stride;
@@ -270,16 +283,18 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
                 }
             const bool whole = key + TILE - 1 <= w_lo && (key > w_hi - window || key + TILE <= sinks);
             if (!whole) {
-                // Bit j: this lane's row sees key + 4 half + j.
-                const int ahead = pos - key - 4 * half;
-                const unsigned long long upto = below(ahead + 1), inside = ~below(ahead - window + 1) | below(sinks - key - 4 * half);
-                const unsigned long long seen = upto & inside;
+                // Bit j of a part: this lane's row sees the part's key 4 half + j.
 #pragma unroll
                 for (int u = 0; u < PARTS; ++u) {
-                    const unsigned bits = (unsigned)(seen >> (32 * u));
+                    const int first = key + 32 * u + 4 * half, ahead = pos - first;
+                    const unsigned unseen = ~(below(ahead + 1) & (~below(ahead - window + 1) | below(sinks - first)));
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) s[u][r] = neg_inf();
+                    for (int r = 0; r < 16; ++r) {
+                        // -inf by its bits: no compare, no condition register.
+                        const float one = s[u][r];
+                        const unsigned hide = (unsigned)__builtin_amdgcn_sbfe((int)unseen, 8 * (r >> 2) + (r & 3), 1);
+                        s[u][r] = __builtin_bit_cast(float, (hide & 0xff800000u) | (~hide & __builtin_bit_cast(unsigned, one)));
+                    }
                 }
             }
             float most = neg_inf();
@@ -291,10 +306,12 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
             most = most == neg_inf() ? most : most * factor;
             if (__any(most > m + SLACK)) {
                 const float next = fmaxf(m, most);
-                const float down = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+                if (__any(m != neg_inf())) {  // not the first tile
+                    const float down = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) o[i] *= down;
-                l *= down;
+                    for (int i = 0; i < D / 32; ++i) o[i] *= down;
+                    l *= down;
+                }
                 m = next;
             }
             const float by = m == neg_inf() ? 0.0f : m;  // a row that sees nothing yet has weights of 2^(-inf)
@@ -329,22 +346,22 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
 
     l += __shfl_xor(l, 32);
     const float by = 1.0f / l;
-    bool bad = false;
+    float zero = 0.0f;  // NaN once a result is not finite
     const bool real = wave_row + c < all_rows;
     T *out = static_cast<T *>(w.dev_out) + ((long long)(start + pos) * w.heads + my_head) * D;
-    typedef T tx4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const f32x4 y = f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]} * by;
-            bad |= y[0] != y[0] || y[1] != y[1] || y[2] != y[2] || y[3] != y[3];
-            if (real) *reinterpret_cast<tx4 *>(out + 32 * i + 8 * (r >> 2) + 4 * half) = __builtin_convertvector(y, tx4);
+            const u32x2 z = {pack<BF>(y[0], y[1]), pack<BF>(y[2], y[3])};
+            zero = add_pair<BF>(z[1], add_pair<BF>(z[0], zero, 0.0f), 0.0f);
+            if (real) *reinterpret_cast<u32x2 *>(out + 32 * i + 8 * (r >> 2) + 4 * half) = z;
         }
-    unsigned long long again = __ballot(bad && real);
+    unsigned long long again = __ballot(zero != 0.0f && real);
     again |= again >> 32;
     for (unsigned rows = (unsigned)again; rows; rows &= rows - 1) {
-        const int r = __builtin_ctz(rows), p = pos_of(wave_row + r), head = kv * a.per + (int)(wave_row + r - (long long)p * a.per);
+        const int r = __builtin_ctz(rows), p = pos_of(wave_row + r), head = kv * a.per + wave_row + r - p * a.per;
         redo_row<D, T>(static_cast<const T *>(w.q.dev) + (long long)(start + p) * w.q.token_stride + (long long)head * w.q.head_stride, k_base,
                        w.k.token_stride, v_base, w.v.token_stride, p, w.scale * 1.44269504088896341f, window, sinks,
                        static_cast<T *>(w.dev_out) + ((long long)(start + p) * w.heads + head) * D, lane);
@@ -373,6 +390,10 @@ hipError_t launch_window(const rec_window &w, hipStream_t s)
     a.w = w;
     a.per = w.heads / w.kv_heads;
     a.tiles = (int)(window_blocks(w) / w.kv_heads);
+    // per in (2^(n-1), 2^n]: 2^(31+n) / per rounded up fits 32 bits and is exact for rows of 31.
+    const unsigned bits = a.per == 1 ? 0 : 32 - __builtin_clz((unsigned)a.per - 1);
+    a.shift = 31 + bits;
+    a.magic = (unsigned)(((1ull << a.shift) + a.per - 1) / a.per);
     return w.head_dim == 32 ? window_as<32>(a, s) : w.head_dim == 64 ? window_as<64>(a, s) : window_as<128>(a, s);
 }
 
