@@ -38,6 +38,7 @@ typedef short s16x2 __attribute__((ext_vector_type(2)));
 constexpr int ROWS = 16;       // query rows of a wave
 constexpr int TILE = 64;       // keys
 constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
+constexpr float LOWEST = -3.4e38f;  // the maximum of a row that has seen nothing but scores of -inf
 constexpr int CUS = 256;
 
 struct AttendArgs {
@@ -53,19 +54,18 @@ struct AttendArgs {
 
 __device__ inline float neg_inf() { return -__builtin_inff(); }
 
-// Terms of eight query elements x in units of 2^-4k of `scale`; x becomes what is left.
+// What a row's sums are multiplied by in the end, from its weights' sum and their maximum's exponent.
+__device__ inline float inverse(float l, float m) { return l == 0.0f && m == neg_inf() ? 0.0f : 1.0f / l; }
+
+// Terms of eight query elements x in units of `scale`; x becomes what is left.
 __device__ inline u32x2 term_of(float (&x)[8], float scale)
 {
     u32x2 r;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         s16x2 w = {0, 0};
-        const float most = 448.0f * scale;
-        float y[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = __builtin_amdgcn_fmed3f(x[4 * i + j], -most, most);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, y[0], y[1], scale, false);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, y[2], y[3], scale, true);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i], x[4 * i + 1], scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i + 2], x[4 * i + 3], scale, true);
         const unsigned bits = __builtin_bit_cast(unsigned, w);
         const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bits, scale, false);
         const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bits, scale, true);
@@ -87,8 +87,8 @@ struct Query {
     i32x8 b[STEPS];
     int scale[STEPS];
 
-    // `row`: this lane's row (lane % 16) or null; `flip`: its sign changes.
-    __device__ inline void load(const void *row, bool flip, int g)
+    // `row`: this lane's row (lane % 16) or null; its elements times `sign`.
+    __device__ inline void load(const void *row, float sign, int g)
     {
         using T = std::conditional_t<BF, __bf16, _Float16>;
         typedef T tx8 __attribute__((ext_vector_type(8)));
@@ -106,7 +106,7 @@ struct Query {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float f = (float)v[i];
-                    x[p][h][i] = flip ? -f : f;
+                    x[p][h][i] = f * sign;
                     most[p] = max(most[p], __builtin_bit_cast(unsigned, f) & 0x7fffffffu);
                 }
             }
@@ -115,16 +115,21 @@ struct Query {
         unsigned byte[PARTS];
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            // The exponent that E4M3 blocks of the cache have; 255 where the query is not finite.
-            const int e = (int)(most[p] >> 23) - 127 - 8 + ((most[p] & 0x7fffffu) > 0x680000u ? 1 : 0);
-            byte[p] = most[p] >= 0x7f800000u ? 255u : (unsigned)(min(max(e, -110), 119) + 127);
+            // So that the largest is at most 448, and no term overflows; 255 where the query is not finite.
+            const int e = max((int)(most[p] >> 23) - 127 - 8 + ((most[p] & 0x7fffffu) > 0x600000u ? 1 : 0), -110);
+            byte[p] = most[p] >= 0x7f800000u ? 255u : (unsigned)(e + 127);
+            const float unit = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[p][h][i] *= unit;
         }
         u32x4 term[TERMS][PARTS];
 #pragma unroll
         for (int t = 0; t < TERMS; ++t)
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) {
-                const float s = __builtin_bit_cast(float, (byte[p] - 4 * t) << 23);
+                const float s = t == 0 ? 1.0f : t == 1 ? 0x1p-4f : 0x1p-8f;
                 const u32x2 lo = term_of(x[p][0], s), hi = term_of(x[p][1], s);
                 term[t][p] = u32x4{lo[0], lo[1], hi[0], hi[1]};
             }
@@ -274,32 +279,42 @@ struct Sums {
     float m;
 };
 
+// Bytes of 255 where the bits of a nibble are set.
+__device__ inline unsigned bytes_of(unsigned nibble)
+{
+    const unsigned ones = nibble * 0x204081u & 0x01010101u;
+    return (ones << 8) - ones;
+}
+
 // Tokens of a lane's 16 that count as zero whatever their bytes are: 0 * NaN would reach the
 // rows that do not see a value.  Those are the ones that no row sees (bit t of `used` clear) and,
-// a block at a time, those whose block is NaN.  Returns the blocks (bit b) of which row c,
-// which sees the tokens in `seen`, sees a NaN.
+// a block at a time, those whose block is NaN; a scale of 2^-127 does it, and for the former no
+// code that is NaN itself.  Returns the blocks (bit b) of which row c, which sees the tokens in
+// `seen`, sees a NaN.
 template <int FMT, int D>
 __device__ inline unsigned clear_values(Tile<FMT, D> &t, unsigned used, unsigned seen)
 {
     unsigned nan = 0;
 #pragma unroll
-    for (int b = 0; b < D / BLOCK; ++b) {
-        unsigned bad = 0;
+    for (int x = 0; x < 4; ++x) {
+        const unsigned keep = bytes_of(used >> (4 * x) & 15u), mine = bytes_of(seen >> (4 * x) & 15u);
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-            const unsigned shift = 8 * (x & 3);
-            if ((t.vs[b][x >> 2] >> shift & 255u) == 255u || !(used >> x & 1u)) {
-                bad |= 1u << x;
-                t.vs[b][x >> 2] &= ~(255u << shift);
-                if constexpr (FMT == REC_MX4) t.v[b][0][x >> 2] &= ~(255u << shift);
-                else t.v[b][x >> 3][(x >> 1) & 3] &= ~(0xffffu << (16 * (x & 1)));
+        for (int b = 0; b < D / BLOCK; ++b) {
+            const unsigned s = t.vs[b][x], top = ((s & 0x7f7f7f7fu) + 0x01010101u) & s & 0x80808080u;  // bytes of 255
+            nan |= (top & mine) != 0 ? 1u << b : 0u;
+            t.vs[b][x] = s & keep & ~((top << 1) - (top >> 7));
+            if constexpr (FMT == REC_MX8) {
+                t.v[b][x >> 1][2 * (x & 1)] &= __builtin_amdgcn_perm(keep, keep, 0x01010000u);
+                t.v[b][x >> 1][2 * (x & 1) + 1] &= __builtin_amdgcn_perm(keep, keep, 0x03030202u);
             }
         }
-        if (bad & seen) nan |= 1u << b;
     }
     nan |= (unsigned)__shfl_xor((int)nan, 16);
     return nan | (unsigned)__shfl_xor((int)nan, 32);
 }
+
+// Bits [0, n) of a lane's 16 tokens, for any n.
+__device__ inline unsigned below(int n) { return (1u << min(max(n, 0), 16)) - 1u; }
 
 // Where a wave's row goes.
 __device__ inline long long out_row(const AttendArgs &a, int b, int kv, int row)
@@ -326,19 +341,18 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
         if (threadIdx.x == 0 && kv == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)b);
         len = len < 0 ? 0 : most_tokens;
     }
-    // Positions of this wave's rows: of its first, its last, and this lane's.
+    // Positions of this wave's rows: of its first, its last, and this lane's; -1 sees nothing.
     const int first_row = row_tile * ROWS, last_row = min(first_row + ROWS, a.rows) - 1, row = min(first_row + c, last_row);
     const bool together = a.q.candidates != 0;
-    const int before = len - (together ? 1 : a.q.queries);
-    const int p_lo = before + (together ? 0 : first_row / a.per), p_hi = before + (together ? 0 : last_row / a.per);
-    const int pos = before + (together ? 0 : row / a.per);
+    auto position = [&](int row) { return together ? len - 1 : max(len - a.q.queries + row / a.per, -1); };
+    const int p_lo = position(first_row), p_hi = position(last_row), pos = position(row);
     const int window = a.q.window == 0 ? 0x7fffffff : a.q.window, sinks = a.q.sinks;
 
     // Tiles that some row sees something of: [0, n_sink) and [n_from, n_to).
     int n_from = 0, n_sink = 0, n_to = 0;
     if (p_hi >= 0) {
         n_to = p_hi / TILE + 1;
-        n_from = max(max(p_lo, 0) - window + 1, 0) / TILE;
+        n_from = max(p_lo - window + 1, 0) / TILE;
         n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from);
     }
     const int tiles = n_sink + n_to - n_from, each = (tiles + a.splits - 1) / a.splits;
@@ -349,14 +363,20 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
     for (int i = 0; i < D / 16; ++i) sum.o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     sum.l = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     sum.m = neg_inf();
+    unsigned saw = 0;  // not 0: this lane's row has seen a key
 
     if (begin + wave < end) {
         const long long row_bytes = 2ll * (b * a.q.batch_stride + (row / a.per) * a.q.query_stride + (kv * a.per + row % a.per) * a.q.head_stride);
         Query<D, BF> q;
-        q.load(first_row + c <= last_row ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr, a.q.scale < 0.0f, g);
-        const float factor = __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
+        q.load(first_row + c <= last_row ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr,
+               a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);
+        // Positive, so that masked scores stay at -inf.
+        const float factor = a.q.scale == 0.0f ? 1.0f : __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
         const int32_t *table = a.q.dev_pages_of + b * a.q.table_stride;
         const int groups = 1 << (shift - 4);
+        const unsigned char *first_page = a.c.pages + (long long)kv * groups * group_bytes<FMT>(D);
+        const unsigned page_bytes = (unsigned)(a.c.kv_heads * groups * group_bytes<FMT>(D));
+        const unsigned pages = (unsigned)min(a.c.num_pages, 1ll << 31);
 
         // Tile n of the walk starts at this key.
         auto key_of = [&](int n) { return (n < n_sink ? n : n_from + n - n_sink) * TILE; };
@@ -367,9 +387,9 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
             return page;
         };
         auto group_at = [&](int page, int token) {
-            const bool ok = page >= 0 && page < a.c.num_pages;
-            const long long index = ok ? ((long long)page * a.c.kv_heads + kv) * groups + ((token >> 4) & (groups - 1)) : 0;
-            return a.c.pages + index * group_bytes<FMT>(D);
+            const bool ok = (unsigned)page < pages;  // else some group that is there: its tokens count for nothing
+            const unsigned in_page = ok ? (unsigned)((token >> 4) & (groups - 1)) * group_bytes<FMT>(D) : 0u;
+            return first_page + ((unsigned long long)(ok ? (unsigned)page : 0u) * page_bytes + in_page);
         };
 
         int n = begin + wave, key = key_of(n);
@@ -388,28 +408,32 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
             if (more) tile.load_keys(group_at(k_page, key_next + 16 * (c >> 2)), c, g);
 
             // Groups come with their page or not at all.
-            const bool there = v_page >= 0 && v_page < a.c.num_pages;
+            const bool there = (unsigned)v_page < pages;
             const bool whole = key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there);
-            unsigned seen = 0xffffu, nan = 0;  // bit t: row c sees token t of group g; bit b: and a NaN in block b
+            unsigned nan = 0;  // bit b: row c sees a NaN in block b
             if (!whole) {
-                const int first = key + 16 * g, from = max(p_lo, 0) - window;
-                unsigned used = 0;  // bit t: some row sees token t
-                seen = 0;
-#pragma unroll
-                for (int t = 0; t < 16; ++t) {
-                    const int j = first + t;
-                    if (j <= pos && (pos - j < window || j < sinks)) seen |= 1u << t;
-                    if (j <= p_hi && (j > from || j < sinks)) used |= 1u << t;
-                }
+                // Bit t: row c sees token t of group g; some row does.
+                const int first = key + 16 * g;
+                auto upto = [&](int at) { return below(max(at - first, -1) + 1); };
+                auto before = [&](int at) { return below(max(at - first, -1) - window + 1); };
+                unsigned seen = upto(pos) & (~before(pos) | below(sinks - first));
+                unsigned used = upto(p_hi) & (~before(p_lo) | below(sinks - first));
                 if (!there) {
                     if (used && c == 0)
                         report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)b * (unsigned)a.q.table_width + (unsigned)(first >> shift));
                     seen = used = 0;
                 }
+                saw |= seen;
                 nan = clear_values<FMT, D>(tile, used, seen);
 #pragma unroll
-                for (int t = 0; t < 16; ++t)
-                    if (!(seen >> t & 1u)) s[t & 3][t >> 2] = neg_inf();
+                for (int t = 0; t < 16; ++t) {
+                    // -inf by its bits: no compare, no condition register.
+                    const float one = s[t & 3][t >> 2];
+                    const unsigned hide = (unsigned)__builtin_amdgcn_sbfe((int)~seen, t, 1);
+                    s[t & 3][t >> 2] = __builtin_bit_cast(float, (hide & 0xff800000u) | (~hide & __builtin_bit_cast(unsigned, one)));
+                }
+            } else {
+                saw = 1;
             }
 
             float most = neg_inf();
@@ -420,18 +444,18 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
             most = most == neg_inf() ? most : most * factor;
             if (__any(most > sum.m + SLACK)) {
                 const float m = fmaxf(sum.m, most);
-                const float down = sum.m == m ? 1.0f : __builtin_amdgcn_exp2f(sum.m - m);
+                if (__any(sum.m != neg_inf())) {  // not the first tile
+                    const float down = sum.m == m ? 1.0f : __builtin_amdgcn_exp2f(sum.m - m);
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) sum.o[i] *= down;
-                sum.l *= down;
+                    for (int i = 0; i < D / 16; ++i) sum.o[i] *= down;
+                    sum.l *= down;
+                }
                 sum.m = m;
             }
+            const float by = sum.m == neg_inf() ? 0.0f : sum.m;  // a row that sees nothing yet has weights of 2^(-inf)
             float p[16];
 #pragma unroll
-            for (int t = 0; t < 16; ++t) p[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t & 3][t >> 2], factor, -sum.m));
-            if (!whole)
-#pragma unroll
-                for (int t = 0; t < 16; ++t) p[t] = seen >> t & 1u ? p[t] : 0.0f;
+            for (int t = 0; t < 16; ++t) p[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t & 3][t >> 2], factor, -by));
 
             // Weights as bf16, for fp16 results with what that rounding left out beside them.
             constexpr int TERMS = BF ? 1 : 2;
@@ -483,6 +507,11 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
         }
     }
 
+    // All of a row's scores may be -inf, which is not the same as having none: the maximum tells.
+    saw |= (unsigned)__shfl_xor((int)saw, 16);
+    saw |= (unsigned)__shfl_xor((int)saw, 32);
+    if (saw && sum.m == neg_inf() && sum.l[0] == 0.0f) sum.m = LOWEST;
+
     const long long out = out_row(a, b, kv, row);
     const bool real = first_row + c <= last_row;
     const long long all_rows = (long long)a.q.batch * a.q.queries * a.q.heads;
@@ -495,7 +524,7 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
                 for (int i = 0; i < D / 16; ++i)
                     *reinterpret_cast<f32x4 *>(a.part_o + (split * all_rows + out) * D + 16 * i + 4 * g) = sum.o[i];
         } else if (real) {
-            const float by = l == 0.0f ? 0.0f : 1.0f / l;
+            const float by = inverse(l, sum.m);
             typedef T tx4 __attribute__((ext_vector_type(4)));
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
@@ -521,7 +550,7 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const f32x2 ml = ml_of[w][r];
-                const float by = ml[0] == neg_inf() && ml[1] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml[0] - m);
+                const float by = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - m);
                 l += ml[1] * by;
                 x += *reinterpret_cast<const f32x4 *>(&o_of[w][r][col]) * by;
                 y += *reinterpret_cast<const f32x4 *>(&o_of[w][r][col + 4]) * by;
@@ -534,7 +563,7 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
                 if (col == 0) a.part_ml[split * all_rows + to] = f32x2{m, l};
             } else {
                 typedef T tx8 __attribute__((ext_vector_type(8)));
-                const float by = l == 0.0f ? 0.0f : 1.0f / l;
+                const float by = inverse(l, m);
                 x *= by;
                 y *= by;
                 const f32x8 z = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
@@ -560,11 +589,11 @@ __global__ __launch_bounds__(256) void combine_kernel(const float *part_o, const
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < splits; ++s) {
         const f32x2 ml = part_ml[s * rows + row];
-        const float by = ml[0] == neg_inf() && ml[1] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml[0] - m);
+        const float by = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - m);
         l += ml[1] * by;
         x += *reinterpret_cast<const f32x4 *>(part_o + (s * rows + row) * D + col) * by;
     }
-    x *= l == 0.0f ? 0.0f : 1.0f / l;
+    x *= inverse(l, m);
     *reinterpret_cast<tx4 *>(static_cast<T *>(out) + row * D + col) = __builtin_convertvector(x, tx4);
 }
 
@@ -587,7 +616,7 @@ Plan plan_of(const Cache &c, const rec_query &q)
         const long long apart = q.candidates ? 0 : std::min<long long>(q.queries - 1, (ROWS - 1) / p.per + 1);
         tiles = std::min(tiles, (q.window + apart + TILE - 2) / TILE + 1 + (q.sinks + TILE - 1ll) / TILE);
     }
-    p.waves = tiles >= 4 && pairs < 16 * CUS ? 4 : tiles >= 2 && pairs < 32 * CUS ? 2 : 1;
+    p.waves = tiles >= 4 && pairs < 4 * CUS ? 4 : tiles >= 2 && pairs < 8 * CUS ? 2 : 1;
     p.splits = 1;
     if (pairs * p.waves < 12 * CUS && tiles > 2 * p.waves)
         p.splits = (int)std::max(1ll, std::min({(tiles + 2 * p.waves - 1) / (2 * p.waves), (16 * CUS + pairs * p.waves - 1) / (pairs * p.waves), 64ll}));

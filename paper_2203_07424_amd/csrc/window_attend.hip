@@ -286,7 +286,7 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
                 // Bit j of a part: this lane's row sees the part's key 4 half + j.
 #pragma unroll
                 for (int u = 0; u < PARTS; ++u) {
-                    const int first = key + 32 * u + 4 * half, ahead = pos - first;
+                    const int first = key + 32 * u + 4 * half, ahead = max(pos - first, -1);
                     const unsigned unseen = ~(below(ahead + 1) & (~below(ahead - window + 1) | below(sinks - first)));
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {

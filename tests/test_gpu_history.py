@@ -363,6 +363,27 @@ def test_nan_and_infinite_queries(b):
     O.assert_close(got, want, off)
 
 
+@pytest.mark.parametrize("fmt,lengths,width", [("mx4", [40, 150], 5), ("mx8", [40, 150], 5), ("mx4", [3000], 100)])
+def test_scores_of_minus_infinity(b, fmt, lengths, width):
+    """Keys whose scores are -inf have no weight beside others, and alone leave no result (0 / 0)."""
+    s = Histories(b, lengths, 1, 64, fmt, 32, seed=16, width=width)
+    q = torch.full((len(lengths), 1, 2, 64), 3.0e38, dtype=BF).cuda()      # sums of products beyond fp32
+    k = torch.full((len(s.slots), 1, 64), -1.0e38)
+    ends = [int(e) for e in s.ends[1:]]
+    k[ends[0] - 2] = 0.0                                               # one key of the first history is seen with score 0
+    s.cache.write(k.cuda(), torch.from_numpy(s.v).float().cuda(), s.slots.cuda())
+    got = s.cache.attend(q, s.table, s.len_t, scale=1.0).double().cpu().numpy()
+    want = s.v[ends[0] - 2, 0]
+    assert (np.abs(got[0, 0] - want) <= 2.0 ** -8 * np.abs(want)).all()
+    assert np.isnan(got[1:]).all()
+    got = s.cache.attend(q, s.table, s.len_t, scale=1.0, window=1).double().cpu().numpy()     # the key behind it: -inf alone
+    assert np.isnan(got).all()
+    got = s.cache.attend(q, s.table, s.len_t, scale=0.0).double().cpu().numpy()
+    for i, e in enumerate(ends):
+        mean = s.v[int(s.ends[i]):e, 0].mean(0)
+        assert (np.abs(got[i, 0] - mean) <= 2.0 ** -8 * np.abs(mean) + 2.0 ** -8 * np.abs(s.v[int(s.ends[i]):e, 0]).mean(0)).all()
+
+
 def test_queries_of_wide_range(b):
     """Elements of a query from its type's largest to its smallest."""
     s = Histories(b, [70, 33], 1, 64, "mx8", 32, seed=11)
