@@ -58,11 +58,25 @@ __device__ inline f32x2 two_values(unsigned w)
     else return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, 1.0f, AT != 0);
 }
 
+// Division by a number that the host knows: n / d = n * magic >> shift in 64 bits, for n below
+// 2^31.  With d in (2^(k-1), 2^k], 2^(31+k) / d rounded up fits 32 bits and is off by less than
+// 2^k / 2^(31+k) of itself.
+struct Divider {
+    unsigned magic = 0, shift = 0;
+    Divider() = default;
+    explicit Divider(int d)
+    {
+        shift = 31 + (d == 1 ? 0 : 32 - __builtin_clz((unsigned)d - 1));
+        magic = (unsigned)(((1ull << shift) + d - 1) / d);
+    }
+    __device__ int of(int n) const { return (int)((unsigned long long)(unsigned)n * magic >> shift); }
+};
+
 hipError_t launch_write(const Cache &c, int format, int d, const rec_rows &k, const rec_rows &v, int dtype,
                         const int64_t *slots, long long tokens, hipStream_t s);
 hipError_t launch_read(const Cache &c, int format, int d, const int64_t *slots, long long tokens, int dtype,
                        void *k, void *v, hipStream_t s);
-long long attend_threads(const Cache &c, const rec_query &q);
+long long attend_threads(const Cache &c, int format, int d, const rec_query &q);
 size_t attend_workspace(const Cache &c, int format, int d, const rec_query &q);
 hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *workspace, hipStream_t s);
 long long window_blocks(const rec_window &w);  // of 256 threads

@@ -59,7 +59,7 @@ rec_status check_query(const rec_history *h, const rec_query *q)
     if ((int64_t)q->table_width * h->page_tokens > MOST_TOKENS || (int64_t)q->queries * q->heads >= 1ll << 31 ||
         (int64_t)q->queries * q->heads * q->batch >= 1ll << 31)
         return REC_ERR_OVERFLOW;
-    return rec::hist::attend_threads(cache_of(h), *q) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
+    return rec::hist::attend_threads(cache_of(h), h->format, h->head_dim, *q) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
 }
 
 bool rows_fit(const rec_rows &r, int size)

@@ -41,13 +41,21 @@ constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
 constexpr float LOWEST = -3.4e38f;  // the maximum of a row that has seen nothing but scores of -inf
 constexpr int CUS = 256;
 
+// Waves that a SIMD holds at once; the compiler gives a wave at most its share of registers.
+__host__ __device__ constexpr int waves_of(int format, int d, bool bf)
+{
+    return d == 128 ? (format == REC_MX4 && bf ? 3 : 2) : d == 64 ? (format == REC_MX4 && bf ? 4 : 3) : 4;
+}
+
 struct AttendArgs {
     Cache c;
     rec_query q;
     int per;        // query heads of a kv head
+    Divider by_per;
     int rows;       // queries * per
     int row_tiles;  // of ROWS
     int splits;
+    Divider inner, heads;  // by splits * row_tiles, by kv_heads
     float *part_o;   // [splits][batch * queries * heads][D]
     f32x2 *part_ml;  // [splits][batch * queries * heads]
 };
@@ -106,7 +114,7 @@ struct Query {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float f = (float)v[i];
-                    x[p][h][i] = f * sign;
+                    x[p][h][i] = f;
                     most[p] = max(most[p], __builtin_bit_cast(unsigned, f) & 0x7fffffffu);
                 }
             }
@@ -118,7 +126,7 @@ struct Query {
             // So that the largest is at most 448, and no term overflows; 255 where the query is not finite.
             const int e = max((int)(most[p] >> 23) - 127 - 8 + ((most[p] & 0x7fffffu) > 0x600000u ? 1 : 0), -110);
             byte[p] = most[p] >= 0x7f800000u ? 255u : (unsigned)(e + 127);
-            const float unit = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
+            const float unit = sign * __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -319,21 +327,19 @@ __device__ inline unsigned below(int n) { return (1u << min(max(n, 0), 16)) - 1u
 // Where a wave's row goes.
 __device__ inline long long out_row(const AttendArgs &a, int b, int kv, int row)
 {
-    const int i = row / a.per;
+    const int i = a.by_per.of(row);
     return ((long long)b * a.q.queries + i) * a.q.heads + kv * a.per + (row - i * a.per);
 }
 
 template <int FMT, int D, bool BF, int W>
-__global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend_kernel(AttendArgs a)
+__global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(AttendArgs a)
 {
     using T = std::conditional_t<BF, __bf16, _Float16>;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-    unsigned at = blockIdx.x;
-    const int split = (int)(at % (unsigned)a.splits);
-    at /= (unsigned)a.splits;
-    const int row_tile = (int)(at % (unsigned)a.row_tiles);
-    at /= (unsigned)a.row_tiles;
-    const int kv = (int)(at % (unsigned)a.c.kv_heads), b = (int)(at / (unsigned)a.c.kv_heads);
+    const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    // Parts of a history's head next to each other, then its heads, whose groups share a page.
+    const int pair = a.inner.of((int)blockIdx.x), part = (int)blockIdx.x - pair * a.splits * a.row_tiles;
+    const int b = a.heads.of(pair), kv = pair - b * a.c.kv_heads;
+    const int row_tile = a.splits == 1 ? part : part / a.splits, split = part - row_tile * a.splits;
 
     const int shift = a.c.page_shift, most_tokens = a.q.table_width << shift;
     int len = a.q.dev_lengths[b];
@@ -344,7 +350,7 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
     // Positions of this wave's rows: of its first, its last, and this lane's; -1 sees nothing.
     const int first_row = row_tile * ROWS, last_row = min(first_row + ROWS, a.rows) - 1, row = min(first_row + c, last_row);
     const bool together = a.q.candidates != 0;
-    auto position = [&](int row) { return together ? len - 1 : max(len - a.q.queries + row / a.per, -1); };
+    auto position = [&](int row) { return together ? len - 1 : max(len - a.q.queries + a.by_per.of(row), -1); };
     const int p_lo = position(first_row), p_hi = position(last_row), pos = position(row);
     const int window = a.q.window == 0 ? 0x7fffffff : a.q.window, sinks = a.q.sinks;
 
@@ -366,7 +372,8 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : D == 64 ? 3 : 4) void attend
     unsigned saw = 0;  // not 0: this lane's row has seen a key
 
     if (begin + wave < end) {
-        const long long row_bytes = 2ll * (b * a.q.batch_stride + (row / a.per) * a.q.query_stride + (kv * a.per + row % a.per) * a.q.head_stride);
+        const int query = a.by_per.of(row), head = kv * a.per + row - query * a.per;
+        const long long row_bytes = 2 * (b * a.q.batch_stride + query * a.q.query_stride + head * a.q.head_stride);
         Query<D, BF> q;
         q.load(first_row + c <= last_row ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr,
                a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);
@@ -602,7 +609,7 @@ struct Plan {
     long long rows;  // of the whole call
 };
 
-Plan plan_of(const Cache &c, const rec_query &q)
+Plan plan_of(const Cache &c, int format, int d, const rec_query &q)
 {
     Plan p;
     p.per = q.heads / c.kv_heads;
@@ -610,6 +617,8 @@ Plan plan_of(const Cache &c, const rec_query &q)
     const long long rows = (long long)q.queries * p.per;
     p.row_tiles = (int)((rows + ROWS - 1) / ROWS);
     const long long pairs = (long long)q.batch * c.kv_heads * p.row_tiles;
+    p.waves = p.splits = 1;
+    if (pairs == 0) return p;
     // Most tiles that a wave's rows can see something of.
     long long tiles = (((long long)q.table_width << c.page_shift) + TILE - 1) / TILE;
     if (q.window) {
@@ -617,9 +626,10 @@ Plan plan_of(const Cache &c, const rec_query &q)
         tiles = std::min(tiles, (q.window + apart + TILE - 2) / TILE + 1 + (q.sinks + TILE - 1ll) / TILE);
     }
     p.waves = tiles >= 4 && pairs < 4 * CUS ? 4 : tiles >= 2 && pairs < 8 * CUS ? 2 : 1;
-    p.splits = 1;
-    if (pairs * p.waves < 12 * CUS && tiles > 2 * p.waves)
-        p.splits = (int)std::max(1ll, std::min({(tiles + 2 * p.waves - 1) / (2 * p.waves), (16 * CUS + pairs * p.waves - 1) / (pairs * p.waves), 64ll}));
+    // Long histories of few pairs: as many parts as are all at work at once (a part too many waits
+    // for a place and then reads alone: 4 parts of 256 pairs in 3 places 221 us, 3 parts 199), of two tiles a wave at least.
+    const long long room = 4ll * waves_of(format, d, q.dtype == REC_BF16) * CUS / (pairs * p.waves);
+    p.splits = (int)std::max(1ll, std::min({room, tiles / (2 * p.waves), 64ll}));
     return p;
 }
 
@@ -646,26 +656,29 @@ hipError_t attend_of(const AttendArgs &a, const Plan &p, hipStream_t s)
 
 }  // namespace
 
-long long attend_threads(const Cache &c, const rec_query &q)
+long long attend_threads(const Cache &c, int format, int d, const rec_query &q)
 {
-    const Plan p = plan_of(c, q);
+    const Plan p = plan_of(c, format, d, q);
     return (long long)q.batch * c.kv_heads * p.row_tiles * p.splits * 64 * p.waves;
 }
 
-size_t attend_workspace(const Cache &c, int, int d, const rec_query &q)
+size_t attend_workspace(const Cache &c, int format, int d, const rec_query &q)
 {
     if (q.batch == 0 || q.queries == 0) return 0;
-    const Plan p = plan_of(c, q);
+    const Plan p = plan_of(c, format, d, q);
     return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)p.rows * ((size_t)d * sizeof(float) + sizeof(f32x2));
 }
 
 hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *workspace, hipStream_t s)
 {
-    const Plan p = plan_of(c, q);
+    const Plan p = plan_of(c, format, d, q);
     AttendArgs a;
     a.c = c;
     a.q = q;
     a.per = p.per;
+    a.by_per = Divider(p.per);
+    a.inner = Divider(p.splits * p.row_tiles);
+    a.heads = Divider(c.kv_heads);
     a.rows = (int)((long long)q.queries * p.per);
     a.row_tiles = p.row_tiles;
     a.splits = p.splits;

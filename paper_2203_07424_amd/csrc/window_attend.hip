@@ -42,8 +42,8 @@ constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
 struct WindowArgs {
     rec_window w;
     int per;  // query heads of a kv head
-    unsigned magic, shift;  // row / per = row * magic >> shift, in 64 bits, for rows below 2^31
-    int tiles;              // of BLOCK_ROWS, more than there can be
+    Divider by_per;
+    int tiles;  // of BLOCK_ROWS, more than there can be
 };
 
 __device__ inline float neg_inf() { return -__builtin_inff(); }
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
     if (first_row < 0 || first_row >= all_rows) return;
 
     const int window = w.window == 0 ? 0x7fffffff : w.window, sinks = w.sinks;
-    auto pos_of = [&](int row) { return (int)((unsigned long long)(unsigned)min(row, all_rows - 1) * a.magic >> a.shift); };
+    auto pos_of = [&](int row) { return a.by_per.of(min(row, all_rows - 1)); };
     const int p_lo = pos_of(first_row), p_hi = pos_of(first_row + BLOCK_ROWS - 1);
     const int wave_row = first_row + wave * WAVE_ROWS;
     const bool busy = wave_row < all_rows;
@@ -390,10 +390,7 @@ hipError_t launch_window(const rec_window &w, hipStream_t s)
     a.w = w;
     a.per = w.heads / w.kv_heads;
     a.tiles = (int)(window_blocks(w) / w.kv_heads);
-    // per in (2^(n-1), 2^n]: 2^(31+n) / per rounded up fits 32 bits and is exact for rows of 31.
-    const unsigned bits = a.per == 1 ? 0 : 32 - __builtin_clz((unsigned)a.per - 1);
-    a.shift = 31 + bits;
-    a.magic = (unsigned)(((1ull << a.shift) + a.per - 1) / a.per);
+    a.by_per = Divider(a.per);
     return w.head_dim == 32 ? window_as<32>(a, s) : w.head_dim == 64 ? window_as<64>(a, s) : window_as<128>(a, s);
 }
 
