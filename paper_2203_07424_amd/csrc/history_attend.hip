@@ -95,22 +95,34 @@ struct Query {
     i32x8 b[STEPS];
     int scale[STEPS];
 
-    // `row`: this lane's row (lane % 16) or null; its elements times `sign`.
-    __device__ inline void load(const void *row, float sign, int g)
+    static constexpr int PARTS = D == 128 ? 2 : 1;  // 16 elements of this lane each
+    u32x4 raw[PARTS][2];
+
+    // `row`: this lane's row (lane % 16) or null.
+    __device__ inline void fetch(const void *row, int g)
+    {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                raw[p][h] = u32x4{0u, 0u, 0u, 0u};
+                if (row) raw[p][h] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(row) + 2 * (64 * p + 16 * (D == 32 ? g & 1 : g) + 8 * h));
+            }
+    }
+
+    // What was fetched, times `sign`, as terms.
+    __device__ inline void convert(float sign, int g)
     {
         using T = std::conditional_t<BF, __bf16, _Float16>;
         typedef T tx8 __attribute__((ext_vector_type(8)));
-        constexpr int PARTS = D == 128 ? 2 : 1;  // 16 elements of this lane each
         float x[PARTS][2][8];
         unsigned most[PARTS];
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            const int first = 64 * p + 16 * (D == 32 ? g & 1 : g);
             most[p] = 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                tx8 v = {};
-                if (row) v = *reinterpret_cast<const tx8 *>(static_cast<const T *>(row) + first + 8 * h);
+                const tx8 v = __builtin_bit_cast(tx8, raw[p][h]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float f = (float)v[i];
@@ -374,9 +386,6 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
     if (begin + wave < end) {
         const int query = a.by_per.of(row), head = kv * a.per + row - query * a.per;
         const long long row_bytes = 2 * (b * a.q.batch_stride + query * a.q.query_stride + head * a.q.head_stride);
-        Query<D, BF> q;
-        q.load(first_row + c <= last_row ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr,
-               a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);
         // Positive, so that masked scores stay at -inf.
         const float factor = a.q.scale == 0.0f ? 1.0f : __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
         const int32_t *table = a.q.dev_pages_of + b * a.q.table_stride;
@@ -401,11 +410,14 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
 
         int n = begin + wave, key = key_of(n);
         int k_page = page_of(key + 16 * (c >> 2)), v_page = page_of(key + 16 * g);
+        Query<D, BF> q;
+        q.fetch(first_row + c <= last_row ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr, g);
         Tile<FMT, D> tile;
         tile.load_keys(group_at(k_page, key + 16 * (c >> 2)), c, g);
         tile.load_values(group_at(v_page, key + 16 * g), c);
         k_page = n + W < end ? page_of(key_of(n + W) + 16 * (c >> 2)) : -1;
         int v_next = n + W < end ? page_of(key_of(n + W) + 16 * g) : -1;
+        q.convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);  // while the first tile is on its way
         for (;; n += W) {
             const bool more = n + W < end;
             const int key_next = more ? key_of(n + W) : 0;
