@@ -42,8 +42,9 @@ constexpr float LOWEST = -3.4e38f;  // the maximum of a row that has seen nothin
 constexpr int CUS = 256;
 
 // Waves that a SIMD holds at once; the compiler gives a wave at most its share of registers.
-__host__ __device__ constexpr int waves_of(int format, int d, bool bf)
+__host__ __device__ constexpr int waves_of(int format, int d, bool bf, int heads)
 {
+    if (heads > 1) return d == 32 && format == REC_MX4 ? 3 : 2;
     return d == 128 ? (format == REC_MX4 && bf ? 3 : 2) : d == 64 ? (format == REC_MX4 && bf ? 4 : 3) : 4;
 }
 
@@ -55,7 +56,7 @@ struct AttendArgs {
     int rows;       // queries * per
     int row_tiles;  // of ROWS
     int splits;
-    Divider inner, heads;  // by splits * row_tiles, by kv_heads
+    Divider inner, heads;  // by splits * row_tiles, by the waves that have a history's kv heads
     float *part_o;   // [splits][batch * queries * heads][D]
     f32x2 *part_ml;  // [splits][batch * queries * heads]
 };
@@ -292,10 +293,11 @@ __device__ inline unsigned pack(float a, float b)
     return __builtin_bit_cast(unsigned, r);
 }
 
-// What a wave carries: for query row lane % 16, columns 16 i + 4 (lane / 16) ... + 3.
-template <int D>
+// What a wave carries: for query row lane % 16, columns 16 i + 4 (lane / 16) ... + 3.  With several
+// kv heads a wave, o[h] holds the products with head h's values, of which only its own rows count.
+template <int D, int HEADS>
 struct Sums {
-    f32x4 o[D / 16], l;
+    f32x4 o[HEADS][D / 16], l;
     float m;
 };
 
@@ -343,24 +345,28 @@ __device__ inline long long out_row(const AttendArgs &a, int b, int kv, int row)
     return ((long long)b * a.q.queries + i) * a.q.heads + kv * a.per + (row - i * a.per);
 }
 
-template <int FMT, int D, bool BF, int W>
-__global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(AttendArgs a)
+template <int FMT, int D, bool BF, int W, int HEADS>
+__global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_kernel(AttendArgs a)
 {
+    static_assert(HEADS == 1 || W == 1, "several heads a wave: only where there are waves enough");
+    constexpr int SLOT = ROWS / HEADS;  // rows of a kv head
     using T = std::conditional_t<BF, __bf16, _Float16>;
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int slot = c / SLOT, r = c % SLOT;  // which of the wave's kv heads, and its row
     // Parts of a history's head next to each other, then its heads, whose groups share a page.
     const int pair = a.inner.of((int)blockIdx.x), part = (int)blockIdx.x - pair * a.splits * a.row_tiles;
-    const int b = a.heads.of(pair), kv = pair - b * a.c.kv_heads;
+    const int b = a.heads.of(pair), first_kv = pair * HEADS - b * a.c.kv_heads, kv = first_kv + slot;
     const int row_tile = a.splits == 1 ? part : part / a.splits, split = part - row_tile * a.splits;
 
     const int shift = a.c.page_shift, most_tokens = a.q.table_width << shift;
     int len = a.q.dev_lengths[b];
     if (len < 0 || len > most_tokens) {
-        if (threadIdx.x == 0 && kv == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)b);
+        if (threadIdx.x == 0 && first_kv == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)b);
         len = len < 0 ? 0 : most_tokens;
     }
     // Positions of this wave's rows: of its first, its last, and this lane's; -1 sees nothing.
-    const int first_row = row_tile * ROWS, last_row = min(first_row + ROWS, a.rows) - 1, row = min(first_row + c, last_row);
+    const int first_row = row_tile * ROWS, last_row = min(first_row + SLOT, a.rows) - 1, row = min(first_row + r, last_row);
+    const bool real = first_row + r <= last_row;
     const bool together = a.q.candidates != 0;
     auto position = [&](int row) { return together ? len - 1 : max(len - a.q.queries + a.by_per.of(row), -1); };
     const int p_lo = position(first_row), p_hi = position(last_row), pos = position(row);
@@ -376,9 +382,11 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
     const int tiles = n_sink + n_to - n_from, each = (tiles + a.splits - 1) / a.splits;
     const int begin = min(split * each, tiles), end = min(begin + each, tiles);
 
-    Sums<D> sum;
+    Sums<D, HEADS> sum;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) sum.o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) sum.o[h][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     sum.l = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     sum.m = neg_inf();
     unsigned saw = 0;  // not 0: this lane's row has seen a key
@@ -390,8 +398,9 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
         const float factor = a.q.scale == 0.0f ? 1.0f : __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
         const int32_t *table = a.q.dev_pages_of + b * a.q.table_stride;
         const int groups = 1 << (shift - 4);
-        const unsigned char *first_page = a.c.pages + (long long)kv * groups * group_bytes<FMT>(D);
-        const unsigned page_bytes = (unsigned)(a.c.kv_heads * groups * group_bytes<FMT>(D));
+        const int head_bytes = groups * group_bytes<FMT>(D);
+        const unsigned char *first_page = a.c.pages + (long long)first_kv * head_bytes;
+        const unsigned page_bytes = (unsigned)(a.c.kv_heads * head_bytes);
         const unsigned pages = (unsigned)min(a.c.num_pages, 1ll << 31);
 
         // Tile n of the walk starts at this key.
@@ -411,25 +420,37 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
         int n = begin + wave, key = key_of(n);
         int k_page = page_of(key + 16 * (c >> 2)), v_page = page_of(key + 16 * g);
         Query<D, BF> q;
-        q.fetch(first_row + c <= last_row ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr, g);
-        Tile<FMT, D> tile;
-        tile.load_keys(group_at(k_page, key + 16 * (c >> 2)), c, g);
-        tile.load_values(group_at(v_page, key + 16 * g), c);
+        q.fetch(real ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr, g);
+        Tile<FMT, D> tile[HEADS];
+        auto load_keys = [&](int h, int key) { tile[h].load_keys(group_at(k_page, key + 16 * (c >> 2)) + h * head_bytes, c, g); };
+        auto load_values = [&](int h, int page, int key) { tile[h].load_values(group_at(page, key + 16 * g) + h * head_bytes, c); };
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) load_keys(h, key);
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) load_values(h, v_page, key);
         k_page = n + W < end ? page_of(key_of(n + W) + 16 * (c >> 2)) : -1;
         int v_next = n + W < end ? page_of(key_of(n + W) + 16 * g) : -1;
         q.convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);  // while the first tile is on its way
         for (;; n += W) {
             const bool more = n + W < end;
             const int key_next = more ? key_of(n + W) : 0;
-            f32x4 s[4] = {scores<FMT, D, BF, 0>(tile, q, g), scores<FMT, D, BF, 1>(tile, q, g), scores<FMT, D, BF, 2>(tile, q, g),
-                          scores<FMT, D, BF, 3>(tile, q, g)};
-            // The next tile's keys and values take the place of this one's as soon as that is used.
-            if (more) tile.load_keys(group_at(k_page, key_next + 16 * (c >> 2)), c, g);
+            f32x4 s[4];
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h) {
+                const f32x4 mine[4] = {scores<FMT, D, BF, 0>(tile[h], q, g), scores<FMT, D, BF, 1>(tile[h], q, g),
+                                       scores<FMT, D, BF, 2>(tile[h], q, g), scores<FMT, D, BF, 3>(tile[h], q, g)};
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[x][i] = h == 0 || slot == h ? mine[x][i] : s[x][i];
+                // The next tile's keys and values take the place of this one's as soon as that is used.
+                if (more) load_keys(h, key_next);
+            }
 
             // Groups come with their page or not at all.
             const bool there = (unsigned)v_page < pages;
             const bool whole = key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there);
-            unsigned nan = 0;  // bit b: row c sees a NaN in block b
+            unsigned nan = 0;  // bit 4 h + b: row c sees a NaN in block b of head h's values
             if (!whole) {
                 // Bit t: row c sees token t of group g; some row does.
                 const int first = key + 16 * g;
@@ -443,7 +464,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
                     seen = used = 0;
                 }
                 saw |= seen;
-                nan = clear_values<FMT, D>(tile, used, seen);
+#pragma unroll
+                for (int h = 0; h < HEADS; ++h) nan |= clear_values<FMT, D>(tile[h], used, seen) << (4 * h);
 #pragma unroll
                 for (int t = 0; t < 16; ++t) {
                     // -inf by its bits: no compare, no condition register.
@@ -466,7 +488,9 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
                 if (__any(sum.m != neg_inf())) {  // not the first tile
                     const float down = sum.m == m ? 1.0f : __builtin_amdgcn_exp2f(sum.m - m);
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) sum.o[i] *= down;
+                    for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) sum.o[h][i] *= down;
                     sum.l *= down;
                 }
                 sum.m = m;
@@ -496,27 +520,33 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
 #pragma unroll
                 for (int h = 0; h < 2; ++h) sum.l = product(ones, w[k][h], sum.l);
 #pragma unroll
-            for (int i = 0; i < D / BLOCK; ++i) {
-                u32x4 lo, hi;
-                value_operands<FMT, D, 0>(tile, i, lo, hi);
+            for (int h = 0; h < HEADS; ++h)
 #pragma unroll
-                for (int k = 0; k < TERMS; ++k) {
-                    sum.o[2 * i] = product(lo, w[k][0], sum.o[2 * i]);
-                    sum.o[2 * i + 1] = product(hi, w[k][0], sum.o[2 * i + 1]);
-                }
-                value_operands<FMT, D, 1>(tile, i, lo, hi);
+                for (int i = 0; i < D / BLOCK; ++i) {
+                    f32x4 &x = sum.o[h][2 * i], &y = sum.o[h][2 * i + 1];
+                    u32x4 lo, hi;
+                    value_operands<FMT, D, 0>(tile[h], i, lo, hi);
 #pragma unroll
-                for (int k = 0; k < TERMS; ++k) {
-                    sum.o[2 * i] = product(lo, w[k][1], sum.o[2 * i]);
-                    sum.o[2 * i + 1] = product(hi, w[k][1], sum.o[2 * i + 1]);
+                    for (int k = 0; k < TERMS; ++k) {
+                        x = product(lo, w[k][0], x);
+                        y = product(hi, w[k][0], y);
+                    }
+                    value_operands<FMT, D, 1>(tile[h], i, lo, hi);
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) {
+                        x = product(lo, w[k][1], x);
+                        y = product(hi, w[k][1], y);
+                    }
                 }
-            }
             if (nan)
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    if (nan >> (i / 2) & 1u) sum.o[i] += __builtin_nanf("");
+                for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+                        if (nan >> (4 * h + i / 2) & 1u) sum.o[h][i] += __builtin_nanf("");
             if (!more) break;
-            tile.load_values(group_at(v_next, key_next + 16 * g), c);
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h) load_values(h, v_next, key_next);
             key = key_next;
             v_page = v_next;
             if (n + 2 * W < end) {
@@ -531,8 +561,14 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
     saw |= (unsigned)__shfl_xor((int)saw, 32);
     if (saw && sum.m == neg_inf() && sum.l[0] == 0.0f) sum.m = LOWEST;
 
+    f32x4 o[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        o[i] = sum.o[0][i];
+#pragma unroll
+        for (int h = 1; h < HEADS; ++h) o[i] = slot == h ? sum.o[h][i] : o[i];
+    }
     const long long out = out_row(a, b, kv, row);
-    const bool real = first_row + c <= last_row;
     const long long all_rows = (long long)a.q.batch * a.q.queries * a.q.heads;
     if constexpr (W == 1) {
         const float l = sum.l[0];
@@ -541,13 +577,13 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
             if (real)
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
-                    *reinterpret_cast<f32x4 *>(a.part_o + (split * all_rows + out) * D + 16 * i + 4 * g) = sum.o[i];
+                    *reinterpret_cast<f32x4 *>(a.part_o + (split * all_rows + out) * D + 16 * i + 4 * g) = o[i];
         } else if (real) {
             const float by = inverse(l, sum.m);
             typedef T tx4 __attribute__((ext_vector_type(4)));
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
-                *reinterpret_cast<tx4 *>(static_cast<T *>(a.q.dev_out) + out * D + 16 * i + 4 * g) = __builtin_convertvector(sum.o[i] * by, tx4);
+                *reinterpret_cast<tx4 *>(static_cast<T *>(a.q.dev_out) + out * D + 16 * i + 4 * g) = __builtin_convertvector(o[i] * by, tx4);
         }
     } else {
         // Rows of all waves in LDS; a thread then joins eight columns of a row.
@@ -555,7 +591,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF)) void attend_kernel(At
         __shared__ float o_of[W][ROWS][LD];
         __shared__ f32x2 ml_of[W][ROWS];
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(&o_of[wave][c][16 * i + 4 * g]) = sum.o[i];
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(&o_of[wave][c][16 * i + 4 * g]) = o[i];
         if (g == 0) ml_of[wave][c] = f32x2{sum.m, sum.l[0]};
         __syncthreads();
         for (int i = threadIdx.x; i < ROWS * D / 8; i += 64 * W) {
@@ -618,6 +654,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const float *part_o, const
 
 struct Plan {
     int waves, splits, row_tiles, per;
+    int heads;       // kv heads of a wave
     long long rows;  // of the whole call
 };
 
@@ -629,7 +666,7 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q)
     const long long rows = (long long)q.queries * p.per;
     p.row_tiles = (int)((rows + ROWS - 1) / ROWS);
     const long long pairs = (long long)q.batch * c.kv_heads * p.row_tiles;
-    p.waves = p.splits = 1;
+    p.waves = p.splits = p.heads = 1;
     if (pairs == 0) return p;
     // Most tiles that a wave's rows can see something of.
     long long tiles = (((long long)q.table_width << c.page_shift) + TILE - 1) / TILE;
@@ -638,9 +675,12 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q)
         tiles = std::min(tiles, (q.window + apart + TILE - 2) / TILE + 1 + (q.sinks + TILE - 1ll) / TILE);
     }
     p.waves = tiles >= 4 && pairs < 4 * CUS ? 4 : tiles >= 2 && pairs < 8 * CUS ? 2 : 1;
+    // A wave has room for the rows of several kv heads: masks, exponentials and the rows' terms
+    // then cost it no more than for one.
+    if (d <= 64 && pairs >= 16 * CUS) p.heads = rows <= ROWS / 2 && c.kv_heads % 2 == 0 ? 2 : 1;
     // Long histories of few pairs: as many parts as are all at work at once (a part too many waits
     // for a place and then reads alone: 4 parts of 256 pairs in 3 places 221 us, 3 parts 199), of two tiles a wave at least.
-    const long long room = 4ll * waves_of(format, d, q.dtype == REC_BF16) * CUS / (pairs * p.waves);
+    const long long room = 4ll * waves_of(format, d, q.dtype == REC_BF16, 1) * CUS / (pairs * p.waves);
     p.splits = (int)std::max(1ll, std::min({room, tiles / (2 * p.waves), 64ll}));
     return p;
 }
@@ -648,10 +688,15 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q)
 template <int FMT, int D, bool BF>
 hipError_t attend_as(const AttendArgs &a, const Plan &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)((long long)a.q.batch * a.c.kv_heads * p.row_tiles * p.splits));
-    if (p.waves == 4) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 4>), grid, dim3(256), 0, s, a);
-    else if (p.waves == 2) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 2>), grid, dim3(128), 0, s, a);
-    else hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1>), grid, dim3(64), 0, s, a);
+    const dim3 grid((unsigned)((long long)a.q.batch * a.c.kv_heads / p.heads * p.row_tiles * p.splits));
+    if constexpr (D <= 64)
+        if (p.heads == 2) {
+            hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 2>), grid, dim3(64), 0, s, a);
+            return hipGetLastError();
+        }
+    if (p.waves == 4) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 4, 1>), grid, dim3(256), 0, s, a);
+    else if (p.waves == 2) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 2, 1>), grid, dim3(128), 0, s, a);
+    else hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 1>), grid, dim3(64), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     const int each = 256 / (D / 4);
@@ -690,7 +735,7 @@ hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, 
     a.per = p.per;
     a.by_per = Divider(p.per);
     a.inner = Divider(p.splits * p.row_tiles);
-    a.heads = Divider(c.kv_heads);
+    a.heads = Divider(c.kv_heads / p.heads);
     a.rows = (int)((long long)q.queries * p.per);
     a.row_tiles = p.row_tiles;
     a.splits = p.splits;
