@@ -628,28 +628,47 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
     }
 }
 
-// Joins the parts of a row: four columns a thread, always in the same order.
+// Joins the at most 64 parts of a row by a block: a lane looks up a part's weight, then groups
+// of D / 4 threads add up a share of the parts' sums, all loaded at once, and meet in LDS.  Always in the same order.  (A thread for all parts of its columns took 20 us for 64.)
 template <int D, bool BF>
 __global__ __launch_bounds__(256) void combine_kernel(const float *part_o, const f32x2 *part_ml, int splits, long long rows, void *out)
 {
     using T = std::conditional_t<BF, __bf16, _Float16>;
     typedef T tx4 __attribute__((ext_vector_type(4)));
-    constexpr int EACH = D / 4;
-    const long long row = (long long)blockIdx.x * (256 / EACH) + threadIdx.x / EACH;
-    if (row >= rows) return;
-    const int col = threadIdx.x % EACH * 4;
-    float m = neg_inf();
-    for (int s = 0; s < splits; ++s) m = fmaxf(m, part_ml[s * rows + row][0]);
-    float l = 0.0f;
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < splits; ++s) {
-        const f32x2 ml = part_ml[s * rows + row];
-        const float by = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - m);
-        l += ml[1] * by;
-        x += *reinterpret_cast<const f32x4 *>(part_o + (s * rows + row) * D + col) * by;
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ float weight[64];
+    __shared__ f32x4 sums[GROUPS][LANES];
+    const long long row = blockIdx.x;
+    const int col = threadIdx.x % LANES, group = threadIdx.x / LANES, lane = threadIdx.x & 63;
+    f32x2 ml = {neg_inf(), 0.0f};
+    if (lane < splits) ml = part_ml[lane * rows + row];
+    // The parts' sums are on their way while their weights are worked out.
+    f32x4 part[64 / GROUPS];
+#pragma unroll
+    for (int i = 0; i < 64 / GROUPS; ++i) {
+        part[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (group + i * GROUPS < splits) part[i] = *reinterpret_cast<const f32x4 *>(part_o + ((group + i * GROUPS) * rows + row) * D + 4 * col);
     }
+    float m = ml[0];
+#pragma unroll
+    for (int i = 32; i; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
+    const float by = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - m);
+    float l = ml[1] * by;
+#pragma unroll
+    for (int i = 32; i; i >>= 1) l += __shfl_xor(l, i);
+    if (threadIdx.x < 64) weight[lane] = by;
+    __syncthreads();
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 64 / GROUPS; ++i)
+        if (group + i * GROUPS < splits) x += part[i] * weight[group + i * GROUPS];
+    sums[group][col] = x;
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) x += sums[i][col];
     x *= inverse(l, m);
-    *reinterpret_cast<tx4 *>(static_cast<T *>(out) + row * D + col) = __builtin_convertvector(x, tx4);
+    *reinterpret_cast<tx4 *>(static_cast<T *>(out) + row * D + 4 * col) = __builtin_convertvector(x, tx4);
 }
 
 struct Plan {
@@ -699,9 +718,7 @@ hipError_t attend_as(const AttendArgs &a, const Plan &p, hipStream_t s)
     else hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 1>), grid, dim3(64), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    const int each = 256 / (D / 4);
-    hipLaunchKernelGGL((combine_kernel<D, BF>), dim3((unsigned)((p.rows + each - 1) / each)), dim3(256), 0, s, a.part_o, a.part_ml, p.splits,
-                       p.rows, a.q.dev_out);
+    hipLaunchKernelGGL((combine_kernel<D, BF>), dim3((unsigned)p.rows), dim3(256), 0, s, a.part_o, a.part_ml, p.splits, p.rows, a.q.dev_out);
     return hipGetLastError();
 }
 
