@@ -139,7 +139,8 @@ __device__ void redo_row(const T *q, const T *k, long long k_stride, const T *v,
         float most = x;
         for (int s = 32; s; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
         const float next = fmaxf(m, most);
-        const float p = seen ? __builtin_amdgcn_exp2f(x - next) : 0.0f;
+        // Scores of -inf alone so far have no weight beside a finite one to come.
+        const float p = seen ? __builtin_amdgcn_exp2f(x - (next == neg_inf() ? 0.0f : next)) : 0.0f;
         const float down = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
         m = next;
         float sum = p;
