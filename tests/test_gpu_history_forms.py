@@ -128,3 +128,27 @@ def test_a_row_computed_again_has_no_weight_on_scores_of_minus_infinity(b):
         # the sum's weights are exact; the mean is rounded once, and once more in sums of at most 25 terms in fp32
         assert (np.abs(got[row, 0] - want)[fine] <= 2.0 ** -8 * np.abs(want)[fine] + 2.0 ** -20).all(), row
     assert np.isnan(got[:70]).all() and np.isnan(got[95:]).all()
+
+
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("dtype,d", [(BF, 32), (HF, 64), (F32, 128), (F32, 64)])
+def test_every_16_bit_number_is_stored_nearest(b, fmt, dtype, d):
+    """Each finite bf16 or fp16 number as a block's largest, beside numbers up to its size; fp32 the same with lower bits."""
+    g = gen(47)
+    bits = torch.arange(0, 2 ** 15, 7, dtype=torch.int32)
+    top = bits.to(torch.int16).view(HF if dtype == HF else BF).float()
+    top = top[torch.isfinite(top)]
+    if dtype == F32:
+        top = torch.cat((top * (1 - 2.0 ** -10 * torch.rand(top.shape, generator=g)), torch.tensor([3.4028234e38, 1.8125 * 2.0 ** 127, 1.75 * 2.0 ** 127])))
+    x = top[:, None] * (2 * torch.rand(len(top), d, generator=g) - 1)
+    x[:, ::32] = top[:, None]
+    x = x.to(dtype)[:, None]
+    n = len(x)
+    c = b.HistoryCache(-(-n // 64), 64, 1, d, fmt)
+    slots = torch.arange(n).cuda()
+    c.write(x.cuda(), x.flip(2).contiguous().cuda(), slots)
+    assert c.check()[0] == b.REC_OK
+    rk, rv = c.read(slots, F32)
+    codes, scales = O.quantise(x.double().numpy().reshape(-1, 32), fmt)
+    want = torch.from_numpy(O.values(codes, fmt) * O.scale_values(scales)[:, None]).view(n, 1, d)
+    assert torch.equal(rk.cpu().double(), want) and torch.equal(rv.cpu().double(), want.flip(2))
