@@ -693,14 +693,21 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q)
         const long long apart = q.candidates ? 0 : std::min<long long>(q.queries - 1, (ROWS - 1) / p.per + 1);
         tiles = std::min(tiles, (q.window + apart + TILE - 2) / TILE + 1 + (q.sinks + TILE - 1ll) / TILE);
     }
-    p.waves = tiles >= 4 && pairs < 4 * CUS ? 4 : tiles >= 2 && pairs < 8 * CUS ? 2 : 1;
+    // Several waves for a history where there are few pairs, and where the longest may be much longer than most:
+    // a wave that has it alone works on when all others are done.  64-wide mx4, 4 kv heads, lengths up to 2000,
+    // log-uniform or all alike, four waves against one or two: 1600 pairs 72 -> 51 us or 174 -> 171 (up to 8000), 4096 pairs
+    // 53 -> 34 us, 8192 pairs 80 -> 65 us or 111 -> 122.  (80 events: 14.0 us with one wave, 15.0 with four.)
+    p.waves = (tiles >= 4 && pairs < 4 * CUS) || (tiles >= 16 && pairs <= 32 * CUS) ? 4 : tiles >= 2 && pairs < 8 * CUS ? 2 : 1;
     // A wave has room for the rows of several kv heads: masks, exponentials and the rows' terms
     // then cost it no more than for one.
-    if (d <= 64 && pairs >= 16 * CUS) p.heads = rows <= ROWS / 2 && c.kv_heads % 2 == 0 ? 2 : 1;
+    if (d <= 64 && p.waves == 1 && pairs >= 16 * CUS) p.heads = rows <= ROWS / 2 && c.kv_heads % 2 == 0 ? 2 : 1;
     // Long histories of few pairs: as many parts as are all at work at once (a part too many waits
     // for a place and then reads alone: 4 parts of 256 pairs in 3 places 221 us, 3 parts 199), of two tiles a wave at least.
+    // Where pairs alone take all places, parts of eight tiles a wave, up to four, for the longest of ragged
+    // histories (1600 pairs up to 8000 long 51 -> 43 us; all alike 171 -> 178).
     const long long room = 4ll * waves_of(format, d, q.dtype == REC_BF16, 1) * CUS / (pairs * p.waves);
-    p.splits = (int)std::max(1ll, std::min({room, tiles / (2 * p.waves), 64ll}));
+    const long long parts = room > 1 ? std::min({room, tiles / (2 * p.waves), 64ll}) : p.waves == 4 ? std::min(tiles / (8 * p.waves), 4ll) : 1;
+    p.splits = (int)std::max(1ll, parts);
     return p;
 }
 

@@ -152,3 +152,17 @@ def test_every_16_bit_number_is_stored_nearest(b, fmt, dtype, d):
     codes, scales = O.quantise(x.double().numpy().reshape(-1, 32), fmt)
     want = torch.from_numpy(O.values(codes, fmt) * O.scale_values(scales)[:, None]).view(n, 1, d)
     assert torch.equal(rk.cpu().double(), want) and torch.equal(rv.cpu().double(), want.flip(2))
+
+
+@pytest.mark.parametrize("batch,width,most,long", [(1024, 8, 300, ()), (1100, 70, 90, (4400, 2000, 2100)), (2100, 20, 90, (1200,)), (4200, 20, 60, (1000, 1279))])
+def test_a_few_much_longer_than_most(b, batch, width, most, long):
+    """Blocks of one wave whose histories are divided; of four, with parts and without; and more pairs than those are for."""
+    d = 64
+    n = many_lengths(batch, most, 2)
+    n[6:6 + len(long)] = long
+    s = Histories(b, n, 2, d, "mx4", 64, seed=48, width=width)
+    q = torch.randn(batch, 1, 4, d, generator=gen(49)).to(BF).cuda()
+    for window, sinks in ((0, 0), (70, 4)):
+        got = s.cache.attend(q, s.table, s.len_t, window=window, sinks=sinks)
+        check_some(s, q, got, [*range(10), *range(10, batch, 211)], d ** -0.5, window, sinks, what=window)
+    assert s.cache.check()[0] == b.REC_OK
