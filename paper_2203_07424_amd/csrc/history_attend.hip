@@ -22,6 +22,11 @@
 // Few pairs of history and head are divided: among the waves of a block, which meet in
 // LDS, and, where that leaves compute units idle, among blocks, whose parts
 // combine_kernel joins.
+//
+// Long histories are bound by the cache's bytes (32 of 32768 events, 8 kv heads of 128, mx4: 200 us, 5.7 TB/s), many
+// short ones by a chain of length, page and tile and the exponentials behind it (4096 of about 80 events, 2 kv heads
+// of 32, mx8, fp16: 18 us, 2.5 TB/s), candidates by the keys that several row tiles read (64 x 50 over up to 1004
+// events: 22 us).
 #include <algorithm>
 
 #include "history.h"
