@@ -58,6 +58,15 @@ __device__ inline f32x2 two_values(unsigned w)
     else return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, 1.0f, AT != 0);
 }
 
+// -inf where bit `bit` of `unseen` is set, else x, in two instructions.  The compiler may not look through
+// the bit: it would make a comparison and a selection of it (five a score).
+__device__ inline float unless_hidden(float x, unsigned unseen, int bit)
+{
+    unsigned hide = (unsigned)__builtin_amdgcn_sbfe((int)unseen, bit, 1);
+    asm("" : "+v"(hide));
+    return __builtin_bit_cast(float, (hide & 0xff800000u) | (~hide & __builtin_bit_cast(unsigned, x)));
+}
+
 // Division by a number that the host knows: n / d = n * magic >> shift in 64 bits, for n below
 // 2^31.  With d in (2^(k-1), 2^k], 2^(31+k) / d rounded up fits 32 bits and is off by less than
 // 2^k / 2^(31+k) of itself.

@@ -472,12 +472,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
 #pragma unroll
                 for (int h = 0; h < HEADS; ++h) nan |= clear_values<FMT, D>(tile[h], used, seen) << (4 * h);
 #pragma unroll
-                for (int t = 0; t < 16; ++t) {
-                    // -inf by its bits: no compare, no condition register.
-                    const float one = s[t & 3][t >> 2];
-                    const unsigned hide = (unsigned)__builtin_amdgcn_sbfe((int)~seen, t, 1);
-                    s[t & 3][t >> 2] = __builtin_bit_cast(float, (hide & 0xff800000u) | (~hide & __builtin_bit_cast(unsigned, one)));
-                }
+                for (int t = 0; t < 16; ++t) s[t & 3][t >> 2] = unless_hidden(s[t & 3][t >> 2], ~seen, t);
             } else {
                 saw = 1;
             }

@@ -21,7 +21,7 @@
 //
 // Bound by matrix instructions and the exponentials between them: 16 histories of 4096 events, 16 heads of 128 over
 // 4 kv heads, window 1024 + 4: 557 us, 867 TFLOP/s, 72 % of a large product of the vendor's library.  Of 256 ragged ones up to 1000
-// events (8 heads of 64, window 200 + 4: 43 us) by masks and exponentials, and the last blocks.  A third
+// events (8 heads of 64, window 200 + 4: 42 us) by masks and exponentials, and the last blocks.  A third
 // tile on its way to LDS brought nothing (617 against 604 us in a trace).
 #include <algorithm>
 
@@ -295,12 +295,7 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
                     const int first = key + 32 * u + 4 * half, ahead = max(pos - first, -1);
                     const unsigned unseen = ~(below(ahead + 1) & (~below(ahead - window + 1) | below(sinks - first)));
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        // -inf by its bits: no compare, no condition register.
-                        const float one = s[u][r];
-                        const unsigned hide = (unsigned)__builtin_amdgcn_sbfe((int)unseen, 8 * (r >> 2) + (r & 3), 1);
-                        s[u][r] = __builtin_bit_cast(float, (hide & 0xff800000u) | (~hide & __builtin_bit_cast(unsigned, one)));
-                    }
+                    for (int r = 0; r < 16; ++r) s[u][r] = unless_hidden(s[u][r], unseen, 8 * (r >> 2) + (r & 3));
                 }
             }
             float most = neg_inf();
