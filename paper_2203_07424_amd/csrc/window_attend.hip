@@ -20,7 +20,7 @@
 // a row whose result is not finite is computed again, key by key, from the keys it sees (redo_row()).
 //
 // Bound by matrix instructions and the exponentials between them: 16 histories of 4096 events, 16 heads of 128 over
-// 4 kv heads, window 1024 + 4: 557 us, 867 TFLOP/s, 72 % of a large product of the vendor's library.  Of 256 ragged ones up to 1000
+// 4 kv heads, window 1024 + 4: 557 to 568 us, 860 TFLOP/s, 71 % of a large product of the vendor's library.  Of 256 ragged ones up to 1000
 // events (8 heads of 64, window 200 + 4: 42 us) by masks and exponentials, and the last blocks.  A third
 // tile on its way to LDS brought nothing (617 against 604 us in a trace).
 #include <algorithm>
