@@ -340,6 +340,53 @@ __device__ inline unsigned clear_values(Tile<FMT, D> &t, unsigned used, unsigned
     return nan | (unsigned)__shfl_xor((int)nan, 32);
 }
 
+// Codes that are NaN under any scale (E4M3 has two; write_kernel makes neither, but a place that was never written may
+// hold them) count as zero too, and rows that see one get NaN in its column: a product of ones, where such a code is and where a
+// row sees its token, tells which.  Only where rows of a wave see different tokens; else clear_values() left none but
+// what all of them see.
+template <int D>
+__device__ inline void clear_nan_codes(Tile<REC_MX8, D> &t, unsigned seen, f32x4 (&o)[D / 16])
+{
+    auto nan_bytes = [](unsigned codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };  // their top bits
+    unsigned found = 0;
+#pragma unroll
+    for (int b = 0; b < D / BLOCK; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) found |= nan_bytes(t.v[b][i >> 2][i & 3]);
+    if (!__any(found != 0)) return;
+#pragma unroll
+    for (int b = 0; b < D / BLOCK; ++b) {
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
+        auto half = [&](auto h) {  // eight tokens
+            constexpr int H = h();
+            Tile<REC_MX8, D> ones;
+            u32x4 sees, lo, hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                unsigned codes = t.v[b][H][i];
+                asm("" : "+v"(codes));  // looked at again: what was found above would take a register a word
+                const unsigned top = nan_bytes(codes);
+                ones.v[b][H][i] = (top >> 7) * 0x38u;
+                t.v[b][H][i] = codes & ~((top << 1) - (top >> 7));
+                sees[i] = (seen >> (8 * H + 2 * i) & 1u) * 0x3f80u | (seen >> (8 * H + 2 * i + 1) & 1u) * 0x3f800000u;
+            }
+            ones.vs[b] = u32x4{0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+            value_operands<REC_MX8, D, H>(ones, b, lo, hi);
+            x = product(lo, sees, x);
+            y = product(hi, sees, y);
+            __builtin_amdgcn_sched_barrier(0);  // in these registers, then the next half
+        };
+        half(std::integral_constant<int, 0>());
+        half(std::integral_constant<int, 1>());
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            o[2 * b][i] = x[i] != 0.0f ? __builtin_nanf("") : o[2 * b][i];
+            o[2 * b + 1][i] = y[i] != 0.0f ? __builtin_nanf("") : o[2 * b + 1][i];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // Bits [0, n) of a lane's 16 tokens, for any n.
 __device__ inline unsigned below(int n) { return (1u << min(max(n, 0), 16)) - 1u; }
 
@@ -470,7 +517,11 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
                 }
                 saw |= seen;
 #pragma unroll
-                for (int h = 0; h < HEADS; ++h) nan |= clear_values<FMT, D>(tile[h], used, seen) << (4 * h);
+                for (int h = 0; h < HEADS; ++h) {
+                    nan |= clear_values<FMT, D>(tile[h], used, seen) << (4 * h);
+                    if constexpr (FMT == REC_MX8)
+                        if (p_lo != p_hi) clear_nan_codes<D>(tile[h], seen, sum.o[h]);
+                }
 #pragma unroll
                 for (int t = 0; t < 16; ++t) s[t & 3][t >> 2] = unless_hidden(s[t & 3][t >> 2], ~seen, t);
             } else {

@@ -1,0 +1,83 @@
+"""User histories at the edges of their contract: what a row does not see, whatever it holds."""
+import numpy as np
+import pytest
+import torch
+
+import history_oracle as O
+from test_gpu_history import BF, HF, F32, Histories, gen
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2203_07424_amd import binding
+    return binding
+
+
+@pytest.fixture(autouse=True)
+def say(request):
+    print(request.node.name, flush=True)
+
+
+# ------------------------------------------------------------ codes that are NaN
+def poke_value(s, row, head, column, byte):
+    """Sets the code of one column of a stored value (mx8), under the scale that is there."""
+    page, at = divmod(int(s.slots[row]), s.page_tokens)
+    block, j = divmod(column, 32)
+    d = s.d
+    place = 16 * d + ((16 * block + j % 16) * 16 + at % 16) * 2 + j // 16
+    s.cache.pages[page, head, at // 16, place] = byte
+
+
+@pytest.mark.parametrize("d,kv,per,dtype", [(32, 2, 1, HF), (64, 1, 4, BF), (128, 2, 2, BF), (128, 1, 3, HF)])
+@pytest.mark.parametrize("batch", [1, 2060])           # few pairs; enough for two kv heads a wave
+def test_a_code_that_is_nan_reaches_only_the_rows_that_see_it(b, d, kv, per, dtype, batch):
+    """E4M3 has codes that are NaN under any scale.  No call stores one, but a place that was never written may hold
+    it, and a length may count that place."""
+    n, nq, window, sinks = 100, 5, 40, 2
+    if batch > 1 and d == 128:
+        batch = 40
+    # For each history a token, the column and the head: seen by some queries, by none, by all; first of a window, last token.
+    where = [(98, 0), (97, d - 1), (99, 17), (57, 5), (58, 16), (60, d // 2), (30, 3), (1, 20), (2, 9), (70, 31)]
+    for shift in range(len(where) if batch == 1 else 1):
+        s = Histories(b, [n] * batch, kv, d, "mx8", 32, seed=51)
+        q = torch.randn(batch, nq, kv * per, d, generator=gen(52)).to(dtype).cuda()
+        at = {i: where[(i + shift) % len(where)] for i in range(min(batch, len(where)))}
+        for i, (token, column) in at.items():
+            poke_value(s, int(s.ends[i]) + token, i % kv, column, 0x7f if i % 2 else 0xff)
+        s.k, s.v = (x.double().cpu().numpy() for x in s.cache.read(s.slots.cuda(), F32))
+        for (token, column), i in zip(at.values(), at):
+            assert np.isnan(s.v[s.ends[i] + token, i % kv, column])
+        got = s.cache.attend(q, s.table, s.len_t, window=window, sinks=sinks)
+        qn = q.double().cpu().numpy()
+        for i in [*at, batch - 1]:
+            want, off = np.zeros(qn.shape[1:]), np.zeros(qn.shape[1:])
+            for h in range(kv * per):
+                k, v = (x[s.ends[i]:s.ends[i + 1], h // per] for x in (s.k, s.v))
+                want[:, h], off[:, h] = O.attend_rows(qn[i, :, h], k, v, range(n - nq, n), d ** -0.5, window, sinks, dtype)
+            if i in at:     # one column of the rows that see the token, and of the heads that share the kv head
+                token, column = at[i]
+                for x in range(nq):
+                    sees = O.sees(n - nq + x, token, window, sinks)
+                    assert np.isnan(want[x]).sum() == (per if sees else 0), (i, token, x)
+            O.assert_close(got[i], want, off, (i, at.get(i)))
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("fill", [0x7f, 0x7e])
+def test_places_within_a_length_that_were_never_written(b, d, fill):
+    """The last two tokens of each history were left out of the write: earlier queries are as if they were not there."""
+    n, nq = 70, 4
+    s = Histories(b, [n, n], 1, d, "mx8", 32, seed=53)
+    k, v = s.cache.read(s.slots.cuda(), F32)
+    s.cache.pages.fill_(fill)
+    slots = s.slots.clone()
+    for e in s.ends[1:]:
+        slots[e - 2:e] = -1
+    s.cache.write(k, v, slots.cuda())
+    q = torch.randn(2, nq, 2, d, generator=gen(54)).to(BF).cuda()
+    s.k, s.v = (x.double().cpu().numpy() for x in s.cache.read(s.slots.cuda(), F32))
+    want, off = s.expect(q, d ** -0.5, 0, 0, False)
+    assert np.isfinite(want[:, :2]).all() and (fill != 0x7f or np.isnan(want[:, 2:]).all())
+    O.assert_close(s.cache.attend(q, s.table, s.len_t), want, off)
