@@ -228,7 +228,6 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
     for (int i = 0; i < D / 16; ++i) {
         q[i] = *reinterpret_cast<const u32x4 *>(q_row + 16 * i + 8 * half);
         if (w.scale < 0.0f) q[i] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
-        if (w.scale == 0.0f) q[i] = u32x4{0u, 0u, 0u, 0u};
     }
     // Positive, so that masked scores stay at -inf.
     const float factor = w.scale == 0.0f ? 1.0f : __builtin_fabsf(w.scale) * 1.44269504088896341f;
@@ -268,6 +267,14 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
     float m = neg_inf(), l = 0.0f;
 
     fetch(key_of(0), 0);
+    if (w.scale == 0.0f)  // the query counts as zeros; where it is not finite there is no result (0 * inf)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                l = add_pair<BF>(q[i][j], l, 0.0f);
+                q[i][j] = 0u;
+            }
     for (int n = 0; n < count; ++n) {
         const int key = key_of(n);
         // This wave's part of tile n has arrived and its reads of the other buffer are done; then

@@ -81,3 +81,36 @@ def test_places_within_a_length_that_were_never_written(b, d, fill):
     want, off = s.expect(q, d ** -0.5, 0, 0, False)
     assert np.isfinite(want[:, :2]).all() and (fill != 0x7f or np.isnan(want[:, 2:]).all())
     O.assert_close(s.cache.attend(q, s.table, s.len_t), want, off)
+
+
+# ------------------------------------------------------------------- scale of zero
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_a_query_that_is_not_finite_has_no_result_under_a_scale_of_zero(b, dtype, d):
+    """0 * inf is NaN: in whole histories and over the cache; other rows get the mean of what they see."""
+    n, heads = 45, 2
+    q, k, v = (torch.randn(n, h, d, generator=gen(60 + h)).to(dtype) for h in (heads, 1, 1))
+    bad = {(0, 0): float("inf"), (7, 1): float("nan"), (31, 0): float("-inf"), (44, 1): float("inf")}
+    for i, ((row, head), x) in enumerate(bad.items()):
+        q[row, head, (5 * i) % d] = x
+    q[20, 0] = torch.finfo(dtype).max              # large, and finite
+    q, k, v = q.cuda(), k.cuda(), v.cuda()
+    vn = v.double().cpu().numpy()[:, 0]
+    want, off = np.zeros((n, heads, d)), np.zeros((n, heads, d))
+    for row in range(n):
+        for head in range(heads):
+            want[row, head] = np.nan if (row, head) in bad else vn[:row + 1].mean(0)
+            # weights and the mean are rounded to the type
+            off[row, head] = O.EPS[dtype] * (np.abs(want[row, head]) + np.abs(vn[:row + 1]).mean(0)) + 2.0 ** -20
+    O.assert_close(b.attend_window(q, k, v, torch.tensor([0, n], dtype=torch.int32).cuda(), scale=0.0), want, off)
+
+    cache = b.HistoryCache(2, 32, 1, d, "mx8")
+    slots = torch.arange(n).cuda()
+    cache.write(k, v, slots)
+    vn = cache.read(slots, F32)[1].double().cpu().numpy()[:, 0]
+    for row in range(n):
+        for head in range(heads):
+            want[row, head] = np.nan if (row, head) in bad else vn[:row + 1].mean(0)
+            off[row, head] = O.EPS[dtype] * (np.abs(want[row, head]) + np.abs(vn[:row + 1]).mean(0)) + 2.0 ** -20
+    got = cache.attend(q[None], torch.arange(2, dtype=torch.int32)[None].cuda(), torch.tensor([n], dtype=torch.int32).cuda(), scale=0.0)
+    O.assert_close(got[0], want, off)
