@@ -15,7 +15,7 @@
 // instead, so that what 16 lanes (keys) or 32 (values) read at once lies in 256 different bytes of
 // the 64 banks.
 //
-// The running maximum moves only when a tile's exceeds it by 2^8.  Masks are looked at in
+// The running maximum moves only when a tile's exceeds it by 2^8 (fp16: 2^4).  Masks are looked at in
 // tiles that some row of the wave sees partly, and a masked weight is 0.  Since 0 * NaN is NaN,
 // a row whose result is not finite is computed again, key by key, from the keys it sees (redo_row()).
 //
@@ -42,7 +42,13 @@ typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
 constexpr int WAVE_ROWS = 32, BLOCK_ROWS = WAVE_ROWS * WAVES;
-constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
+
+// The largest weight of a row lies between 2^lift and 2^(lift + slack).  bf16 has fp32's exponents, so that a weight's rounding is
+// of itself however small it is.  fp16 ends at 2^16 and, in steps of 2^-24, below: there a weight is off by at most 2^-36 of the largest,
+// so that 2^25 tokens of least weight are off by no more than the type's own rounding.  (Weights of at most 1 lost what was below
+// 2^-25 of the largest, and with it up to all of a result that thousands of small weights make.)
+constexpr float lift_of(bool bf) { return bf ? 0.0f : 11.0f; }
+constexpr float slack_of(bool bf) { return bf ? 8.0f : 4.0f; }
 
 struct WindowArgs {
     rec_window w;
@@ -264,7 +270,8 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
-    float m = neg_inf(), l = 0.0f;
+    constexpr float LIFT = lift_of(BF), SLACK = slack_of(BF);
+    float m = neg_inf(), l = 0.0f;  // m: the exponent of weight 1, LIFT below the largest score's
 
     fetch(key_of(0), 0);
     if (w.scale == 0.0f)  // the query counts as zeros; where it is not finite there is no result (0 * inf)
@@ -312,8 +319,9 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[u][r]);
             most = larger_half(most);
             most = most == neg_inf() ? most : most * factor;
-            if (__any(most > m + SLACK)) {
-                const float next = fmaxf(m, most);
+            if (__any(most > m + (LIFT + SLACK))) {
+                // Scores so large that LIFT would be lost in rounding do without it.
+                const float next = fmaxf(m, __builtin_fabsf(most) < 0x1p20f ? most - LIFT : most);
                 if (__any(m != neg_inf())) {  // not the first tile
                     const float down = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
 #pragma unroll

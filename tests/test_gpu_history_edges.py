@@ -114,3 +114,25 @@ def test_a_query_that_is_not_finite_has_no_result_under_a_scale_of_zero(b, dtype
             off[row, head] = O.EPS[dtype] * (np.abs(want[row, head]) + np.abs(vn[:row + 1]).mean(0)) + 2.0 ** -20
     got = cache.attend(q[None], torch.arange(2, dtype=torch.int32)[None].cuda(), torch.tensor([n], dtype=torch.int32).cuda(), scale=0.0)
     O.assert_close(got[0], want, off)
+
+
+# ------------------------------------------------- small weights beside a large one
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("below", [10.0, 14.0, 17.5, 20.0])
+@pytest.mark.parametrize("first", [True, False])
+def test_many_small_weights_beside_a_large_one(b, dtype, d, below, first):
+    """One key is e^below more likely than each of 4000 others, and its value is zero, so that the others are the result.
+    A weight is its type's rounding of itself, or off by at most 2^-36 of the largest (fp16 ends where bf16 and fp32 go on)."""
+    n = 4001
+    q, k, v = torch.zeros(n, 1, d), torch.zeros(n, 1, d), torch.rand(n, 1, d, generator=gen(61)) + 0.5
+    at = 0 if first else n - 3
+    q[:, 0, 3], k[at, 0, 3], v[at] = 4.0, below / 4, 0.0
+    q, k, v = (x.to(dtype).cuda() for x in (q, k, v))
+    got = b.attend_window(q, k, v, torch.tensor([0, n], dtype=torch.int32).cuda(), scale=1.0)
+    rows = [at + 1, at + 2, n - 2, n - 1] if not first else [1, 63, 64, 65, 1000, n - 1]
+    qn, kn, vn = (x.double().cpu().numpy()[:, 0] for x in (q, k, v))
+    want, off = O.attend_rows(qn[rows], kn, vn, rows, 1.0, 0, 0, dtype)
+    if dtype == HF:
+        off += np.array(rows)[:, None] * 2.0 ** -36 * np.abs(vn).max()
+    O.assert_close(got[rows, 0], want, off)
