@@ -382,9 +382,10 @@ def rec_window_attend(w: rec_window) -> int:
 
 
 def rec_history_check(dev_fault: torch.Tensor) -> Tuple[int, int, int]:
-    """(status, position, REC_FAULT_* word); the last two -1 without a fault."""
+    """(status, position, REC_FAULT_* word) of a record on the current device; the last two -1 without a fault.
+    Waits for the current stream: calls on others are counted once their work is done."""
     pos, word = C.c_int64(-1), C.c_int32(-1)
-    st = _lib.rec_history_check(_ptr(dev_fault), _stream(), C.byref(pos), C.byref(word))
+    st = _lib.rec_history_check(_ptr(dev_fault), _stream_on(dev_fault.get_device(), "rec_history_check"), C.byref(pos), C.byref(word))
     return st, pos.value, word.value
 
 
@@ -597,6 +598,8 @@ def _faults(device) -> torch.Tensor:
 
 def _stream_on(index: int, call: str) -> int:
     """The current stream of device `index`, which has to be the current device: kernels start there."""
+    if index < 0:
+        raise ValueError(f"{call}: the tensors are not on a device")
     if torch._C._cuda_getDevice() != index:
         raise ValueError(f"{call}: the tensors are on cuda:{index}, the current device is another")
     return torch._C._cuda_getCurrentRawStream(index)
@@ -721,7 +724,8 @@ class HistoryCache:
         return out
 
     def check(self) -> Tuple[int, int, int]:
-        """Waits; (status, position, REC_FAULT_* word) of the first fault since the last check."""
+        """(status, position, REC_FAULT_* word) of the first fault since the last check, of calls on the current stream
+        (waited for) and of what others have done by now."""
         return rec_history_check(self.fault)
 
 

@@ -1,0 +1,66 @@
+"""Host side of user histories: devices, fault records, counts that no launch takes.  No device."""
+import ctypes as C
+
+import pytest
+import torch
+
+from test_history_refusals import PTR, cache, rows
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2203_07424_amd import binding
+    return binding
+
+
+class Library:
+    """In the library's place: notes calls, and says that all is well."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append(name) or 0
+
+
+class OnDevice:
+    """A tensor of device `index`, as far as the binding looks at it."""
+    dtype, device = torch.int64, "cuda"
+
+    def __init__(self, index, words=4, contiguous=True):
+        self.index, self.words, self.contiguous = index, words, contiguous
+
+    def get_device(self):
+        return self.index
+
+    def numel(self):
+        return self.words
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def data_ptr(self):
+        return PTR
+
+
+@pytest.fixture
+def device_0(b, monkeypatch):
+    """The current device is 0, its current stream 7."""
+    lib = Library()
+    monkeypatch.setattr(b, "_lib", lib)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: {0: 7}[index], raising=False)
+    monkeypatch.setattr(b, "_stream", lambda: 7)
+    return lib
+
+
+def test_a_record_is_checked_on_its_own_device(b, device_0):
+    """Not on the current one's stream, which knows nothing of the record's calls."""
+    assert b.rec_history_check(OnDevice(0)) == (b.REC_OK, -1, -1)
+    assert device_0.calls == ["rec_history_check"]
+    h = object.__new__(b.HistoryCache)
+    h.fault = OnDevice(1)
+    for call in (h.check, lambda: b.rec_history_check(OnDevice(1)), lambda: b.rec_history_check(OnDevice(-1))):
+        with pytest.raises(ValueError):
+            call()
+    assert device_0.calls == ["rec_history_check"]
