@@ -381,9 +381,16 @@ def rec_window_attend(w: rec_window) -> int:
     return _lib.rec_window_attend(C.byref(w), _stream())
 
 
+def _is_record(fault: torch.Tensor) -> bool:
+    """Words next to each other: kernels write REC_FAULT_WORDS of them from the first on."""
+    return fault.dtype is torch.int64 and fault.numel() >= REC_FAULT_WORDS and fault.is_contiguous()
+
+
 def rec_history_check(dev_fault: torch.Tensor) -> Tuple[int, int, int]:
     """(status, position, REC_FAULT_* word) of a record on the current device; the last two -1 without a fault.
     Waits for the current stream: calls on others are counted once their work is done."""
+    if not _is_record(dev_fault):
+        raise ValueError(f"rec_history_check: a fault record is a contiguous int64 [{REC_FAULT_WORDS}]")
     pos, word = C.c_int64(-1), C.c_int32(-1)
     st = _lib.rec_history_check(_ptr(dev_fault), _stream_on(dev_fault.get_device(), "rec_history_check"), C.byref(pos), C.byref(word))
     return st, pos.value, word.value
@@ -733,7 +740,7 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: to
                   window: int = 0, sinks: int = 0, fault: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Whole histories attend to themselves (rec_window_attend()).  q: [tokens, heads, head_dim], k and v:
     [tokens, kv_heads, head_dim], fp16 or bf16, any token and head strides; offsets: int32 [batch + 1].
-    fault: int64 [REC_FAULT_WORDS], all -1, for rec_history_check(), or None."""
+    fault: int64 [REC_FAULT_WORDS], contiguous, all -1, for rec_history_check(), or None."""
     code, index = _ATTEND_CODES.get(q.dtype), q.get_device()
     if code is None or index < 0 or q.dim() != 3 or k.dim() != 3 or k.shape != v.shape:
         raise ValueError("rec_window_attend: q must be [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim] on a device, "
@@ -745,8 +752,8 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: to
         raise ValueError("rec_window_attend: q, k and v must agree in tokens, head_dim, type and device, rows contiguous")
     if offsets.dtype is not _I32 or offsets.get_device() != index or offsets.dim() != 1 or offsets.shape[0] < 1 or not offsets.is_contiguous():
         raise ValueError(f"rec_window_attend: offsets must be a contiguous int32 [batch + 1] on {q.device}")
-    if fault is not None and (fault.dtype is not _I64 or fault.get_device() != index or fault.numel() < REC_FAULT_WORDS):
-        raise ValueError(f"rec_window_attend: fault must be int64 [{REC_FAULT_WORDS}] on {q.device}")
+    if fault is not None and (fault.get_device() != index or not _is_record(fault)):
+        raise ValueError(f"rec_window_attend: fault must be a contiguous int64 [{REC_FAULT_WORDS}] on {q.device}")
     out = torch.empty_like(q, memory_format=torch.contiguous_format)
     st = _lib.rec_window_attend(
         _WINDOW.pack(q.data_ptr(), q_token, q_head, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, out.data_ptr(), code,

@@ -136,3 +136,18 @@ def test_many_small_weights_beside_a_large_one(b, dtype, d, below, first):
     if dtype == HF:
         off += np.array(rows)[:, None] * 2.0 ** -36 * np.abs(vn).max()
     O.assert_close(got[rows, 0], want, off)
+
+
+# ------------------------------------------------------------------- fault records
+def test_fault_records_that_have_words_between(b):
+    """Refused: kernels write four adjacent words."""
+    q = torch.zeros(4, 1, 32, dtype=BF, device="cuda")
+    offsets = torch.tensor([0, 4], dtype=torch.int32).cuda()
+    words = torch.full((16,), -1, dtype=torch.int64, device="cuda")
+    for fault in (words[::2], words[:3], words.int()):
+        with pytest.raises(ValueError):
+            b.attend_window(q, q, q, offsets, fault=fault)
+        with pytest.raises(ValueError):
+            b.rec_history_check(fault)
+    b.attend_window(q, q, q, offsets, fault=words[4:8])
+    assert b.rec_history_check(words[4:8]) == (b.REC_OK, -1, -1) and bool((words == -1).all())

@@ -64,3 +64,13 @@ def test_a_record_is_checked_on_its_own_device(b, device_0):
         with pytest.raises(ValueError):
             call()
     assert device_0.calls == ["rec_history_check"]
+
+
+def test_records_that_a_kernel_would_write_past(b, device_0):
+    """Four adjacent 64-bit words: fewer, others between them, or smaller ones are none."""
+    small = OnDevice(0)
+    small.dtype = torch.int32
+    for fault in (OnDevice(0, words=3), OnDevice(0, contiguous=False), small):
+        with pytest.raises(ValueError):
+            b.rec_history_check(fault)
+    assert device_0.calls == []
