@@ -44,7 +44,8 @@
  * allocated, calls only enqueue kernels on `stream` (so they can be captured), and
  * host-checkable faults return at once with nothing enqueued.  Faults only the
  * device can see never stop a call, touch nothing outside the buffers, and go into
- * the record dev_fault where there is one.
+ * the record dev_fault where there is one.  Arrays of 32-bit and 64-bit words lie on 4
+ * and 8 bytes (REC_ERR_ARG).
  */
 #ifndef REC_HISTORY_H
 #define REC_HISTORY_H

@@ -23,6 +23,9 @@ bool shape_fits(const rec_history *h)
 
 bool aligned(const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Words of `size` bytes, where there are any, on their own alignment.
+bool words_fit(const void *p, unsigned size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) == 0; }
+
 // Strides whose rows all start on 16 bytes.
 bool stride_fits(int64_t stride, int size) { return stride * size % 16 == 0; }
 
@@ -43,7 +46,7 @@ rec_status check_rows(const rec_history *h, int32_t dtype, const int64_t *dev_sl
     if (!h) return REC_ERR_ARG;
     if (!shape_fits(h)) return REC_ERR_SHAPE;
     if (!aligned(h->dev_pages) || (dtype != REC_F32 && dtype != REC_F16 && dtype != REC_BF16) || tokens < 0) return REC_ERR_ARG;
-    if (tokens && (!dev_slots || (reinterpret_cast<uintptr_t>(dev_slots) & 7u))) return REC_ERR_ARG;
+    if (!words_fit(h->dev_fault, 8) || (tokens && (!dev_slots || !words_fit(dev_slots, 8)))) return REC_ERR_ARG;
     if (tokens >= 1ll << 30 || tokens * h->kv_heads >= 1ll << 30) return REC_ERR_OVERFLOW;
     return REC_OK;
 }
@@ -118,10 +121,11 @@ rec_status rec_history_attend(const rec_history *h, const rec_query *q, void *de
 {
     const rec_status st = check_query(h, q);
     if (st != REC_OK) return st;
-    if (!aligned(h->dev_pages)) return REC_ERR_ARG;
+    if (!aligned(h->dev_pages) || !words_fit(h->dev_fault, 8)) return REC_ERR_ARG;
     if (q->batch == 0 || q->queries == 0) return REC_OK;
     if (!aligned(q->dev_q) || !aligned(q->dev_out) || !stride_fits(q->batch_stride, 2) || !stride_fits(q->query_stride, 2) ||
-        !stride_fits(q->head_stride, 2) || !q->dev_lengths || (q->table_width > 0 && !q->dev_pages_of))
+        !stride_fits(q->head_stride, 2) || !q->dev_lengths || !words_fit(q->dev_lengths, 4) || (q->table_width > 0 && !q->dev_pages_of) ||
+        !words_fit(q->dev_pages_of, 4))
         return REC_ERR_ARG;
     const size_t need = rec::hist::attend_workspace(cache_of(h), h->format, h->head_dim, *q);
     if (need && (!aligned(dev_workspace) || workspace_bytes < need)) return REC_ERR_ARG;
@@ -138,13 +142,15 @@ rec_status rec_window_attend(const rec_window *w, void *stream)
     if (w->tokens > MOST_TOKENS || w->tokens * w->heads >= 1ll << 31) return REC_ERR_OVERFLOW;
     if (rec::hist::window_blocks(*w) * 256 > MOST_THREADS || !tiles_fit(w->k) || !tiles_fit(w->v)) return REC_ERR_OVERFLOW;
     if (w->tokens == 0 || w->batch == 0) return REC_OK;
-    if (!rows_fit(w->q, 2) || !rows_fit(w->k, 2) || !rows_fit(w->v, 2) || !aligned(w->dev_out) || !w->dev_offsets) return REC_ERR_ARG;
+    if (!rows_fit(w->q, 2) || !rows_fit(w->k, 2) || !rows_fit(w->v, 2) || !aligned(w->dev_out) || !w->dev_offsets ||
+        !words_fit(w->dev_offsets, 4) || !words_fit(w->dev_fault, 8))
+        return REC_ERR_ARG;
     return status_of(rec::hist::launch_window(*w, static_cast<hipStream_t>(stream)));
 }
 
 rec_status rec_history_check(uint64_t *dev_fault, void *stream, int64_t *first_bad_pos, int32_t *word)
 {
-    if (!dev_fault) return REC_ERR_ARG;
+    if (!dev_fault || !words_fit(dev_fault, 8)) return REC_ERR_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     unsigned long long f[REC_FAULT_WORDS];
     if (hipStreamSynchronize(s) != hipSuccess) return REC_ERR_DEVICE;

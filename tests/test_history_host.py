@@ -74,3 +74,19 @@ def test_records_that_a_kernel_would_write_past(b, device_0):
         with pytest.raises(ValueError):
             b.rec_history_check(fault)
     assert device_0.calls == []
+
+
+def test_pointers_that_no_load_of_their_type_takes(b):
+    """32-bit and 64-bit words off their alignment: a scalar load rounds such an address down, an atomic faults."""
+    from test_history_refusals import query, window
+    h, odd = cache(b), cache(b, dev_fault=PTR + 4)
+    raw = lambda name: getattr(b._lib, name)  # noqa: E731
+    assert raw("rec_history_write")(C.byref(odd), C.byref(rows(b)), C.byref(rows(b)), b.REC_F32, PTR, 4, None) == b.REC_ERR_ARG
+    assert raw("rec_history_read")(C.byref(odd), PTR, 4, b.REC_F32, PTR, PTR, None) == b.REC_ERR_ARG
+    attend = lambda h, **kw: raw("rec_history_attend")(C.byref(h), C.byref(query(b, **kw)), None, 0, None)  # noqa: E731
+    assert attend(odd) == b.REC_ERR_ARG
+    for kw in (dict(dev_lengths=PTR + 2), dict(dev_pages_of=PTR + 1)):
+        assert attend(h, **kw) == b.REC_ERR_ARG, kw
+    for kw in (dict(dev_fault=PTR + 4), dict(dev_offsets=PTR + 2)):
+        assert raw("rec_window_attend")(C.byref(window(b, **kw)), None) == b.REC_ERR_ARG, kw
+    assert raw("rec_history_check")(PTR + 4, None, None, None) == b.REC_ERR_ARG
