@@ -112,7 +112,8 @@ typedef struct {
  * Device faults: REC_FAULT_SLOT (the row is left out), REC_FAULT_VALUE.
  * A slot that is named twice in one call holds one of its rows or a mixture.
  * REC_ERR_ARG: null, misaligned, bad enum, tokens < 0; REC_ERR_SHAPE: a shape that
- * rec_history_bytes() refuses; REC_ERR_OVERFLOW: tokens * kv_heads >= 2^30.
+ * rec_history_bytes() refuses; REC_ERR_OVERFLOW: 2^30 tokens, or
+ * ceil(tokens / 16) * kv_heads > 2^26 - 4 (more threads than a launch can have).
  */
 REC_API rec_status rec_history_write(const rec_history *h, const rec_rows *k, const rec_rows *v,
                                      int32_t dtype, const int64_t *dev_slots, int64_t tokens, void *stream);

@@ -81,6 +81,7 @@ struct Divider {
     __device__ int of(int n) const { return (int)((unsigned long long)(unsigned)n * magic >> shift); }
 };
 
+long long rows_threads(const Cache &c, long long tokens);  // along x, for keys or values
 hipError_t launch_write(const Cache &c, int format, int d, const rec_rows &k, const rec_rows &v, int dtype,
                         const int64_t *slots, long long tokens, hipStream_t s);
 hipError_t launch_read(const Cache &c, int format, int d, const int64_t *slots, long long tokens, int dtype,

@@ -47,7 +47,7 @@ rec_status check_rows(const rec_history *h, int32_t dtype, const int64_t *dev_sl
     if (!shape_fits(h)) return REC_ERR_SHAPE;
     if (!aligned(h->dev_pages) || (dtype != REC_F32 && dtype != REC_F16 && dtype != REC_BF16) || tokens < 0) return REC_ERR_ARG;
     if (!words_fit(h->dev_fault, 8) || (tokens && (!dev_slots || !words_fit(dev_slots, 8)))) return REC_ERR_ARG;
-    if (tokens >= 1ll << 30 || tokens * h->kv_heads >= 1ll << 30) return REC_ERR_OVERFLOW;
+    if (tokens >= 1ll << 30 || rec::hist::rows_threads(cache_of(h), tokens) > MOST_THREADS) return REC_ERR_OVERFLOW;
     return REC_OK;
 }
 

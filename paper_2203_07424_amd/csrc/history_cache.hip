@@ -505,11 +505,7 @@ struct Rows {
     rec_rows k, v;
 };
 
-dim3 grid_of(const Cache &c, long long tokens)
-{
-    const long long waves = (tokens + 15) / 16 * c.kv_heads;
-    return dim3((unsigned)((waves + THREADS / 64 - 1) / (THREADS / 64)), 2);
-}
+dim3 grid_of(const Cache &c, long long tokens) { return dim3((unsigned)(rows_threads(c, tokens) / THREADS), 2); }
 
 template <int FMT, int DT, int D>
 hipError_t write_as(const Cache &c, const Rows &in, const int64_t *slots, long long tokens, hipStream_t s)
@@ -546,6 +542,12 @@ hipError_t with_all(int format, int dtype, int d, const F &f)
 }
 
 }  // namespace
+
+long long rows_threads(const Cache &c, long long tokens)
+{
+    const long long waves = (tokens + 15) / 16 * c.kv_heads;
+    return (waves + THREADS / 64 - 1) / (THREADS / 64) * THREADS;
+}
 
 hipError_t launch_write(const Cache &c, int format, int d, const rec_rows &k, const rec_rows &v, int dtype,
                         const int64_t *slots, long long tokens, hipStream_t s)

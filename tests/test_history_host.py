@@ -90,3 +90,14 @@ def test_pointers_that_no_load_of_their_type_takes(b):
     for kw in (dict(dev_fault=PTR + 4), dict(dev_offsets=PTR + 2)):
         assert raw("rec_window_attend")(C.byref(window(b, **kw)), None) == b.REC_ERR_ARG, kw
     assert raw("rec_history_check")(PTR + 4, None, None, None) == b.REC_ERR_ARG
+
+
+@pytest.mark.parametrize("kv_heads", [1, 2, 3, 1024])
+def test_more_rows_than_a_launch_has_threads_for(b, kv_heads):
+    """A wave has 16 rows of a head, a block four, and a launch under 2^32 threads: refused as such, before it fails."""
+    h, r = cache(b, kv_heads=kv_heads), rows(b)
+    blocks = lambda n: -(-(-(-n // 16) * kv_heads) // 4)  # noqa: E731
+    first = next(n for n in range((1 << 30) // kv_heads - 200, (1 << 30) // kv_heads + 200) if blocks(n) * 256 >= 1 << 32)
+    for n in (first, first + 1, 1 << 30):
+        assert b._lib.rec_history_write(C.byref(h), C.byref(r), C.byref(r), b.REC_F32, PTR, n, None) == b.REC_ERR_OVERFLOW, n
+        assert b._lib.rec_history_read(C.byref(h), PTR, n, b.REC_F32, PTR, PTR, None) == b.REC_ERR_OVERFLOW, n
