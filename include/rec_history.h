@@ -200,7 +200,8 @@ typedef struct {
 
 REC_API rec_status rec_window_attend(const rec_window *w, void *stream);
 
-/* Waits for `stream`, reads a fault record and clears it.  REC_OK, REC_ERR_LENGTHS
+/* Waits for `stream`, reads a fault record and clears what it read: faults that work on other
+ * streams adds meanwhile stay for the next check.  REC_OK, REC_ERR_LENGTHS
  * (REC_FAULT_LENGTH), REC_ERR_INDEX_RANGE (REC_FAULT_SLOT or REC_FAULT_PAGE) or
  * REC_ERR_VALUE (REC_FAULT_VALUE), the first of these that applies, with its position
  * in *first_bad_pos (may be null; -1 without a fault) and its word in *word (may be null). */

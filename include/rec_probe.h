@@ -15,6 +15,8 @@
  *
  * Which kernel a layer's launch takes, and which stages of a forward share a launch
  * (host code, no device).
+ *
+ * How a checked fault record of user histories is cleared.
  */
 #ifndef REC_PROBE_H
 #define REC_PROBE_H
@@ -101,6 +103,10 @@ REC_API rec_status rec_probe_plan_pooling(const rec_model *m, int32_t batch, int
  * waves, deal[2] units a wave at most, a unit four wave-wide accesses.  left: -1, the launch of the scan or of
  * scan and a few lookups; else compute units without a block of the launch of many lookups. */
 REC_API rec_status rec_probe_dense_copy(int32_t rows, int32_t columns, int32_t pad, int32_t left, int32_t *deal);
+
+/* The end of rec_history_check() (rec_history.h): words of a fault record become all ones where they
+ * still are what was read before, seen[] (host memory, as many words as a record has).  REC_ERR_ARG: null, misaligned. */
+REC_API rec_status rec_probe_clear_faults(uint64_t *dev_fault, const uint64_t *seen, void *stream);
 
 #ifdef __cplusplus
 }

@@ -32,6 +32,11 @@ struct Cache {
     unsigned long long *fault;
 };
 
+// A fault record's words, as they were read.
+struct Faults {
+    unsigned long long word[REC_FAULT_WORDS];
+};
+
 __device__ inline void report(unsigned long long *fault, int word, unsigned long long position)
 {
     if (fault) atomicMin(fault + word, position);
@@ -91,7 +96,7 @@ size_t attend_workspace(const Cache &c, int format, int d, const rec_query &q);
 hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *workspace, hipStream_t s);
 long long window_blocks(const rec_window &w);  // of 256 threads
 hipError_t launch_window(const rec_window &w, hipStream_t s);
-hipError_t launch_clear_faults(unsigned long long *fault, hipStream_t s);
+hipError_t launch_clear_faults(unsigned long long *fault, const Faults &seen, hipStream_t s);
 
 }  // namespace hist
 }  // namespace rec

@@ -1,5 +1,6 @@
 // Host side of include/rec_history.h: checks, and nothing else.
 #include "history.h"
+#include "rec_probe.h"
 
 namespace {
 
@@ -152,10 +153,11 @@ rec_status rec_history_check(uint64_t *dev_fault, void *stream, int64_t *first_b
 {
     if (!dev_fault || !words_fit(dev_fault, 8)) return REC_ERR_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    unsigned long long f[REC_FAULT_WORDS];
+    rec::hist::Faults read;
+    const auto &f = read.word;
     if (hipStreamSynchronize(s) != hipSuccess) return REC_ERR_DEVICE;
-    if (hipMemcpy(f, dev_fault, sizeof(f), hipMemcpyDeviceToHost) != hipSuccess) return REC_ERR_DEVICE;
-    if (rec::hist::launch_clear_faults(reinterpret_cast<unsigned long long *>(dev_fault), s) != hipSuccess) return REC_ERR_DEVICE;
+    if (hipMemcpy(&read, dev_fault, sizeof(read), hipMemcpyDeviceToHost) != hipSuccess) return REC_ERR_DEVICE;
+    if (rec::hist::launch_clear_faults(reinterpret_cast<unsigned long long *>(dev_fault), read, s) != hipSuccess) return REC_ERR_DEVICE;
     if (hipStreamSynchronize(s) != hipSuccess) return REC_ERR_DEVICE;
     for (int i = 0; i < REC_FAULT_WORDS; ++i) {
         if (f[i] == ~0ull) continue;
@@ -166,6 +168,14 @@ rec_status rec_history_check(uint64_t *dev_fault, void *stream, int64_t *first_b
     if (first_bad_pos) *first_bad_pos = -1;
     if (word) *word = -1;
     return REC_OK;
+}
+
+rec_status rec_probe_clear_faults(uint64_t *dev_fault, const uint64_t *seen, void *stream)
+{
+    if (!dev_fault || !words_fit(dev_fault, 8) || !seen) return REC_ERR_ARG;
+    rec::hist::Faults read;
+    for (int i = 0; i < REC_FAULT_WORDS; ++i) read.word[i] = seen[i];
+    return status_of(rec::hist::launch_clear_faults(reinterpret_cast<unsigned long long *>(dev_fault), read, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

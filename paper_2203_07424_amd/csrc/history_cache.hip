@@ -496,9 +496,10 @@ __global__ __launch_bounds__(THREADS) void read_kernel(Cache c, const int64_t *s
     }
 }
 
-__global__ void clear_faults_kernel(unsigned long long *fault)
+// A word that has been lowered since it was read stays.
+__global__ void clear_faults_kernel(unsigned long long *fault, Faults seen)
 {
-    if (threadIdx.x < REC_FAULT_WORDS) fault[threadIdx.x] = ~0ull;
+    if (threadIdx.x < REC_FAULT_WORDS) atomicCAS(fault + threadIdx.x, seen.word[threadIdx.x], ~0ull);
 }
 
 struct Rows {
@@ -562,9 +563,9 @@ hipError_t launch_read(const Cache &c, int format, int d, const int64_t *slots, 
     return with_all(format, dtype, d, [&](auto fmt, auto dt, auto dim) { return read_as<fmt(), dt(), dim()>(c, slots, tokens, k, v, s); });
 }
 
-hipError_t launch_clear_faults(unsigned long long *fault, hipStream_t s)
+hipError_t launch_clear_faults(unsigned long long *fault, const Faults &seen, hipStream_t s)
 {
-    hipLaunchKernelGGL(clear_faults_kernel, dim3(1), dim3(64), 0, s, fault);
+    hipLaunchKernelGGL(clear_faults_kernel, dim3(1), dim3(64), 0, s, fault, seen);
     return hipGetLastError();
 }
 

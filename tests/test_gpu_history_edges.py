@@ -151,3 +151,14 @@ def test_fault_records_that_have_words_between(b):
             b.rec_history_check(fault)
     b.attend_window(q, q, q, offsets, fault=words[4:8])
     assert b.rec_history_check(words[4:8]) == (b.REC_OK, -1, -1) and bool((words == -1).all())
+
+
+def test_a_fault_that_comes_while_a_record_is_checked_stays(b):
+    """A check clears what it read: a word that another stream has lowered since is the next check's."""
+    record = torch.tensor([5, -1, 7, 9], dtype=torch.int64).cuda()
+    assert b.rec_probe_clear_faults(record, [5, -1, 8, 9]) == b.REC_OK
+    assert record.tolist() == [-1, -1, 7, -1]
+    assert b.rec_probe_clear_faults(record, [-1, -1, -1, -1]) == b.REC_OK      # read before there was any
+    assert record.tolist() == [-1, -1, 7, -1]
+    assert b.rec_history_check(record) == (b.REC_ERR_INDEX_RANGE, 7, b.REC_FAULT_PAGE)
+    assert b.rec_history_check(record) == (b.REC_OK, -1, -1)
