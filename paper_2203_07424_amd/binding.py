@@ -622,13 +622,20 @@ def _stream_on(index: int, call: str) -> int:
     return torch._C._cuda_getCurrentRawStream(index)
 
 
+def _no_backward(call: str) -> None:
+    """For a call with inputs that require grad: refused where a result without gradients would lose them unseen."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{call} has no backward pass: detach its inputs, or call it under torch.no_grad()")
+
+
 class HistoryCache:
     """Keys and values of user histories in 4 or 8 bits a number (include/rec_history.h), and
     attention over them.
 
     The pages are one uint8 tensor, the cache's own or the caller's (`pages`, of
     [num_pages, kv_heads, page_tokens / 16, bytes of a group]); which page holds what is the
-    caller's bookkeeping.  Calls go to the current stream and only enqueue."""
+    caller's bookkeeping.  Calls go to the current stream and only enqueue.  They serve: there is no
+    backward pass, and inputs that require grad are refused unless grad mode is off."""
 
     def __init__(self, num_pages: int, page_tokens: int, kv_heads: int, head_dim: int, fmt: str = "mx4",
                  device: str = "cuda:0", pages: Optional[torch.Tensor] = None):
@@ -672,6 +679,8 @@ class HistoryCache:
     def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
         """k, v: [tokens, kv_heads, head_dim] (any token and head strides), fp32, fp16 or bf16;
         slots: int64 [tokens], page * page_tokens + place, -1 for a row to leave out."""
+        if k.requires_grad or v.requires_grad:
+            _no_backward("rec_history_write")
         n = self._slots("rec_history_write", slots)
         code = _DTYPE_CODES.get(k.dtype)
         if code is None:
@@ -701,6 +710,8 @@ class HistoryCache:
         """q: [batch, queries, heads, head_dim] or, one query each, [batch, heads, head_dim], fp16 or bf16
         (any strides but the last); pages_of: int32 [batch, width], a history's pages in order; lengths:
         int32 [batch].  scale: 1 / sqrt(head_dim) if None.  Returns attention outputs of q's shape, contiguous."""
+        if q.requires_grad:
+            _no_backward("rec_history_attend")
         index, code = self._index, _ATTEND_CODES.get(q.dtype)
         if q.dim() == 4:
             batch, queries, heads, dim = q.shape
@@ -750,7 +761,9 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: to
                   window: int = 0, sinks: int = 0, fault: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Whole histories attend to themselves (rec_window_attend()).  q: [tokens, heads, head_dim], k and v:
     [tokens, kv_heads, head_dim], fp16 or bf16, any token and head strides; offsets: int32 [batch + 1].
-    fault: int64 [REC_FAULT_WORDS], contiguous, all -1, for rec_history_check(), or None."""
+    fault: int64 [REC_FAULT_WORDS], contiguous, all -1, for rec_history_check(), or None.  No backward pass, as in HistoryCache."""
+    if q.requires_grad or k.requires_grad or v.requires_grad:
+        _no_backward("rec_window_attend")
     code, index = _ATTEND_CODES.get(q.dtype), q.get_device()
     if code is None or index < 0 or q.dim() != 3 or k.dim() != 3 or k.shape != v.shape:
         raise ValueError("rec_window_attend: q must be [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim] on a device, "

@@ -101,3 +101,20 @@ def test_more_rows_than_a_launch_has_threads_for(b, kv_heads):
     for n in (first, first + 1, 1 << 30):
         assert b._lib.rec_history_write(C.byref(h), C.byref(r), C.byref(r), b.REC_F32, PTR, n, None) == b.REC_ERR_OVERFLOW, n
         assert b._lib.rec_history_read(C.byref(h), PTR, n, b.REC_F32, PTR, PTR, None) == b.REC_ERR_OVERFLOW, n
+
+
+def test_tensors_that_require_grad_are_refused(b):
+    """There is no backward pass, and a result without one would lose gradients without a word."""
+    x = torch.zeros(10, 2, 64, dtype=torch.float16)
+    y, at = x.clone().requires_grad_(), torch.zeros(10, dtype=torch.int64)
+    h = object.__new__(b.HistoryCache)
+    h._index, h.head_dim, h.kv_heads, h.device = 0, 64, 2, "cuda:0"
+    calls = [lambda q, k, v: b.attend_window(q, k, v, at.int()), lambda q, k, v: h.write(k, v, at), lambda q, k, v: h.attend(q, at[:, None].int(), at.int())]
+    for call, which in zip(calls, ((0, 1, 2), (1, 2), (0,))):
+        for i in which:
+            args = [y if j == i else x for j in range(3)]
+            with pytest.raises(ValueError, match="backward"):
+                call(*args)
+            with torch.no_grad(), pytest.raises(ValueError) as e:      # what the call says next: not on a device
+                call(*args)
+            assert "backward" not in str(e.value)
