@@ -61,6 +61,13 @@ def plain(q, k, v, position, window, sinks):
     return (torch.softmax(x, 0)[..., None] * v).sum(0)
 
 
+def off_by(got, want) -> float:
+    """The largest error, of the largest output.  NaN would pass any bound that is compared with it."""
+    if got.shape != want.shape or not (torch.isfinite(got).all() and torch.isfinite(want).all()):
+        raise ArithmeticError(f"user_histories: {tuple(got.shape)} against {tuple(want.shape)}, or numbers that are not finite")
+    return float((got.float() - want).abs().max() / want.abs().max())
+
+
 def main(argv=None) -> dict:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--users", type=int, default=256)
@@ -88,8 +95,7 @@ def main(argv=None) -> dict:
         return x[:, :HEADS], x[:, HEADS:HEADS + KV_HEADS], x[:, HEADS + KV_HEADS:]
 
     def compare(stage, got, want):
-        off = float((got.float() - want).abs().max() / want.abs().max())
-        worst[stage] = max(worst.get(stage, 0.0), off)
+        worst[stage] = max(worst.get(stage, 0.0), off_by(got, want))
 
     def timed(stage, call):
         torch.cuda.synchronize()
