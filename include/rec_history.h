@@ -181,6 +181,7 @@ REC_API rec_status rec_history_attend(const rec_history *h, const rec_query *q, 
  *   dev_fault     as in rec_history; may be null
  * Device faults: REC_FAULT_LENGTH (offsets that decrease, or do not run from 0 to tokens,
  * are brought into that range; rows of no history are not written).
+ * Rows near a value that is not finite are computed a second time, several times as slowly.
  * REC_ERR_ARG, REC_ERR_SHAPE as above; REC_ERR_OVERFLOW: tokens * heads >= 2^31, more
  * than 2^24 workgroups (tokens * heads / 128 + batch * kv_heads), a token stride of k or v that is
  * negative or >= 2^23 elements.

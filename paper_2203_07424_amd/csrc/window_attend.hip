@@ -17,7 +17,7 @@
 //
 // The running maximum moves only when a tile's exceeds it by 2^8 (fp16: 2^4).  Masks are looked at in
 // tiles that some row of the wave sees partly, and a masked weight is 0.  Since 0 * NaN is NaN,
-// a row whose result is not finite is computed again, key by key, from the keys it sees (redo_row()).
+// rows whose results are not finite are computed again, from what they see (again()).
 //
 // Bound by matrix instructions and the exponentials between them: 16 histories of 4096 events, 16 heads of 128 over
 // 4 kv heads, window 1024 + 4: 557 to 568 us, 860 TFLOP/s, 71 % of a large product of the vendor's library.  Of 256 ragged ones up to 1000
@@ -105,8 +105,6 @@ __device__ inline int value_place(int row, int piece)
     return piece ^ (D == 32 ? 0 : D == 64 ? (row & 2) << 1 : (row & 3) << 2);
 }
 
-__device__ inline bool sees(int pos, int j, int window, int sinks) { return j <= pos && (pos - j < window || j < sinks); }
-
 // The larger of lanes l and l ^ 32.
 __device__ inline float larger_half(float x)
 {
@@ -129,48 +127,146 @@ __device__ inline unsigned below(int n) { return (1u << min(max(n, 0), 28)) - 1u
 // fit 31 bits (launch_window()'s callers see to that).
 __device__ inline int first_tile(int offset, int per, int b) { return (int)((unsigned)offset * (unsigned)per / BLOCK_ROWS) + b; }
 
-// One row by a wave, from nothing but what it sees.
-template <int D, typename T>
-__device__ void redo_row(const T *q, const T *k, long long k_stride, const T *v, long long v_stride, int pos, float factor, int window,
-                         int sinks, T *out, int lane)
+// A wave's rows once more, of which those in `rows` are stored: numbers of the values that are not finite count as zeros, and
+// products of ones, where such a number is and where a row sees its key, tell whose results they are.  A slow path without barriers
+// in few registers: 32 columns at a time, flags first, then sums; keys, queries and values straight from memory, values two bytes a
+// lane.  Weights are such that no sum of finite numbers overflows, however large they are: at most 2^-40 in bf16, which goes on below.
+// 4 histories of 4096 events (16 heads of 128 over 4), one with a NaN value in its first event, that all rows see: 0.33 -> 2.5 ms; 256 of
+// 160 events (8 heads of 64) 37 -> 68 us.  (A wave that took a row at a time, key by key: 23 ms and 701 us.)
+template <int D, bool BF, typename T>
+__device__ inline void again(const WindowArgs &a, int start, int len, int kv, int wave_row, unsigned rows, int lane)
 {
-    constexpr int EACH = (D + 63) / 64;
-    float m = neg_inf(), l = 0.0f, o[EACH] = {};
-    for (int t0 = 0; t0 <= pos; t0 += 64) {
-        const int j = t0 + lane;
-        const bool seen = sees(pos, j, window, sinks);
-        float x = neg_inf();
-        if (seen) {
-            x = 0.0f;
-            for (int e = 0; e < D; ++e) x += (float)q[e] * (float)k[j * k_stride + e];
-            x *= factor;
+    constexpr unsigned TOP = BF ? 0x7f80u : 0x7c00u, ONE = BF ? 0x3f80u : 0x3c00u;
+    constexpr float LIFT = BF ? -40.0f : lift_of(false);
+    const rec_window &w = a.w;
+    const int c = lane & 31, half = lane >> 5, all_rows = len * a.per;
+    auto pos_of = [&](int row) { return a.by_per.of(min(row, all_rows - 1)); };
+    const int w_lo = pos_of(wave_row), w_hi = pos_of(wave_row + WAVE_ROWS - 1), pos = pos_of(wave_row + c);
+    const int head = kv * a.per + min(wave_row + c, all_rows - 1) - pos * a.per;
+    const int window = w.window == 0 ? 0x7fffffff : w.window, sinks = w.sinks;
+    const T *k_base = static_cast<const T *>(w.k.dev) + (long long)start * w.k.token_stride + (long long)kv * w.k.head_stride;
+    const T *v_base = static_cast<const T *>(w.v.dev) + (long long)start * w.v.token_stride + (long long)kv * w.v.head_stride;
+    const T *q_row = static_cast<const T *>(w.q.dev) + (long long)(start + pos) * w.q.token_stride + (long long)head * w.q.head_stride + 8 * half;
+    T *out = static_cast<T *>(w.dev_out) + ((long long)(start + pos) * w.heads + head) * D + 4 * half;
+    const int n_to = w_hi / 32 + 1, n_from = max(w_lo - window + 1, 0) / 32;
+    const int n_sink = min((min(sinks, w_hi + 1) + 31) / 32, n_from), count = n_sink + n_to - n_from;
+    auto key_of = [&](int n) { return (n < n_sink ? n : n_from + n - n_sink) * 32; };
+
+    // Scores of 32 keys, in powers of two: s[r] is that of key 8 (r / 4) + r % 4 behind key + 4 half.  Bit r of `seen`: the row sees it.
+    auto scores = [&](int key, unsigned &seen) {
+        const T *k_row = k_base + key * w.k.token_stride + min(c, len - 1 - key) * (int)w.k.token_stride + 8 * half;
+        f32x16 s = {};
+#pragma unroll 1
+        for (int i = 0; i < D; i += 16) s = product<BF>(*reinterpret_cast<const u32x4 *>(k_row + i), *reinterpret_cast<const u32x4 *>(q_row + i), s);
+        const int first = key + 4 * half, ahead = max(pos - first, -1);
+        const unsigned shown = below(ahead + 1) & (~below(ahead - window + 1) | below(sinks - first));
+        seen = (shown & 0xfu) | (shown >> 4 & 0xf0u) | (shown >> 8 & 0xf00u) | (shown >> 12 & 0xf000u);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = unless_hidden(s[r] * (w.scale * 1.44269504088896341f), ~seen, r);
+        return s;
+    };
+    // Numbers of this lane's column in the eight keys that s[8 t ...] belong to; f(finite, bits) of each.
+    auto values = [&](int key, int column, int t, auto f) {
+        const T *tile = v_base + key * w.v.token_stride + column;
+        u32x4 r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int row = min(16 * t + 8 * (e >> 2) + 4 * half + (e & 3), len - 1 - key);
+            const unsigned x = __builtin_bit_cast(unsigned short, tile[row * (int)w.v.token_stride + c]), y = f((x & TOP) != TOP, x);
+            r[e >> 1] = e & 1 ? r[e >> 1] | y << 16 : y;
         }
-        const unsigned long long who = __ballot(seen);
-        if (!who) continue;
-        float most = x;
-        for (int s = 32; s; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
-        const float next = fmaxf(m, most);
-        // Scores of -inf alone so far have no weight beside a finite one to come.
-        const float p = seen ? __builtin_amdgcn_exp2f(x - (next == neg_inf() ? 0.0f : next)) : 0.0f;
-        const float down = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
-        m = next;
-        float sum = p;
-        for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
-        l = l * down + sum;
-        for (int i = 0; i < EACH; ++i) o[i] *= down;
-        for (int s = 0; s < 64; ++s) {
-            if (!(who >> s & 1)) continue;
-            const float ps = __shfl(p, s);
-            for (int i = 0; i < EACH; ++i)
-                if (64 * i + lane < D) o[i] += ps * (float)v[(t0 + s) * v_stride + 64 * i + lane];
+        return r;
+    };
+
+#pragma unroll 1
+    for (int column = 0; column < D; column += 32) {
+        // Bit r: the row sees NaN (or an infinity under a weight of 0), inf, -inf in the column of o[r].
+        unsigned nan = 0, up = 0, down = 0;
+#pragma unroll 1
+        for (int n = 0; n < count; ++n) {
+            const int key = key_of(n);
+#pragma unroll 1
+            for (int t = 0; t < 2; ++t) {
+                const u32x4 odd = values(key, column, t, [](bool finite, unsigned x) { return finite ? 0u : x; });
+                if (!__any((odd[0] | odd[1] | odd[2] | odd[3]) != 0)) continue;
+                unsigned seen, lost = 0;
+                {
+                    const f32x16 s = scores(key, seen);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) lost |= s[r] == neg_inf() ? 1u << r : 0u;
+                    lost &= seen;
+                }
+                // Bits r where a row that sees a key by `keys` sees a number of `which` in it.
+                auto meet = [&](auto which, unsigned keys) {
+                    u32x4 ones, sees;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        ones[j] = (which(odd[j] & 0xffffu) ? ONE : 0u) | (which(odd[j] >> 16) ? ONE << 16 : 0u);
+                        sees[j] = (keys >> (8 * t + 2 * j) & 1u) * ONE | (keys >> (8 * t + 2 * j + 1) & 1u) * (ONE << 16);
+                    }
+                    const f32x16 met = product<BF>(ones, sees, f32x16{});
+                    unsigned bits = 0;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) bits |= met[r] != 0.0f ? 1u << r : 0u;
+                    __builtin_amdgcn_sched_barrier(0);
+                    return bits;
+                };
+                nan |= meet([](unsigned x) { return (x & 0x7fffu) > TOP; }, seen);
+                nan |= meet([](unsigned x) { return x != 0u; }, lost);
+                up |= meet([](unsigned x) { return x == TOP; }, seen & ~lost);
+                down |= meet([](unsigned x) { return x == (TOP | 0x8000u); }, seen & ~lost);
+            }
+        }
+        nan |= up & down;
+
+        f32x16 o = {};
+        float m = neg_inf(), l = 0.0f;
+#pragma unroll 1
+        for (int n = 0; n < count; ++n) {
+            const int key = key_of(n);
+            unsigned seen;
+            f32x16 s = scores(key, seen);
+            float most = neg_inf();
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[r]);
+            most = larger_half(most);
+            const float next = fmaxf(m, !BF && __builtin_fabsf(most) >= 0x1p20f ? most : most - LIFT);
+            const float by = next == neg_inf() ? 0.0f : next, less = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+            m = next;
+            l *= less;
+            o *= less;
+            u32x4 p[2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i >> 2][i & 3] = pack<BF>(__builtin_amdgcn_exp2f(s[2 * i] - by), __builtin_amdgcn_exp2f(s[2 * i + 1] - by));
+                l = add_pair<BF>(p[i >> 2][i & 3], l);
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                __builtin_amdgcn_sched_barrier(0);
+                o = product<BF>(values(key, column, t, [](bool finite, unsigned x) { return finite ? x : 0u; }), p[t], o);
+            }
+        }
+
+        l += __shfl_xor(l, 32);
+        const float by = 1.0f / l;
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            f32x4 y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                y[j] = o[r + j] * by;
+                if (up >> (r + j) & 1u) y[j] += __builtin_inff();  // NaN where all of the row is
+                if (down >> (r + j) & 1u) y[j] -= __builtin_inff();
+                if (nan >> (r + j) & 1u) y[j] = __builtin_nanf("");
+            }
+            if (rows >> c & 1u) *reinterpret_cast<u32x2 *>(out + column + 2 * r) = u32x2{pack<BF>(y[0], y[1]), pack<BF>(y[2], y[3])};
         }
     }
-    for (int i = 0; i < EACH; ++i)
-        if (64 * i + lane < D) out[64 * i + lane] = (T)(o[i] / l);
 }
 
 template <int D, bool BF>
-__global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(WindowArgs a)
+__global__ __launch_bounds__(THREADS, D == 128 ? 3 : 5) void window_kernel(WindowArgs a)
 {
     using T = std::conditional_t<BF, __bf16, _Float16>;
     constexpr int TILE = D == 32 ? 64 : 32, PARTS = TILE / 32;  // keys; every thread fetches 16 bytes of them at least
@@ -374,14 +470,8 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 3 : 4) void window_kernel(Windo
             zero = add_pair<BF>(z[1], add_pair<BF>(z[0], zero, 0.0f), 0.0f);
             if (real) *reinterpret_cast<u32x2 *>(out + 32 * i + 8 * (r >> 2) + 4 * half) = z;
         }
-    unsigned long long again = __ballot(zero != 0.0f && real);
-    again |= again >> 32;
-    for (unsigned rows = (unsigned)again; rows; rows &= rows - 1) {
-        const int r = __builtin_ctz(rows), p = pos_of(wave_row + r), head = kv * a.per + wave_row + r - p * a.per;
-        redo_row<D, T>(static_cast<const T *>(w.q.dev) + (long long)(start + p) * w.q.token_stride + (long long)head * w.q.head_stride, k_base,
-                       w.k.token_stride, v_base, w.v.token_stride, p, w.scale * 1.44269504088896341f, window, sinks,
-                       static_cast<T *>(w.dev_out) + ((long long)(start + p) * w.heads + head) * D, lane);
-    }
+    unsigned long long odd = __ballot(zero != 0.0f && real);
+    if (odd) again<D, BF, T>(a, start, len, kv, wave_row, (unsigned)(odd | odd >> 32), lane);
 }
 
 template <int D>

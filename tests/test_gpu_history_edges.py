@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import history_oracle as O
-from test_gpu_history import BF, HF, F32, Histories, gen
+from test_gpu_history import BF, HF, F32, Histories, expect_whole, gen, whole
 
 pytestmark = pytest.mark.gpu
 
@@ -162,3 +162,25 @@ def test_a_fault_that_comes_while_a_record_is_checked_stays(b):
     assert record.tolist() == [-1, -1, 7, -1]
     assert b.rec_history_check(record) == (b.REC_ERR_INDEX_RANGE, 7, b.REC_FAULT_PAGE)
     assert b.rec_history_check(record) == (b.REC_OK, -1, -1)
+
+
+# ------------------------------------------------------- rows that are computed again
+@pytest.mark.parametrize("d,dtype", [(32, HF), (32, BF), (64, BF), (64, HF), (128, BF), (128, HF)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (1, 3), (100, 0), (37, 5), (64, 64), (30, 200), (257, 1)])
+def test_rows_beside_numbers_that_are_not_finite(b, d, dtype, window, sinks):
+    """Rows that see them, in a column or in all, and rows of the same tiles that do not."""
+    lengths = [300, 1, 64]
+    q, k, v, offsets = whole(lengths, 4, 2, d, dtype, 70)
+    v[2, 0, 5] = float("nan")
+    v[130, 1, d - 1] = float("inf")
+    v[131, 1, d - 1] = float("-inf")
+    v[200, 0] = float("nan")
+    k[250, 1, 7] = float("nan")
+    q[290, 3, 0] = float("inf")
+    k[300, 0, 0] = float("-inf")
+    v[301 + 20, 1] = float("inf")
+    want, off = expect_whole(q, k, v, lengths, d ** -0.5, window, sinks)
+    got = b.attend_window(q, k, v, offsets, window=window, sinks=sinks)
+    gn = got.double().cpu().numpy()
+    assert np.array_equal(np.isposinf(gn), np.isposinf(want)) and np.array_equal(np.isneginf(gn), np.isneginf(want))
+    O.assert_close(got, want, off)
