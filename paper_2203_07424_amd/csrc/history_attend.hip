@@ -16,7 +16,7 @@
 // scaled conversions look at a scale's exponent bits only, so one shift puts a scale
 // byte in place.  A product with ones sums the weights as they were rounded.
 //
-// The running maximum moves only when a tile's exceeds it by 2^8: weights stay below 2^8,
+// The running maximum moves only when a tile's exceeds it by 2^8: weights stay within 2^8 of it,
 // and the accumulators are rescaled a few times a history instead of every tile.
 //
 // Few pairs of history and head are divided: among the waves of a block, which meet in
@@ -42,7 +42,9 @@ typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int ROWS = 16;       // query rows of a wave
 constexpr int TILE = 64;       // keys
-constexpr float SLACK = 8.0f;  // how far, in powers of two, weights may pass 1
+// A row's largest weight lies between 2^-ROOM and 2^(SLACK - ROOM): sums over 2^31 tokens of values up to fp32's largest
+// stay in its range, and weights are rounded to bf16 of themselves down to 2^-86 of the largest.
+constexpr float SLACK = 8.0f, ROOM = 40.0f;
 constexpr float LOWEST = -3.4e38f;  // the maximum of a row that has seen nothing but scores of -inf
 constexpr int CUS = 256;
 
@@ -303,7 +305,7 @@ __device__ inline unsigned pack(float a, float b)
 template <int D, int HEADS>
 struct Sums {
     f32x4 o[HEADS][D / 16], l;
-    float m;
+    float m;  // exponent of weight 1, ROOM above the largest score's
 };
 
 // Bytes of 255 where the bits of a nibble are set.
@@ -534,8 +536,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
             most = most == neg_inf() ? most : most * factor;
-            if (__any(most > sum.m + SLACK)) {
-                const float m = fmaxf(sum.m, most);
+            if (__any(most > sum.m + (SLACK - ROOM))) {
+                const float m = fmaxf(sum.m, most + ROOM);
                 if (__any(sum.m != neg_inf())) {  // not the first tile
                     const float down = sum.m == m ? 1.0f : __builtin_amdgcn_exp2f(sum.m - m);
 #pragma unroll

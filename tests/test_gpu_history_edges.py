@@ -184,3 +184,33 @@ def test_rows_beside_numbers_that_are_not_finite(b, d, dtype, window, sinks):
     gn = got.double().cpu().numpy()
     assert np.array_equal(np.isposinf(gn), np.isposinf(want)) and np.array_equal(np.isneginf(gn), np.isneginf(want))
     O.assert_close(got, want, off)
+
+
+# --------------------------------------------------- values next to the range's end
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("lengths,kv,per,d", [([200, 3], 1, 2, 64), ([5000], 2, 1, 128), ([90] * 2060, 2, 2, 32)])
+def test_means_of_the_largest_values(b, fmt, lengths, kv, per, d):
+    """A mean of values up to 2^128 is no larger than they are; their sum is.  One wave, several, parts, two heads a wave."""
+    s = Histories(b, lengths, kv, d, fmt, 32, seed=80)
+    g = gen(81)
+    v = torch.sign(torch.randn(1, kv, d, generator=g)) * 2.0 ** 127 * (1 + 0.75 * torch.rand(len(s.slots), kv, d, generator=g))
+    k = torch.from_numpy(s.k).float()
+    s.cache.write(k.cuda(), v.cuda(), s.slots.cuda())
+    s.k, s.v = (x.double().cpu().numpy() for x in s.cache.read(s.slots.cuda(), F32))
+    assert np.abs(s.v).max() > 2.5e38 and np.isfinite(s.v).all()
+    q = torch.randn(len(lengths), 1, kv * per, d, generator=g).to(BF).cuda()
+    got = s.cache.attend(q, s.table, s.len_t)
+    qn = q.double().cpu().numpy()
+    for i in sorted({0, len(lengths) // 2, len(lengths) - 1}):
+        for h in range(kv * per):
+            kk, vv = (x[s.ends[i]:s.ends[i + 1], h // per] for x in (s.k, s.v))
+            want, off = O.attend_rows(qn[i, :, h], kk, vv, [lengths[i] - 1], d ** -0.5, 0, 0, BF)
+            O.assert_close(got[i, :, h], want, off, (i, h))
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_means_of_the_largest_values_in_whole_histories(b, d):
+    q, k, v, offsets = whole([150, 1, 40], 2, 1, d, BF, 82, fused=False)
+    v = (torch.sign(v[:1].float()) * 2.0 ** 127 * (1 + 0.9 * torch.rand(v.shape, generator=gen(83)).cuda())).to(BF)
+    for window, sinks in ((0, 0), (20, 3)):
+        O.assert_close(b.attend_window(q, k, v, offsets, window=window, sinks=sinks), *expect_whole(q, k, v, [150, 1, 40], d ** -0.5, window, sinks))
