@@ -16,13 +16,14 @@
  * Which kernel a layer's launch takes, and which stages of a forward share a launch
  * (host code, no device).
  *
- * How a checked fault record of user histories is cleared.
+ * The form of a launch of cached attention, and how a checked fault record of user histories is cleared.
  */
 #ifndef REC_PROBE_H
 #define REC_PROBE_H
 
 #include <stdint.h>
 #include "rec.h"
+#include "rec_history.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -103,6 +104,11 @@ REC_API rec_status rec_probe_plan_pooling(const rec_model *m, int32_t batch, int
  * waves, deal[2] units a wave at most, a unit four wave-wide accesses.  left: -1, the launch of the scan or of
  * scan and a few lookups; else compute units without a block of the launch of many lookups. */
 REC_API rec_status rec_probe_dense_copy(int32_t rows, int32_t columns, int32_t pad, int32_t left, int32_t *deal);
+
+/* What rec_history_attend() would run for a query (host code, no device; pointers are not looked at): form[0] waves
+ * of a block, which share a history and kv head, form[1] parts of it in blocks of their own, form[2] kv heads of a wave.
+ * Errors as there; REC_ERR_ARG on a null form. */
+REC_API rec_status rec_probe_history_form(const rec_history *h, const rec_query *q, int32_t *form);
 
 /* The end of rec_history_check() (rec_history.h): words of a fault record become all ones where they
  * still are what was read before, seen[] (host memory, as many words as a record has).  REC_ERR_ARG: null, misaligned. */

@@ -57,7 +57,7 @@ EXPORTS = ("rec_create", "rec_destroy", "rec_workspace_bytes", "rec_bind_workspa
            "rec_synth_fill_table", "rec_probe_mfma", "rec_probe_scan", "rec_probe_fc_form", "rec_probe_plan",
            "rec_probe_plan_joined", "rec_probe_plan_pooling", "rec_probe_dense_copy",
            "rec_history_bytes", "rec_history_write", "rec_history_read", "rec_history_attend_workspace_bytes",
-           "rec_history_attend", "rec_window_attend", "rec_history_check", "rec_probe_clear_faults")
+           "rec_history_attend", "rec_window_attend", "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
 
 
 class rec_config(C.Structure):
@@ -168,6 +168,8 @@ _lib.rec_window_attend.restype = C.c_int
 _lib.rec_window_attend.argtypes = [_vp, _vp]
 _lib.rec_history_check.restype = C.c_int
 _lib.rec_history_check.argtypes = [_vp, _vp, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
+_lib.rec_probe_history_form.restype = C.c_int
+_lib.rec_probe_history_form.argtypes = [_vp, _vp, C.POINTER(C.c_int32)]
 _lib.rec_probe_clear_faults.restype = C.c_int
 _lib.rec_probe_clear_faults.argtypes = [_vp, C.POINTER(C.c_uint64), _vp]
 # The same layouts for one packing call, a quarter of the time of setting a structure's fields.
@@ -396,6 +398,13 @@ def rec_history_check(dev_fault: torch.Tensor) -> Tuple[int, int, int]:
     pos, word = C.c_int64(-1), C.c_int32(-1)
     st = _lib.rec_history_check(_ptr(dev_fault), _stream_on(dev_fault.get_device(), "rec_history_check"), C.byref(pos), C.byref(word))
     return st, pos.value, word.value
+
+
+def rec_probe_history_form(h: rec_history, q: rec_query) -> Tuple[int, int, int, int]:
+    """(status, waves of a block, parts of a history, kv heads of a wave)."""
+    form = (C.c_int32 * 3)()
+    st = _lib.rec_probe_history_form(C.byref(h), C.byref(q), form)
+    return (st, *form)
 
 
 def rec_probe_clear_faults(dev_fault: torch.Tensor, seen: Sequence[int]) -> int:

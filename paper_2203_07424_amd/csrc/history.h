@@ -92,6 +92,7 @@ hipError_t launch_write(const Cache &c, int format, int d, const rec_rows &k, co
 hipError_t launch_read(const Cache &c, int format, int d, const int64_t *slots, long long tokens, int dtype,
                        void *k, void *v, hipStream_t s);
 long long attend_threads(const Cache &c, int format, int d, const rec_query &q);
+void attend_form(const Cache &c, int format, int d, const rec_query &q, int32_t (&form)[3]);  // waves of a block, parts, kv heads of a wave
 size_t attend_workspace(const Cache &c, int format, int d, const rec_query &q);
 hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *workspace, hipStream_t s);
 long long window_blocks(const rec_window &w);  // of 256 threads

@@ -170,6 +170,17 @@ rec_status rec_history_check(uint64_t *dev_fault, void *stream, int64_t *first_b
     return REC_OK;
 }
 
+rec_status rec_probe_history_form(const rec_history *h, const rec_query *q, int32_t *form)
+{
+    if (!form) return REC_ERR_ARG;
+    const rec_status st = check_query(h, q);
+    if (st != REC_OK) return st;
+    int32_t f[3];
+    rec::hist::attend_form(cache_of(h), h->format, h->head_dim, *q, f);
+    for (int i = 0; i < 3; ++i) form[i] = f[i];
+    return REC_OK;
+}
+
 rec_status rec_probe_clear_faults(uint64_t *dev_fault, const uint64_t *seen, void *stream)
 {
     if (!dev_fault || !words_fit(dev_fault, 8) || !seen) return REC_ERR_ARG;

@@ -796,6 +796,14 @@ long long attend_threads(const Cache &c, int format, int d, const rec_query &q)
     return (long long)q.batch * c.kv_heads * p.row_tiles * p.splits * 64 * p.waves;
 }
 
+void attend_form(const Cache &c, int format, int d, const rec_query &q, int32_t (&form)[3])
+{
+    const Plan p = plan_of(c, format, d, q);
+    form[0] = p.waves;
+    form[1] = p.splits;
+    form[2] = p.heads;
+}
+
 size_t attend_workspace(const Cache &c, int format, int d, const rec_query &q)
 {
     if (q.batch == 0 || q.queries == 0) return 0;

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import history_oracle as O
+from test_gpu_history_forms import check_some, many_lengths
 from test_gpu_history import BF, HF, F32, Histories, expect_whole, gen, whole
 
 pytestmark = pytest.mark.gpu
@@ -214,3 +215,30 @@ def test_means_of_the_largest_values_in_whole_histories(b, d):
     v = (torch.sign(v[:1].float()) * 2.0 ** 127 * (1 + 0.9 * torch.rand(v.shape, generator=gen(83)).cuda())).to(BF)
     for window, sinks in ((0, 0), (20, 3)):
         O.assert_close(b.attend_window(q, k, v, offsets, window=window, sinks=sinks), *expect_whole(q, k, v, [150, 1, 40], d ** -0.5, window, sinks))
+
+
+# ------------------------------------------------------------- forms, as they are taken
+@pytest.mark.parametrize("form,batch,width,most,long,kv,d,fmt,dtype,queries", [
+    ((1, 2, 1), 1024, 8, 500, (512,), 2, 64, "mx4", BF, 1),               # a wave a block, two parts
+    ((1, 2, 1), 1024, 8, 500, (512, 511), 2, 32, "mx8", HF, 3),
+    ((1, 1, 1), 2048, 2, 128, (), 2, 128, "mx8", BF, 1),                  # a wave for all of a history
+    ((2, 1, 1), 700, 8, 400, (512,), 2, 64, "mx8", HF, 2),                # two waves
+    ((2, 2, 1), 512, 8, 500, (512, 449), 2, 64, "mx4", BF, 1),            # in two parts
+    ((4, 1, 1), 300, 4, 256, (), 2, 128, "mx4", HF, 2),                   # four
+    ((4, 2, 1), 1100, 75, 90, (4800, 2000, 2100), 2, 64, "mx4", BF, 1),   # in parts, for the few long ones
+    ((4, 16, 1), 8, 128, 3000, (8192, 8191), 2, 64, "mx4", HF, 18),        # in as many as work at once
+    ((1, 1, 2), 4200, 4, 200, (256,), 2, 64, "mx8", BF, 2)])              # two kv heads a wave
+def test_forms_by_size(b, form, batch, width, most, long, kv, d, fmt, dtype, queries):
+    n = many_lengths(batch, most, 3)
+    n[6:6 + len(long)] = long[:max(0, len(n) - 6)]
+    n = n[:batch]
+    s = Histories(b, n, kv, d, fmt, 64, seed=90, width=width)
+    q = torch.randn(batch, queries, 2 * kv, d, generator=gen(91)).to(dtype).cuda()
+    for window, sinks in ((0, 0), (150, 3)):
+        query = b.rec_query(q.data_ptr(), q.data_ptr(), *q.stride()[:3], b._ATTEND_CODES[dtype], batch, queries, 2 * kv, s.table.data_ptr(),
+                            s.table.stride(0), width, s.len_t.data_ptr(), 1.0, window, sinks, 0)
+        if not window:
+            assert b.rec_probe_history_form(s.cache._h, query) == (b.REC_OK, *form)
+        got = s.cache.attend(q, s.table, s.len_t, window=window, sinks=sinks)
+        check_some(s, q, got, sorted({*range(min(batch, 9)), *range(9, batch, 211)}), d ** -0.5, window, sinks, what=(window, sinks))
+    assert s.cache.check()[0] == b.REC_OK
