@@ -242,3 +242,73 @@ def test_forms_by_size(b, form, batch, width, most, long, kv, d, fmt, dtype, que
         got = s.cache.attend(q, s.table, s.len_t, window=window, sinks=sinks)
         check_some(s, q, got, sorted({*range(min(batch, 9)), *range(9, batch, 211)}), d ** -0.5, window, sinks, what=(window, sinks))
     assert s.cache.check()[0] == b.REC_OK
+
+
+# --------------------------------------------------------- nothing outside the buffers
+def guarded(rows, columns, dtype, margin=64):
+    """A buffer of rows with `margin` more on both sides, all of one pattern, and the rows by themselves."""
+    whole = torch.full((rows + 2 * margin, columns), 0x5A, dtype=torch.uint8, device="cuda").repeat_interleave(torch.finfo(dtype).bits // 8, 1)
+    return whole, whole[margin:margin + rows].view(dtype)
+
+
+def untouched(whole, rows, margin=64):
+    return bool((whole[:margin] == 0x5A).all()) and bool((whole[margin + rows:] == 0x5A).all())
+
+
+@pytest.mark.parametrize("offsets", [[0, 20, 20, 50], [0, 30, 20, 50], [0, 10, 60, 50], [-5, 10, 20, 50], [5, 10, 20, 50], [0, 10, 20, 49], [0, 10, 20, 5000],
+                                     [50, 0, 50, 0], [-2 ** 31, 2 ** 31 - 1, -1, 50], [0, 50, 50, 50]])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_outputs_of_whole_histories_stay_within_their_buffer(b, offsets, d):
+    heads, n = 2, 50
+    q, k, v, _ = whole([n], heads, 1, d, BF, 95, fused=False)
+    buffer, out = guarded(n, heads * d, BF)
+    fault, at = b._faults("cuda:0"), torch.tensor(offsets, dtype=torch.int32).cuda()
+    r = lambda t: b.rec_rows(t.data_ptr(), t.stride(0), t.stride(1))  # noqa: E731
+    w = b.rec_window(r(q), r(k), r(v), out.data_ptr(), b.REC_BF16, len(offsets) - 1, n, heads, 1, d, at.data_ptr(), d ** -0.5, 0, 0, fault.data_ptr())
+    assert b.rec_window_attend(w) == b.REC_OK
+    torch.cuda.synchronize()
+    assert untouched(buffer, n)
+    good = offsets in ([0, 20, 20, 50], [0, 50, 50, 50])
+    assert (b.rec_history_check(fault)[0] == b.REC_OK) == good
+    if good:
+        lengths = [y - x for x, y in zip(offsets, offsets[1:])]
+        O.assert_close(out.view(n, heads, d), *expect_whole(q, k, v, lengths, d ** -0.5, 0, 0))
+
+
+@pytest.mark.parametrize("lengths,queries,width", [([1, 0, 40], 1, 4), ([100, 7, 64], 5, 4), ([3000], 1, 100), ([9, -4, 10 ** 6], 3, 4)])
+def test_outputs_over_the_cache_stay_within_their_buffer(b, lengths, queries, width):
+    """One wave, several rows, parts; lengths that are none."""
+    d, heads = 64, 2
+    s = Histories(b, [max(0, min(n, 32 * width)) for n in lengths], 1, d, "mx8", 32, seed=96, width=width)
+    q = torch.randn(len(lengths), queries, heads, d, generator=gen(97)).to(BF).cuda()
+    rows = len(lengths) * queries * heads
+    buffer, out = guarded(rows, d, BF)
+    s.cache.attend(q, s.table, torch.tensor(lengths, dtype=torch.int32).cuda(), out=out.view(q.shape))
+    torch.cuda.synchronize()
+    assert untouched(buffer, rows)
+    want, off = s.expect(q, d ** -0.5, 0, 0, False)
+    O.assert_close(out.view(q.shape), want, off)
+
+
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_a_write_touches_its_slots_and_nothing_else(b, fmt, d):
+    """Every byte of places that are not named stays: whole groups, parts of groups, single slots."""
+    kv, pages, page_tokens = 2, 6, 32
+    cache = b.HistoryCache(pages, page_tokens, kv, d, fmt)
+    slots = torch.cat((torch.arange(32, 55), torch.tensor([3, 100, -1, 101, 191]), torch.arange(128, 160)))
+    k, v = (torch.randn(len(slots), kv, d, generator=gen(98 + i)).cuda() for i in range(2))
+    raw = {}
+    for fill in (0x00, 0xff, 0xa5):
+        cache.pages.fill_(fill)
+        cache.write(k, v, slots.cuda())
+        raw[fill] = cache.pages.cpu().numpy()
+    same = (raw[0x00] == raw[0xff]) & (raw[0x00] == raw[0xa5])         # written: the same bytes whatever was there
+    kept = (raw[0x00] == 0x00) & (raw[0xff] == 0xff) & (raw[0xa5] == 0xa5)
+    assert (same | kept).all() and not (same & kept).any()
+    named = int((slots >= 0).sum())
+    assert int(same.sum()) == named * kv * d * (17 if fmt == "mx4" else 33) // 16
+    ours = {int(x) // 16 for x in slots if x >= 0}
+    for group in range(pages * page_tokens // 16):
+        page, g = divmod(group, page_tokens // 16)
+        assert same[page, :, g].any() == (group in ours)
