@@ -312,3 +312,38 @@ def test_a_write_touches_its_slots_and_nothing_else(b, fmt, d):
     for group in range(pages * page_tokens // 16):
         page, g = divmod(group, page_tokens // 16)
         assert same[page, :, g].any() == (group in ours)
+
+
+# ---------------------------------------------------------- how exactly a query is held
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("dtype,bits", [(BF, 8), (BF, 13), (BF, 16), (HF, 8), (HF, 13)])
+def test_small_elements_of_a_query_beside_a_large_one(b, fmt, d, dtype, bits):
+    """A score that is one small element alone, 2^-bits of the largest of its 32, which meets zeros.  A query's terms end at half of
+    2^-13 (fp16: 2^-17) where its largest is at least 224, so that the score is off by that; besides, the weight's and the output's rounding."""
+    batch, heads = 40, 4
+    g = gen(100 + bits)
+    column = torch.randint(0, d, (batch,), generator=g)
+    beside = column // 32 * 32 + (column + 1 + torch.randint(0, 31, (batch,), generator=g)) % 32
+    beside = torch.where(beside == column, column // 32 * 32 + (column + 1) % 32, beside)
+    top = 2.0 ** (10 if dtype == HF else 20)
+    q = (1 + torch.rand(batch, heads, d, generator=g)) * top * 2.0 ** -bits
+    q[torch.arange(batch), :, beside] = top * (1 + torch.rand(batch, heads, generator=g))
+    q = q.to(dtype)
+    k = torch.zeros(2 * batch, 1, d)
+    k[1::2, 0][torch.arange(batch), column] = 1.0
+    v = torch.zeros(2 * batch, 1, d)
+    v[1::2] = torch.randn(batch, 1, d, generator=g)
+    cache = b.HistoryCache(batch, 16, 1, d, fmt)
+    slots = (torch.arange(batch)[:, None] * 16 + torch.arange(2)).reshape(-1).cuda()
+    cache.write(k.cuda(), v.cuda(), slots)
+    v = cache.read(slots, F32)[1].cpu().double().numpy()[1::2, 0]
+    scale = 2.0 ** bits / top
+    got = cache.attend(q.cuda(), torch.arange(batch, dtype=torch.int32)[:, None].cuda(), torch.full((batch,), 2, dtype=torch.int32).cuda(), scale=scale)
+    qn = q.double().numpy()
+    x = qn[np.arange(batch), :, column.numpy()] * scale                                    # [batch, heads]
+    want = (1 / (1 + np.exp(-x)))[..., None] * v[:, None]
+    largest = np.abs(qn).max(-1)
+    score = scale * largest * (2.0 ** -14 if dtype == BF else 2.0 ** -18) / 224 + np.abs(x) * (d + 8) * 2.0 ** -24
+    off = (2 * O.EPS[dtype] + 2 * score[..., None] + 2.0 ** -20) * np.abs(want) + 2.0 ** -25
+    O.assert_close(got, want, off)
