@@ -30,7 +30,8 @@
  * amax is over 1.75 (1.8125) times its power of two; at least -110 and at most 125
  * (119), so that whatever is read back is a finite fp32.  Elements are rounded to
  * nearest, ties to even, and saturate.  A block with a NaN or an infinity has the
- * byte 255, reads back as NaN and is reported.
+ * byte 255, reads back as NaN and is reported.  Nothing else is written; what a query
+ * gets from a place that was never written, where it sees one, may be anything.
  *
  * Pages: [num_pages][kv_heads][page_tokens / 16] groups.  A group holds 16 tokens of
  * one head, D = head_dim:

@@ -317,19 +317,20 @@ __device__ inline unsigned bytes_of(unsigned nibble)
 
 // Tokens of a lane's 16 that count as zero whatever their bytes are: 0 * NaN would reach the
 // rows that do not see a value.  Those are the ones that no row sees (bit t of `used` clear) and,
-// a block at a time, those whose block is NaN; a scale of 2^-127 does it, and for the former no
-// code that is NaN itself.  Returns the blocks (bit b) of which row c, which sees the tokens in
-// `seen`, sees a NaN.
+// a block at a time, those whose block is NaN, or under a scale that no write makes, which could be
+// infinite; a scale of 2^-127 does it, and for the former no code that is NaN itself.  Returns the
+// blocks (bit b) of which row c, which sees the tokens in `seen`, sees one of those.
 template <int FMT, int D>
 __device__ inline unsigned clear_values(Tile<FMT, D> &t, unsigned used, unsigned seen)
 {
+    constexpr unsigned NO_SCALE = FMT == REC_MX4 ? 253u : 247u;
     unsigned nan = 0;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
         const unsigned keep = bytes_of(used >> (4 * x) & 15u), mine = bytes_of(seen >> (4 * x) & 15u);
 #pragma unroll
         for (int b = 0; b < D / BLOCK; ++b) {
-            const unsigned s = t.vs[b][x], top = ((s & 0x7f7f7f7fu) + 0x01010101u) & s & 0x80808080u;  // bytes of 255
+            const unsigned s = t.vs[b][x], top = ((s & 0x7f7f7f7fu) + (256u - NO_SCALE) * 0x01010101u) & s & 0x80808080u;  // bytes from NO_SCALE on
             nan |= (top & mine) != 0 ? 1u << b : 0u;
             t.vs[b][x] = s & keep & ~((top << 1) - (top >> 7));
             if constexpr (FMT == REC_MX8) {

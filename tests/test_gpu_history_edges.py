@@ -347,3 +347,56 @@ def test_small_elements_of_a_query_beside_a_large_one(b, fmt, d, dtype, bits):
     score = scale * largest * (2.0 ** -14 if dtype == BF else 2.0 ** -18) / 224 + np.abs(x) * (d + 8) * 2.0 ** -24
     off = (2 * O.EPS[dtype] + 2 * score[..., None] + 2.0 ** -20) * np.abs(want) + 2.0 ** -25
     O.assert_close(got, want, off)
+
+
+# --------------------------------------------------------- scales that no write makes
+@pytest.mark.parametrize("fmt", ["mx4", "mx8"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_infinite_places_within_a_length_that_were_never_written(b, fmt, d):
+    """Bytes of 254: the largest codes under a scale of 2^127, beyond fp32."""
+    n, nq = 70, 4
+    s = Histories(b, [n, n], 1, d, fmt, 32, seed=55)
+    k, v = s.cache.read(s.slots.cuda(), F32)
+    s.cache.pages.fill_(254)
+    slots = s.slots.clone()
+    for e in s.ends[1:]:
+        slots[e - 2:e] = -1
+    s.cache.write(k, v, slots.cuda())
+    q = torch.randn(2, nq, 2, d, generator=gen(56)).to(BF).cuda()
+    s.k, s.v = (x.double().cpu().numpy() for x in s.cache.read(s.slots.cuda(), F32))
+    assert np.isinf(s.v[s.ends[1] - 1]).all()
+    want, off = s.expect(q, d ** -0.5, 0, 0, False)
+    assert np.isfinite(want[:, :2]).all() and np.isnan(want[:, 2:]).all()
+    O.assert_close(s.cache.attend(q, s.table, s.len_t), want, off)
+
+
+@pytest.mark.parametrize("fmt,byte", [("mx4", 253), ("mx4", 254), ("mx8", 247), ("mx8", 254)])
+@pytest.mark.parametrize("d,kv,per,dtype", [(32, 2, 1, HF), (64, 1, 4, BF), (128, 2, 2, BF)])
+@pytest.mark.parametrize("batch", [10, 2060])
+def test_a_value_under_a_scale_that_no_write_makes_reaches_only_the_rows_that_see_it(b, fmt, byte, d, kv, per, dtype, batch):
+    """Infinite where its codes are large: in its 32 columns of the rows that see it (which may be anything there), and nowhere else."""
+    n, nq, window, sinks = 100, 5, 40, 2
+    if batch > 10 and d == 128:
+        batch = 40
+    where = [98, 97, 99, 57, 58, 60, 30, 1, 2, 70]        # seen by some queries, by none, by all
+    s = Histories(b, [n] * batch, kv, d, fmt, 32, seed=57)
+    q = torch.randn(batch, nq, kv * per, d, generator=gen(58)).to(dtype).cuda()
+    for i, token in enumerate(where):
+        page, at = divmod(int(s.slots[int(s.ends[i]) + token]), 32)
+        scales = 32 * (d // 2 if fmt == "mx4" else d) + d // 2
+        s.cache.pages[page, i % kv, at // 16, scales + (i % (d // 32)) * 16 + at % 16] = byte
+    got = s.cache.attend(q, s.table, s.len_t, window=window, sinks=sinks)
+    qn = q.double().cpu().numpy()
+    for i in [*range(len(where)), batch - 1]:
+        want, off = np.zeros(qn.shape[1:]), np.zeros(qn.shape[1:])
+        for h in range(kv * per):
+            k, v = (x[s.ends[i]:s.ends[i + 1], h // per] for x in (s.k, s.v))
+            want[:, h], off[:, h] = O.attend_rows(qn[i, :, h], k, v, range(n - nq, n), d ** -0.5, window, sinks, dtype)
+        result = got[i].clone()
+        if i < len(where):
+            for x in range(nq):
+                if O.sees(n - nq + x, where[i], window, sinks):
+                    heads, columns = slice(i % kv * per, (i % kv + 1) * per), slice(i % (d // 32) * 32, (i % (d // 32) + 1) * 32)
+                    want[x, heads, columns] = 0.0
+                    result[x, heads, columns] = 0.0
+        O.assert_close(result, want, off, i)
