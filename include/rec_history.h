@@ -6,6 +6,7 @@
  * each event into a key and a value per head and let queries - the next event, or
  * candidate items - attend to them.  A server keeps those between requests:
  *
+ *   rec_rotate_heads()     its queries and keys are normalised and rotated by position
  *   rec_window_attend()    a whole new history attends to itself
  *   rec_history_write()    its keys and values enter the cache, 4 or 8 bits a number
  *   rec_history_attend()   later queries attend to what the cache holds
@@ -201,6 +202,45 @@ typedef struct {
 } rec_window;
 
 REC_API rec_status rec_window_attend(const rec_window *w, void *stream);
+
+/*
+ * Queries and keys of events, normalised per head and rotated by their position, in one pass.
+ *
+ *   y = x / sqrt(mean(x^2) + eps) * w         a row of head_dim columns; y = x without a weight w
+ *   (y_a, y_b) -> (y_a cos t - y_b sin t,  y_a sin t + y_b cos t)     t = position * dev_frequencies[i]
+ *
+ * for the pairs i = 0 .. pairs - 1 of the first 2 * pairs columns: (a, b) = (i, i + pairs), or, interleaved,
+ * (2 i, 2 i + 1).  Columns behind those are not rotated; pairs = 0 rotates none.
+ *
+ *   q, k           [tokens][heads][head_dim], [tokens][kv_heads][head_dim] of dtype (REC_F32, REC_F16, REC_BF16);
+ *                  one of heads and kv_heads may be 0, and its rows and weight null
+ *   q_out, k_out   the same shapes and type, rows that do not overlap; they may be q and k themselves
+ *                  (the same address and strides) and may not overlap them otherwise
+ *   head_dim       32, 64 or 128
+ *   dev_positions  int32 or, wide = 1, int64 [tokens], of either sign
+ *   dev_frequencies  double [pairs], radians a position; pairs a multiple of 8, at most head_dim / 2
+ *   dev_q_weight, dev_k_weight   float [head_dim], 16-byte aligned, or null: those rows are not normalised
+ *   eps            >= 0
+ * Squares are summed in fp32, or in 64 bits where that would overflow or vanish; angles are worked out in 64 bits.
+ * REC_ERR_ARG: null, misaligned, bad enum, negative counts or eps, rows of q_out or k_out that overlap;
+ * REC_ERR_SHAPE: head_dim or pairs; REC_ERR_OVERFLOW: more than 2^20 heads, or more threads
+ * than a launch can have (2^32; a wave has 2 to 32 rows).
+ */
+typedef struct {
+    rec_rows q, k, q_out, k_out;
+    int32_t dtype;
+    int32_t heads, kv_heads, head_dim;
+    int64_t tokens;
+    const void *dev_positions;
+    int32_t wide;
+    int32_t pairs;
+    const double *dev_frequencies;
+    int32_t interleaved;
+    float eps;
+    const float *dev_q_weight, *dev_k_weight;
+} rec_turn;
+
+REC_API rec_status rec_rotate_heads(const rec_turn *t, void *stream);
 
 /* Waits for `stream`, reads a fault record and clears what it read: faults that work on other
  * streams adds meanwhile stay for the next check.  REC_OK, REC_ERR_LENGTHS

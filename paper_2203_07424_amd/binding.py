@@ -57,7 +57,7 @@ EXPORTS = ("rec_create", "rec_destroy", "rec_workspace_bytes", "rec_bind_workspa
            "rec_synth_fill_table", "rec_probe_mfma", "rec_probe_scan", "rec_probe_fc_form", "rec_probe_plan",
            "rec_probe_plan_joined", "rec_probe_plan_pooling", "rec_probe_dense_copy",
            "rec_history_bytes", "rec_history_write", "rec_history_read", "rec_history_attend_workspace_bytes",
-           "rec_history_attend", "rec_window_attend", "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
+           "rec_history_attend", "rec_window_attend", "rec_rotate_heads", "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
 
 
 class rec_config(C.Structure):
@@ -91,6 +91,13 @@ class rec_window(C.Structure):
                 ("batch", C.c_int32), ("tokens", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dev_offsets", C.c_void_p), ("scale", C.c_float), ("window", C.c_int32),
                 ("sinks", C.c_int32), ("dev_fault", C.c_void_p)]
+
+
+class rec_turn(C.Structure):
+    _fields_ = [("q", rec_rows), ("k", rec_rows), ("q_out", rec_rows), ("k_out", rec_rows), ("dtype", C.c_int32), ("heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("tokens", C.c_int64), ("dev_positions", C.c_void_p),
+                ("wide", C.c_int32), ("pairs", C.c_int32), ("dev_frequencies", C.c_void_p), ("interleaved", C.c_int32),
+                ("eps", C.c_float), ("dev_q_weight", C.c_void_p), ("dev_k_weight", C.c_void_p)]
 
 
 _vp = C.c_void_p
@@ -166,6 +173,8 @@ _lib.rec_history_attend.restype = C.c_int
 _lib.rec_history_attend.argtypes = [_vp, _vp, _vp, C.c_size_t, _vp]
 _lib.rec_window_attend.restype = C.c_int
 _lib.rec_window_attend.argtypes = [_vp, _vp]
+_lib.rec_rotate_heads.restype = C.c_int
+_lib.rec_rotate_heads.argtypes = [_vp, _vp]
 _lib.rec_history_check.restype = C.c_int
 _lib.rec_history_check.argtypes = [_vp, _vp, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
 _lib.rec_probe_history_form.restype = C.c_int
@@ -174,7 +183,8 @@ _lib.rec_probe_clear_faults.restype = C.c_int
 _lib.rec_probe_clear_faults.argtypes = [_vp, C.POINTER(C.c_uint64), _vp]
 # The same layouts for one packing call, a quarter of the time of setting a structure's fields.
 _ROWS, _QUERY, _WINDOW = struct.Struct("@Pqq"), struct.Struct("@PPqqqiiiiPqiPfiii"), struct.Struct("@PqqPqqPqqPiiqiiiPfiiP")
-assert (_ROWS.size, _QUERY.size, _WINDOW.size) == (C.sizeof(rec_rows), C.sizeof(rec_query), C.sizeof(rec_window))
+_TURN = struct.Struct("@PqqPqqPqqPqqiiiiqPiiPifPP")
+assert (_ROWS.size, _QUERY.size, _WINDOW.size, _TURN.size) == tuple(map(C.sizeof, (rec_rows, rec_query, rec_window, rec_turn)))
 
 
 class RecError(RuntimeError):
@@ -383,6 +393,10 @@ def rec_history_attend(h: rec_history, q: rec_query, workspace=None) -> int:
 
 def rec_window_attend(w: rec_window) -> int:
     return _lib.rec_window_attend(C.byref(w), _stream())
+
+
+def rec_rotate_heads(t: rec_turn) -> int:
+    return _lib.rec_rotate_heads(C.byref(t), _stream())
 
 
 def _is_record(fault: torch.Tensor) -> bool:
@@ -794,3 +808,58 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: to
     if st:
         raise RecError(st, "rec_window_attend")
     return out
+
+
+def _turn_rows(what: str, x: Optional[torch.Tensor], out: Optional[torch.Tensor], weight: Optional[torch.Tensor], like: torch.Tensor):
+    """Address and strides of x and of where its result goes (made here if None), its heads, its weight's address, the result."""
+    if x is None:
+        if out is not None or weight is not None:
+            raise ValueError(f"rec_rotate_heads: {what} is None, but not its result or weight")
+        return (0, 0, 0), (0, 0, 0), 0, 0, None
+    index = like.get_device()
+    if x.dim() != 3 or x.dtype is not like.dtype or x.get_device() != index or x.shape[0] != like.shape[0] or x.shape[2] != like.shape[2]:
+        raise ValueError("rec_rotate_heads: q must be [tokens, heads, head_dim] and k [tokens, kv_heads, head_dim] on one device, fp32, fp16 or bf16")
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index:
+        raise ValueError(f"rec_rotate_heads: the result of {what} must be of its shape, type and device")
+    (token, head, column), (out_token, out_head, out_column) = x.stride(), out.stride()
+    if column != 1 or out_column != 1:
+        raise ValueError(f"rec_rotate_heads: rows of {what} and of its result must be contiguous")
+    if weight is not None:
+        if weight.dtype is not _F32 or weight.shape != x.shape[2:] or weight.get_device() != index or not weight.is_contiguous():
+            raise ValueError(f"rec_rotate_heads: the weight of {what} must be a contiguous fp32 [{x.shape[2]}] on {like.device}")
+        if weight.requires_grad:
+            _no_backward("rec_rotate_heads")
+    if x.requires_grad or out.requires_grad:
+        _no_backward("rec_rotate_heads")
+    return (x.data_ptr(), token, head), (out.data_ptr(), out_token, out_head), x.shape[1], weight.data_ptr() if weight is not None else 0, out
+
+
+def rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: torch.Tensor,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 interleaved: bool = False, q_out: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Norms of queries and keys per head and their rotation by position, in one pass (rec_rotate_heads()).
+
+    q: [tokens, heads, head_dim], k: [tokens, kv_heads, head_dim], fp32, fp16 or bf16, any token and head strides; either may be None.
+    positions: int32 or int64 [tokens]; frequencies: float64 [pairs], radians a position, pairs a multiple of 8 (0: no rotation).
+    q_weight, k_weight: fp32 [head_dim], or None: those rows are only rotated.  interleaved: columns 2 i and 2 i + 1 are a pair,
+    else i and i + pairs.  Results are contiguous, or go to q_out and k_out, which may be q and k.  No backward pass, as in HistoryCache."""
+    like = q if q is not None else k
+    code, index = (None, -1) if like is None else (_DTYPE_CODES.get(like.dtype), like.get_device())
+    if code is None or index < 0 or like.dim() != 3:
+        raise ValueError("rec_rotate_heads: q must be [tokens, heads, head_dim] and k [tokens, kv_heads, head_dim] on one device, fp32, fp16 or bf16")
+    q_at, q_to, heads, q_w, q_out = _turn_rows("q", q, q_out, q_weight, like)
+    k_at, k_to, kv_heads, k_w, k_out = _turn_rows("k", k, k_out, k_weight, like)
+    tokens, _, dim = like.shape
+    if positions.shape != (tokens,) or positions.dtype not in (_I32, _I64) or positions.get_device() != index or not positions.is_contiguous():
+        raise ValueError(f"rec_rotate_heads: positions must be a contiguous int32 or int64 [{tokens}] on {like.device}")
+    if frequencies.dim() != 1 or frequencies.dtype is not torch.float64 or frequencies.get_device() != index or not frequencies.is_contiguous():
+        raise ValueError(f"rec_rotate_heads: frequencies must be a contiguous float64 vector on {like.device}")
+    st = _lib.rec_rotate_heads(
+        _TURN.pack(*q_at, *k_at, *q_to, *k_to, code, heads, kv_heads, dim, tokens, positions.data_ptr(), positions.dtype is _I64,
+                   frequencies.shape[0], frequencies.data_ptr(), 1 if interleaved else 0, eps, q_w, k_w), _stream_on(index, "rec_rotate_heads"))
+    if st:
+        raise RecError(st, "rec_rotate_heads")
+    return q_out, k_out

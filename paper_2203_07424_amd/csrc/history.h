@@ -97,6 +97,8 @@ size_t attend_workspace(const Cache &c, int format, int d, const rec_query &q);
 hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *workspace, hipStream_t s);
 long long window_blocks(const rec_window &w);  // of 256 threads
 hipError_t launch_window(const rec_window &w, hipStream_t s);
+long long rotate_threads(const rec_turn &t);
+hipError_t launch_rotate(const rec_turn &t, hipStream_t s);
 hipError_t launch_clear_faults(unsigned long long *fault, const Faults &seen, hipStream_t s);
 
 }  // namespace hist

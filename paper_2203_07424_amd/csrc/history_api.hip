@@ -1,4 +1,6 @@
 // Host side of include/rec_history.h: checks, and nothing else.
+#include <utility>
+
 #include "history.h"
 #include "rec_probe.h"
 
@@ -74,6 +76,19 @@ bool rows_fit(const rec_rows &r, int size)
 // Tiles of 64 rows are addressed from their first one in 31 bits.
 bool tiles_fit(const rec_rows &r) { return r.token_stride >= 0 && r.token_stride < 1ll << 23; }
 
+// Rows [tokens][heads][d] that have no element in common.
+bool rows_apart(const rec_rows &r, int64_t tokens, int64_t heads, int64_t d)
+{
+    int64_t near = r.head_stride < 0 ? -r.head_stride : r.head_stride, far = r.token_stride < 0 ? -r.token_stride : r.token_stride;
+    int64_t n_near = heads, n_far = tokens;
+    if (near > far) {
+        std::swap(near, far);
+        std::swap(n_near, n_far);
+    }
+    // Bounds as quotients: products of strides and counts may not fit 64 bits.
+    return (n_near == 1 || near >= d) && (n_far == 1 || (far >= d && (n_near == 1 || (far - d) / near >= n_near - 1)));
+}
+
 rec_status status_of(hipError_t e) { return e == hipSuccess ? REC_OK : REC_ERR_DEVICE; }
 
 }  // namespace
@@ -147,6 +162,25 @@ rec_status rec_window_attend(const rec_window *w, void *stream)
         !words_fit(w->dev_offsets, 4) || !words_fit(w->dev_fault, 8))
         return REC_ERR_ARG;
     return status_of(rec::hist::launch_window(*w, static_cast<hipStream_t>(stream)));
+}
+
+rec_status rec_rotate_heads(const rec_turn *t, void *stream)
+{
+    if (!t || (t->dtype != REC_F32 && t->dtype != REC_F16 && t->dtype != REC_BF16) || t->tokens < 0 || t->heads < 0 || t->kv_heads < 0 ||
+        (t->wide != 0 && t->wide != 1) || (t->interleaved != 0 && t->interleaved != 1) || !(t->eps >= 0.0f))
+        return REC_ERR_ARG;
+    if (!head_dim_fits(t->head_dim) || t->pairs < 0 || t->pairs % 8 || t->pairs > t->head_dim / 2) return REC_ERR_SHAPE;
+    const int64_t all = (int64_t)t->heads + t->kv_heads;
+    if (all > 1 << 20) return REC_ERR_OVERFLOW;
+    if (t->tokens == 0 || all == 0) return REC_OK;
+    if (t->tokens > MOST_TOKENS || rec::hist::rotate_threads(*t) > MOST_THREADS) return REC_ERR_OVERFLOW;
+    const int size = t->dtype == REC_F32 ? 4 : 2;
+    if (t->heads && (!rows_fit(t->q, size) || !rows_fit(t->q_out, size) || !rows_apart(t->q_out, t->tokens, t->heads, t->head_dim))) return REC_ERR_ARG;
+    if (t->kv_heads && (!rows_fit(t->k, size) || !rows_fit(t->k_out, size) || !rows_apart(t->k_out, t->tokens, t->kv_heads, t->head_dim))) return REC_ERR_ARG;
+    if (t->pairs && (!t->dev_positions || !words_fit(t->dev_positions, t->wide ? 8 : 4) || !t->dev_frequencies || !words_fit(t->dev_frequencies, 8)))
+        return REC_ERR_ARG;
+    if ((t->dev_q_weight && !aligned(t->dev_q_weight)) || (t->dev_k_weight && !aligned(t->dev_k_weight))) return REC_ERR_ARG;
+    return status_of(rec::hist::launch_rotate(*t, static_cast<hipStream_t>(stream)));
 }
 
 rec_status rec_history_check(uint64_t *dev_fault, void *stream, int64_t *first_bad_pos, int32_t *word)
