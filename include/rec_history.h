@@ -10,6 +10,8 @@
  *   rec_window_attend()    a whole new history attends to itself
  *   rec_history_write()    its keys and values enter the cache, 4 or 8 bits a number
  *   rec_history_attend()   later queries attend to what the cache holds
+ *   rec_history_summarise(), _select(), _attend_selected()
+ *                          or, of a long history, to the pages that score highest only
  *   rec_history_read()     stored keys and values are read back
  *
  * What a query sees.  The query at position p (counted from 0 in its history) sees
@@ -70,8 +72,10 @@ enum { REC_MX4 = 0, REC_MX8 = 1 };
  * calls that find faults only lower the words. */
 enum {
     REC_FAULT_LENGTH = 0,  /* history with a negative or too large length, or bad offsets     */
-    REC_FAULT_SLOT = 1,    /* position in dev_slots of a slot outside the cache               */
-    REC_FAULT_PAGE = 2,    /* history * table_width + column of a page outside the cache      */
+    REC_FAULT_SLOT = 1,    /* position in dev_slots of a slot outside the cache, or in dev_chosen of a page
+                              that the history does not have                                  */
+    REC_FAULT_PAGE = 2,    /* history * table_width + column (or position in dev_which) of a page outside
+                              the cache                                                       */
     REC_FAULT_VALUE = 3,   /* position in dev_slots of a row with a NaN or an infinity         */
     REC_FAULT_WORDS = 4
 };
@@ -171,6 +175,51 @@ REC_API size_t rec_history_attend_workspace_bytes(const rec_history *h, const re
  * > 2^31 - 1024, or more threads than a launch can have (2^32). */
 REC_API rec_status rec_history_attend(const rec_history *h, const rec_query *q, void *dev_workspace,
                                       size_t workspace_bytes, void *stream);
+
+/*
+ * Chosen pages.  Of a long history a query need not see all: each page has a mean key, and each query attends,
+ * for each kv head, to the pages whose means score highest with it.
+ *
+ * rec_history_summarise() writes the mean keys of `pages` pages, bf16 [kv_heads][head_dim] each, into
+ * dev_means [num_pages][kv_heads][head_dim] (16-byte aligned): those of a page dev_which[i] (int32; -1: left out) at that
+ * page.  All page_tokens places count, so a page has its turn once it is full; NaN where a key is NaN.  A page that is
+ * named twice is written twice, alike.
+ * Device faults: REC_FAULT_PAGE (position in dev_which; nothing is written for it).
+ * REC_ERR_ARG: null, misaligned, pages < 0; REC_ERR_SHAPE as above; REC_ERR_OVERFLOW: more threads than a launch can have.
+ */
+REC_API rec_status rec_history_summarise(const rec_history *h, const int32_t *dev_which, int32_t pages, void *dev_means, void *stream);
+
+/*
+ * rec_history_select() chooses `count` pages for each query and kv head, of those up to the one that the query
+ * stands in: the first `first` of the history and the last `last` always (of which the query's own is one), and
+ * between them those with the highest scores
+ *
+ *   score = max over the heads n of the kv head of  <q_n, mean>
+ *
+ * in 64 bits; of equal ones the earlier.  A product that is NaN counts for nothing; a page outside the cache, or
+ * without a product that counts, scores -infinity.  dev_chosen [batch][queries][kv_heads][count], int32, gets the pages'
+ * numbers in their history, ascending, -1 behind them where there are fewer.  The means of the last `last` pages are not
+ * looked at, so a page that is not full yet needs none.
+ *   q              as for rec_history_attend(); dev_out and scale are not looked at, window and sinks are 0
+ *   count          >= first + last, first >= 0, last >= 1
+ * Device faults: REC_FAULT_LENGTH, REC_FAULT_PAGE as there.
+ * REC_ERR_ARG: null, misaligned, bad counts, a workspace too small; REC_ERR_SHAPE, REC_ERR_OVERFLOW as there.
+ */
+REC_API size_t rec_history_select_workspace_bytes(const rec_history *h, const rec_query *q, int32_t count);
+REC_API rec_status rec_history_select(const rec_history *h, const rec_query *q, const void *dev_means, int32_t count, int32_t first,
+                                      int32_t last, int32_t *dev_chosen, void *dev_workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * rec_history_attend_selected(): rec_history_attend() where each query and kv head sees, of what its position allows, only
+ * the pages in dev_chosen, int32 [batch][queries][kv_heads][count], in any order.  An entry of -1 is none; a page that
+ * is named twice counts twice.  window and sinks are 0.
+ * Device faults: REC_FAULT_LENGTH, REC_FAULT_PAGE as there, and REC_FAULT_SLOT: position in dev_chosen of an entry that is
+ * neither -1 nor under table_width (it is not seen).  Errors as there; REC_ERR_ARG: count < 1; REC_ERR_OVERFLOW: count * page_tokens
+ * > 2^31 - 1024.
+ */
+REC_API size_t rec_history_attend_selected_workspace_bytes(const rec_history *h, const rec_query *q, int32_t count);
+REC_API rec_status rec_history_attend_selected(const rec_history *h, const rec_query *q, const int32_t *dev_chosen, int32_t count,
+                                               void *dev_workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Whole histories attend to themselves, without a cache.

@@ -57,7 +57,8 @@ EXPORTS = ("rec_create", "rec_destroy", "rec_workspace_bytes", "rec_bind_workspa
            "rec_synth_fill_table", "rec_probe_mfma", "rec_probe_scan", "rec_probe_fc_form", "rec_probe_plan",
            "rec_probe_plan_joined", "rec_probe_plan_pooling", "rec_probe_dense_copy",
            "rec_history_bytes", "rec_history_write", "rec_history_read", "rec_history_attend_workspace_bytes",
-           "rec_history_attend", "rec_window_attend", "rec_rotate_heads", "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
+           "rec_history_attend", "rec_history_summarise", "rec_history_select_workspace_bytes", "rec_history_select",
+           "rec_history_attend_selected_workspace_bytes", "rec_history_attend_selected", "rec_window_attend", "rec_rotate_heads", "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
 
 
 class rec_config(C.Structure):
@@ -171,6 +172,16 @@ _lib.rec_history_attend_workspace_bytes.restype = C.c_size_t
 _lib.rec_history_attend_workspace_bytes.argtypes = [_vp, _vp]
 _lib.rec_history_attend.restype = C.c_int
 _lib.rec_history_attend.argtypes = [_vp, _vp, _vp, C.c_size_t, _vp]
+_lib.rec_history_summarise.restype = C.c_int
+_lib.rec_history_summarise.argtypes = [_vp, _vp, C.c_int32, _vp, _vp]
+_lib.rec_history_select_workspace_bytes.restype = C.c_size_t
+_lib.rec_history_select_workspace_bytes.argtypes = [_vp, _vp, C.c_int32]
+_lib.rec_history_select.restype = C.c_int
+_lib.rec_history_select.argtypes = [_vp, _vp, _vp, C.c_int32, C.c_int32, C.c_int32, _vp, _vp, C.c_size_t, _vp]
+_lib.rec_history_attend_selected_workspace_bytes.restype = C.c_size_t
+_lib.rec_history_attend_selected_workspace_bytes.argtypes = [_vp, _vp, C.c_int32]
+_lib.rec_history_attend_selected.restype = C.c_int
+_lib.rec_history_attend_selected.argtypes = [_vp, _vp, _vp, C.c_int32, _vp, C.c_size_t, _vp]
 _lib.rec_window_attend.restype = C.c_int
 _lib.rec_window_attend.argtypes = [_vp, _vp]
 _lib.rec_rotate_heads.restype = C.c_int
@@ -389,6 +400,32 @@ def rec_history_attend_workspace_bytes(h: rec_history, q: rec_query) -> int:
 def rec_history_attend(h: rec_history, q: rec_query, workspace=None) -> int:
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     return _lib.rec_history_attend(C.byref(h), C.byref(q), _ptr(workspace), nbytes, _stream())
+
+
+def _bytes(workspace: Optional[torch.Tensor]) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def rec_history_summarise(h: rec_history, dev_which, pages: int, dev_means) -> int:
+    return _lib.rec_history_summarise(C.byref(h), _ptr(dev_which), int(pages), _ptr(dev_means), _stream())
+
+
+def rec_history_select_workspace_bytes(h: rec_history, q: rec_query, count: int) -> int:
+    return int(_lib.rec_history_select_workspace_bytes(C.byref(h), C.byref(q), int(count)))
+
+
+def rec_history_select(h: rec_history, q: rec_query, dev_means, count: int, first: int, last: int, dev_chosen, workspace=None) -> int:
+    return _lib.rec_history_select(C.byref(h), C.byref(q), _ptr(dev_means), int(count), int(first), int(last), _ptr(dev_chosen),
+                                   _ptr(workspace), _bytes(workspace), _stream())
+
+
+def rec_history_attend_selected_workspace_bytes(h: rec_history, q: rec_query, count: int) -> int:
+    return int(_lib.rec_history_attend_selected_workspace_bytes(C.byref(h), C.byref(q), int(count)))
+
+
+def rec_history_attend_selected(h: rec_history, q: rec_query, dev_chosen, count: int, workspace=None) -> int:
+    return _lib.rec_history_attend_selected(C.byref(h), C.byref(q), _ptr(dev_chosen), int(count), _ptr(workspace), _bytes(workspace),
+                                            _stream())
 
 
 def rec_window_attend(w: rec_window) -> int:
@@ -772,6 +809,110 @@ class HistoryCache:
                                      _stream_on(index, "rec_history_attend"))
         if st:
             self._ok(st, "rec_history_attend")
+        return out
+
+    def summarise(self, which: torch.Tensor, means: torch.Tensor) -> torch.Tensor:
+        """Mean keys of the pages `which` (int32 [n], -1 for none), which are full, into means: bf16 [num_pages, kv_heads, head_dim],
+        contiguous.  Returns means."""
+        if which.dim() != 1 or which.dtype is not _I32 or which.get_device() != self._index or not which.is_contiguous():
+            raise ValueError(f"rec_history_summarise: which must be a contiguous int32 vector on {self.device}")
+        self._means("rec_history_summarise", means)
+        st = _lib.rec_history_summarise(self._ref, which.data_ptr(), which.shape[0], means.data_ptr(),
+                                        _stream_on(self._index, "rec_history_summarise"))
+        if st:
+            self._ok(st, "rec_history_summarise")
+        return means
+
+    def _means(self, call: str, means: torch.Tensor) -> None:
+        if means.requires_grad:
+            _no_backward(call)
+        if means.shape != (self._h.num_pages, self.kv_heads, self.head_dim) or means.dtype is not torch.bfloat16 \
+                or means.get_device() != self._index or not means.is_contiguous():
+            raise ValueError(f"{call}: means must be a contiguous bfloat16 [{self._h.num_pages}, {self.kv_heads}, {self.head_dim}] on "
+                             f"{self.device}")
+
+    def _query(self, call: str, q: torch.Tensor, pages_of: torch.Tensor, lengths: torch.Tensor, out: int, scale: Optional[float],
+               candidates: bool) -> Tuple[bytes, tuple]:
+        """A query without window and sinks as rec_query, and the shapes that decide its workspace."""
+        if q.requires_grad:
+            _no_backward(call)
+        index, code = self._index, _ATTEND_CODES.get(q.dtype)
+        if q.dim() == 4:
+            batch, queries, heads, dim = q.shape
+            by_batch, by_query, by_head, by_column = q.stride()
+        elif q.dim() == 3:
+            (batch, heads, dim), queries = q.shape, 1
+            (by_batch, by_head, by_column), by_query = q.stride(), 0
+        else:
+            code = None
+        if code is None or dim != self.head_dim or q.get_device() != index or by_column != 1:
+            raise ValueError(f"{call}: q must be fp16 or bf16 [batch, (queries,) heads, {self.head_dim}] on {self.device}, rows contiguous")
+        if pages_of.dim() != 2 or pages_of.dtype is not _I32 or pages_of.get_device() != index or pages_of.shape[0] != batch \
+                or (pages_of.stride(1) != 1 and pages_of.shape[1] > 1):
+            raise ValueError(f"{call}: pages_of must be int32 [{batch}, width] on {self.device}, rows contiguous")
+        if lengths.dtype is not _I32 or lengths.get_device() != index or lengths.shape != (batch,) or not lengths.is_contiguous():
+            raise ValueError(f"{call}: lengths must be a contiguous int32 [{batch}] on {self.device}")
+        width = pages_of.shape[1]
+        query = _QUERY.pack(q.data_ptr(), out, by_batch, by_query, by_head, code, batch, queries, heads, pages_of.data_ptr(),
+                            pages_of.stride(0), width, lengths.data_ptr(), dim ** -0.5 if scale is None else scale, 0, 0,
+                            1 if candidates else 0)
+        return query, (batch, queries, heads, width, candidates, code)
+
+    def _workspace(self, ask, query: bytes, shapes: tuple, *more: int) -> Optional[torch.Tensor]:
+        """As many bytes as `ask` says for these shapes, or None."""
+        key = (ask.__name__, shapes, more)
+        need = self._workspaces.get(key)
+        if need is None:
+            need = ask(self._ref, query, *more)
+            if len(self._workspaces) >= 1024:
+                self._workspaces.clear()
+            self._workspaces[key] = need
+        return torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+
+    def _result(self, call: str, q: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
+        if out is None:
+            return torch.empty_like(q, memory_format=torch.contiguous_format)
+        if out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != self._index or not out.is_contiguous():
+            raise ValueError(f"{call}: out must be contiguous and of q's shape, type and device")
+        return out
+
+    def select(self, q: torch.Tensor, means: torch.Tensor, pages_of: torch.Tensor, lengths: torch.Tensor, count: int, first: int = 1,
+               last: int = 1, candidates: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """For each query and kv head the numbers of `count` pages of its history, ascending, -1 behind them where there are fewer:
+        the first `first`, the last `last` up to the query's own, and between them those whose means (of summarise()) have the
+        largest product with one of the kv head's queries.  q, pages_of, lengths and candidates as for attend().  Returns int32
+        [batch, (queries,) kv_heads, count] for attend_selected()."""
+        call = "rec_history_select"
+        query, shapes = self._query(call, q, pages_of, lengths, 0, 1.0, candidates)
+        self._means(call, means)
+        shape = (*q.shape[:-2], self.kv_heads, count)
+        if out is None:
+            out = torch.empty(shape, dtype=_I32, device=self.device) if count >= 0 else means
+        elif out.shape != shape or out.dtype is not _I32 or out.get_device() != self._index or not out.is_contiguous():
+            raise ValueError(f"{call}: out must be a contiguous int32 {list(shape)} on {self.device}")
+        workspace = self._workspace(_lib.rec_history_select_workspace_bytes, query, shapes, count)
+        st = _lib.rec_history_select(self._ref, query, means.data_ptr(), count, first, last, out.data_ptr(), _ptr(workspace),
+                                     _bytes(workspace), _stream_on(self._index, call))
+        if st:
+            self._ok(st, call)
+        return out
+
+    def attend_selected(self, q: torch.Tensor, chosen: torch.Tensor, pages_of: torch.Tensor, lengths: torch.Tensor,
+                        scale: Optional[float] = None, candidates: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """attend() over the chosen pages only: chosen is int32 [batch, (queries,) kv_heads, count], contiguous, as select() gives it,
+        numbers of pages in their history in any order, -1 for none."""
+        call = "rec_history_attend_selected"
+        out = self._result(call, q, out)
+        query, shapes = self._query(call, q, pages_of, lengths, out.data_ptr(), scale, candidates)
+        if chosen.dim() != q.dim() or chosen.shape[:-1] != (*q.shape[:-2], self.kv_heads) or chosen.dtype is not _I32 \
+                or chosen.get_device() != self._index or not chosen.is_contiguous():
+            raise ValueError(f"{call}: chosen must be a contiguous int32 {[*q.shape[:-2], self.kv_heads]} and a count on {self.device}")
+        count = chosen.shape[-1]
+        workspace = self._workspace(_lib.rec_history_attend_selected_workspace_bytes, query, shapes, count)
+        st = _lib.rec_history_attend_selected(self._ref, query, chosen.data_ptr(), count, _ptr(workspace), _bytes(workspace),
+                                              _stream_on(self._index, call))
+        if st:
+            self._ok(st, call)
         return out
 
     def check(self) -> Tuple[int, int, int]:

@@ -95,6 +95,20 @@ long long attend_threads(const Cache &c, int format, int d, const rec_query &q);
 void attend_form(const Cache &c, int format, int d, const rec_query &q, int32_t (&form)[3]);  // waves of a block, parts, kv heads of a wave
 size_t attend_workspace(const Cache &c, int format, int d, const rec_query &q);
 hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, void *workspace, hipStream_t s);
+long long chosen_threads(const Cache &c, int format, int d, const rec_query &q, int count);
+size_t chosen_workspace(const Cache &c, int format, int d, const rec_query &q, int count);
+hipError_t launch_chosen(const Cache &c, int format, int d, const rec_query &q, const int32_t *chosen, int count, void *workspace, hipStream_t s);
+hipError_t launch_means(const Cache &c, int format, int d, const int32_t *which, int pages, void *means, hipStream_t s);
+long long means_threads(const Cache &c, int d, int pages);
+struct Select {
+    const void *means;
+    int count, first, last;
+    int32_t *chosen;
+    unsigned long long *keys;  // a score's, as whole numbers of the same order: [batch * queries * kv_heads][table_width]
+};
+long long select_threads(const Cache &c, const rec_query &q);
+size_t select_workspace(const Cache &c, const rec_query &q, int count);
+hipError_t launch_select(const Cache &c, int d, const rec_query &q, const Select &sel, hipStream_t s);
 long long window_blocks(const rec_window &w);  // of 256 threads
 hipError_t launch_window(const rec_window &w, hipStream_t s);
 long long rotate_threads(const rec_turn &t);

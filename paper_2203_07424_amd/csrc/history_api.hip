@@ -54,7 +54,8 @@ rec_status check_rows(const rec_history *h, int32_t dtype, const int64_t *dev_sl
     return REC_OK;
 }
 
-rec_status check_query(const rec_history *h, const rec_query *q)
+// Shapes and counts of a query, whatever reads it.
+rec_status check_counts(const rec_history *h, const rec_query *q)
 {
     if (!h || !q) return REC_ERR_ARG;
     if (!shape_fits(h)) return REC_ERR_SHAPE;
@@ -65,8 +66,48 @@ rec_status check_query(const rec_history *h, const rec_query *q)
     if ((int64_t)q->table_width * h->page_tokens > MOST_TOKENS || (int64_t)q->queries * q->heads >= 1ll << 31 ||
         (int64_t)q->queries * q->heads * q->batch >= 1ll << 31)
         return REC_ERR_OVERFLOW;
+    return REC_OK;
+}
+
+rec_status check_query(const rec_history *h, const rec_query *q)
+{
+    const rec_status st = check_counts(h, q);
+    if (st != REC_OK) return st;
     return rec::hist::attend_threads(cache_of(h), h->format, h->head_dim, *q) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
 }
+
+// Calls in which all that stands before a query may be seen.
+rec_status check_unmasked(const rec_history *h, const rec_query *q)
+{
+    const rec_status st = check_counts(h, q);
+    return st == REC_OK && (q->window || q->sinks) ? REC_ERR_ARG : st;
+}
+
+rec_status check_select(const rec_history *h, const rec_query *q, int32_t count)
+{
+    const rec_status st = check_unmasked(h, q);
+    if (st != REC_OK) return st;
+    if (count < 1) return REC_ERR_ARG;
+    return rec::hist::select_threads(cache_of(h), *q) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
+}
+
+rec_status check_chosen(const rec_history *h, const rec_query *q, int32_t count)
+{
+    const rec_status st = check_unmasked(h, q);
+    if (st != REC_OK) return st;
+    if (count < 1) return REC_ERR_ARG;
+    if ((int64_t)count * h->page_tokens > MOST_TOKENS) return REC_ERR_OVERFLOW;
+    return rec::hist::chosen_threads(cache_of(h), h->format, h->head_dim, *q, count) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
+}
+
+// What a query that has something to do points to, but for its results.
+bool query_fits(const rec_query *q)
+{
+    return aligned(q->dev_q) && stride_fits(q->batch_stride, 2) && stride_fits(q->query_stride, 2) && stride_fits(q->head_stride, 2) &&
+           q->dev_lengths && words_fit(q->dev_lengths, 4) && (q->table_width == 0 || q->dev_pages_of) && words_fit(q->dev_pages_of, 4);
+}
+
+bool workspace_fits(size_t need, const void *dev, size_t bytes) { return !need || (aligned(dev) && bytes >= need); }
 
 bool rows_fit(const rec_rows &r, int size)
 {
@@ -139,14 +180,59 @@ rec_status rec_history_attend(const rec_history *h, const rec_query *q, void *de
     if (st != REC_OK) return st;
     if (!aligned(h->dev_pages) || !words_fit(h->dev_fault, 8)) return REC_ERR_ARG;
     if (q->batch == 0 || q->queries == 0) return REC_OK;
-    if (!aligned(q->dev_q) || !aligned(q->dev_out) || !stride_fits(q->batch_stride, 2) || !stride_fits(q->query_stride, 2) ||
-        !stride_fits(q->head_stride, 2) || !q->dev_lengths || !words_fit(q->dev_lengths, 4) || (q->table_width > 0 && !q->dev_pages_of) ||
-        !words_fit(q->dev_pages_of, 4))
-        return REC_ERR_ARG;
-    const size_t need = rec::hist::attend_workspace(cache_of(h), h->format, h->head_dim, *q);
-    if (need && (!aligned(dev_workspace) || workspace_bytes < need)) return REC_ERR_ARG;
+    if (!query_fits(q) || !aligned(q->dev_out)) return REC_ERR_ARG;
+    if (!workspace_fits(rec::hist::attend_workspace(cache_of(h), h->format, h->head_dim, *q), dev_workspace, workspace_bytes)) return REC_ERR_ARG;
     return status_of(rec::hist::launch_attend(cache_of(h), h->format, h->head_dim, *q, dev_workspace,
                                               static_cast<hipStream_t>(stream)));
+}
+
+rec_status rec_history_summarise(const rec_history *h, const int32_t *dev_which, int32_t pages, void *dev_means, void *stream)
+{
+    if (!h) return REC_ERR_ARG;
+    if (!shape_fits(h)) return REC_ERR_SHAPE;
+    if (!aligned(h->dev_pages) || !words_fit(h->dev_fault, 8) || pages < 0) return REC_ERR_ARG;
+    if (pages && (!dev_which || !words_fit(dev_which, 4) || !aligned(dev_means))) return REC_ERR_ARG;
+    const Cache c = cache_of(h);
+    if (rec::hist::means_threads(c, h->head_dim, pages) > MOST_THREADS) return REC_ERR_OVERFLOW;
+    if (pages == 0) return REC_OK;
+    return status_of(rec::hist::launch_means(c, h->format, h->head_dim, dev_which, pages, dev_means, static_cast<hipStream_t>(stream)));
+}
+
+size_t rec_history_select_workspace_bytes(const rec_history *h, const rec_query *q, int32_t count)
+{
+    return check_select(h, q, count) != REC_OK ? 0 : rec::hist::select_workspace(cache_of(h), *q, count);
+}
+
+rec_status rec_history_select(const rec_history *h, const rec_query *q, const void *dev_means, int32_t count, int32_t first,
+                              int32_t last, int32_t *dev_chosen, void *dev_workspace, size_t workspace_bytes, void *stream)
+{
+    const rec_status st = check_select(h, q, count);
+    if (st != REC_OK) return st;
+    if (first < 0 || last < 1 || (int64_t)first + last > count || !words_fit(h->dev_fault, 8)) return REC_ERR_ARG;
+    if (q->batch == 0 || q->queries == 0) return REC_OK;
+    if (!query_fits(q) || !aligned(dev_means) || !dev_chosen || !words_fit(dev_chosen, 4)) return REC_ERR_ARG;
+    const Cache c = cache_of(h);
+    if (!workspace_fits(rec::hist::select_workspace(c, *q, count), dev_workspace, workspace_bytes)) return REC_ERR_ARG;
+    const rec::hist::Select sel = {dev_means, count, first, last, dev_chosen, static_cast<unsigned long long *>(dev_workspace)};
+    return status_of(rec::hist::launch_select(c, h->head_dim, *q, sel, static_cast<hipStream_t>(stream)));
+}
+
+size_t rec_history_attend_selected_workspace_bytes(const rec_history *h, const rec_query *q, int32_t count)
+{
+    return check_chosen(h, q, count) != REC_OK ? 0 : rec::hist::chosen_workspace(cache_of(h), h->format, h->head_dim, *q, count);
+}
+
+rec_status rec_history_attend_selected(const rec_history *h, const rec_query *q, const int32_t *dev_chosen, int32_t count,
+                                       void *dev_workspace, size_t workspace_bytes, void *stream)
+{
+    const rec_status st = check_chosen(h, q, count);
+    if (st != REC_OK) return st;
+    if (!aligned(h->dev_pages) || !words_fit(h->dev_fault, 8)) return REC_ERR_ARG;
+    if (q->batch == 0 || q->queries == 0) return REC_OK;
+    if (!query_fits(q) || !aligned(q->dev_out) || !dev_chosen || !words_fit(dev_chosen, 4)) return REC_ERR_ARG;
+    const Cache c = cache_of(h);
+    if (!workspace_fits(rec::hist::chosen_workspace(c, h->format, h->head_dim, *q, count), dev_workspace, workspace_bytes)) return REC_ERR_ARG;
+    return status_of(rec::hist::launch_chosen(c, h->format, h->head_dim, *q, dev_chosen, count, dev_workspace, static_cast<hipStream_t>(stream)));
 }
 
 rec_status rec_window_attend(const rec_window *w, void *stream)
