@@ -12,6 +12,8 @@
  *   rec_history_attend()   later queries attend to what the cache holds
  *   rec_history_summarise(), _select(), _attend_selected()
  *                          or, of a long history, to the pages that score highest only
+ *   rec_history_attend_shared()
+ *                          or to what many histories begin with and each one's own
  *   rec_history_read()     stored keys and values are read back
  *
  * What a query sees.  The query at position p (counted from 0 in its history) sees
@@ -220,6 +222,20 @@ REC_API rec_status rec_history_select(const rec_history *h, const rec_query *q, 
 REC_API size_t rec_history_attend_selected_workspace_bytes(const rec_history *h, const rec_query *q, int32_t count);
 REC_API rec_status rec_history_attend_selected(const rec_history *h, const rec_query *q, const int32_t *dev_chosen, int32_t count,
                                                void *dev_workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Histories that begin alike.  rec_history_attend_shared(): rec_history_attend() where the histories of a batch all begin with the
+ * same tokens, *dev_prefix_length (int32, on the device) of them in the pages dev_prefix_pages, int32 [prefix_width]; q describes what
+ * each has behind them, its pages, its length and its queries.  A query sees the whole prefix and, of its own history, what it
+ * would see by itself; one that stands before its own history's first token sees nothing, but for candidates, which then see
+ * the prefix.  The prefix is read once for many queries.  window and sinks are 0.
+ * Device faults: as there; of the prefix REC_FAULT_LENGTH with position batch, REC_FAULT_PAGE with position
+ * batch * table_width + column.  Errors as there; REC_ERR_ARG: prefix_width < 0, dev_prefix_pages (where prefix_width > 0) or
+ * dev_prefix_length null or misaligned; REC_ERR_OVERFLOW: prefix_width * page_tokens > 2^31 - 1024.
+ */
+REC_API size_t rec_history_attend_shared_workspace_bytes(const rec_history *h, const rec_query *q, int32_t prefix_width);
+REC_API rec_status rec_history_attend_shared(const rec_history *h, const rec_query *q, const int32_t *dev_prefix_pages, int32_t prefix_width,
+                                             const int32_t *dev_prefix_length, void *dev_workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Whole histories attend to themselves, without a cache.

@@ -58,7 +58,7 @@ EXPORTS = ("rec_create", "rec_destroy", "rec_workspace_bytes", "rec_bind_workspa
            "rec_probe_plan_joined", "rec_probe_plan_pooling", "rec_probe_dense_copy",
            "rec_history_bytes", "rec_history_write", "rec_history_read", "rec_history_attend_workspace_bytes",
            "rec_history_attend", "rec_history_summarise", "rec_history_select_workspace_bytes", "rec_history_select",
-           "rec_history_attend_selected_workspace_bytes", "rec_history_attend_selected", "rec_window_attend", "rec_rotate_heads", "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
+           "rec_history_attend_selected_workspace_bytes", "rec_history_attend_selected", "rec_history_attend_shared_workspace_bytes", "rec_history_attend_shared", "rec_window_attend", "rec_rotate_heads", "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
 
 
 class rec_config(C.Structure):
@@ -182,6 +182,10 @@ _lib.rec_history_attend_selected_workspace_bytes.restype = C.c_size_t
 _lib.rec_history_attend_selected_workspace_bytes.argtypes = [_vp, _vp, C.c_int32]
 _lib.rec_history_attend_selected.restype = C.c_int
 _lib.rec_history_attend_selected.argtypes = [_vp, _vp, _vp, C.c_int32, _vp, C.c_size_t, _vp]
+_lib.rec_history_attend_shared_workspace_bytes.restype = C.c_size_t
+_lib.rec_history_attend_shared_workspace_bytes.argtypes = [_vp, _vp, C.c_int32]
+_lib.rec_history_attend_shared.restype = C.c_int
+_lib.rec_history_attend_shared.argtypes = [_vp, _vp, _vp, C.c_int32, _vp, _vp, C.c_size_t, _vp]
 _lib.rec_window_attend.restype = C.c_int
 _lib.rec_window_attend.argtypes = [_vp, _vp]
 _lib.rec_rotate_heads.restype = C.c_int
@@ -426,6 +430,15 @@ def rec_history_attend_selected_workspace_bytes(h: rec_history, q: rec_query, co
 def rec_history_attend_selected(h: rec_history, q: rec_query, dev_chosen, count: int, workspace=None) -> int:
     return _lib.rec_history_attend_selected(C.byref(h), C.byref(q), _ptr(dev_chosen), int(count), _ptr(workspace), _bytes(workspace),
                                             _stream())
+
+
+def rec_history_attend_shared_workspace_bytes(h: rec_history, q: rec_query, prefix_width: int) -> int:
+    return int(_lib.rec_history_attend_shared_workspace_bytes(C.byref(h), C.byref(q), int(prefix_width)))
+
+
+def rec_history_attend_shared(h: rec_history, q: rec_query, dev_prefix_pages, prefix_width: int, dev_prefix_length, workspace=None) -> int:
+    return _lib.rec_history_attend_shared(C.byref(h), C.byref(q), _ptr(dev_prefix_pages), int(prefix_width), _ptr(dev_prefix_length),
+                                          _ptr(workspace), _bytes(workspace), _stream())
 
 
 def rec_window_attend(w: rec_window) -> int:
@@ -911,6 +924,27 @@ class HistoryCache:
         workspace = self._workspace(_lib.rec_history_attend_selected_workspace_bytes, query, shapes, count)
         st = _lib.rec_history_attend_selected(self._ref, query, chosen.data_ptr(), count, _ptr(workspace), _bytes(workspace),
                                               _stream_on(self._index, call))
+        if st:
+            self._ok(st, call)
+        return out
+
+    def attend_shared(self, q: torch.Tensor, prefix_pages: torch.Tensor, prefix_length: torch.Tensor, pages_of: torch.Tensor,
+                      lengths: torch.Tensor, scale: Optional[float] = None, candidates: bool = False,
+                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """attend() for histories that all begin with the same tokens: prefix_length (int32 [1] on the device) of them, in
+        prefix_pages (int32 [width], contiguous).  pages_of and lengths are of what each history has behind them."""
+        call = "rec_history_attend_shared"
+        out = self._result(call, q, out)
+        query, shapes = self._query(call, q, pages_of, lengths, out.data_ptr(), scale, candidates)
+        index = self._index
+        if prefix_pages.dim() != 1 or prefix_pages.dtype is not _I32 or prefix_pages.get_device() != index or not prefix_pages.is_contiguous():
+            raise ValueError(f"{call}: prefix_pages must be a contiguous int32 vector on {self.device}")
+        if prefix_length.numel() != 1 or prefix_length.dtype is not _I32 or prefix_length.get_device() != index:
+            raise ValueError(f"{call}: prefix_length must be one int32 on {self.device}")
+        width = prefix_pages.shape[0]
+        workspace = self._workspace(_lib.rec_history_attend_shared_workspace_bytes, query, shapes, width)
+        st = _lib.rec_history_attend_shared(self._ref, query, prefix_pages.data_ptr(), width, prefix_length.data_ptr(), _ptr(workspace),
+                                            _bytes(workspace), _stream_on(index, call))
         if st:
             self._ok(st, call)
         return out

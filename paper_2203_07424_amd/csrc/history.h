@@ -98,6 +98,21 @@ hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, 
 long long chosen_threads(const Cache &c, int format, int d, const rec_query &q, int count);
 size_t chosen_workspace(const Cache &c, int format, int d, const rec_query &q, int count);
 hipError_t launch_chosen(const Cache &c, int format, int d, const rec_query &q, const int32_t *chosen, int count, void *workspace, hipStream_t s);
+// Parts of the outputs, as rec_history_attend() has them where it divides histories; `most`: how many at most.
+struct Parts {
+    float *o;             // [parts][rows][head_dim]
+    float *ml;            // [parts][rows]: a maximum's exponent and a sum
+};
+int own_parts(const Cache &c, int format, int d, const rec_query &q, int most);
+hipError_t launch_own_parts(const Cache &c, int format, int d, const rec_query &q, int most, const Parts &to, hipStream_t s);
+struct Prefix {
+    const int32_t *pages;
+    int width;
+    const int32_t *length;
+};
+long long shared_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
+size_t shared_workspace(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
+hipError_t launch_shared(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s);
 hipError_t launch_means(const Cache &c, int format, int d, const int32_t *which, int pages, void *means, hipStream_t s);
 long long means_threads(const Cache &c, int d, int pages);
 struct Select {

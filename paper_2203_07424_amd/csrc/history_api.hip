@@ -1,4 +1,5 @@
 // Host side of include/rec_history.h: checks, and nothing else.
+#include <algorithm>
 #include <utility>
 
 #include "history.h"
@@ -98,6 +99,19 @@ rec_status check_chosen(const rec_history *h, const rec_query *q, int32_t count)
     if (count < 1) return REC_ERR_ARG;
     if ((int64_t)count * h->page_tokens > MOST_TOKENS) return REC_ERR_OVERFLOW;
     return rec::hist::chosen_threads(cache_of(h), h->format, h->head_dim, *q, count) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
+}
+
+rec_status check_shared(const rec_history *h, const rec_query *q, int32_t prefix_width)
+{
+    const rec_status st = check_unmasked(h, q);
+    if (st != REC_OK) return st;
+    if (prefix_width < 0) return REC_ERR_ARG;
+    if ((int64_t)prefix_width * h->page_tokens > MOST_TOKENS) return REC_ERR_OVERFLOW;
+    const Cache c = cache_of(h);
+    return std::max(rec::hist::attend_threads(c, h->format, h->head_dim, *q), rec::hist::shared_threads(c, h->format, h->head_dim, *q, prefix_width)) >
+                   MOST_THREADS
+               ? REC_ERR_OVERFLOW
+               : REC_OK;
 }
 
 // What a query that has something to do points to, but for its results.
@@ -233,6 +247,27 @@ rec_status rec_history_attend_selected(const rec_history *h, const rec_query *q,
     const Cache c = cache_of(h);
     if (!workspace_fits(rec::hist::chosen_workspace(c, h->format, h->head_dim, *q, count), dev_workspace, workspace_bytes)) return REC_ERR_ARG;
     return status_of(rec::hist::launch_chosen(c, h->format, h->head_dim, *q, dev_chosen, count, dev_workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t rec_history_attend_shared_workspace_bytes(const rec_history *h, const rec_query *q, int32_t prefix_width)
+{
+    return check_shared(h, q, prefix_width) != REC_OK ? 0 : rec::hist::shared_workspace(cache_of(h), h->format, h->head_dim, *q, prefix_width);
+}
+
+rec_status rec_history_attend_shared(const rec_history *h, const rec_query *q, const int32_t *dev_prefix_pages, int32_t prefix_width,
+                                     const int32_t *dev_prefix_length, void *dev_workspace, size_t workspace_bytes, void *stream)
+{
+    const rec_status st = check_shared(h, q, prefix_width);
+    if (st != REC_OK) return st;
+    if (!aligned(h->dev_pages) || !words_fit(h->dev_fault, 8)) return REC_ERR_ARG;
+    if (q->batch == 0 || q->queries == 0) return REC_OK;
+    if (!query_fits(q) || !aligned(q->dev_out) || (prefix_width && !dev_prefix_pages) || !words_fit(dev_prefix_pages, 4) || !dev_prefix_length ||
+        !words_fit(dev_prefix_length, 4))
+        return REC_ERR_ARG;
+    const Cache c = cache_of(h);
+    if (!workspace_fits(rec::hist::shared_workspace(c, h->format, h->head_dim, *q, prefix_width), dev_workspace, workspace_bytes)) return REC_ERR_ARG;
+    const rec::hist::Prefix prefix = {dev_prefix_pages, prefix_width, dev_prefix_length};
+    return status_of(rec::hist::launch_shared(c, h->format, h->head_dim, *q, prefix, dev_workspace, static_cast<hipStream_t>(stream)));
 }
 
 rec_status rec_window_attend(const rec_window *w, void *stream)

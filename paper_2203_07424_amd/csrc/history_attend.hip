@@ -391,6 +391,7 @@ struct Plan {
     int waves, splits, row_tiles, per;
     int heads;       // kv heads of a wave
     long long rows;  // of the whole call
+    bool join = true;  // parts become results
 };
 
 // two_heads: a wave may have two kv heads.
@@ -441,7 +442,7 @@ hipError_t attend_as(const AttendArgs &a, const Plan &p, hipStream_t s)
     else if (p.waves == 2) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 2, 1, CHOSEN>), grid, dim3(128), 0, s, a);
     else hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 1, CHOSEN>), grid, dim3(64), 0, s, a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.splits == 1) return e;
+    if (e != hipSuccess || p.splits == 1 || !p.join) return e;
     hipLaunchKernelGGL((combine_kernel<D, BF>), dim3((unsigned)p.rows), dim3(256), 0, s, a.part_o, a.part_ml, p.splits, p.rows, a.q.dev_out);
     return hipGetLastError();
 }
@@ -500,7 +501,26 @@ Plan chosen_plan_of(const Cache &c, int format, int d, const rec_query &q, int c
     return plan_of(c, format, d, one, false);
 }
 
+Plan own_plan_of(const Cache &c, int format, int d, const rec_query &q, int most)
+{
+    Plan p = plan_of(c, format, d, q);
+    p.splits = std::min(p.splits, most);
+    p.join = false;
+    return p;
+}
+
 }  // namespace
+
+int own_parts(const Cache &c, int format, int d, const rec_query &q, int most) { return own_plan_of(c, format, d, q, most).splits; }
+
+hipError_t launch_own_parts(const Cache &c, int format, int d, const rec_query &q, int most, const Parts &to, hipStream_t s)
+{
+    const Plan p = own_plan_of(c, format, d, q, most);
+    AttendArgs a = args_of(c, d, q, p, to.o);
+    a.part_ml = reinterpret_cast<f32x2 *>(to.ml);
+    a.parted = true;
+    return attend_any(a, p, format, d, s);
+}
 
 long long attend_threads(const Cache &c, int format, int d, const rec_query &q) { return threads_of(c, q, plan_of(c, format, d, q)); }
 

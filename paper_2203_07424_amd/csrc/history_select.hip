@@ -384,7 +384,7 @@ SelectArgs args_of(const Cache &c, const rec_query &q)
     a.walks = (tiles + a.each - 1) / a.each;
     a.walks = a.walks < 1 ? 1 : a.walks;
     a.by_walks = Divider(a.walks);
-    a.by_query_tiles = Divider(a.query_tiles);
+    a.by_query_tiles = Divider(std::max(a.query_tiles, 1));
     a.by_heads = Divider(c.kv_heads);
     return a;
 }
