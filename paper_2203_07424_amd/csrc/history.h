@@ -98,13 +98,13 @@ hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, 
 long long chosen_threads(const Cache &c, int format, int d, const rec_query &q, int count);
 size_t chosen_workspace(const Cache &c, int format, int d, const rec_query &q, int count);
 hipError_t launch_chosen(const Cache &c, int format, int d, const rec_query &q, const int32_t *chosen, int count, void *workspace, hipStream_t s);
-// Parts of the outputs, as rec_history_attend() has them where it divides histories; `most`: how many at most.
+// Sums of rows in parts, [parts][rows][head_dim], and for each a maximum's exponent and the weights' sum, [parts][rows][2].
 struct Parts {
-    float *o;             // [parts][rows][head_dim]
-    float *ml;            // [parts][rows]: a maximum's exponent and a sum
+    float *o, *ml;
 };
-int own_parts(const Cache &c, int format, int d, const rec_query &q, int most);
-hipError_t launch_own_parts(const Cache &c, int format, int d, const rec_query &q, int most, const Parts &to, hipStream_t s);
+int own_parts(const Cache &c, int format, int d, const rec_query &q);
+// Histories behind `before` parts: results if own_parts() is 1, else that many parts more.
+hipError_t launch_behind(const Cache &c, int format, int d, const rec_query &q, const Parts &parts, int before, hipStream_t s);
 struct Prefix {
     const int32_t *pages;
     int width;

@@ -64,7 +64,27 @@ struct AttendArgs {
     const int32_t *chosen;  // [q.batch][kv_heads][width] pages of the history, or -1
     int width, queries;
     Divider by_queries;
+    // Histories behind a prefix: their rows' sums over it, which results include.
+    int before;            // parts of it
+    const float *before_o;
+    const f32x2 *before_ml;
 };
+
+// What a launch attends to: histories, pages of them that were chosen, histories behind a prefix.
+enum { WHOLE, CHOSEN, BEHIND };
+
+// Joins a row's sums, weights' sum l and maximum's exponent m with those of a part: x's columns of all of them.
+template <int N>
+__device__ inline void add_part(f32x4 (&x)[N], float &l, float &m, const float *part, int stride, f32x2 ml)
+{
+    const float most = fmaxf(m, ml[0]);
+    const float mine = m == neg_inf() ? (l == 0.0f ? 0.0f : l) : __builtin_amdgcn_exp2f(m - most);
+    const float its = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - most);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = x[i] * mine + *reinterpret_cast<const f32x4 *>(part + stride * i) * its;
+    l = l * mine + ml[1] * its;
+    m = most;
+}
 
 // Where a wave's row goes.
 __device__ inline long long out_row(const AttendArgs &a, int b, int kv, int row)
@@ -73,12 +93,12 @@ __device__ inline long long out_row(const AttendArgs &a, int b, int kv, int row)
     return ((long long)b * a.q.queries + i) * a.q.heads + kv * a.per + (row - i * a.per);
 }
 
-// CHOSEN: tokens are those of the chosen pages, one page after the other, and all rows stand at one position.
-template <int FMT, int D, bool BF, int W, int HEADS, bool CHOSEN>
+// KIND CHOSEN: tokens are those of the chosen pages, one page after the other, and all rows stand at one position.
+template <int FMT, int D, bool BF, int W, int HEADS, int KIND>
 __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_kernel(AttendArgs a)
 {
     static_assert(HEADS == 1 || W == 1, "several heads a wave: only where there are waves enough");
-    static_assert(HEADS == 1 || !CHOSEN, "every kv head has pages of its own");
+    static_assert(HEADS == 1 || KIND != CHOSEN, "every kv head has pages of its own");
     constexpr int SLOT = ROWS / HEADS;  // rows of a kv head
     using T = std::conditional_t<BF, __bf16, _Float16>;
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
@@ -89,7 +109,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
     const int row_tile = a.splits == 1 ? part : part / a.splits, split = part - row_tile * a.splits;
 
     const int shift = a.c.page_shift, most_tokens = a.q.table_width << shift;
-    const int history = CHOSEN ? a.by_queries.of(b) : b, query_of_history = b - history * a.queries;  // the latter for chosen pages
+    const int history = KIND == CHOSEN ? a.by_queries.of(b) : b, query_of_history = b - history * a.queries;  // the latter for chosen pages
     int len = a.q.dev_lengths[history];
     if (len < 0 || len > most_tokens) {
         if (threadIdx.x == 0 && first_kv == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)history);
@@ -100,7 +120,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
     const bool real = first_row + r <= last_row;
     const bool together = a.q.candidates != 0;
     auto position = [&](int row) {
-        if constexpr (CHOSEN) return together ? len - 1 : max(len - a.queries + query_of_history, -1);
+        if constexpr (KIND == CHOSEN) return together ? len - 1 : max(len - a.queries + query_of_history, -1);
         else return together ? len - 1 : max(len - a.q.queries + a.by_per.of(row), -1);
     };
     const int p_lo = position(first_row), p_hi = position(last_row), pos = position(row);
@@ -109,9 +129,9 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
     // Tiles that some row sees something of: [0, n_sink) and [n_from, n_to).
     int n_from = 0, n_sink = 0, n_to = 0;
     if (p_hi >= 0) {
-        n_to = CHOSEN ? (int)((((long long)a.width << shift) + TILE - 1) / TILE) : p_hi / TILE + 1;
-        if constexpr (!CHOSEN) n_from = max(p_lo - window + 1, 0) / TILE;
-        if constexpr (!CHOSEN) n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from);
+        n_to = KIND == CHOSEN ? (int)((((long long)a.width << shift) + TILE - 1) / TILE) : p_hi / TILE + 1;
+        if constexpr (KIND != CHOSEN) n_from = max(p_lo - window + 1, 0) / TILE;
+        if constexpr (KIND != CHOSEN) n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from);
     }
     const int tiles = n_sink + n_to - n_from, each = (tiles + a.splits - 1) / a.splits;
     const int begin = min(split * each, tiles), end = min(begin + each, tiles);
@@ -127,11 +147,11 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
 
     if (begin + wave < end) {
         const int query = a.by_per.of(row), head = kv * a.per + row - query * a.per;
-        const long long row_bytes = 2 * (history * a.q.batch_stride + (CHOSEN ? query_of_history : query) * a.q.query_stride + head * a.q.head_stride);
+        const long long row_bytes = 2 * (history * a.q.batch_stride + (KIND == CHOSEN ? query_of_history : query) * a.q.query_stride + head * a.q.head_stride);
         // Positive, so that masked scores stay at -inf.
         const float factor = a.q.scale == 0.0f ? 1.0f : __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
         const int32_t *table = a.q.dev_pages_of + history * a.q.table_stride;
-        const int32_t *chosen = a.chosen + (CHOSEN ? ((long long)b * a.c.kv_heads + first_kv) * a.width : 0);
+        const int32_t *chosen = a.chosen + (KIND == CHOSEN ? ((long long)b * a.c.kv_heads + first_kv) * a.width : 0);
         const int groups = 1 << (shift - 4);
         const int head_bytes = groups * group_bytes<FMT>(D);
         const unsigned char *first_page = a.c.pages + (long long)first_kv * head_bytes;
@@ -153,7 +173,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
         };
         auto page_of = [&](int token) {
             int page = -1;
-            if constexpr (CHOSEN) page = page_at(number_of(token));
+            if constexpr (KIND == CHOSEN) page = page_at(number_of(token));
             else if (token < len) page = table[token >> shift];
             return page;
         };
@@ -164,8 +184,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
         };
 
         int n = begin + wave, key = key_of(n);
-        int k_page = page_of(key + 16 * (c >> 2)), v_number = CHOSEN ? number_of(key + 16 * g) : 0;
-        int v_page = CHOSEN ? page_at(v_number) : page_of(key + 16 * g);
+        int k_page = page_of(key + 16 * (c >> 2)), v_number = KIND == CHOSEN ? number_of(key + 16 * g) : 0;
+        int v_page = KIND == CHOSEN ? page_at(v_number) : page_of(key + 16 * g);
         Query<D, BF> q;
         q.fetch(real ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr, g);
         Tile<FMT, D> tile[HEADS];
@@ -176,8 +196,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
 #pragma unroll
         for (int h = 0; h < HEADS; ++h) load_values(h, v_page, key);
         k_page = n + W < end ? page_of(key_of(n + W) + 16 * (c >> 2)) : -1;
-        int v_number_next = CHOSEN && n + W < end ? number_of(key_of(n + W) + 16 * g) : -1;
-        int v_next = n + W >= end ? -1 : CHOSEN ? page_at(v_number_next) : page_of(key_of(n + W) + 16 * g);
+        int v_number_next = KIND == CHOSEN && n + W < end ? number_of(key_of(n + W) + 16 * g) : -1;
+        int v_next = n + W >= end ? -1 : KIND == CHOSEN ? page_at(v_number_next) : page_of(key_of(n + W) + 16 * g);
         q.convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);  // while the first tile is on its way
         for (;; n += W) {
             const bool more = n + W < end;
@@ -198,8 +218,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
             // Groups come with their page or not at all.
             const bool there = (unsigned)v_page < pages;
             // Where group g's tokens stand in the history.
-            const int first = CHOSEN ? (v_number << shift) + ((key + 16 * g) & ((1 << shift) - 1)) : key + 16 * g;
-            bool whole = CHOSEN ? __all(there && first + 15 <= p_hi) : key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there);
+            const int first = KIND == CHOSEN ? (v_number << shift) + ((key + 16 * g) & ((1 << shift) - 1)) : key + 16 * g;
+            bool whole = KIND == CHOSEN ? __all(there && first + 15 <= p_hi) : key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there);
             unsigned nan = 0;  // bit 4 h + b: row c sees a NaN in block b of head h's values
             if (!whole) {
                 // Bit t: row c sees token t of group g; some row does.
@@ -208,13 +228,13 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
                 unsigned seen = upto(pos) & (~before(pos) | below(sinks - first));
                 unsigned used = upto(p_hi) & (~before(p_lo) | below(sinks - first));
                 if (!there) {
-                    if constexpr (CHOSEN) {
+                    if constexpr (KIND == CHOSEN) {
                         used = (unsigned)v_number < (unsigned)a.q.table_width && v_number << shift <= p_hi;
                         if (!used && v_number != -1 && (unsigned)v_number >= (unsigned)a.q.table_width && c == 0)
                             report(a.c.fault, REC_FAULT_SLOT, (unsigned long long)(chosen - a.chosen + ((key + 16 * g) >> shift)));
                     }
                     if (used && c == 0)
-                        report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)history * (unsigned)a.q.table_width + (unsigned)(CHOSEN ? v_number : first >> shift));
+                        report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)history * (unsigned)a.q.table_width + (unsigned)(KIND == CHOSEN ? v_number : first >> shift));
                     seen = used = 0;
                 }
                 saw |= seen;
@@ -305,7 +325,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
             v_number = v_number_next;
             if (n + 2 * W < end) {
                 k_page = page_of(key_of(n + 2 * W) + 16 * (c >> 2));
-                if constexpr (CHOSEN) {
+                if constexpr (KIND == CHOSEN) {
                     v_number_next = number_of(key_of(n + 2 * W) + 16 * g);
                     v_next = page_at(v_number_next);
                 } else {
@@ -338,7 +358,10 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
                 for (int i = 0; i < D / 16; ++i)
                     *reinterpret_cast<f32x4 *>(a.part_o + (split * all_rows + out) * D + 16 * i + 4 * g) = o[i];
         } else if (real) {
-            const float by = inverse(l, sum.m);
+            float m = sum.m, total = l;
+            if constexpr (KIND == BEHIND)
+                for (int i = 0; i < a.before; ++i) add_part(o, total, m, a.before_o + (i * all_rows + out) * D + 4 * g, 16, a.before_ml[i * all_rows + out]);
+            const float by = inverse(total, m);
             typedef T tx4 __attribute__((ext_vector_type(4)));
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
@@ -377,6 +400,12 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
                 if (col == 0) a.part_ml[split * all_rows + to] = f32x2{m, l};
             } else {
                 typedef T tx8 __attribute__((ext_vector_type(8)));
+                if constexpr (KIND == BEHIND) {
+                    f32x4 both[2] = {x, y};
+                    for (int i = 0; i < a.before; ++i) add_part(both, l, m, a.before_o + (i * all_rows + to) * D + col, 4, a.before_ml[i * all_rows + to]);
+                    x = both[0];
+                    y = both[1];
+                }
                 const float by = inverse(l, m);
                 x *= by;
                 y *= by;
@@ -429,18 +458,18 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, bool two_hea
     return p;
 }
 
-template <int FMT, int D, bool BF, bool CHOSEN>
+template <int FMT, int D, bool BF, int KIND>
 hipError_t attend_as(const AttendArgs &a, const Plan &p, hipStream_t s)
 {
     const dim3 grid((unsigned)((long long)a.q.batch * a.c.kv_heads / p.heads * p.row_tiles * p.splits));
-    if constexpr (D <= 64 && !CHOSEN)
+    if constexpr (D <= 64 && KIND != CHOSEN)
         if (p.heads == 2) {
-            hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 2, false>), grid, dim3(64), 0, s, a);
+            hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 2, KIND>), grid, dim3(64), 0, s, a);
             return hipGetLastError();
         }
-    if (p.waves == 4) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 4, 1, CHOSEN>), grid, dim3(256), 0, s, a);
-    else if (p.waves == 2) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 2, 1, CHOSEN>), grid, dim3(128), 0, s, a);
-    else hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 1, CHOSEN>), grid, dim3(64), 0, s, a);
+    if (p.waves == 4) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 4, 1, KIND>), grid, dim3(256), 0, s, a);
+    else if (p.waves == 2) hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 2, 1, KIND>), grid, dim3(128), 0, s, a);
+    else hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 1, KIND>), grid, dim3(64), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1 || !p.join) return e;
     hipLaunchKernelGGL((combine_kernel<D, BF>), dim3((unsigned)p.rows), dim3(256), 0, s, a.part_o, a.part_ml, p.splits, p.rows, a.q.dev_out);
@@ -450,8 +479,10 @@ hipError_t attend_as(const AttendArgs &a, const Plan &p, hipStream_t s)
 template <int FMT, int D>
 hipError_t attend_of(const AttendArgs &a, const Plan &p, hipStream_t s)
 {
-    if (a.chosen) return a.q.dtype == REC_BF16 ? attend_as<FMT, D, true, true>(a, p, s) : attend_as<FMT, D, false, true>(a, p, s);
-    return a.q.dtype == REC_BF16 ? attend_as<FMT, D, true, false>(a, p, s) : attend_as<FMT, D, false, false>(a, p, s);
+    const bool bf = a.q.dtype == REC_BF16;
+    if (a.chosen) return bf ? attend_as<FMT, D, true, CHOSEN>(a, p, s) : attend_as<FMT, D, false, CHOSEN>(a, p, s);
+    if (a.before) return bf ? attend_as<FMT, D, true, BEHIND>(a, p, s) : attend_as<FMT, D, false, BEHIND>(a, p, s);
+    return bf ? attend_as<FMT, D, true, WHOLE>(a, p, s) : attend_as<FMT, D, false, WHOLE>(a, p, s);
 }
 
 hipError_t attend_any(const AttendArgs &a, const Plan &p, int format, int d, hipStream_t s)
@@ -478,6 +509,7 @@ AttendArgs args_of(const Cache &c, int d, const rec_query &q, const Plan &p, voi
     a.parted = p.splits > 1;
     a.chosen = nullptr;
     a.width = a.queries = 0;
+    a.before = 0;
     return a;
 }
 
@@ -501,24 +533,20 @@ Plan chosen_plan_of(const Cache &c, int format, int d, const rec_query &q, int c
     return plan_of(c, format, d, one, false);
 }
 
-Plan own_plan_of(const Cache &c, int format, int d, const rec_query &q, int most)
-{
-    Plan p = plan_of(c, format, d, q);
-    p.splits = std::min(p.splits, most);
-    p.join = false;
-    return p;
-}
-
 }  // namespace
 
-int own_parts(const Cache &c, int format, int d, const rec_query &q, int most) { return own_plan_of(c, format, d, q, most).splits; }
+int own_parts(const Cache &c, int format, int d, const rec_query &q) { return plan_of(c, format, d, q).splits; }
 
-hipError_t launch_own_parts(const Cache &c, int format, int d, const rec_query &q, int most, const Parts &to, hipStream_t s)
+hipError_t launch_behind(const Cache &c, int format, int d, const rec_query &q, const Parts &parts, int before, hipStream_t s)
 {
-    const Plan p = own_plan_of(c, format, d, q, most);
-    AttendArgs a = args_of(c, d, q, p, to.o);
-    a.part_ml = reinterpret_cast<f32x2 *>(to.ml);
-    a.parted = true;
+    Plan p = plan_of(c, format, d, q);
+    p.join = false;
+    const long long at = before * p.rows;
+    AttendArgs a = args_of(c, d, q, p, parts.o + at * d);
+    a.part_ml = reinterpret_cast<f32x2 *>(parts.ml) + at;
+    a.before = p.splits > 1 ? 0 : before;
+    a.before_o = parts.o;
+    a.before_ml = reinterpret_cast<const f32x2 *>(parts.ml);
     return attend_any(a, p, format, d, s);
 }
 

@@ -1,9 +1,12 @@
 // Attention of many histories that begin with the same tokens.
 //
-// prefix_kernel: the rows of all histories' queries against the shared tokens.  A wave has RT tiles of 16 rows of a kv
-// head, so that a tile of 64 keys and values is loaded, and its values made into bf16, once for all of them; its four
-// neighbours in the block have the same rows and other keys, and meet it in LDS.  The products are those of history_attend.hip.
-// attend_kernel has what each history holds of its own, as parts, and combine_kernel joins both.
+// The rows of all histories' queries against the shared tokens are large products, those of history_attend.hip.
+// wide_kernel: a block has 128 rows of a kv head or more, four waves of RT tiles of 16, and two such groups of waves, which
+// have every other tile of keys and meet in LDS in the end.  The four waves of a group share a tile's values: each makes a
+// quarter of them into bf16, in the order of the operands, in LDS, while the tile before is multiplied.  Keys go into the products as they are stored.
+// narrow_kernel: one tile of 16 rows, whose keys four waves share.
+//
+// What that leaves are parts of the rows' sums; attend_kernel joins them with what each history holds of its own.
 #include <algorithm>
 
 #include "history_attend_body.h"
@@ -12,13 +15,8 @@ namespace rec {
 namespace hist {
 namespace {
 
-constexpr int WAVES = 4;
 constexpr int CUS = 256;
-constexpr int MOST_PARTS = 64;  // of a row, of which half may be the prefix's
-
-// Row tiles of a wave, and waves that a SIMD holds at once: as many as its registers hold.
-__host__ __device__ constexpr int row_tiles_of(int d, bool bf) { return d == 128 ? 2 : d == 64 ? (bf ? 3 : 2) : 4; }
-__host__ __device__ constexpr int waves_of(int format, int d, bool bf) { return d == 128 && !(format == REC_MX4 && bf) ? 1 : 2; }
+constexpr int MOST_PARTS = 32;  // of the prefix
 
 struct SharedArgs {
     Cache c;
@@ -33,9 +31,9 @@ struct SharedArgs {
 };
 
 template <int FMT, int D, bool BF>
-__global__ __launch_bounds__(64 * WAVES, waves_of(FMT, D, BF)) void prefix_kernel(SharedArgs a)
+__global__ __launch_bounds__(256) void narrow_kernel(SharedArgs a)
 {
-    constexpr int RT = row_tiles_of(D, BF), W = WAVES;
+    constexpr int RT = 1, W = 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     // Blocks of one kv head are kv_heads apart: they have its keys and values in one L2 where that divides the XCDs.
     const int rest = a.by_heads.of((int)blockIdx.x), kv = (int)blockIdx.x - rest * a.c.kv_heads;
@@ -243,8 +241,296 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(FMT, D, BF)) void prefix_kerne
     }
 }
 
+// Row tiles of a wave: as many as 256 registers hold.
+__host__ __device__ constexpr int row_tiles_of(int d, bool bf)
+{
+    return d == 32 ? (bf ? 4 : 3) : d == 64 ? (bf ? 3 : 2) : bf ? 2 : 1;
+}
+constexpr int ROW_WAVES = 4, GROUPS = 2;  // of a block
+
+// This lane's codes and scales of one block of 32 columns of a tile's values.
+template <int FMT, int D>
+__device__ inline void load_block(Tile<FMT, 32> &t, const unsigned char *vg, int b, int c)
+{
+    constexpr int CB = code_bytes<FMT>(D), WIDE = Tile<FMT, 32>::WIDE;
+    const unsigned char *vp = vg + GROUP * CB + (b * GROUP + c) * GROUP * WIDE;
+#pragma unroll
+    for (int w = 0; w < WIDE; ++w) t.v[0][w] = *reinterpret_cast<const u32x4 *>(vp + 16 * w);
+    t.vs[0] = *reinterpret_cast<const u32x4 *>(vg + 2 * GROUP * CB + GROUP * (D / BLOCK) + b * GROUP);
+}
+
+// Tokens that are not `seen` become zeros, whatever their bytes are.
+template <int FMT>
+__device__ inline void hide(Tile<FMT, 32> &t, unsigned seen)
+{
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const unsigned keep = bytes_of(seen >> (4 * x) & 15u);
+        t.vs[0][x] &= keep;
+        if constexpr (FMT == REC_MX8) {
+            t.v[0][x >> 1][2 * (x & 1)] &= __builtin_amdgcn_perm(keep, keep, 0x01010000u);
+            t.v[0][x >> 1][2 * (x & 1) + 1] &= __builtin_amdgcn_perm(keep, keep, 0x03030202u);
+        }
+    }
+}
+
+template <int FMT, int D, bool BF>
+__global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(SharedArgs a)
+{
+    constexpr int RT = row_tiles_of(D, BF), TERMS = BF ? 1 : 2;
+    constexpr int VALUES = D * TILE / 8, SUMS = ROW_WAVES * RT * (D / 16) * 64;  // 16 bytes each: a tile's values, a group's sums
+    __shared__ u32x4 lds[GROUPS * 2 * VALUES > SUMS ? GROUPS * 2 * VALUES : SUMS];
+    __shared__ f32x2 ml_of[ROW_WAVES][RT][ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int part_of_rows = wave % ROW_WAVES, group = wave / ROW_WAVES;
+    // Blocks of one kv head are kv_heads apart: they have its keys and values in one L2 where that divides the XCDs.
+    const int rest = a.by_heads.of((int)blockIdx.x), kv = (int)blockIdx.x - rest * a.c.kv_heads;
+    const int row_block = a.by_splits.of(rest), split = rest - row_block * a.splits;
+    const int first_row = (row_block * ROW_WAVES + part_of_rows) * RT * ROWS;
+
+    const int shift = a.c.page_shift, most_tokens = a.prefix.width << shift;
+    int len = *a.prefix.length;
+    if (len < 0 || len > most_tokens) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)a.q.batch);
+        len = len < 0 ? 0 : most_tokens;
+    }
+    const int tiles = (len + TILE - 1) / TILE, each = (tiles + a.splits - 1) / a.splits;
+    const int begin = min(split * each, tiles), end = min(begin + each, tiles);
+
+    f32x4 o[RT][D / 16], l[RT];
+    float m[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[t][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        l[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        m[t] = neg_inf();
+    }
+    unsigned saw = 0;  // not 0: this wave's rows have seen a key
+
+    // Positive, so that masked scores stay at -inf.
+    const float factor = a.q.scale == 0.0f ? 1.0f : __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
+    const int groups = 1 << (shift - 4), head_bytes = groups * group_bytes<FMT>(D);
+    const unsigned char *first_page = a.c.pages + (long long)kv * head_bytes;
+    const unsigned page_bytes = (unsigned)(a.c.kv_heads * head_bytes);
+    const unsigned pages = (unsigned)min(a.c.num_pages, 1ll << 31);
+    auto page_of = [&](int n, int in_tile) {
+        int page = -1;
+        if (n < end && n * TILE + in_tile < len) page = a.prefix.pages[(n * TILE + in_tile) >> shift];
+        return page;
+    };
+    auto group_at = [&](int page, int token) {
+        const bool ok = (unsigned)page < pages;  // else some group that is there: its tokens count for nothing
+        const unsigned in_page = ok ? (unsigned)((token >> 4) & (groups - 1)) * group_bytes<FMT>(D) : 0u;
+        return first_page + ((unsigned long long)(ok ? (unsigned)page : 0u) * page_bytes + in_page);
+    };
+    // Bit t: token t of this lane's group of tile n is seen.
+    auto seen_of = [&](int n, int page) { return (unsigned)page < pages ? below(len - n * TILE - 16 * g) : 0u; };
+
+    // What this wave makes of a tile's values: both halves of a block of 32 columns, one of them, or nothing.
+    const int block = D == 128 ? part_of_rows : D == 64 ? part_of_rows >> 1 : 0;
+    u32x4 *const values = lds + group * 2 * VALUES;
+    Tile<FMT, 32> made;
+    auto load_made = [&](int n, int page) { load_block<FMT, D>(made, group_at(page, n * TILE + 16 * g), block, c); };
+    auto make = [&](unsigned seen, bool whole, int buffer) {
+        if (!whole) hide<FMT>(made, seen);
+        u32x4 *to = values + buffer * VALUES + block * 4 * 64 + lane;
+        auto half = [&](auto h) {
+            u32x4 lo, hi;
+            value_operands<FMT, 32, h()>(made, 0, lo, hi);
+            to[(2 * h()) * 64] = lo;
+            to[(2 * h() + 1) * 64] = hi;
+        };
+        if (D == 128 || (part_of_rows & 1) == 0) half(std::integral_constant<int, 0>());
+        if (D == 128 || (part_of_rows & 1) == 1) half(std::integral_constant<int, 1>());
+    };
+
+    int n = begin + group;
+    int page = page_of(n, 16 * g), page_next = page_of(n + GROUPS, 16 * g);
+    int k_page = page_of(n, 16 * (c >> 2)), k_next = page_of(n + GROUPS, 16 * (c >> 2));
+    Tile<FMT, D> tile;  // keys only
+    Query<D, BF> q[RT];
+    load_made(n, page);
+    tile.load_keys(group_at(k_page, n * TILE + 16 * (c >> 2)), c, g);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int row = first_row + t * ROWS + c;
+        const char *from = nullptr;
+        if (row < a.rows) {
+            const int at = a.by_per.of(row), b = a.by_queries.of(at);
+            from = static_cast<const char *>(a.q.dev_q) + 2 * (b * a.q.batch_stride + (at - b * a.q.queries) * a.q.query_stride + (kv * a.per + row - at * a.per) * a.q.head_stride);
+        }
+        q[t].fetch(from, g);
+    }
+    // The weights of the tile before, and its values: none yet.
+    u32x4 w[RT][TERMS][2];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) w[t][k][0] = w[t][k][1] = u32x4{0u, 0u, 0u, 0u};
+    for (int i = threadIdx.x % (64 * ROW_WAVES); i < VALUES; i += 64 * ROW_WAVES) values[VALUES + i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int t = 0; t < RT; ++t) q[t].convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);
+    __syncthreads();
+
+    // o += values of a buffer times w, and l the weights.
+    auto multiply = [&](int buffer) {
+        const u32x4 *from = values + buffer * VALUES + lane;
+        const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) l[t] = product(ones, w[t][k][h], l[t]);
+#pragma unroll
+        for (int i = 0; i < D / BLOCK; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 lo = from[(4 * i + 2 * h) * 64], hi = from[(4 * i + 2 * h + 1) * 64];
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) {
+                        o[t][2 * i] = product(lo, w[t][k][h], o[t][2 * i]);
+                        o[t][2 * i + 1] = product(hi, w[t][k][h], o[t][2 * i + 1]);
+                    }
+            }
+    };
+
+    // Each turn a group scores its next tile and multiplies the one before it, whose weights are ready: matrix instructions and
+    // exponentials that do not wait for each other.
+    const int turns = (end - begin + GROUPS - 1) / GROUPS;
+    for (int turn = 0; turn < turns; ++turn, n += GROUPS) {
+        const unsigned seen = seen_of(n, page);
+        const bool whole = __all(seen == 0xffffu);
+        saw |= seen;
+        f32x4 s[RT][4];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            s[t][0] = scores<FMT, D, BF, 0>(tile, q[t], g);
+            s[t][1] = scores<FMT, D, BF, 1>(tile, q[t], g);
+            s[t][2] = scores<FMT, D, BF, 2>(tile, q[t], g);
+            s[t][3] = scores<FMT, D, BF, 3>(tile, q[t], g);
+        }
+        make(seen, whole, turn & 1);
+        if (!whole) {
+            if (page != -1 && (unsigned)page >= pages && c == 0)
+                report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)a.q.batch * (unsigned)a.q.table_width + (unsigned)((n * TILE + 16 * g) >> shift));
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i & 3][i >> 2] = unless_hidden(s[t][i & 3][i >> 2], ~seen, i);
+        }
+        // The next tile's codes, and where the one's behind it are.
+        tile.load_keys(group_at(k_next, (n + GROUPS) * TILE + 16 * (c >> 2)), c, g);
+        load_made(n + GROUPS, page_next);
+        page = page_next;
+        page_next = page_of(n + 2 * GROUPS, 16 * g);
+        k_next = page_of(n + 2 * GROUPS, 16 * (c >> 2));
+
+        // A lane's own scores tell whether some row's maximum has to move.
+        float most[RT], down[RT];
+        bool moves = false;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            most[t] = neg_inf();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most[t] = fmaxf(most[t], s[t][i & 3][i >> 2]);
+            moves |= most[t] != neg_inf() && most[t] * factor > m[t] + (SLACK - ROOM);
+        }
+        moves = __any(moves);
+        if (moves)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                float x = fmaxf(most[t], __shfl_xor(most[t], 16));
+                x = fmaxf(x, __shfl_xor(x, 32));
+                x = x == neg_inf() ? x : x * factor;
+                const float up = x > m[t] + (SLACK - ROOM) ? fmaxf(m[t], x + ROOM) : m[t];
+                down[t] = m[t] == up ? 1.0f : m[t] == neg_inf() ? 0.0f : __builtin_amdgcn_exp2f(m[t] - up);
+                m[t] = up;
+            }
+        u32x4 w_next[RT][TERMS][2];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const float by = m[t] == neg_inf() ? 0.0f : m[t];
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i & 3][i >> 2], factor, -by));
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w_next[t][0][h][i] = pack(p[8 * h + 2 * i], p[8 * h + 2 * i + 1]);
+                    if constexpr (TERMS == 2) {
+                        const unsigned word = w_next[t][0][h][i];
+                        w_next[t][1][h][i] = pack(p[8 * h + 2 * i] - __builtin_bit_cast(float, word << 16),
+                                                  p[8 * h + 2 * i + 1] - __builtin_bit_cast(float, word & 0xffff0000u));
+                    }
+                }
+        }
+        multiply((turn + 1) & 1);
+        if (moves)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) o[t][i] *= down[t];
+                l[t] *= down[t];
+            }
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) w[t][k][h] = w_next[t][k][h];
+        __syncthreads();
+    }
+    multiply((turns + 1) & 1);
+    __syncthreads();
+    // All scores may be -inf, which is not the same as having none: the maximum tells.
+    saw |= (unsigned)__shfl_xor((int)saw, 16);
+    saw |= (unsigned)__shfl_xor((int)saw, 32);
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+        if (saw && m[t] == neg_inf() && l[t][0] == 0.0f) m[t] = LOWEST;
+
+    // The second group's sums join the first's.
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(lds) + part_of_rows * RT * (D / 16) * 64 + lane;
+    if (group == 1) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) sums[(t * (D / 16) + i) * 64] = o[t][i];
+            if (g == 0) ml_of[part_of_rows][t][c] = f32x2{m[t], l[t][0]};
+        }
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const long long all_rows = (long long)a.q.batch * a.q.queries * a.q.heads;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int row = first_row + t * ROWS + c;
+        if (row >= a.rows) break;
+        const int at = a.by_per.of(row), b = a.by_queries.of(at);
+        // A query before its history's first token sees nothing.
+        const bool sees = a.q.candidates || min(max(a.q.dev_lengths[b], 0), a.q.table_width << shift) - a.q.queries + at - b * a.q.queries >= 0;
+        const f32x2 ml = ml_of[part_of_rows][t][c];
+        const float most = fmaxf(m[t], ml[0]);
+        const float mine = m[t] == neg_inf() ? (l[t][0] == 0.0f ? 0.0f : l[t][0]) : __builtin_amdgcn_exp2f(m[t] - most);
+        const float its = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - most);
+        const long long to = split * all_rows + (long long)at * a.q.heads + kv * a.per + (row - at * a.per);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            const f32x4 x = o[t][i] * mine + sums[(t * (D / 16) + i) * 64] * its;
+            *reinterpret_cast<f32x4 *>(a.part_o + to * D + 16 * i + 4 * g) = sees ? x : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        if (g == 0) a.part_ml[to] = sees ? f32x2{most, l[t][0] * mine + ml[1] * its} : f32x2{neg_inf(), 0.0f};
+    }
+}
+
 struct Plan {
     long long rows;  // of the whole call
+    bool wide;
     int blocks;      // of rows and kv heads
     int splits, own;
 };
@@ -253,24 +539,37 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int prefix_w
 {
     Plan p;
     p.rows = (long long)q.batch * q.queries * q.heads;
-    const long long of_head = p.rows / c.kv_heads, rows = row_tiles_of(d, q.dtype == REC_BF16) * ROWS;
-    p.blocks = (int)((of_head + rows - 1) / rows * c.kv_heads);
-    p.own = own_parts(c, format, d, q, MOST_PARTS / 2);
-    const long long tiles = (((long long)prefix_width << c.page_shift) + TILE - 1) / TILE;
-    // As many parts of the prefix as are all at work at once, of two tiles a wave at least.
-    p.splits = (int)std::max(1ll, std::min({(long long)waves_of(format, d, q.dtype == REC_BF16) * CUS / std::max(p.blocks, 1), tiles / (2 * WAVES), (long long)MOST_PARTS / 2}));
+    const bool bf = q.dtype == REC_BF16;
+    const long long of_head = p.rows / c.kv_heads;
+    p.wide = of_head > 2 * ROWS;
+    const int per_block = p.wide ? row_tiles_of(d, bf) * ROW_WAVES * ROWS : ROWS;
+    p.blocks = (int)((of_head + per_block - 1) / per_block * c.kv_heads);
+    p.own = own_parts(c, format, d, q);
+    // Parts of the prefix: as many as end soonest, at what a block's start and end cost beside its tiles, where so many
+    // blocks work at once.
+    const long long tiles = (((long long)prefix_width << c.page_shift) + TILE - 1) / TILE, waves = p.wide ? GROUPS : 4, at_once = p.wide ? CUS : 2 * CUS;
+    long long best = 0;
+    p.splits = 1;
+    for (int s = 1; s <= MOST_PARTS; ++s) {
+        const long long each = (tiles + s - 1) / s, turns = (each + waves - 1) / waves, cost = (p.blocks * (long long)s + at_once - 1) / at_once * (turns + 6);
+        if (s == 1 || cost < best) {
+            best = cost;
+            p.splits = s;
+        }
+    }
     return p;
 }
 
 template <int FMT, int D, bool BF>
 hipError_t shared_as(const SharedArgs &a, const Plan &p, int format, hipStream_t s)
 {
-    hipLaunchKernelGGL((prefix_kernel<FMT, D, BF>), dim3((unsigned)(p.blocks * p.splits)), dim3(64 * WAVES), 0, s, a);
+    const dim3 grid((unsigned)(p.blocks * p.splits));
+    if (p.wide) hipLaunchKernelGGL((wide_kernel<FMT, D, BF>), grid, dim3(64 * ROW_WAVES * GROUPS), 0, s, a);
+    else hipLaunchKernelGGL((narrow_kernel<FMT, D, BF>), grid, dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const Parts own = {a.part_o + p.splits * p.rows * D, reinterpret_cast<float *>(a.part_ml + p.splits * p.rows)};
-    e = launch_own_parts(a.c, format, D, a.q, MOST_PARTS / 2, own, s);
-    if (e != hipSuccess) return e;
+    e = launch_behind(a.c, format, D, a.q, {a.part_o, reinterpret_cast<float *>(a.part_ml)}, p.splits, s);
+    if (e != hipSuccess || p.own == 1) return e;
     hipLaunchKernelGGL((combine_kernel<D, BF>), dim3((unsigned)p.rows), dim3(256), 0, s, a.part_o, a.part_ml, p.splits + p.own, p.rows, a.q.dev_out);
     return hipGetLastError();
 }
@@ -286,14 +585,14 @@ hipError_t shared_of(const SharedArgs &a, const Plan &p, int format, hipStream_t
 long long shared_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
 {
     const Plan p = plan_of(c, format, d, q, prefix_width);
-    return std::max((long long)p.blocks * p.splits * 64 * WAVES, p.rows * 256);
+    return std::max((long long)p.blocks * p.splits * 64 * ROW_WAVES * GROUPS, p.own == 1 ? 0 : p.rows * 256);
 }
 
 size_t shared_workspace(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
 {
     if (q.batch == 0 || q.queries == 0) return 0;
     const Plan p = plan_of(c, format, d, q, prefix_width);
-    return (size_t)(p.splits + p.own) * (size_t)p.rows * ((size_t)d * sizeof(float) + sizeof(f32x2));
+    return (size_t)(p.splits + (p.own == 1 ? 0 : p.own)) * (size_t)p.rows * ((size_t)d * sizeof(float) + sizeof(f32x2));
 }
 
 hipError_t launch_shared(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s)
@@ -311,7 +610,7 @@ hipError_t launch_shared(const Cache &c, int format, int d, const rec_query &q, 
     a.rows = (int)(p.rows / c.kv_heads);
     a.splits = p.splits;
     a.part_o = static_cast<float *>(workspace);
-    a.part_ml = reinterpret_cast<f32x2 *>(a.part_o + (p.splits + p.own) * p.rows * d);
+    a.part_ml = reinterpret_cast<f32x2 *>(a.part_o + (p.splits + (p.own == 1 ? 0 : p.own)) * p.rows * d);
     if (format == REC_MX4)
         return d == 32 ? shared_of<REC_MX4, 32>(a, p, format, s) : d == 64 ? shared_of<REC_MX4, 64>(a, p, format, s) : shared_of<REC_MX4, 128>(a, p, format, s);
     return d == 32 ? shared_of<REC_MX8, 32>(a, p, format, s) : d == 64 ? shared_of<REC_MX8, 64>(a, p, format, s) : shared_of<REC_MX8, 128>(a, p, format, s);
