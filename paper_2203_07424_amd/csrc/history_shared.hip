@@ -274,12 +274,35 @@ __device__ inline void hide(Tile<FMT, 32> &t, unsigned seen)
     }
 }
 
+// Pieces of 16 bytes of a key's codes.  A lane has one or two of each of its four keys: the one that it begins with.
+template <int FMT, int D>
+constexpr int PIECES = code_bytes<FMT>(D) / 16;
+template <int FMT, int D>
+__device__ inline int piece_of(int g) { return PIECES<FMT, D> == 1 ? 0 : PIECES<FMT, D> == 2 ? g & 1 : g; }
+
+// Step i of the x-th product of scores(), of a key's pieces and its scales `ks`, so that steps which wait for each other can be apart.
+template <int FMT, int D, bool BF, int X>
+__device__ inline void add_scores(f32x4 &r, const u32x4 (&k)[PIECES<FMT, D> == 8 ? 2 : 1], const unsigned (&ks)[D / BLOCK], const Query<D, BF> &q, int i, int g)
+{
+    constexpr int SW = D / BLOCK, AT = D == 32 ? X : D == 64 ? 2 * (X & 1) : 0;
+    i32x8 a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        a[j] = (int)k[0][j];
+        a[4 + j] = (int)k[PIECES<FMT, D> == 8 ? 1 : 0][j];
+    }
+    const int s = (int)(D == 32 ? ks[0] : D == 64 ? ks[(X >> 1) % SW] >> (8 * (g & 1)) : ks[X % SW] >> (8 * g));
+    if (i == 0) r = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    r = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.b[i], r, FMT == REC_MX4 ? 4 : 0, 0, AT, s, 0, q.scale[i]);
+}
+
 template <int FMT, int D, bool BF>
 __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(SharedArgs a)
 {
     constexpr int RT = row_tiles_of(D, BF), TERMS = BF ? 1 : 2;
     constexpr int VALUES = D * TILE / 8, SUMS = ROW_WAVES * RT * (D / 16) * 64;  // 16 bytes each: a tile's values, a group's sums
     __shared__ u32x4 lds[GROUPS * 2 * VALUES > SUMS ? GROUPS * 2 * VALUES : SUMS];
+    __shared__ u32x4 keys_of[GROUPS][PIECES<FMT, D>][4][16];  // a tile's keys: piece, product, lane % 16
     __shared__ f32x2 ml_of[ROW_WAVES][RT][ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int part_of_rows = wave % ROW_WAVES, group = wave / ROW_WAVES;
@@ -348,10 +371,35 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
     int n = begin + group;
     int page = page_of(n, 16 * g), page_next = page_of(n + GROUPS, 16 * g);
     int k_page = page_of(n, 16 * (c >> 2)), k_next = page_of(n + GROUPS, 16 * (c >> 2));
-    Tile<FMT, D> tile;  // keys only
+    // Keys' codes go to LDS as the products take them, once for the group; their scales are each wave's own.
+    unsigned ks[D / BLOCK];
+    auto load_keys = [&](int n, int page) {
+        constexpr int CB = code_bytes<FMT>(D), SW = D / BLOCK;
+        const unsigned char *from = group_at(page, n * TILE + 16 * (c >> 2));
+        const unsigned char *row = from + (4 * (c & 3) + g) * CB;  // lane group g brings the g-th product's
+#pragma unroll
+        for (int i = 0; i < (PIECES<FMT, D> + ROW_WAVES - 1) / ROW_WAVES; ++i) {
+            const int piece = i * ROW_WAVES + part_of_rows;
+            if (PIECES<FMT, D> % ROW_WAVES == 0 || piece < PIECES<FMT, D>)
+                __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)(row + 16 * piece),
+                                                 (__attribute__((address_space(3))) void *)&keys_of[group][piece][0][0], 16, 0, 0);
+        }
+        const unsigned char *scales = from + 2 * GROUP * CB + 4 * (c & 3) * SW;
+        if constexpr (SW == 1) {
+            ks[0] = *reinterpret_cast<const unsigned *>(scales);
+        } else if constexpr (SW == 2) {
+            const u32x2 x = *reinterpret_cast<const u32x2 *>(scales);
+            ks[0] = x[0];
+            ks[1] = x[1];
+        } else {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(scales);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ks[j] = x[j];
+        }
+    };
     Query<D, BF> q[RT];
     load_made(n, page);
-    tile.load_keys(group_at(k_page, n * TILE + 16 * (c >> 2)), c, g);
+    load_keys(n, k_page);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         const int row = first_row + t * ROWS + c;
@@ -368,69 +416,95 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int k = 0; k < TERMS; ++k) w[t][k][0] = w[t][k][1] = u32x4{0u, 0u, 0u, 0u};
-    for (int i = threadIdx.x % (64 * ROW_WAVES); i < VALUES; i += 64 * ROW_WAVES) values[VALUES + i] = u32x4{0u, 0u, 0u, 0u};
+    for (int i = part_of_rows * 64 + lane; i < VALUES; i += 64 * ROW_WAVES) values[VALUES + i] = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
     for (int t = 0; t < RT; ++t) q[t].convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);
+    // Loads that go to LDS are not among those that a barrier waits for.
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
 
-    // o += values of a buffer times w, and l the weights.
-    auto multiply = [&](int buffer) {
-        const u32x4 *from = values + buffer * VALUES + lane;
+    // o += values of a buffer times w, and l the weights.  A block's operands are on their way while the one before is multiplied.
+    u32x4 operand[2][4];
+    auto fetch = [&](int buffer, int i) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) operand[i & 1][x] = values[buffer * VALUES + (4 * i + x) * 64 + lane];
+    };
+    auto multiply = [&](int buffer) {  // block 0 is fetched
         const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int k = 0; k < TERMS; ++k)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) l[t] = product(ones, w[t][k][h], l[t]);
-#pragma unroll
-        for (int i = 0; i < D / BLOCK; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x4 lo = from[(4 * i + 2 * h) * 64], hi = from[(4 * i + 2 * h + 1) * 64];
+        for (int i = 0; i < D / BLOCK; ++i) {
+            if (i + 1 < D / BLOCK) fetch(buffer, i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i == 0)
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int k = 0; k < TERMS; ++k) {
-                        o[t][2 * i] = product(lo, w[t][k][h], o[t][2 * i]);
-                        o[t][2 * i + 1] = product(hi, w[t][k][h], o[t][2 * i + 1]);
+                    for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) l[t] = product(ones, w[t][k][h], l[t]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        o[t][2 * i] = product(operand[i & 1][2 * h], w[t][k][h], o[t][2 * i]);
+                        o[t][2 * i + 1] = product(operand[i & 1][2 * h + 1], w[t][k][h], o[t][2 * i + 1]);
                     }
-            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
 
-    // Each turn a group scores its next tile and multiplies the one before it, whose weights are ready: matrix instructions and
-    // exponentials that do not wait for each other.
+    // A turn has two halves.  In the first a group scores its next tile and multiplies the one before it, whose weights are
+    // ready, with all matrix instructions one after the other; in the second it makes weights of the scores.  The two groups, of each of
+    // which a SIMD has a wave, are half a turn apart, so that one's matrix instructions run beside the other's exponentials.
     const int turns = (end - begin + GROUPS - 1) / GROUPS;
+    fetch(1, 0);
+    if (group == 1) __syncthreads();
     for (int turn = 0; turn < turns; ++turn, n += GROUPS) {
         const unsigned seen = seen_of(n, page);
         const bool whole = __all(seen == 0xffffu);
         saw |= seen;
+        __builtin_amdgcn_s_setprio(1);  // before the other group's exponentials
+        u32x4 k[4][PIECES<FMT, D> == 8 ? 2 : 1];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int j = 0; j < (PIECES<FMT, D> == 8 ? 2 : 1); ++j) k[x][j] = keys_of[group][piece_of<FMT, D>(g) + 4 * j][x][c];
+        multiply((turn + 1) & 1);
         f32x4 s[RT][4];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            s[t][0] = scores<FMT, D, BF, 0>(tile, q[t], g);
-            s[t][1] = scores<FMT, D, BF, 1>(tile, q[t], g);
-            s[t][2] = scores<FMT, D, BF, 2>(tile, q[t], g);
-            s[t][3] = scores<FMT, D, BF, 3>(tile, q[t], g);
-        }
+        for (int i = 0; i < Query<D, BF>::STEPS; ++i)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                add_scores<FMT, D, BF, 0>(s[t][0], k[0], ks, q[t], i, g);
+                add_scores<FMT, D, BF, 1>(s[t][1], k[1], ks, q[t], i, g);
+                add_scores<FMT, D, BF, 2>(s[t][2], k[2], ks, q[t], i, g);
+                add_scores<FMT, D, BF, 3>(s[t][3], k[3], ks, q[t], i, g);
+            }
         make(seen, whole, turn & 1);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) asm volatile("" : "+v"(s[t][0]), "+v"(s[t][1]), "+v"(s[t][2]), "+v"(s[t][3]));  // else they are worked out where they are used
+        __builtin_amdgcn_s_setprio(0);
+        __syncthreads();
+
+        // The next tile's codes, and where the one's behind it are.
+        load_keys(n + GROUPS, k_next);
+        load_made(n + GROUPS, page_next);
+        const int page_now = page;
+        page = page_next;
+        page_next = page_of(n + 2 * GROUPS, 16 * g);
+        k_next = page_of(n + 2 * GROUPS, 16 * (c >> 2));
         if (!whole) {
-            if (page != -1 && (unsigned)page >= pages && c == 0)
+            if (page_now != -1 && (unsigned)page_now >= pages && c == 0)
                 report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)a.q.batch * (unsigned)a.q.table_width + (unsigned)((n * TILE + 16 * g) >> shift));
 #pragma unroll
             for (int t = 0; t < RT; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i & 3][i >> 2] = unless_hidden(s[t][i & 3][i >> 2], ~seen, i);
         }
-        // The next tile's codes, and where the one's behind it are.
-        tile.load_keys(group_at(k_next, (n + GROUPS) * TILE + 16 * (c >> 2)), c, g);
-        load_made(n + GROUPS, page_next);
-        page = page_next;
-        page_next = page_of(n + 2 * GROUPS, 16 * g);
-        k_next = page_of(n + 2 * GROUPS, 16 * (c >> 2));
-
         // A lane's own scores tell whether some row's maximum has to move.
-        float most[RT], down[RT];
+        float most[RT];
         bool moves = false;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
@@ -439,18 +513,19 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
             for (int i = 0; i < 16; ++i) most[t] = fmaxf(most[t], s[t][i & 3][i >> 2]);
             moves |= most[t] != neg_inf() && most[t] * factor > m[t] + (SLACK - ROOM);
         }
-        moves = __any(moves);
-        if (moves)
+        if (__any(moves))
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 float x = fmaxf(most[t], __shfl_xor(most[t], 16));
                 x = fmaxf(x, __shfl_xor(x, 32));
                 x = x == neg_inf() ? x : x * factor;
                 const float up = x > m[t] + (SLACK - ROOM) ? fmaxf(m[t], x + ROOM) : m[t];
-                down[t] = m[t] == up ? 1.0f : m[t] == neg_inf() ? 0.0f : __builtin_amdgcn_exp2f(m[t] - up);
+                const float down = m[t] == up ? 1.0f : m[t] == neg_inf() ? 0.0f : __builtin_amdgcn_exp2f(m[t] - up);
                 m[t] = up;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) o[t][i] *= down;
+                l[t] *= down;
             }
-        u32x4 w_next[RT][TERMS][2];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             const float by = m[t] == neg_inf() ? 0.0f : m[t];
@@ -461,31 +536,20 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    w_next[t][0][h][i] = pack(p[8 * h + 2 * i], p[8 * h + 2 * i + 1]);
+                    w[t][0][h][i] = pack(p[8 * h + 2 * i], p[8 * h + 2 * i + 1]);
                     if constexpr (TERMS == 2) {
-                        const unsigned word = w_next[t][0][h][i];
-                        w_next[t][1][h][i] = pack(p[8 * h + 2 * i] - __builtin_bit_cast(float, word << 16),
-                                                  p[8 * h + 2 * i + 1] - __builtin_bit_cast(float, word & 0xffff0000u));
+                        const unsigned word = w[t][0][h][i];
+                        w[t][1][h][i] = pack(p[8 * h + 2 * i] - __builtin_bit_cast(float, word << 16),
+                                             p[8 * h + 2 * i + 1] - __builtin_bit_cast(float, word & 0xffff0000u));
                     }
                 }
         }
-        multiply((turn + 1) & 1);
-        if (moves)
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) o[t][i] *= down[t];
-                l[t] *= down[t];
-            }
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int k = 0; k < TERMS; ++k)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) w[t][k][h] = w_next[t][k][h];
+        fetch(turn & 1, 0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     }
     multiply((turns + 1) & 1);
+    if (group == 0) __syncthreads();
     __syncthreads();
     // All scores may be -inf, which is not the same as having none: the maximum tells.
     saw |= (unsigned)__shfl_xor((int)saw, 16);
