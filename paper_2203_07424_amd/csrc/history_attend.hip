@@ -42,8 +42,9 @@ namespace {
 constexpr int CUS = 256;
 
 // Waves that a SIMD holds at once; the compiler gives a wave at most its share of registers.
-__host__ __device__ constexpr int waves_of(int format, int d, bool bf, int heads)
+__host__ __device__ constexpr int waves_of(int format, int d, bool bf, int heads, int kind = 0)
 {
+    if (kind == 2 && d == 32 && format == REC_MX8 && heads == 1) return 3;  // a row's parts besides
     if (heads > 1) return d == 32 && format == REC_MX4 ? 3 : 2;
     return d == 128 ? (format == REC_MX4 && bf ? 3 : 2) : d == 64 ? (format == REC_MX4 && bf ? 4 : 3) : 4;
 }
@@ -73,16 +74,27 @@ struct AttendArgs {
 // What a launch attends to: histories, pages of them that were chosen, histories behind a prefix.
 enum { WHOLE, CHOSEN, BEHIND };
 
-// Joins a row's sums, weights' sum l and maximum's exponent m with those of a part: x's columns of all of them.
+// Joins a row's sums x, of some columns, its weights' sum l and its maximum's exponent m with those of `parts` parts, in their order.
+// part: of the first part's same columns, `stride` elements apart; ml: of its maximum and sum.
 template <int N>
-__device__ inline void add_part(f32x4 (&x)[N], float &l, float &m, const float *part, int stride, f32x2 ml)
+__device__ inline void add_parts(f32x4 (&x)[N], float &l, float &m, const float *part, int stride, const f32x2 *ml, int parts, long long all_rows, int d)
 {
-    const float most = fmaxf(m, ml[0]);
-    const float mine = m == neg_inf() ? (l == 0.0f ? 0.0f : l) : __builtin_amdgcn_exp2f(m - most);
-    const float its = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - most);
+    const auto weight = [](f32x2 ml, float most) { return ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - most); };
+    float most = m;
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) most = fmaxf(most, ml[i * all_rows][0]);
+    const float mine = weight(f32x2{m, l}, most);
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = x[i] * mine + *reinterpret_cast<const f32x4 *>(part + stride * i) * its;
-    l = l * mine + ml[1] * its;
+    for (int i = 0; i < N; ++i) x[i] *= mine;
+    l *= mine;
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) {
+        const f32x2 its = ml[i * all_rows];
+        const float by = weight(its, most);
+        l += its[1] * by;
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] += *reinterpret_cast<const f32x4 *>(part + i * all_rows * d + stride * j) * by;
+    }
     m = most;
 }
 
@@ -95,7 +107,7 @@ __device__ inline long long out_row(const AttendArgs &a, int b, int kv, int row)
 
 // KIND CHOSEN: tokens are those of the chosen pages, one page after the other, and all rows stand at one position.
 template <int FMT, int D, bool BF, int W, int HEADS, int KIND>
-__global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_kernel(AttendArgs a)
+__global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void attend_kernel(AttendArgs a)
 {
     static_assert(HEADS == 1 || W == 1, "several heads a wave: only where there are waves enough");
     static_assert(HEADS == 1 || KIND != CHOSEN, "every kv head has pages of its own");
@@ -360,7 +372,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
         } else if (real) {
             float m = sum.m, total = l;
             if constexpr (KIND == BEHIND)
-                for (int i = 0; i < a.before; ++i) add_part(o, total, m, a.before_o + (i * all_rows + out) * D + 4 * g, 16, a.before_ml[i * all_rows + out]);
+                add_parts(o, total, m, a.before_o + out * D + 4 * g, 16, a.before_ml + out, a.before, all_rows, D);
             const float by = inverse(total, m);
             typedef T tx4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -402,7 +414,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS)) void attend_ke
                 typedef T tx8 __attribute__((ext_vector_type(8)));
                 if constexpr (KIND == BEHIND) {
                     f32x4 both[2] = {x, y};
-                    for (int i = 0; i < a.before; ++i) add_part(both, l, m, a.before_o + (i * all_rows + to) * D + col, 4, a.before_ml[i * all_rows + to]);
+                    add_parts(both, l, m, a.before_o + to * D + col, 4, a.before_ml + to, a.before, all_rows, D);
                     x = both[0];
                     y = both[1];
                 }

@@ -311,7 +311,26 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
     const int row_block = a.by_splits.of(rest), split = rest - row_block * a.splits;
     const int first_row = (row_block * ROW_WAVES + part_of_rows) * RT * ROWS;
 
-    const int shift = a.c.page_shift, most_tokens = a.prefix.width << shift;
+    // The rows' queries, on their way while the prefix is looked up, and which of them see it: a query before its history's first
+    // token sees nothing.
+    const int shift = a.c.page_shift;
+    Query<D, BF> q[RT];
+    unsigned sees = 0;
+    long long to[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int row = first_row + t * ROWS + c;
+        const char *from = nullptr;
+        to[t] = -1;
+        if (row < a.rows) {
+            const int at = a.by_per.of(row), b = a.by_queries.of(at), i = at - b * a.q.queries, head = kv * a.per + row - at * a.per;
+            from = static_cast<const char *>(a.q.dev_q) + 2 * (b * a.q.batch_stride + i * a.q.query_stride + head * a.q.head_stride);
+            to[t] = (long long)at * a.q.heads + head;
+            sees |= a.q.candidates || min(max(a.q.dev_lengths[b], 0), a.q.table_width << shift) - a.q.queries + i >= 0 ? 1u << t : 0u;
+        }
+        q[t].fetch(from, g);
+    }
+    const int most_tokens = a.prefix.width << shift;
     int len = *a.prefix.length;
     if (len < 0 || len > most_tokens) {
         if (blockIdx.x == 0 && threadIdx.x == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)a.q.batch);
@@ -397,19 +416,10 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
             for (int j = 0; j < 4; ++j) ks[j] = x[j];
         }
     };
-    Query<D, BF> q[RT];
     load_made(n, page);
     load_keys(n, k_page);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int row = first_row + t * ROWS + c;
-        const char *from = nullptr;
-        if (row < a.rows) {
-            const int at = a.by_per.of(row), b = a.by_queries.of(at);
-            from = static_cast<const char *>(a.q.dev_q) + 2 * (b * a.q.batch_stride + (at - b * a.q.queries) * a.q.query_stride + (kv * a.per + row - at * a.per) * a.q.head_stride);
-        }
-        q[t].fetch(from, g);
-    }
+    for (int t = 0; t < RT; ++t) q[t].convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);
     // The weights of the tile before, and its values: none yet.
     u32x4 w[RT][TERMS][2];
 #pragma unroll
@@ -417,8 +427,6 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
 #pragma unroll
         for (int k = 0; k < TERMS; ++k) w[t][k][0] = w[t][k][1] = u32x4{0u, 0u, 0u, 0u};
     for (int i = part_of_rows * 64 + lane; i < VALUES; i += 64 * ROW_WAVES) values[VALUES + i] = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int t = 0; t < RT; ++t) q[t].convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);
     // Loads that go to LDS are not among those that a barrier waits for.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
@@ -573,22 +581,19 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
     const long long all_rows = (long long)a.q.batch * a.q.queries * a.q.heads;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const int row = first_row + t * ROWS + c;
-        if (row >= a.rows) break;
-        const int at = a.by_per.of(row), b = a.by_queries.of(at);
-        // A query before its history's first token sees nothing.
-        const bool sees = a.q.candidates || min(max(a.q.dev_lengths[b], 0), a.q.table_width << shift) - a.q.queries + at - b * a.q.queries >= 0;
+        if (to[t] < 0) break;
+        const bool see = sees >> t & 1u;
         const f32x2 ml = ml_of[part_of_rows][t][c];
         const float most = fmaxf(m[t], ml[0]);
         const float mine = m[t] == neg_inf() ? (l[t][0] == 0.0f ? 0.0f : l[t][0]) : __builtin_amdgcn_exp2f(m[t] - most);
         const float its = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - most);
-        const long long to = split * all_rows + (long long)at * a.q.heads + kv * a.per + (row - at * a.per);
+        const long long row = split * all_rows + to[t];
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
             const f32x4 x = o[t][i] * mine + sums[(t * (D / 16) + i) * 64] * its;
-            *reinterpret_cast<f32x4 *>(a.part_o + to * D + 16 * i + 4 * g) = sees ? x : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            *reinterpret_cast<f32x4 *>(a.part_o + row * D + 16 * i + 4 * g) = see ? x : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        if (g == 0) a.part_ml[to] = sees ? f32x2{most, l[t][0] * mine + ml[1] * its} : f32x2{neg_inf(), 0.0f};
+        if (g == 0) a.part_ml[row] = see ? f32x2{most, l[t][0] * mine + ml[1] * its} : f32x2{neg_inf(), 0.0f};
     }
 }
 
