@@ -116,7 +116,13 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int slot = c / SLOT, r = c % SLOT;  // which of the wave's kv heads, and its row
     // Parts of a history's head next to each other, then its heads, whose groups share a page.
-    const int pair = a.inner.of((int)blockIdx.x), part = (int)blockIdx.x - pair * a.splits * a.row_tiles;
+    // Queries of one history may have chosen the same pages: neighbours run on one XCD, of which blocks take turns.
+    int block = (int)blockIdx.x;
+    if constexpr (KIND == CHOSEN) {
+        const int all = (int)gridDim.x, xcd = block & 7;
+        block = xcd * (all >> 3) + min(xcd, all & 7) + (block >> 3);
+    }
+    const int pair = a.inner.of(block), part = block - pair * a.splits * a.row_tiles;
     const int b = a.heads.of(pair), first_kv = pair * HEADS - b * a.c.kv_heads, kv = first_kv + slot;
     const int row_tile = a.splits == 1 ? part : part / a.splits, split = part - row_tile * a.splits;
 
@@ -138,10 +144,30 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
     const int p_lo = position(first_row), p_hi = position(last_row), pos = position(row);
     const int window = a.q.window == 0 ? 0x7fffffff : a.q.window, sinks = a.q.sinks;
 
+    // Chosen pages: lane i has the i-th of 64, its number in the history and its page, or -1.  A window of them is looked up at once, and
+    // a tile's pages are all in one.
+    const int32_t *const table = a.q.dev_pages_of + history * a.q.table_stride;
+    const int32_t *const chosen = a.chosen + (KIND == CHOSEN ? ((long long)b * a.c.kv_heads + first_kv) * a.width : 0);
+    int window_at = -1, window_number = -1, window_page = -1;
+    auto look_up = [&](int at) {
+        window_at = at;
+        const int i = 64 * at + lane;
+        window_number = i < a.width ? chosen[i] : -1;
+        window_page = -1;
+        if ((unsigned)window_number < (unsigned)a.q.table_width && window_number << shift <= p_hi) window_page = table[window_number];
+    };
+
     // Tiles that some row sees something of: [0, n_sink) and [n_from, n_to).
     int n_from = 0, n_sink = 0, n_to = 0;
     if (p_hi >= 0) {
-        n_to = KIND == CHOSEN ? (int)((((long long)a.width << shift) + TILE - 1) / TILE) : p_hi / TILE + 1;
+        if constexpr (KIND == CHOSEN) {
+            look_up(0);
+            int last = a.width;  // pages up to the last one, where that is known
+            if (a.width <= 64) last = 64 - __builtin_clzll(__ballot(window_number != -1) | 1ull);
+            n_to = (int)((((long long)last << shift) + TILE - 1) / TILE);
+        } else {
+            n_to = p_hi / TILE + 1;
+        }
         if constexpr (KIND != CHOSEN) n_from = max(p_lo - window + 1, 0) / TILE;
         if constexpr (KIND != CHOSEN) n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from);
     }
@@ -162,8 +188,6 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
         const long long row_bytes = 2 * (history * a.q.batch_stride + (KIND == CHOSEN ? query_of_history : query) * a.q.query_stride + head * a.q.head_stride);
         // Positive, so that masked scores stay at -inf.
         const float factor = a.q.scale == 0.0f ? 1.0f : __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
-        const int32_t *table = a.q.dev_pages_of + history * a.q.table_stride;
-        const int32_t *chosen = a.chosen + (KIND == CHOSEN ? ((long long)b * a.c.kv_heads + first_kv) * a.width : 0);
         const int groups = 1 << (shift - 4);
         const int head_bytes = groups * group_bytes<FMT>(D);
         const unsigned char *first_page = a.c.pages + (long long)first_kv * head_bytes;
@@ -172,22 +196,19 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
 
         // Tile n of the walk starts at this key.
         auto key_of = [&](int n) { return (n < n_sink ? n : n_from + n - n_sink) * TILE; };
-        // Which page of the history a group's first token lies in (-1: none was chosen), and which of the cache, or -1.
-        auto number_of = [&](int token) {
-            int number = -1;
-            if (token >> shift < a.width) number = chosen[token >> shift];
-            return number;
-        };
-        auto page_at = [&](int number) {
-            int page = -1;
-            if ((unsigned)number < (unsigned)a.q.table_width && number << shift <= p_hi) page = table[number];
-            return page;
-        };
+        // The page of a group's first token, or -1.
         auto page_of = [&](int token) {
             int page = -1;
-            if constexpr (KIND == CHOSEN) page = page_at(number_of(token));
+            if constexpr (KIND == CHOSEN) page = __shfl(window_page, token >> shift);
             else if (token < len) page = table[token >> shift];
             return page;
+        };
+        // Chosen pages: its number in the history.
+        auto number_of = [&](int token) { return KIND == CHOSEN ? __shfl(window_number, token >> shift) : 0; };
+        // Before the pages of tile n are asked for.
+        auto at_tile = [&](int n) {
+            if constexpr (KIND == CHOSEN)
+                if (n >> shift != window_at) look_up(n >> shift);
         };
         auto group_at = [&](int page, int token) {
             const bool ok = (unsigned)page < pages;  // else some group that is there: its tokens count for nothing
@@ -196,8 +217,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
         };
 
         int n = begin + wave, key = key_of(n);
-        int k_page = page_of(key + 16 * (c >> 2)), v_number = KIND == CHOSEN ? number_of(key + 16 * g) : 0;
-        int v_page = KIND == CHOSEN ? page_at(v_number) : page_of(key + 16 * g);
+        at_tile(n);
+        int k_page = page_of(key + 16 * (c >> 2)), v_page = page_of(key + 16 * g), v_number = number_of(key + 16 * g);
         Query<D, BF> q;
         q.fetch(real ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr, g);
         Tile<FMT, D> tile[HEADS];
@@ -207,9 +228,15 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
         for (int h = 0; h < HEADS; ++h) load_keys(h, key);
 #pragma unroll
         for (int h = 0; h < HEADS; ++h) load_values(h, v_page, key);
-        k_page = n + W < end ? page_of(key_of(n + W) + 16 * (c >> 2)) : -1;
-        int v_number_next = KIND == CHOSEN && n + W < end ? number_of(key_of(n + W) + 16 * g) : -1;
-        int v_next = n + W >= end ? -1 : KIND == CHOSEN ? page_at(v_number_next) : page_of(key_of(n + W) + 16 * g);
+        k_page = -1;
+        int v_next = -1, v_number_next = -1;
+        auto ask = [&](int n) {
+            at_tile(n);
+            k_page = page_of(key_of(n) + 16 * (c >> 2));
+            v_next = page_of(key_of(n) + 16 * g);
+            v_number_next = number_of(key_of(n) + 16 * g);
+        };
+        if (n + W < end) ask(n + W);
         q.convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);  // while the first tile is on its way
         for (;; n += W) {
             const bool more = n + W < end;
@@ -336,13 +363,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
             v_page = v_next;
             v_number = v_number_next;
             if (n + 2 * W < end) {
-                k_page = page_of(key_of(n + 2 * W) + 16 * (c >> 2));
-                if constexpr (KIND == CHOSEN) {
-                    v_number_next = number_of(key_of(n + 2 * W) + 16 * g);
-                    v_next = page_at(v_number_next);
-                } else {
-                    v_next = page_of(key_of(n + 2 * W) + 16 * g);
-                }
+                ask(n + 2 * W);
             }
         }
     }

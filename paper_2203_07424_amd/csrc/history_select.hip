@@ -3,12 +3,12 @@
 // means_kernel: a lane has 32 columns of a token at a time, one scale's, and adds up its tokens'; lanes meet by
 // exchanges that halve the columns of each.  Bound by the keys' bytes.
 //
-// score_kernel: products of queries and means, in 64 bits on the matrix instructions (16 x 16 x 4): which of two pages
+// score_pages(): products of queries and means, in 64 bits on the matrix instructions (16 x 16 x 4): which of two pages
 // comes first must not hang on the order of a sum.  Operands are bf16 or fp16 numbers, so that their products are exact.
 // A wave has 16 rows (the heads of as many queries as fit) and walks over tiles of 16 pages.
 //
-// choose_kernel: a score becomes a whole number of the same order; the one that `count` pages reach is found bit
-// by bit, from the first in which the scores differ, by counting over a wave's ballots, and mostly long before the last bit.
+// choose(): a score becomes a whole number of the same order; the one that `count` pages reach is found by halving the range of
+// numbers it lies in and counting over a wave's ballots.
 #include <algorithm>
 
 #include "history.h"
@@ -127,6 +127,9 @@ __device__ inline u64 key_of(f64 x)
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
+// What a key was made of.
+__device__ inline f64 number_of(u64 key) { return __builtin_bit_cast(f64, key >> 63 ? key & ~(1ull << 63) : ~key); }
+
 // A history's length, brought into its range.
 __device__ inline int length_of(const SelectArgs &a, int b, bool tell)
 {
@@ -146,117 +149,200 @@ __device__ inline int pages_up_to(const SelectArgs &a, int len, int i)
     return p < 0 ? 0 : (p >> a.c.page_shift) + 1;
 }
 
-template <int D, bool BF>
-__global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a)
+// Tiles n, n + step ... before `end` of pages [from, to).
+struct Walk {
+    int from, to, n, step, end;
+};
+
+// Scores of a wave's 16 rows: the heads of `queries` queries from first_query on, of history b and kv head kv, over the pages of
+// walk(), which is asked once the rows are on their way.  store(query - first_query, page, key).  FEW: at most four rows, on 4 x 4 x 4,
+// which has four products of as many pages and takes half the time.
+template <int D, bool BF, bool FEW, class W, class F>
+__device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first_query, int queries, const W &walk, const F &store)
 {
     constexpr int N = D / 4;  // columns of a lane: group g has N g ...
-    const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-    const int wave = (int)(blockIdx.x * (THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
-    const int rest = a.by_walks.of(wave), walk = wave - rest * a.walks;
-    const int pair = a.by_query_tiles.of(rest), tile = rest - pair * a.query_tiles;
-    const int b = a.by_heads.of(pair), kv = pair - b * a.c.kv_heads;
-    if (b >= a.q.batch) return;
-    const int len = length_of(a, b, false);
-    const int first_query = tile * a.at_once, queries = min(a.at_once, a.q.queries - first_query);
-    // Pages that some of the queries may choose.
-    const int to = pages_up_to(a, len, first_query + queries - 1) - a.sel.last, from = a.sel.first;
-    int n = max(from / PAGES, walk * a.each);
-    const int end = min((to + PAGES - 1) / PAGES, (walk + 1) * a.each);
-    if (n >= end) return;
+    constexpr int PER_LANE = FEW ? 1 : 4;  // results
+    const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4, column = FEW ? lane & 3 : j;
+    const int heads = min(a.per, 16), rows = queries * heads, row_tiles = (a.per + 15) / 16;
+    const int row = min(column, rows - 1), query = row / heads;
+    const char *mine = static_cast<const char *>(a.q.dev_q) + 2 * (b * a.q.batch_stride + (first_query + query) * a.q.query_stride + N * g);
+    u32x4 x[N / 8];
+    auto load_rows = [&](int t) {
+        const char *q = mine + 2 * (kv * a.per + min(16 * t + row - query * heads, a.per - 1)) * a.q.head_stride;
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) x[i] = *reinterpret_cast<const u32x4 *>(q + 16 * i);
+    };
+    load_rows(0);
 
+    const Walk w = walk();
     const int32_t *table = a.q.dev_pages_of + b * a.q.table_stride;
     const u32x4 *means = static_cast<const u32x4 *>(a.sel.means);
     auto page_of = [&](int n) {
         const int number = n * PAGES + j;
         int page = -1;
-        if (number >= from && number < to) {
-            page = table[number];
-            if ((long long)page >= a.c.num_pages || page < 0) {
-                if (g == 0) report(a.c.fault, REC_FAULT_PAGE, (u64)b * (unsigned)a.q.table_width + (unsigned)number);
-                page = -1;
-            }
-        }
+        if (n < w.end && number >= w.from && number < w.to) page = table[number];
         return page;
     };
-    const int rows = a.per > 16 ? 16 : queries * a.per, row_tiles = (a.per + 15) / 16;
-    for (; n < end; ++n) {
-        const int page = page_of(n);
-        u32x4 raw[N / 8];
+    auto there = [&](int page) { return page >= 0 && (long long)page < a.c.num_pages; };
+    u32x4 raw[2][N / 8];
+    auto load_means = [&](u32x4 (&raw)[N / 8], int page) {
 #pragma unroll
         for (int i = 0; i < N / 8; ++i) {
             raw[i] = u32x4{0u, 0u, 0u, 0u};
-            if (page >= 0) raw[i] = means[(((long long)page * a.c.kv_heads + kv) * D + N * g) / 8 + i];
+            if (there(page)) raw[i] = means[(((long long)page * a.c.kv_heads + kv) * D + N * g) / 8 + i];
         }
-        const unsigned there = (unsigned)__ballot(page >= 0) & 0xffffu;
-        f64 best[4];
+    };
+    auto element = [](u32x4 w, int k, bool bf) -> f64 {
+        if (bf) return (f64) __builtin_bit_cast(float, k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+        return (f64) __builtin_bit_cast(f16x8, w)[k];
+    };
+    // The means of the next tile are on their way while one is multiplied.
+    auto score = [&](const u32x4 (&raw)[N / 8], int n, int page) {
+        const int number = n * PAGES + j;
+        if (!there(page) && g == 0 && number >= w.from && number < w.to) report(a.c.fault, REC_FAULT_PAGE, (u64)b * (unsigned)a.q.table_width + (unsigned)number);
+        const unsigned known = (unsigned)__ballot(there(page)) & 0xffffu;
+        f64 best[PER_LANE];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) best[r] = -__builtin_inf();
+        for (int r = 0; r < PER_LANE; ++r) best[r] = -__builtin_inf();
         for (int t = 0; t < row_tiles; ++t) {
-            const int row = min(j, rows - 1), query = a.per > 16 ? 0 : row / a.per, head = min(a.per > 16 ? 16 * t + row : row - query * a.per, a.per - 1);
-            const char *q = static_cast<const char *>(a.q.dev_q) + 2 * (b * a.q.batch_stride + (first_query + query) * a.q.query_stride + (kv * a.per + head) * a.q.head_stride + N * g);
-            f64x4 s = {0.0, 0.0, 0.0, 0.0};
+            if (row_tiles > 1) load_rows(t);
+            // Two sums, which do not wait for each other.
+            std::conditional_t<FEW, f64, f64x4> even = {}, odd = {};
 #pragma unroll
-            for (int i = 0; i < N / 8; ++i) {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(q + 16 * i);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float m = __builtin_bit_cast(float, k & 1 ? raw[i][k / 2] & 0xffff0000u : raw[i][k / 2] << 16);
-                    const float x = BF ? __builtin_bit_cast(float, k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16) : (float)__builtin_bit_cast(f16x8, w)[k];
-                    s = __builtin_amdgcn_mfma_f64_16x16x4f64((f64)m, (f64)x, s, 0, 0, 0);
+            for (int i = 0; i < N; i += 2) {
+                u32x4 p = raw[i / 8], q = x[i / 8];
+                if constexpr (D == 128) {  // converted where they are used: all at once they would take 128 registers
+                    if (i % 8 == 0) __builtin_amdgcn_sched_barrier(0);
+                    asm volatile("" : "+v"(p), "+v"(q));
+                }
+                const f64 m = element(p, i % 8, true), m1 = element(p, i % 8 + 1, true), y = element(q, i % 8, BF), y1 = element(q, i % 8 + 1, BF);
+                if constexpr (FEW) {
+                    even = __builtin_amdgcn_mfma_f64_4x4x4f64(m, y, even, 0, 0, 0);
+                    odd = __builtin_amdgcn_mfma_f64_4x4x4f64(m1, y1, odd, 0, 0, 0);
+                } else {
+                    even = __builtin_amdgcn_mfma_f64_16x16x4f64(m, y, even, 0, 0, 0);
+                    odd = __builtin_amdgcn_mfma_f64_16x16x4f64(m1, y1, odd, 0, 0, 0);
                 }
             }
-            // Row r of a lane's four: page 4 r + g.  A product that is NaN counts for nothing.
+            // A product that is NaN counts for nothing.
+            if constexpr (FEW) {
+                best[0] = even + odd > best[0] ? even + odd : best[0];
+            } else {
+                even += odd;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) best[r] = s[r] > best[r] ? s[r] : best[r];
+                for (int r = 0; r < 4; ++r) best[r] = even[r] > best[r] ? even[r] : best[r];
+            }
         }
-        const int heads = min(a.per, 16);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < PER_LANE; ++r) {
             f64 most = best[r];
             for (int d = 1; d < heads; ++d) {
                 const f64 other = __shfl(best[r], lane + d);
                 most = other > most ? other : most;
             }
-            const int in_tile = 4 * r + g, number = n * PAGES + in_tile;
-            const int query = j / heads;
-            if (j == query * heads && query < queries && number >= from && number < to)
-                a.sel.keys[(((long long)b * a.q.queries + first_query + query) * a.c.kv_heads + kv) * a.q.table_width + number] =
-                    key_of(there >> in_tile & 1 ? most : -__builtin_inf());
+            // Row r of a lane's four: page 4 r + g; of four products: page g of the lane's own.
+            const int in_tile = FEW ? (lane >> 2 & 3) * 4 + g : 4 * r + g, number = n * PAGES + in_tile;
+            if (column == query * heads && column < rows && number >= w.from && number < w.to) store(query, number, key_of(known >> in_tile & 1 ? most : -__builtin_inf()));
         }
+    };
+    int n = w.n, page = page_of(n), next = page_of(n + w.step);
+    load_means(raw[0], page);
+    for (; n < w.end; n += 2 * w.step) {
+        load_means(raw[1], next);
+        int after = page_of(n + 2 * w.step);
+        score(raw[0], n, page);
+        if (n + w.step >= w.end) break;
+        load_means(raw[0], after);
+        page = after;
+        after = page_of(n + 3 * w.step);
+        score(raw[1], n + w.step, next);
+        next = after;
     }
 }
 
-// --------------------------------------------------------------------- choice
-// W waves a row, KEYS of its scores in each lane at a time.
-template <int W, int KEYS>
-__global__ __launch_bounds__(64 * W) void choose_kernel(SelectArgs a)
+// Pages that some of a tile's queries may choose between those that all have.
+__device__ inline Walk between(const SelectArgs &a, int there, int n, int step, int most)
 {
-    __shared__ u64 ends[2][W];
-    __shared__ unsigned counts[2][W];
-    __shared__ unsigned before[2][KEYS][W];
-    const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long long row = blockIdx.x;
-    const int at = a.by_heads.of((int)row), kv = (int)row - at * a.c.kv_heads;
-    const int b = a.by_query_tiles.of(at), query = at - b * a.q.queries;
-    const int len = length_of(a, b, threadIdx.x == 0 && kv == 0 && query == 0), there = pages_up_to(a, len, query);
-    int32_t *out = a.sel.chosen + row * a.sel.count;
+    const int to = there - a.sel.last, from = a.sel.first;
+    return {from, to, from / PAGES + n, step, min((to + PAGES - 1) / PAGES, most)};
+}
+
+template <int D, bool BF, bool FEW>
+__global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a)
+{
+    const int wave = (int)(blockIdx.x * (THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    const int rest = a.by_walks.of(wave), walk = wave - rest * a.walks;
+    const int pair = a.by_query_tiles.of(rest), tile = rest - pair * a.query_tiles;
+    const int b = a.by_heads.of(pair), kv = pair - b * a.c.kv_heads;
+    if (b >= a.q.batch) return;
+    const int first_query = tile * a.at_once, queries = min(a.at_once, a.q.queries - first_query);
+    u64 *keys = a.sel.keys + (((long long)b * a.q.queries + first_query) * a.c.kv_heads + kv) * a.q.table_width;
+    score_pages<D, BF, FEW>(
+        a, b, kv, first_query, queries,
+        [&]() {
+            Walk w = between(a, pages_up_to(a, length_of(a, b, false), first_query + queries - 1), 0, 1, (walk + 1) * a.each);
+            w.n = max(w.n, walk * a.each);
+            return w;
+        },
+        [&](int query, int page, u64 key) { keys[(long long)query * a.c.kv_heads * a.q.table_width + page] = key; });
+}
+
+// --------------------------------------------------------------------- choice
+// Sums of lanes up to each, without a trip through LDS or the scalar unit: counts by ballots took 60 cycles each.
+__device__ inline unsigned sums_up_to(unsigned x)
+{
+    auto shifted = [](unsigned x, auto control, auto rows) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, control(), rows(), 0xf, false); };
+    x += shifted(x, std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());  // by 1, 2, 4 and 8 lanes of a row of 16
+    x += shifted(x, std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+    x += shifted(x, std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+    x += shifted(x, std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+    x += shifted(x, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());  // a row's last to the next row
+    x += shifted(x, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());  // lane 31's to the upper half
+    return x;
+}
+__device__ inline unsigned last_lane(unsigned x) { return (unsigned)__builtin_amdgcn_readlane((int)x, 63); }
+// The largest of all lanes.
+__device__ inline unsigned largest(unsigned x)
+{
+    auto shifted = [](unsigned x, auto control, auto rows) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, control(), rows(), 0xf, false); };
+    x = max(x, shifted(x, std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>()));
+    x = max(x, shifted(x, std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>()));
+    x = max(x, shifted(x, std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>()));
+    x = max(x, shifted(x, std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>()));
+    x = max(x, shifted(x, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>()));
+    x = max(x, shifted(x, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>()));
+    return last_lane(x);
+}
+
+// What the waves of a row tell each other.
+template <int W>
+struct Meeting {
+    unsigned words[2][2][W];
+};
+template <>
+struct Meeting<1> {};
+
+// The choice of one row, by W waves with KEYS of its scores in each lane at a time: of the pages up to `there`, whose scores are keys[page - first].
+template <int W, int KEYS>
+__device__ inline void choose(const SelectArgs &a, const u64 *keys, int there, int32_t *out, Meeting<W> &m)
+{
+    const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), thread = 64 * wave + lane;
     if (there <= a.sel.count) {  // all of them
-        for (int i = threadIdx.x; i < a.sel.count; i += 64 * W) out[i] = i < there ? i : -1;
+        for (int i = thread; i < a.sel.count; i += 64 * W) out[i] = i < there ? i : -1;
         return;
     }
     const int first = a.sel.first, last = a.sel.last, want = a.sel.count - first - last, n = there - first - last;
-    for (int i = threadIdx.x; i < first; i += 64 * W) out[i] = i;
-    for (int i = threadIdx.x; i < last; i += 64 * W) out[a.sel.count - last + i] = there - last + i;
+    for (int i = thread; i < first; i += 64 * W) out[i] = i;
+    for (int i = thread; i < last; i += 64 * W) out[a.sel.count - last + i] = there - last + i;
     if (want == 0) return;
 
-    const u64 *keys = a.sel.keys + row * a.q.table_width + first;
     constexpr int CHUNK = 64 * W * KEYS;
     const bool one_chunk = n <= CHUNK;
-    u64 key[KEYS];
+    u64 key[KEYS];  // neighbouring pages'; 0 behind the last
     auto load = [&](int from) {
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
-            const int k = from + (i * W + wave) * 64 + lane;
+            const int k = from + thread * KEYS + i;
             key[i] = k < n ? keys[k] : 0;
         }
     };
@@ -268,55 +354,61 @@ __global__ __launch_bounds__(64 * W) void choose_kernel(SelectArgs a)
     };
     load(0);
     int turn = 0;
-    auto sum = [&](unsigned x) {  // over the waves
-        if constexpr (W == 1) return x;
-        if (lane == 0) counts[turn][wave] = x;
-        __syncthreads();
-        unsigned s = 0;
+    // Two words of each wave to all.
+    auto meet = [&](unsigned x, unsigned y, auto f) {
+        if constexpr (W == 1) {
+            f(0, x, y);
+        } else {
+            if (lane == 0) {
+                m.words[turn][0][wave] = x;
+                m.words[turn][1][wave] = y;
+            }
+            __syncthreads();
 #pragma unroll
-        for (int w = 0; w < W; ++w) s += counts[turn][w];
-        turn ^= 1;
-        return s;
+            for (int w = 0; w < W; ++w) f(w, m.words[turn][0][w], m.words[turn][1][w]);
+            turn ^= 1;
+        }
     };
     auto count = [&](auto is) {
-        unsigned c = 0;
+        unsigned c = 0, all = 0;
         each_chunk([&](int) {
 #pragma unroll
-            for (int i = 0; i < KEYS; ++i) c += (unsigned)__popcll(__ballot(is(key[i])));
+            for (int i = 0; i < KEYS; ++i) c += is(key[i]) ? 1u : 0u;
         });
-        return sum(c);
+        meet(last_lane(sums_up_to(c)), 0, [&](int, unsigned x, unsigned) { all += x; });
+        return all;
     };
 
-    // The bits that all scores begin with.
-    u64 all = ~0ull, any = 0;
+    // The score that `want` pages reach lies in [low, high].  Half way between as numbers, by their upper halves, which takes as many
+    // counts as the scores nearest to it are apart; then, where that does not end, bit by bit.
+    unsigned highest = 0, lowest = 0;  // the latter's complement
     each_chunk([&](int) {
 #pragma unroll
         for (int i = 0; i < KEYS; ++i)
             if (key[i]) {
-                all &= key[i];
-                any |= key[i];
+                highest = max(highest, (unsigned)(key[i] >> 32));
+                lowest = max(lowest, ~(unsigned)(key[i] >> 32));
             }
     });
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        all &= (u64)__shfl_xor((long long)all, d);
-        any |= (u64)__shfl_xor((long long)any, d);
+    unsigned low = ~0u, high = 0;
+    meet(largest(highest), largest(lowest), [&](int, unsigned x, unsigned y) {
+        high = max(high, x);
+        low = min(low, ~y);
+    });
+    bool found = false;
+    for (int i = 0; i < 16 && !found && high - low > 1; ++i) {
+        // Of the numbers that these halves begin, the mean's; not a number, or none between them: half way as they are.
+        const f64 mean = 0.5 * number_of((u64)low << 32) + 0.5 * number_of((u64)high << 32);
+        unsigned middle = (unsigned)(key_of(mean) >> 32);
+        if (!(middle > low && middle <= high)) middle = low + (high - low + 1) / 2;
+        const unsigned c = count([&](u64 k) { return (unsigned)(k >> 32) >= middle; });
+        if (c >= (unsigned)want) low = middle;
+        else high = middle - 1;
+        found = c == (unsigned)want;
     }
-    if constexpr (W > 1) {
-        if (lane == 0) {
-            ends[0][wave] = all;
-            ends[1][wave] = any;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            all &= ends[0][w];
-            any |= ends[1][w];
-        }
-    }
-    const u64 differ = all ^ any;
-    u64 bar = all;  // the score that `want` pages reach
-    if (differ) {
+    u64 bar = (u64)low << 32;
+    if (!found) {
+        const u64 top = (u64)high << 32 | 0xffffffffu, differ = bar ^ top;
         int bit = 63 - __builtin_clzll(differ);
         bar &= bit == 63 ? 0ull : ~0ull << (bit + 1);
         for (; bit >= 0; --bit) {
@@ -331,42 +423,74 @@ __global__ __launch_bounds__(64 * W) void choose_kernel(SelectArgs a)
     // In order: those above the bar, and of those at it the first.
     int taken = 0, tied = 0;  // before this chunk
     each_chunk([&](int from) {
-        if constexpr (W > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < KEYS; ++i) {
-                const unsigned gt = (unsigned)__popcll(__ballot(key[i] > bar)), eq = (unsigned)__popcll(__ballot(key[i] == bar));
-                if (lane == 0) {
-                    before[0][i][wave] = gt;
-                    before[1][i][wave] = eq;
-                }
-            }
-            __syncthreads();
-        }
+        unsigned gt = 0, eq = 0;
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
-            const u64 gt = __ballot(key[i] > bar), eq = __ballot(key[i] == bar);
-            int mine_gt = taken, mine_eq = tied;
-            if constexpr (W > 1) {
-                for (int w = 0; w < wave; ++w) {
-                    mine_gt += (int)before[0][i][w];
-                    mine_eq += (int)before[1][i][w];
-                }
-                for (int w = 0; w < W; ++w) {
-                    taken += (int)before[0][i][w];
-                    tied += (int)before[1][i][w];
-                }
-            } else {
-                taken += __popcll(gt);
-                tied += __popcll(eq);
+            gt += key[i] > bar ? 1u : 0u;
+            eq += key[i] == bar ? 1u : 0u;
+        }
+        const unsigned gt_sum = sums_up_to(gt), eq_sum = sums_up_to(eq);
+        int mine = taken + (int)(gt_sum - gt), mine_tied = tied + (int)(eq_sum - eq);
+        meet(last_lane(gt_sum), last_lane(eq_sum), [&](int w, unsigned x, unsigned y) {
+            taken += (int)x;
+            tied += (int)y;
+            if (W > 1 && w < wave) {
+                mine += (int)x;
+                mine_tied += (int)y;
             }
-            const u64 lower = (1ull << lane) - 1;
-            const int eq_rank = mine_eq + __popcll(eq & lower);
-            const bool tie = key[i] == bar && eq_rank < ties;
-            if (key[i] > bar || tie) out[first + mine_gt + __popcll(gt & lower) + min(eq_rank, ties)] = first + from + (i * W + wave) * 64 + lane;
+        });
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const bool over = key[i] > bar, at = key[i] == bar;
+            if (over || (at && mine_tied < ties)) out[first + mine + min(mine_tied, ties)] = first + from + thread * KEYS + i;
+            mine += over;
+            mine_tied += at;
         }
     });
 }
+
+template <int W, int KEYS>
+__global__ __launch_bounds__(64 * W) void choose_kernel(SelectArgs a)
+{
+    __shared__ Meeting<W> m;
+    const long long row = blockIdx.x;
+    const int at = a.by_heads.of((int)row), kv = (int)row - at * a.c.kv_heads;
+    const int b = a.by_query_tiles.of(at), query = at - b * a.q.queries;
+    const int len = length_of(a, b, threadIdx.x == 0 && kv == 0 && query == 0);
+    choose<W, KEYS>(a, a.sel.keys + row * a.q.table_width + a.sel.first, pages_up_to(a, len, query), a.sel.chosen + row * a.sel.count, m);
+}
+
+// Both in one launch, where the scores of a block's queries fit LDS: all waves score, then each chooses for a query.
+template <int D, bool BF, bool FEW, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void select_kernel(SelectArgs a)
+{
+    extern __shared__ u64 keys[];  // [at_once][table_width]
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int pair = a.by_query_tiles.of((int)blockIdx.x), tile = (int)blockIdx.x - pair * a.query_tiles;
+    const int b = a.by_heads.of(pair), kv = pair - b * a.c.kv_heads;
+    const int first_query = tile * a.at_once, queries = min(a.at_once, a.q.queries - first_query);
+    int len = 0;
+    score_pages<D, BF, FEW>(
+        a, b, kv, first_query, queries,
+        [&]() {
+            len = length_of(a, b, threadIdx.x == 0 && kv == 0 && tile == 0);
+            const int there = pages_up_to(a, len, first_query + queries - 1);
+            return there > a.sel.count ? between(a, there, wave, WAVES, a.q.table_width) : Walk{0, 0, 0, 1, 0};  // else all are chosen
+        },
+        [&](int query, int page, u64 key) { keys[query * a.q.table_width + page] = key; });
+    __syncthreads();
+    Meeting<1> none;
+    for (int i = wave; i < queries; i += WAVES) {
+        const long long row = ((long long)b * a.q.queries + first_query + i) * a.c.kv_heads + kv;
+        choose<1, 8>(a, keys + i * a.q.table_width + a.sel.first, pages_up_to(a, len, first_query + i), a.sel.chosen + row * a.sel.count, none);
+    }
+}
+
+// Keys that a block has in LDS: two blocks of a compute unit at once.
+constexpr int MOST_KEYS = 8192;
+
+// Waves of a block that does both, by the tiles of a row.
+int select_waves(const rec_query &q) { return q.table_width > 16 * PAGES ? 16 : 8; }
 
 SelectArgs args_of(const Cache &c, const rec_query &q)
 {
@@ -374,15 +498,28 @@ SelectArgs args_of(const Cache &c, const rec_query &q)
     a.c = c;
     a.q = q;
     a.per = q.heads / c.kv_heads;
-    a.at_once = a.per >= 16 ? 1 : 16 / a.per;
-    a.query_tiles = (q.queries + a.at_once - 1) / a.at_once;
-    const long long rows = (long long)q.batch * c.kv_heads * a.query_tiles;
     const int tiles = (q.table_width + PAGES - 1) / PAGES;
+    const auto with = [&](int at_once) {
+        a.at_once = std::max(std::min({at_once, a.per >= 16 ? 1 : 16 / a.per, std::max(q.queries, 1)}), 1);
+        a.query_tiles = (q.queries + a.at_once - 1) / a.at_once;
+        return (long long)q.batch * c.kv_heads * a.query_tiles;  // blocks, or rows of waves
+    };
+    // In one launch where a row's pages fit, and where not many tiles are a wave's or blocks are enough for all compute units.
+    a.walks = 0;
+    a.each = 0;
+    if (q.table_width <= MOST_KEYS) {
+        const long long blocks = with(MOST_KEYS / std::max(q.table_width, 1));
+        if (tiles <= 8 * select_waves(q) || blocks >= 256) {
+            a.by_walks = Divider(1);
+            a.by_query_tiles = Divider(std::max(a.query_tiles, 1));
+            a.by_heads = Divider(c.kv_heads);
+            return a;
+        }
+    }
+    const long long rows = with(16);
     // A tile a wave where there are few rows; more where that would be more waves than work at once.
-    a.each = (int)((rows * tiles + 8191) / 8192);
-    a.each = a.each < 1 ? 1 : a.each;
-    a.walks = (tiles + a.each - 1) / a.each;
-    a.walks = a.walks < 1 ? 1 : a.walks;
+    a.each = (int)std::max(1ll, (rows * tiles + 8191) / 8192);
+    a.walks = std::max((tiles + a.each - 1) / a.each, 1);
     a.by_walks = Divider(a.walks);
     a.by_query_tiles = Divider(std::max(a.query_tiles, 1));
     a.by_heads = Divider(c.kv_heads);
@@ -391,7 +528,7 @@ SelectArgs args_of(const Cache &c, const rec_query &q)
 
 long long score_blocks(const SelectArgs &a)
 {
-    return ((long long)a.q.batch * a.c.kv_heads * a.query_tiles * a.walks + THREADS / 64 - 1) / (THREADS / 64);
+    return ((long long)a.q.batch * a.c.kv_heads * a.query_tiles * a.walks + THREADS / 64 - 1) / (THREADS / 64);  // none in one launch
 }
 
 long long means_blocks(const Cache &c, int d, int pages)
@@ -411,13 +548,27 @@ hipError_t means_of(const Cache &c, int d, const int32_t *which, int pages, void
     return hipGetLastError();
 }
 
-template <int D>
-hipError_t score_of(const SelectArgs &a, hipStream_t s)
+template <int D, bool BF, bool FEW>
+hipError_t scored_as(const SelectArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)score_blocks(a));
-    if (a.q.dtype == REC_BF16) hipLaunchKernelGGL((score_kernel<D, true>), grid, dim3(THREADS), 0, s, a);
-    else hipLaunchKernelGGL((score_kernel<D, false>), grid, dim3(THREADS), 0, s, a);
+    if (a.walks == 0) {
+        const dim3 grid((unsigned)((long long)a.q.batch * a.c.kv_heads * a.query_tiles));
+        const size_t lds = sizeof(u64) * a.at_once * std::max(a.q.table_width, 1);
+        if (select_waves(a.q) == 16) hipLaunchKernelGGL((select_kernel<D, BF, FEW, 16>), grid, dim3(1024), lds, s, a);
+        else hipLaunchKernelGGL((select_kernel<D, BF, FEW, 8>), grid, dim3(512), lds, s, a);
+    } else {
+        hipLaunchKernelGGL((score_kernel<D, BF, FEW>), dim3((unsigned)score_blocks(a)), dim3(THREADS), 0, s, a);
+    }
     return hipGetLastError();
+}
+
+// Scores, and in one launch the choice too.
+template <int D>
+hipError_t scored_of(const SelectArgs &a, hipStream_t s)
+{
+    const bool few = a.at_once * a.per <= 4;
+    if (a.q.dtype == REC_BF16) return few ? scored_as<D, true, true>(a, s) : scored_as<D, true, false>(a, s);
+    return few ? scored_as<D, false, true>(a, s) : scored_as<D, false, false>(a, s);
 }
 
 }  // namespace
@@ -431,12 +582,14 @@ hipError_t launch_means(const Cache &c, int format, int d, const int32_t *which,
 
 long long select_threads(const Cache &c, const rec_query &q)
 {
-    return std::max(score_blocks(args_of(c, q)) * THREADS, (long long)q.batch * q.queries * c.kv_heads * 256);
+    const SelectArgs a = args_of(c, q);
+    return a.walks ? std::max(score_blocks(a) * THREADS, (long long)q.batch * q.queries * c.kv_heads * 256)
+                   : (long long)q.batch * c.kv_heads * a.query_tiles * 64 * select_waves(q);
 }
 
 size_t select_workspace(const Cache &c, const rec_query &q, int count)
 {
-    if (q.table_width <= count) return 0;  // all pages are chosen
+    if (q.table_width <= count || args_of(c, q).walks == 0) return 0;
     return (size_t)q.batch * q.queries * c.kv_heads * (size_t)q.table_width * sizeof(u64);
 }
 
@@ -444,9 +597,9 @@ hipError_t launch_select(const Cache &c, int d, const rec_query &q, const Select
 {
     SelectArgs a = args_of(c, q);
     a.sel = sel;
-    if (q.table_width > sel.count && sel.count > sel.first + sel.last) {
-        const hipError_t e = d == 32 ? score_of<32>(a, s) : d == 64 ? score_of<64>(a, s) : score_of<128>(a, s);
-        if (e != hipSuccess) return e;
+    if (a.walks == 0 || (q.table_width > sel.count && sel.count > sel.first + sel.last)) {
+        const hipError_t e = d == 32 ? scored_of<32>(a, s) : d == 64 ? scored_of<64>(a, s) : scored_of<128>(a, s);
+        if (e != hipSuccess || a.walks == 0) return e;
     }
     a.by_query_tiles = Divider(q.queries);
     const dim3 grid((unsigned)((long long)q.batch * q.queries * c.kv_heads));

@@ -60,14 +60,15 @@ def test_queries(b, which):
 
 
 def test_choice(b):
-    h, q = cache(b), query(b, table_width=8)
+    h, q = cache(b, num_pages=100000), query(b, table_width=9000)
     call = lambda means=PTR, count=4, first=1, last=1, out=PTR, ws=PTR, n=1 << 40: b._lib.rec_history_select(  # noqa: E731
         C.byref(h), C.byref(q), means, count, first, last, out, ws, n, None)
     for kw in (dict(means=None), dict(means=PTR + 8), dict(count=0), dict(count=-1), dict(first=-1), dict(last=0), dict(first=4), dict(first=2 ** 31 - 1, last=2 ** 31 - 1),
-               dict(out=None), dict(out=PTR + 2), dict(ws=None), dict(ws=PTR + 8), dict(n=3 * 2 * 8 * 8 - 1)):
+               dict(out=None), dict(out=PTR + 2), dict(ws=None), dict(ws=PTR + 8), dict(n=3 * 2 * 9000 * 8 - 1)):
         assert call(**kw) == b.REC_ERR_ARG, kw
-    assert b.rec_history_select_workspace_bytes(h, q, 4) == 3 * 2 * 8 * 8          # queries, kv heads, pages, a word each
-    assert b.rec_history_select_workspace_bytes(h, q, 8) == 0                      # all pages are chosen
+    assert b.rec_history_select_workspace_bytes(h, q, 4) == 3 * 2 * 9000 * 8       # queries, kv heads, pages, a word each
+    assert b.rec_history_select_workspace_bytes(h, q, 9000) == 0                   # all pages are chosen
+    assert b.rec_history_select_workspace_bytes(h, query(b, table_width=1000), 4) == 0      # a row's scores fit LDS
     assert b.rec_history_select_workspace_bytes(h, q, 0) == 0
 
 
