@@ -731,6 +731,7 @@ class HistoryCache:
         self._h.dev_pages, self._h.dev_fault = pages.data_ptr(), self.fault.data_ptr()
         self._ref = C.byref(self._h)
         self._workspaces: dict = {}      # bytes by the shapes that decide them
+        self._means_shape = (num_pages, kv_heads, head_dim)
 
     def _ok(self, st: int, where: str) -> None:
         if st != REC_OK:
@@ -839,10 +840,8 @@ class HistoryCache:
     def _means(self, call: str, means: torch.Tensor) -> None:
         if means.requires_grad:
             _no_backward(call)
-        if means.shape != (self._h.num_pages, self.kv_heads, self.head_dim) or means.dtype is not torch.bfloat16 \
-                or means.get_device() != self._index or not means.is_contiguous():
-            raise ValueError(f"{call}: means must be a contiguous bfloat16 [{self._h.num_pages}, {self.kv_heads}, {self.head_dim}] on "
-                             f"{self.device}")
+        if means.shape != self._means_shape or means.dtype is not torch.bfloat16 or means.get_device() != self._index or not means.is_contiguous():
+            raise ValueError(f"{call}: means must be a contiguous bfloat16 {list(self._means_shape)} on {self.device}")
 
     def _query(self, call: str, q: torch.Tensor, pages_of: torch.Tensor, lengths: torch.Tensor, out: int, scale: Optional[float],
                candidates: bool) -> Tuple[bytes, tuple]:
@@ -871,16 +870,18 @@ class HistoryCache:
                             1 if candidates else 0)
         return query, (batch, queries, heads, width, candidates, code)
 
-    def _workspace(self, ask, query: bytes, shapes: tuple, *more: int) -> Optional[torch.Tensor]:
-        """As many bytes as `ask` says for these shapes, or None."""
-        key = (ask.__name__, shapes, more)
+    def _workspace(self, ask, key: tuple, query: bytes, count: int) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
+        """As many bytes as `ask` says, with their address and number; key: what decides that."""
         need = self._workspaces.get(key)
         if need is None:
-            need = ask(self._ref, query, *more)
+            need = ask(self._ref, query, count)
             if len(self._workspaces) >= 1024:
                 self._workspaces.clear()
             self._workspaces[key] = need
-        return torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        if not need:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return workspace, workspace.data_ptr(), need
 
     def _result(self, call: str, q: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
         if out is None:
@@ -898,14 +899,14 @@ class HistoryCache:
         call = "rec_history_select"
         query, shapes = self._query(call, q, pages_of, lengths, 0, 1.0, candidates)
         self._means(call, means)
-        shape = (*q.shape[:-2], self.kv_heads, count)
+        shape = (shapes[0], shapes[1], self.kv_heads, count) if q.dim() == 4 else (shapes[0], self.kv_heads, count)
         if out is None:
-            out = torch.empty(shape, dtype=_I32, device=self.device) if count >= 0 else means
+            out = torch.empty(shape, dtype=_I32, device=self.device) if count > 0 else means
         elif out.shape != shape or out.dtype is not _I32 or out.get_device() != self._index or not out.is_contiguous():
             raise ValueError(f"{call}: out must be a contiguous int32 {list(shape)} on {self.device}")
-        workspace = self._workspace(_lib.rec_history_select_workspace_bytes, query, shapes, count)
-        st = _lib.rec_history_select(self._ref, query, means.data_ptr(), count, first, last, out.data_ptr(), _ptr(workspace),
-                                     _bytes(workspace), _stream_on(self._index, call))
+        workspace, at, need = self._workspace(_lib.rec_history_select_workspace_bytes, ("select", shapes, count), query, count)
+        st = _lib.rec_history_select(self._ref, query, means.data_ptr(), count, first, last, out.data_ptr(), at, need,
+                                     _stream_on(self._index, call))
         if st:
             self._ok(st, call)
         return out
@@ -917,13 +918,12 @@ class HistoryCache:
         call = "rec_history_attend_selected"
         out = self._result(call, q, out)
         query, shapes = self._query(call, q, pages_of, lengths, out.data_ptr(), scale, candidates)
-        if chosen.dim() != q.dim() or chosen.shape[:-1] != (*q.shape[:-2], self.kv_heads) or chosen.dtype is not _I32 \
-                or chosen.get_device() != self._index or not chosen.is_contiguous():
-            raise ValueError(f"{call}: chosen must be a contiguous int32 {[*q.shape[:-2], self.kv_heads]} and a count on {self.device}")
-        count = chosen.shape[-1]
-        workspace = self._workspace(_lib.rec_history_attend_selected_workspace_bytes, query, shapes, count)
-        st = _lib.rec_history_attend_selected(self._ref, query, chosen.data_ptr(), count, _ptr(workspace), _bytes(workspace),
-                                              _stream_on(self._index, call))
+        count = chosen.shape[-1] if chosen.dim() else 0
+        shape = (shapes[0], shapes[1], self.kv_heads, count) if q.dim() == 4 else (shapes[0], self.kv_heads, count)
+        if chosen.shape != shape or chosen.dtype is not _I32 or chosen.get_device() != self._index or not chosen.is_contiguous():
+            raise ValueError(f"{call}: chosen must be a contiguous int32 {list(shape[:-1])} and a count on {self.device}")
+        workspace, at, need = self._workspace(_lib.rec_history_attend_selected_workspace_bytes, ("selected", shapes, count), query, count)
+        st = _lib.rec_history_attend_selected(self._ref, query, chosen.data_ptr(), count, at, need, _stream_on(self._index, call))
         if st:
             self._ok(st, call)
         return out
@@ -942,9 +942,9 @@ class HistoryCache:
         if prefix_length.numel() != 1 or prefix_length.dtype is not _I32 or prefix_length.get_device() != index:
             raise ValueError(f"{call}: prefix_length must be one int32 on {self.device}")
         width = prefix_pages.shape[0]
-        workspace = self._workspace(_lib.rec_history_attend_shared_workspace_bytes, query, shapes, width)
-        st = _lib.rec_history_attend_shared(self._ref, query, prefix_pages.data_ptr(), width, prefix_length.data_ptr(), _ptr(workspace),
-                                            _bytes(workspace), _stream_on(index, call))
+        workspace, at, need = self._workspace(_lib.rec_history_attend_shared_workspace_bytes, ("shared", shapes, width), query, width)
+        st = _lib.rec_history_attend_shared(self._ref, query, prefix_pages.data_ptr(), width, prefix_length.data_ptr(), at, need,
+                                            _stream_on(index, call))
         if st:
             self._ok(st, call)
         return out
@@ -985,30 +985,7 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: to
     return out
 
 
-def _turn_rows(what: str, x: Optional[torch.Tensor], out: Optional[torch.Tensor], weight: Optional[torch.Tensor], like: torch.Tensor):
-    """Address and strides of x and of where its result goes (made here if None), its heads, its weight's address, the result."""
-    if x is None:
-        if out is not None or weight is not None:
-            raise ValueError(f"rec_rotate_heads: {what} is None, but not its result or weight")
-        return (0, 0, 0), (0, 0, 0), 0, 0, None
-    index = like.get_device()
-    if x.dim() != 3 or x.dtype is not like.dtype or x.get_device() != index or x.shape[0] != like.shape[0] or x.shape[2] != like.shape[2]:
-        raise ValueError("rec_rotate_heads: q must be [tokens, heads, head_dim] and k [tokens, kv_heads, head_dim] on one device, fp32, fp16 or bf16")
-    if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
-    elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index:
-        raise ValueError(f"rec_rotate_heads: the result of {what} must be of its shape, type and device")
-    (token, head, column), (out_token, out_head, out_column) = x.stride(), out.stride()
-    if column != 1 or out_column != 1:
-        raise ValueError(f"rec_rotate_heads: rows of {what} and of its result must be contiguous")
-    if weight is not None:
-        if weight.dtype is not _F32 or weight.shape != x.shape[2:] or weight.get_device() != index or not weight.is_contiguous():
-            raise ValueError(f"rec_rotate_heads: the weight of {what} must be a contiguous fp32 [{x.shape[2]}] on {like.device}")
-        if weight.requires_grad:
-            _no_backward("rec_rotate_heads")
-    if x.requires_grad or out.requires_grad:
-        _no_backward("rec_rotate_heads")
-    return (x.data_ptr(), token, head), (out.data_ptr(), out_token, out_head), x.shape[1], weight.data_ptr() if weight is not None else 0, out
+_NO_ROWS = (0, 0, 0)
 
 
 def rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: torch.Tensor,
@@ -1022,19 +999,69 @@ def rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     q_weight, k_weight: fp32 [head_dim], or None: those rows are only rotated.  interleaved: columns 2 i and 2 i + 1 are a pair,
     else i and i + pairs.  Results are contiguous, or go to q_out and k_out, which may be q and k.  No backward pass, as in HistoryCache."""
     like = q if q is not None else k
-    code, index = (None, -1) if like is None else (_DTYPE_CODES.get(like.dtype), like.get_device())
+    dtype = None if like is None else like.dtype
+    code, index = (None, -1) if dtype is None else (_DTYPE_CODES.get(dtype), like.get_device())
     if code is None or index < 0 or like.dim() != 3:
         raise ValueError("rec_rotate_heads: q must be [tokens, heads, head_dim] and k [tokens, kv_heads, head_dim] on one device, fp32, fp16 or bf16")
-    q_at, q_to, heads, q_w, q_out = _turn_rows("q", q, q_out, q_weight, like)
-    k_at, k_to, kv_heads, k_w, k_out = _turn_rows("k", k, k_out, k_weight, like)
-    tokens, _, dim = like.shape
-    if positions.shape != (tokens,) or positions.dtype not in (_I32, _I64) or positions.get_device() != index or not positions.is_contiguous():
+    tokens, heads, dim = like.shape
+    q_at = q_to = k_at = k_to = _NO_ROWS
+    kv_heads = q_w = k_w = 0
+    if q is None:
+        heads = 0
+        if q_out is not None or q_weight is not None:
+            raise ValueError("rec_rotate_heads: q is None, but not its result or weight")
+    else:
+        q_at, q_to, q_out = _turn_rows("q", q, q_out, tokens, heads, dim, dtype, index)
+    if k is not None:
+        kv_heads = k.shape[1] if k.dim() == 3 else -1
+        k_at, k_to, k_out = _turn_rows("k", k, k_out, tokens, kv_heads, dim, dtype, index)
+    elif k_out is not None or k_weight is not None:
+        raise ValueError("rec_rotate_heads: k is None, but not its result or weight")
+    if q_weight is not None:
+        q_w = _turn_weight("q", q_weight, dim, index)
+    if k_weight is not None:
+        k_w = _turn_weight("k", k_weight, dim, index)
+    at = positions.dtype
+    if (at is not _I32 and at is not _I64) or positions.shape != (tokens,) or positions.get_device() != index or not positions.is_contiguous():
         raise ValueError(f"rec_rotate_heads: positions must be a contiguous int32 or int64 [{tokens}] on {like.device}")
-    if frequencies.dim() != 1 or frequencies.dtype is not torch.float64 or frequencies.get_device() != index or not frequencies.is_contiguous():
+    if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or frequencies.get_device() != index or not frequencies.is_contiguous():
         raise ValueError(f"rec_rotate_heads: frequencies must be a contiguous float64 vector on {like.device}")
     st = _lib.rec_rotate_heads(
-        _TURN.pack(*q_at, *k_at, *q_to, *k_to, code, heads, kv_heads, dim, tokens, positions.data_ptr(), positions.dtype is _I64,
-                   frequencies.shape[0], frequencies.data_ptr(), 1 if interleaved else 0, eps, q_w, k_w), _stream_on(index, "rec_rotate_heads"))
+        _TURN.pack(*q_at, *k_at, *q_to, *k_to, code, heads, kv_heads, dim, tokens, positions.data_ptr(), at is _I64,
+                   frequencies.numel(), frequencies.data_ptr(), 1 if interleaved else 0, eps, q_w, k_w), _stream_on(index, "rec_rotate_heads"))
     if st:
         raise RecError(st, "rec_rotate_heads")
     return q_out, k_out
+
+
+def _turn_rows(what: str, x: torch.Tensor, out: Optional[torch.Tensor], tokens: int, heads: int, dim: int, dtype, index: int):
+    """Address and strides of x and of where its result goes, and the result, made here if None."""
+    shape = (tokens, heads, dim)
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != index:
+        raise ValueError("rec_rotate_heads: q must be [tokens, heads, head_dim] and k [tokens, kv_heads, head_dim] on one device, fp32, fp16 or bf16")
+    token, head, column = x.stride()
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        to = (out.data_ptr(), heads * dim, dim)
+    else:
+        if out.shape != shape or out.dtype is not dtype or out.get_device() != index:
+            raise ValueError(f"rec_rotate_heads: the result of {what} must be of its shape, type and device")
+        if out.requires_grad:
+            _no_backward("rec_rotate_heads")
+        out_token, out_head, out_column = out.stride()
+        if out_column != 1:
+            raise ValueError(f"rec_rotate_heads: rows of {what}'s result must be contiguous")
+        to = (out.data_ptr(), out_token, out_head)
+    if column != 1:
+        raise ValueError(f"rec_rotate_heads: rows of {what} must be contiguous")
+    if x.requires_grad:
+        _no_backward("rec_rotate_heads")
+    return (x.data_ptr(), token, head), to, out
+
+
+def _turn_weight(what: str, weight: torch.Tensor, dim: int, index: int) -> int:
+    if weight.dtype is not _F32 or weight.shape != (dim,) or weight.get_device() != index or not weight.is_contiguous():
+        raise ValueError(f"rec_rotate_heads: the weight of {what} must be a contiguous fp32 [{dim}] on its device")
+    if weight.requires_grad:
+        _no_backward("rec_rotate_heads")
+    return weight.data_ptr()

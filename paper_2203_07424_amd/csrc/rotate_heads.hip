@@ -16,7 +16,7 @@ typedef double f64;
 
 constexpr int THREADS = 256;
 constexpr int CUS = 256;
-constexpr int STEPS = 4;  // rows of a lane on their way at once
+constexpr int STEPS = 2;  // rows of a lane on their way at once
 
 struct TurnArgs {
     rec_turn t;
@@ -88,6 +88,12 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(TurnArgs a)
         return const_cast<char *>(static_cast<const char *>(r.dev)) +
                SIZE * (token * r.token_stride + (is_k(head) ? head - a.t.heads : head) * r.head_stride);
     };
+    // Weights of queries and keys, ones where there are none, in LDS: in registers they would take as many as the rows on their way.
+    __shared__ float weights[2][D];
+    for (int i = threadIdx.x; i < 2 * D; i += THREADS) {
+        const float *w = i < D ? a.t.dev_q_weight : a.t.dev_k_weight;
+        weights[0][i] = w ? w[i % D] : 1.0f;
+    }
     u32x4 raw[STEPS][2];
     auto load = [&](int from) {
 #pragma unroll
@@ -95,12 +101,13 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(TurnArgs a)
             const int head = from + s * at_once;
             if (there && head < a.all) {
                 const char *p = row_of(a.t.q, a.t.k, head);
-                raw[s][0] = *reinterpret_cast<const u32x4 *>(p + SIZE * c0);
-                raw[s][1] = *reinterpret_cast<const u32x4 *>(p + SIZE * c1);
+                raw[s][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + SIZE * c0));
+                raw[s][1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + SIZE * c1));
             }
         }
     };
     load(first_head);
+    __syncthreads();
 
     float cosine[N], sine[N];
 #pragma unroll
@@ -117,16 +124,6 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(TurnArgs a)
             sincospif(2.0f * (float)turn, &sine[i], &cosine[i]);
         }
     }
-    // Weights of queries and keys; ones where there are none.
-    float wq[2][N], wk[2][N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        wq[0][i] = a.t.dev_q_weight ? a.t.dev_q_weight[c0 + i] : 1.0f;
-        wq[1][i] = a.t.dev_q_weight ? a.t.dev_q_weight[c1 + i] : 1.0f;
-        wk[0][i] = a.t.dev_k_weight ? a.t.dev_k_weight[c0 + i] : 1.0f;
-        wk[1][i] = a.t.dev_k_weight ? a.t.dev_k_weight[c1 + i] : 1.0f;
-    }
-
     for (int from = first_head;; from += STEPS * at_once) {
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
@@ -167,10 +164,11 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(TurnArgs a)
                     for (int i = 0; i < N; ++i) x[h][i] *= by;
             }
             float y[2][N];
+            const float *w = weights[is_k(head) ? 1 : 0];
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                x[0][i] *= is_k(head) ? wk[0][i] : wq[0][i];
-                x[1][i] *= is_k(head) ? wk[1][i] : wq[1][i];
+                x[0][i] *= w[c0 + i];
+                x[1][i] *= w[c1 + i];
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -188,8 +186,8 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(TurnArgs a)
             }
             if (mine) {
                 char *p = row_of(a.t.q_out, a.t.k_out, head);
-                *reinterpret_cast<u32x4 *>(p + SIZE * c0) = narrow<DT>(y[0]);
-                *reinterpret_cast<u32x4 *>(p + SIZE * c1) = narrow<DT>(y[1]);
+                __builtin_nontemporal_store(narrow<DT>(y[0]), reinterpret_cast<u32x4 *>(p + SIZE * c0));
+                __builtin_nontemporal_store(narrow<DT>(y[1]), reinterpret_cast<u32x4 *>(p + SIZE * c1));
             }
         }
         if (from - first_head + STEPS * at_once >= a.all) break;

@@ -109,7 +109,7 @@ def test_means(b):
 def test_python_refuses_tensors_that_do_not_fit(b, monkeypatch):
     monkeypatch.setattr(b, "_lib", None)
     h = object.__new__(b.HistoryCache)
-    h._index, h.head_dim, h.kv_heads, h.device, h._h = 0, 64, 2, "cuda:0", cache(b, num_pages=6)
+    h._index, h.head_dim, h.kv_heads, h.device, h._means_shape = 0, 64, 2, "cuda:0", (6, 2, 64)
     i32 = dict(dtype=torch.int32)
     q, means = on(torch.zeros(3, 2, 4, 64, dtype=torch.bfloat16)), on(torch.zeros(6, 2, 64, dtype=torch.bfloat16))
     table, n, chosen, prefix, one = (on(torch.zeros(s, **i32)) for s in ((3, 5), (3,), (3, 2, 2, 4), (7,), (1,)))
