@@ -13,7 +13,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librec_mi355x.so")
 
 SOURCES = ["scan.hip", "pool.hip", "pool_hot.hip", "gemm.hip", "gemm_big.hip", "gemm_split.hip", "mlp_chain.hip", "tail.hip", "front.hip", "lookup.hip", "interact.hip", "synth_fill.hip", "probe.hip", "rec_api.hip",
-           "history_cache.hip", "history_attend.hip", "history_select.hip", "history_shared.hip", "window_attend.hip", "rotate_heads.hip", "history_api.hip"]
+           "history_cache.hip", "history_attend.hip", "history_select.hip", "history_chosen.hip", "history_shared.hip", "window_attend.hip", "rotate_heads.hip", "history_api.hip"]
 
 # The packed-fp32 target feature is switched off for all device code.  A wave starts
 # with the first 16 words of its kernel's arguments in registers instead of loading

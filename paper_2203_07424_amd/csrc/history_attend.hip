@@ -41,10 +41,13 @@ namespace {
 
 constexpr int CUS = 256;
 
+// What a launch attends to: histories, or histories behind a prefix.
+enum { WHOLE, BEHIND };
+
 // Waves that a SIMD holds at once; the compiler gives a wave at most its share of registers.
-__host__ __device__ constexpr int waves_of(int format, int d, bool bf, int heads, int kind = 0)
+__host__ __device__ constexpr int waves_of(int format, int d, bool bf, int heads, int kind = WHOLE)
 {
-    if (kind == 2 && d == 32 && format == REC_MX8 && heads == 1) return 3;  // a row's parts besides
+    if (kind == BEHIND && d == 32 && format == REC_MX8 && heads == 1) return 3;  // a row's parts besides
     if (heads > 1) return d == 32 && format == REC_MX4 ? 3 : 2;
     return d == 128 ? (format == REC_MX4 && bf ? 3 : 2) : d == 64 ? (format == REC_MX4 && bf ? 4 : 3) : 4;
 }
@@ -61,18 +64,11 @@ struct AttendArgs {
     float *part_o;   // [splits][batch * queries * heads][D]
     f32x2 *part_ml;  // [splits][batch * queries * heads]
     bool parted;     // the results are parts, even of one split
-    // Chosen pages: q has a history for each query then, `queries` of them for each of the caller's.
-    const int32_t *chosen;  // [q.batch][kv_heads][width] pages of the history, or -1
-    int width, queries;
-    Divider by_queries;
     // Histories behind a prefix: their rows' sums over it, which results include.
     int before;            // parts of it
     const float *before_o;
     const f32x2 *before_ml;
 };
-
-// What a launch attends to: histories, pages of them that were chosen, histories behind a prefix.
-enum { WHOLE, CHOSEN, BEHIND };
 
 // Joins a row's sums x, of some columns, its weights' sum l and its maximum's exponent m with those of `parts` parts, in their order.
 // part: of the first part's same columns, `stride` elements apart; ml: of its maximum and sum.
@@ -105,71 +101,39 @@ __device__ inline long long out_row(const AttendArgs &a, int b, int kv, int row)
     return ((long long)b * a.q.queries + i) * a.q.heads + kv * a.per + (row - i * a.per);
 }
 
-// KIND CHOSEN: tokens are those of the chosen pages, one page after the other, and all rows stand at one position.
 template <int FMT, int D, bool BF, int W, int HEADS, int KIND>
 __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void attend_kernel(AttendArgs a)
 {
     static_assert(HEADS == 1 || W == 1, "several heads a wave: only where there are waves enough");
-    static_assert(HEADS == 1 || KIND != CHOSEN, "every kv head has pages of its own");
     constexpr int SLOT = ROWS / HEADS;  // rows of a kv head
     using T = std::conditional_t<BF, __bf16, _Float16>;
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int slot = c / SLOT, r = c % SLOT;  // which of the wave's kv heads, and its row
     // Parts of a history's head next to each other, then its heads, whose groups share a page.
-    // Queries of one history may have chosen the same pages: neighbours run on one XCD, of which blocks take turns.
-    int block = (int)blockIdx.x;
-    if constexpr (KIND == CHOSEN) {
-        const int all = (int)gridDim.x, xcd = block & 7;
-        block = xcd * (all >> 3) + min(xcd, all & 7) + (block >> 3);
-    }
-    const int pair = a.inner.of(block), part = block - pair * a.splits * a.row_tiles;
+    const int pair = a.inner.of((int)blockIdx.x), part = (int)blockIdx.x - pair * a.splits * a.row_tiles;
     const int b = a.heads.of(pair), first_kv = pair * HEADS - b * a.c.kv_heads, kv = first_kv + slot;
     const int row_tile = a.splits == 1 ? part : part / a.splits, split = part - row_tile * a.splits;
 
     const int shift = a.c.page_shift, most_tokens = a.q.table_width << shift;
-    const int history = KIND == CHOSEN ? a.by_queries.of(b) : b, query_of_history = b - history * a.queries;  // the latter for chosen pages
-    int len = a.q.dev_lengths[history];
+    int len = a.q.dev_lengths[b];
     if (len < 0 || len > most_tokens) {
-        if (threadIdx.x == 0 && first_kv == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)history);
+        if (threadIdx.x == 0 && first_kv == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)b);
         len = len < 0 ? 0 : most_tokens;
     }
     // Positions of this wave's rows: of its first, its last, and this lane's; -1 sees nothing.
     const int first_row = row_tile * ROWS, last_row = min(first_row + SLOT, a.rows) - 1, row = min(first_row + r, last_row);
     const bool real = first_row + r <= last_row;
     const bool together = a.q.candidates != 0;
-    auto position = [&](int row) {
-        if constexpr (KIND == CHOSEN) return together ? len - 1 : max(len - a.queries + query_of_history, -1);
-        else return together ? len - 1 : max(len - a.q.queries + a.by_per.of(row), -1);
-    };
+    auto position = [&](int row) { return together ? len - 1 : max(len - a.q.queries + a.by_per.of(row), -1); };
     const int p_lo = position(first_row), p_hi = position(last_row), pos = position(row);
     const int window = a.q.window == 0 ? 0x7fffffff : a.q.window, sinks = a.q.sinks;
-
-    // Chosen pages: lane i has the i-th of 64, its number in the history and its page, or -1.  A window of them is looked up at once, and
-    // a tile's pages are all in one.
-    const int32_t *const table = a.q.dev_pages_of + history * a.q.table_stride;
-    const int32_t *const chosen = a.chosen + (KIND == CHOSEN ? ((long long)b * a.c.kv_heads + first_kv) * a.width : 0);
-    int window_at = -1, window_number = -1, window_page = -1;
-    auto look_up = [&](int at) {
-        window_at = at;
-        const int i = 64 * at + lane;
-        window_number = i < a.width ? chosen[i] : -1;
-        window_page = -1;
-        if ((unsigned)window_number < (unsigned)a.q.table_width && window_number << shift <= p_hi) window_page = table[window_number];
-    };
 
     // Tiles that some row sees something of: [0, n_sink) and [n_from, n_to).
     int n_from = 0, n_sink = 0, n_to = 0;
     if (p_hi >= 0) {
-        if constexpr (KIND == CHOSEN) {
-            look_up(0);
-            int last = a.width;  // pages up to the last one, where that is known
-            if (a.width <= 64) last = 64 - __builtin_clzll(__ballot(window_number != -1) | 1ull);
-            n_to = (int)((((long long)last << shift) + TILE - 1) / TILE);
-        } else {
-            n_to = p_hi / TILE + 1;
-        }
-        if constexpr (KIND != CHOSEN) n_from = max(p_lo - window + 1, 0) / TILE;
-        if constexpr (KIND != CHOSEN) n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from);
+        n_to = p_hi / TILE + 1;
+        n_from = max(p_lo - window + 1, 0) / TILE;
+        n_sink = min((min(sinks, p_hi + 1) + TILE - 1) / TILE, n_from);
     }
     const int tiles = n_sink + n_to - n_from, each = (tiles + a.splits - 1) / a.splits;
     const int begin = min(split * each, tiles), end = min(begin + each, tiles);
@@ -185,9 +149,10 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
 
     if (begin + wave < end) {
         const int query = a.by_per.of(row), head = kv * a.per + row - query * a.per;
-        const long long row_bytes = 2 * (history * a.q.batch_stride + (KIND == CHOSEN ? query_of_history : query) * a.q.query_stride + head * a.q.head_stride);
+        const long long row_bytes = 2 * (b * a.q.batch_stride + query * a.q.query_stride + head * a.q.head_stride);
         // Positive, so that masked scores stay at -inf.
         const float factor = a.q.scale == 0.0f ? 1.0f : __builtin_fabsf(a.q.scale) * 1.44269504088896341f;
+        const int32_t *table = a.q.dev_pages_of + b * a.q.table_stride;
         const int groups = 1 << (shift - 4);
         const int head_bytes = groups * group_bytes<FMT>(D);
         const unsigned char *first_page = a.c.pages + (long long)first_kv * head_bytes;
@@ -199,16 +164,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
         // The page of a group's first token, or -1.
         auto page_of = [&](int token) {
             int page = -1;
-            if constexpr (KIND == CHOSEN) page = __shfl(window_page, token >> shift);
-            else if (token < len) page = table[token >> shift];
+            if (token < len) page = table[token >> shift];
             return page;
-        };
-        // Chosen pages: its number in the history.
-        auto number_of = [&](int token) { return KIND == CHOSEN ? __shfl(window_number, token >> shift) : 0; };
-        // Before the pages of tile n are asked for.
-        auto at_tile = [&](int n) {
-            if constexpr (KIND == CHOSEN)
-                if (n >> shift != window_at) look_up(n >> shift);
         };
         auto group_at = [&](int page, int token) {
             const bool ok = (unsigned)page < pages;  // else some group that is there: its tokens count for nothing
@@ -217,8 +174,7 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
         };
 
         int n = begin + wave, key = key_of(n);
-        at_tile(n);
-        int k_page = page_of(key + 16 * (c >> 2)), v_page = page_of(key + 16 * g), v_number = number_of(key + 16 * g);
+        int k_page = page_of(key + 16 * (c >> 2)), v_page = page_of(key + 16 * g);
         Query<D, BF> q;
         q.fetch(real ? static_cast<const char *>(a.q.dev_q) + row_bytes : nullptr, g);
         Tile<FMT, D> tile[HEADS];
@@ -228,15 +184,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
         for (int h = 0; h < HEADS; ++h) load_keys(h, key);
 #pragma unroll
         for (int h = 0; h < HEADS; ++h) load_values(h, v_page, key);
-        k_page = -1;
-        int v_next = -1, v_number_next = -1;
-        auto ask = [&](int n) {
-            at_tile(n);
-            k_page = page_of(key_of(n) + 16 * (c >> 2));
-            v_next = page_of(key_of(n) + 16 * g);
-            v_number_next = number_of(key_of(n) + 16 * g);
-        };
-        if (n + W < end) ask(n + W);
+        k_page = n + W < end ? page_of(key_of(n + W) + 16 * (c >> 2)) : -1;
+        int v_next = n + W < end ? page_of(key_of(n + W) + 16 * g) : -1;
         q.convert(a.q.scale < 0.0f ? -1.0f : a.q.scale == 0.0f ? 0.0f : 1.0f, g);  // while the first tile is on its way
         for (;; n += W) {
             const bool more = n + W < end;
@@ -256,24 +205,18 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
 
             // Groups come with their page or not at all.
             const bool there = (unsigned)v_page < pages;
-            // Where group g's tokens stand in the history.
-            const int first = KIND == CHOSEN ? (v_number << shift) + ((key + 16 * g) & ((1 << shift) - 1)) : key + 16 * g;
-            bool whole = KIND == CHOSEN ? __all(there && first + 15 <= p_hi) : key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there);
+            const bool whole = key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there);
             unsigned nan = 0;  // bit 4 h + b: row c sees a NaN in block b of head h's values
             if (!whole) {
                 // Bit t: row c sees token t of group g; some row does.
+                const int first = key + 16 * g;
                 auto upto = [&](int at) { return below(max(at - first, -1) + 1); };
                 auto before = [&](int at) { return below(max(at - first, -1) - window + 1); };
                 unsigned seen = upto(pos) & (~before(pos) | below(sinks - first));
                 unsigned used = upto(p_hi) & (~before(p_lo) | below(sinks - first));
                 if (!there) {
-                    if constexpr (KIND == CHOSEN) {
-                        used = (unsigned)v_number < (unsigned)a.q.table_width && v_number << shift <= p_hi;
-                        if (!used && v_number != -1 && (unsigned)v_number >= (unsigned)a.q.table_width && c == 0)
-                            report(a.c.fault, REC_FAULT_SLOT, (unsigned long long)(chosen - a.chosen + ((key + 16 * g) >> shift)));
-                    }
                     if (used && c == 0)
-                        report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)history * (unsigned)a.q.table_width + (unsigned)(KIND == CHOSEN ? v_number : first >> shift));
+                        report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)b * (unsigned)a.q.table_width + (unsigned)(first >> shift));
                     seen = used = 0;
                 }
                 saw |= seen;
@@ -361,9 +304,9 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
             for (int h = 0; h < HEADS; ++h) load_values(h, v_next, key_next);
             key = key_next;
             v_page = v_next;
-            v_number = v_number_next;
             if (n + 2 * W < end) {
-                ask(n + 2 * W);
+                k_page = page_of(key_of(n + 2 * W) + 16 * (c >> 2));
+                v_next = page_of(key_of(n + 2 * W) + 16 * g);
             }
         }
     }
@@ -456,8 +399,7 @@ struct Plan {
     bool join = true;  // parts become results
 };
 
-// two_heads: a wave may have two kv heads.
-Plan plan_of(const Cache &c, int format, int d, const rec_query &q, bool two_heads = true)
+Plan plan_of(const Cache &c, int format, int d, const rec_query &q)
 {
     Plan p;
     p.per = q.heads / c.kv_heads;
@@ -480,7 +422,7 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, bool two_hea
     p.waves = (tiles >= 4 && pairs < 4 * CUS) || (tiles >= 16 && pairs <= 32 * CUS) ? 4 : tiles >= 2 && pairs < 8 * CUS ? 2 : 1;
     // A wave has room for the rows of several kv heads: masks, exponentials and the rows' terms
     // then cost it no more than for one.
-    if (two_heads && d <= 64 && p.waves == 1 && pairs >= 16 * CUS) p.heads = rows <= ROWS / 2 && c.kv_heads % 2 == 0 ? 2 : 1;
+    if (d <= 64 && p.waves == 1 && pairs >= 16 * CUS) p.heads = rows <= ROWS / 2 && c.kv_heads % 2 == 0 ? 2 : 1;
     // Long histories of few pairs: as many parts as are all at work at once (a part too many waits
     // for a place and then reads alone: 4 parts of 256 pairs in 3 places 221 us, 3 parts 199), of two tiles a wave at least.
     // Where pairs alone take all places, parts of eight tiles a wave, up to four, for the longest of ragged
@@ -495,7 +437,7 @@ template <int FMT, int D, bool BF, int KIND>
 hipError_t attend_as(const AttendArgs &a, const Plan &p, hipStream_t s)
 {
     const dim3 grid((unsigned)((long long)a.q.batch * a.c.kv_heads / p.heads * p.row_tiles * p.splits));
-    if constexpr (D <= 64 && KIND != CHOSEN)
+    if constexpr (D <= 64)
         if (p.heads == 2) {
             hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 2, KIND>), grid, dim3(64), 0, s, a);
             return hipGetLastError();
@@ -513,7 +455,6 @@ template <int FMT, int D>
 hipError_t attend_of(const AttendArgs &a, const Plan &p, hipStream_t s)
 {
     const bool bf = a.q.dtype == REC_BF16;
-    if (a.chosen) return bf ? attend_as<FMT, D, true, CHOSEN>(a, p, s) : attend_as<FMT, D, false, CHOSEN>(a, p, s);
     if (a.before) return bf ? attend_as<FMT, D, true, BEHIND>(a, p, s) : attend_as<FMT, D, false, BEHIND>(a, p, s);
     return bf ? attend_as<FMT, D, true, WHOLE>(a, p, s) : attend_as<FMT, D, false, WHOLE>(a, p, s);
 }
@@ -540,8 +481,6 @@ AttendArgs args_of(const Cache &c, int d, const rec_query &q, const Plan &p, voi
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = reinterpret_cast<f32x2 *>(a.part_o + (p.splits > 1 ? p.splits * p.rows * d : 0));
     a.parted = p.splits > 1;
-    a.chosen = nullptr;
-    a.width = a.queries = 0;
     a.before = 0;
     return a;
 }
@@ -549,22 +488,6 @@ AttendArgs args_of(const Cache &c, int d, const rec_query &q, const Plan &p, voi
 size_t workspace_of(const Plan &p, int d) { return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)p.rows * ((size_t)d * sizeof(float) + sizeof(f32x2)); }
 
 long long threads_of(const Cache &c, const rec_query &q, const Plan &p) { return (long long)q.batch * c.kv_heads * p.row_tiles * p.splits * 64 * p.waves; }
-
-// Chosen pages: each query is a history of its own, whose tokens are theirs.
-rec_query by_query(const rec_query &q)
-{
-    rec_query one = q;
-    one.batch = q.batch * q.queries;
-    one.queries = q.queries ? 1 : 0;
-    return one;
-}
-
-Plan chosen_plan_of(const Cache &c, int format, int d, const rec_query &q, int count)
-{
-    rec_query one = by_query(q);
-    one.table_width = count;
-    return plan_of(c, format, d, one, false);
-}
 
 }  // namespace
 
@@ -602,27 +525,6 @@ hipError_t launch_attend(const Cache &c, int format, int d, const rec_query &q, 
 {
     const Plan p = plan_of(c, format, d, q);
     return attend_any(args_of(c, d, q, p, workspace), p, format, d, s);
-}
-
-long long chosen_threads(const Cache &c, int format, int d, const rec_query &q, int count)
-{
-    return threads_of(c, by_query(q), chosen_plan_of(c, format, d, q, count));
-}
-
-size_t chosen_workspace(const Cache &c, int format, int d, const rec_query &q, int count)
-{
-    return q.batch == 0 || q.queries == 0 ? 0 : workspace_of(chosen_plan_of(c, format, d, q, count), d);
-}
-
-hipError_t launch_chosen(const Cache &c, int format, int d, const rec_query &q, const int32_t *chosen, int count, void *workspace, hipStream_t s)
-{
-    const Plan p = chosen_plan_of(c, format, d, q, count);
-    AttendArgs a = args_of(c, d, by_query(q), p, workspace);
-    a.chosen = chosen;
-    a.width = count;
-    a.queries = q.queries;
-    a.by_queries = Divider(q.queries);
-    return attend_any(a, p, format, d, s);
 }
 
 }  // namespace hist

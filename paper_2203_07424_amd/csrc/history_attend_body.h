@@ -345,6 +345,25 @@ __device__ inline void clear_nan_codes(Tile<REC_MX8, D> &t, unsigned seen, f32x4
 // Bits [0, n) of a lane's 16 tokens, for any n.
 __device__ inline unsigned below(int n) { return (1u << min(max(n, 0), 16)) - 1u; }
 
+// Eight columns of a row from the W waves that have a share of its keys: sums x and y, the weights' sum l and the maximum's exponent m.
+template <int W, int LD, int N>
+__device__ inline void join_waves(const float (&o_of)[W][N][LD], const f32x2 (&ml_of)[W][N], int r, int col, float &m, float &l, f32x4 &x, f32x4 &y)
+{
+    m = neg_inf();
+#pragma unroll
+    for (int w = 0; w < W; ++w) m = fmaxf(m, ml_of[w][r][0]);
+    l = 0.0f;
+    x = y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const f32x2 ml = ml_of[w][r];
+        const float by = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - m);
+        l += ml[1] * by;
+        x += *reinterpret_cast<const f32x4 *>(&o_of[w][r][col]) * by;
+        y += *reinterpret_cast<const f32x4 *>(&o_of[w][r][col + 4]) * by;
+    }
+}
+
 // Joins the at most 64 parts of a row by a block: a lane looks up a part's weight, then groups
 // of D / 4 threads add up a share of the parts' sums, all loaded at once, and meet in LDS.  Always in the same order.  (A thread for all parts of its columns took 20 us for 64.)
 template <int D, bool BF>

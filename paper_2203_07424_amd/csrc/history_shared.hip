@@ -215,19 +215,9 @@ __global__ __launch_bounds__(256) void narrow_kernel(SharedArgs a)
         const int at = a.by_per.of(row), b = a.by_queries.of(at);
         // A query before its history's first token sees nothing.
         const bool sees = a.q.candidates || min(max(a.q.dev_lengths[b], 0), a.q.table_width << shift) - a.q.queries + at - b * a.q.queries >= 0;
-        float most = neg_inf();
-#pragma unroll
-        for (int w = 0; w < W; ++w) most = fmaxf(most, ml_of[w][r][0]);
-        float sum = 0.0f;
-        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const f32x2 ml = ml_of[w][r];
-            const float by = ml[0] == neg_inf() ? (ml[1] == 0.0f ? 0.0f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - most);
-            sum += ml[1] * by;
-            x += *reinterpret_cast<const f32x4 *>(&o_of[w][r][col]) * by;
-            y += *reinterpret_cast<const f32x4 *>(&o_of[w][r][col + 4]) * by;
-        }
+        float most, sum;
+        f32x4 x, y;
+        join_waves(o_of, ml_of, r, col, most, sum, x, y);
         if (!sees) {
             most = neg_inf();
             sum = 0.0f;
