@@ -278,7 +278,9 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int count)
     if (blocks == 0) return p;
     // As many waves of a block as are all at work at once, then parts in blocks of their own, of two tiles a wave at least.
     while (p.waves < 8 && 2 * p.waves <= tiles && 2 * p.waves * blocks <= room) p.waves *= 2;
-    p.splits = (int)std::max(1ll, std::min({room / (blocks * p.waves), tiles / (2 * p.waves), 64ll}));
+    // Two parts are not worth their joining.
+    const long long parts = std::min({room / (blocks * p.waves), tiles / (2 * p.waves), 64ll});
+    p.splits = parts > 2 ? (int)parts : 1;
     return p;
 }
 

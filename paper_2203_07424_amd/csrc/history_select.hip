@@ -149,6 +149,50 @@ __device__ inline int pages_up_to(const SelectArgs &a, int len, int i)
     return p < 0 ? 0 : (p >> a.c.page_shift) + 1;
 }
 
+// What lane l + SHIFT of a row of 16 has (beyond it: 0).
+template <int SHIFT>
+__device__ inline f64 later_lane(f64 x)
+{
+    const u64 u = __builtin_bit_cast(u64, x);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, 0x100 + SHIFT, 0xf, 0xf, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), 0x100 + SHIFT, 0xf, 0xf, false);
+    return __builtin_bit_cast(f64, (u64)hi << 32 | lo);
+}
+
+// Sums of lanes up to each.
+__device__ inline unsigned sums_up_to(unsigned x)
+{
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);  // by 1, 2, 4 and 8 lanes of a row of 16
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // a row's last to the next row
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);  // lane 31's to the upper half
+    return x;
+}
+
+// f over all lanes, in each of them, without a trip through LDS or the scalar unit: what a wave that works by itself waits for most.
+template <class F>
+__device__ inline unsigned over_lanes(unsigned x, const F &f)
+{
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));   // lanes l ^ 1
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));   // l ^ 2
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));  // the other four of eight
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));  // the other eight of a row
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = f((unsigned)r[0], (unsigned)r[1]);
+    const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return f((unsigned)h[0], (unsigned)h[1]);
+}
+__device__ inline unsigned total(unsigned x)
+{
+    return over_lanes(x, [](unsigned a, unsigned b) { return a + b; });
+}
+__device__ inline unsigned largest(unsigned x)
+{
+    return over_lanes(x, [](unsigned a, unsigned b) { return max(a, b); });
+}
+
 // Tiles n, n + step ... before `end` of pages [from, to).
 struct Walk {
     int from, to, n, step, end;
@@ -157,50 +201,73 @@ struct Walk {
 // Scores of a wave's 16 rows: the heads of `queries` queries from first_query on, of history b and kv head kv, over the pages of
 // walk(), which is asked once the rows are on their way.  store(query - first_query, page, key).  FEW: at most four rows, on 4 x 4 x 4,
 // which has four products of as many pages and takes half the time.
+// Means are loaded a row after the other (a lane of the operand has a page of its own, and 16 lines at once for 16 lanes
+// were what bounded this) and get to their lanes through `lds`, 16 rows of this wave's own, whose pieces are exchanged by the row's number.
 template <int D, bool BF, bool FEW, class W, class F>
-__device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first_query, int queries, const W &walk, const F &store)
+__device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first_query, int queries, u32x4 *lds, const W &walk, const F &store)
 {
-    constexpr int N = D / 4;  // columns of a lane: group g has N g ...
+    constexpr int N = D / 4;  // columns of a lane: pieces of eight, g, g + 4 ...
+    constexpr int CH = D / 8, AT_ONCE = 64 / CH;  // pieces of a row, rows of a load
     constexpr int PER_LANE = FEW ? 1 : 4;  // results
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4, column = FEW ? lane & 3 : j;
     const int heads = min(a.per, 16), rows = queries * heads, row_tiles = (a.per + 15) / 16;
     const int row = min(column, rows - 1), query = row / heads;
-    const char *mine = static_cast<const char *>(a.q.dev_q) + 2 * (b * a.q.batch_stride + (first_query + query) * a.q.query_stride + N * g);
+    const char *mine = static_cast<const char *>(a.q.dev_q) + 2 * (b * a.q.batch_stride + (first_query + query) * a.q.query_stride + 8 * g);
     u32x4 x[N / 8];
     auto load_rows = [&](int t) {
         const char *q = mine + 2 * (kv * a.per + min(16 * t + row - query * heads, a.per - 1)) * a.q.head_stride;
 #pragma unroll
-        for (int i = 0; i < N / 8; ++i) x[i] = *reinterpret_cast<const u32x4 *>(q + 16 * i);
+        for (int i = 0; i < N / 8; ++i) x[i] = *reinterpret_cast<const u32x4 *>(q + 64 * i);
     };
     load_rows(0);
 
     const Walk w = walk();
     const int32_t *table = a.q.dev_pages_of + b * a.q.table_stride;
     const u32x4 *means = static_cast<const u32x4 *>(a.sel.means);
-    auto page_of = [&](int n) {
-        const int number = n * PAGES + j;
+    // Four tiles at a time: lane group g has the pages of the g-th, and the means of all are on their way together.
+    constexpr int BATCH = 4;
+    auto look_up = [&](int n) {
+        const int tile = n + g * w.step, number = tile * PAGES + j;
         int page = -1;
-        if (n < w.end && number >= w.from && number < w.to) page = table[number];
+        if (tile < w.end && number >= w.from && number < w.to) {
+            page = table[number];
+            if (page < 0 || (long long)page >= a.c.num_pages) {
+                report(a.c.fault, REC_FAULT_PAGE, (u64)b * (unsigned)a.q.table_width + (unsigned)number);
+                page = -1;
+            }
+        }
         return page;
     };
-    auto there = [&](int page) { return page >= 0 && (long long)page < a.c.num_pages; };
-    u32x4 raw[2][N / 8];
-    auto load_means = [&](u32x4 (&raw)[N / 8], int page) {
+    u32x4 loaded[BATCH][N / 8];
+    auto load_means = [&](int pages) {
+#pragma unroll
+        for (int t = 0; t < BATCH; ++t)
+#pragma unroll
+            for (int i = 0; i < N / 8; ++i) {
+                const int page = __shfl(pages, 16 * t + i * AT_ONCE + lane / CH);
+                loaded[t][i] = u32x4{0u, 0u, 0u, 0u};
+                if (page >= 0) loaded[t][i] = means[((long long)page * a.c.kv_heads + kv) * CH + lane % CH];
+            }
+    };
+    auto exchange = [&](const u32x4 (&loaded)[N / 8], u32x4 (&raw)[N / 8]) {
 #pragma unroll
         for (int i = 0; i < N / 8; ++i) {
-            raw[i] = u32x4{0u, 0u, 0u, 0u};
-            if (there(page)) raw[i] = means[(((long long)page * a.c.kv_heads + kv) * D + N * g) / 8 + i];
+            const int row = i * AT_ONCE + lane / CH;
+            lds[row * CH + (lane % CH ^ row % CH)] = loaded[i];
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) raw[i] = lds[j * CH + ((4 * i + g) ^ j % CH)];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     };
     auto element = [](u32x4 w, int k, bool bf) -> f64 {
         if (bf) return (f64) __builtin_bit_cast(float, k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
         return (f64) __builtin_bit_cast(f16x8, w)[k];
     };
-    // The means of the next tile are on their way while one is multiplied.
-    auto score = [&](const u32x4 (&raw)[N / 8], int n, int page) {
-        const int number = n * PAGES + j;
-        if (!there(page) && g == 0 && number >= w.from && number < w.to) report(a.c.fault, REC_FAULT_PAGE, (u64)b * (unsigned)a.q.table_width + (unsigned)number);
-        const unsigned known = (unsigned)__ballot(there(page)) & 0xffffu;
+    // known: bit i, page i of the tile is one.
+    auto score = [&](const u32x4 (&raw)[N / 8], int n, unsigned known) {
         f64 best[PER_LANE];
 #pragma unroll
         for (int r = 0; r < PER_LANE; ++r) best[r] = -__builtin_inf();
@@ -235,28 +302,31 @@ __device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first
         }
 #pragma unroll
         for (int r = 0; r < PER_LANE; ++r) {
+            // The largest of `heads` neighbours from a query's first lane on: of twice as many each time, then of two such sets that overlap.
             f64 most = best[r];
-            for (int d = 1; d < heads; ++d) {
-                const f64 other = __shfl(best[r], lane + d);
-                most = other > most ? other : most;
-            }
+            auto with = [&](f64 other) { most = other > most ? other : most; };
+            if (heads > 1) with(later_lane<1>(most));
+            if (heads > 3) with(later_lane<2>(most));
+            if (heads > 7) with(later_lane<4>(most));
+            if (heads > 15) with(later_lane<8>(most));
+            if (heads & (heads - 1)) with(__shfl(most, lane + heads - (1 << (31 - __builtin_clz(heads)))));
             // Row r of a lane's four: page 4 r + g; of four products: page g of the lane's own.
             const int in_tile = FEW ? (lane >> 2 & 3) * 4 + g : 4 * r + g, number = n * PAGES + in_tile;
             if (column == query * heads && column < rows && number >= w.from && number < w.to) store(query, number, key_of(known >> in_tile & 1 ? most : -__builtin_inf()));
         }
     };
-    int n = w.n, page = page_of(n), next = page_of(n + w.step);
-    load_means(raw[0], page);
-    for (; n < w.end; n += 2 * w.step) {
-        load_means(raw[1], next);
-        int after = page_of(n + 2 * w.step);
-        score(raw[0], n, page);
-        if (n + w.step >= w.end) break;
-        load_means(raw[0], after);
-        page = after;
-        after = page_of(n + 3 * w.step);
-        score(raw[1], n + w.step, next);
-        next = after;
+    int pages = look_up(w.n);
+    for (int n = w.n; n < w.end; n += BATCH * w.step) {
+        load_means(pages);
+        const u64 known = __ballot(pages >= 0);
+        pages = look_up(n + BATCH * w.step);
+#pragma unroll
+        for (int t = 0; t < BATCH; ++t) {
+            if (n + t * w.step >= w.end) break;
+            u32x4 raw[N / 8];
+            exchange(loaded[t], raw);
+            score(raw, n + t * w.step, (unsigned)(known >> (16 * t)) & 0xffffu);
+        }
     }
 }
 
@@ -277,8 +347,9 @@ __global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a)
     if (b >= a.q.batch) return;
     const int first_query = tile * a.at_once, queries = min(a.at_once, a.q.queries - first_query);
     u64 *keys = a.sel.keys + (((long long)b * a.q.queries + first_query) * a.c.kv_heads + kv) * a.q.table_width;
+    __shared__ u32x4 rows[THREADS / 64][PAGES * D / 8];
     score_pages<D, BF, FEW>(
-        a, b, kv, first_query, queries,
+        a, b, kv, first_query, queries, rows[threadIdx.x >> 6],
         [&]() {
             Walk w = between(a, pages_up_to(a, length_of(a, b, false), first_query + queries - 1), 0, 1, (walk + 1) * a.each);
             w.n = max(w.n, walk * a.each);
@@ -288,32 +359,6 @@ __global__ __launch_bounds__(THREADS) void score_kernel(SelectArgs a)
 }
 
 // --------------------------------------------------------------------- choice
-// Sums of lanes up to each, without a trip through LDS or the scalar unit: counts by ballots took 60 cycles each.
-__device__ inline unsigned sums_up_to(unsigned x)
-{
-    auto shifted = [](unsigned x, auto control, auto rows) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, control(), rows(), 0xf, false); };
-    x += shifted(x, std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());  // by 1, 2, 4 and 8 lanes of a row of 16
-    x += shifted(x, std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
-    x += shifted(x, std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
-    x += shifted(x, std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
-    x += shifted(x, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());  // a row's last to the next row
-    x += shifted(x, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());  // lane 31's to the upper half
-    return x;
-}
-__device__ inline unsigned last_lane(unsigned x) { return (unsigned)__builtin_amdgcn_readlane((int)x, 63); }
-// The largest of all lanes.
-__device__ inline unsigned largest(unsigned x)
-{
-    auto shifted = [](unsigned x, auto control, auto rows) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, control(), rows(), 0xf, false); };
-    x = max(x, shifted(x, std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>()));
-    x = max(x, shifted(x, std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>()));
-    x = max(x, shifted(x, std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>()));
-    x = max(x, shifted(x, std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>()));
-    x = max(x, shifted(x, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>()));
-    x = max(x, shifted(x, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>()));
-    return last_lane(x);
-}
-
 // What the waves of a row tell each other.
 template <int W>
 struct Meeting {
@@ -323,36 +368,31 @@ template <>
 struct Meeting<1> {};
 
 // The choice of one row, by W waves with KEYS of its scores in each lane at a time: of the pages up to `there`, whose scores are keys[page - first].
-template <int W, int KEYS>
-__device__ inline void choose(const SelectArgs &a, const u64 *keys, int there, int32_t *out, Meeting<W> &m)
+// ONE: all scores are in lanes at once.
+template <int W, int KEYS, bool ONE>
+__device__ inline void choose_between(const SelectArgs &a, const u64 *keys, int n, int32_t *out, Meeting<W> &m)
 {
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), thread = 64 * wave + lane;
-    if (there <= a.sel.count) {  // all of them
-        for (int i = thread; i < a.sel.count; i += 64 * W) out[i] = i < there ? i : -1;
-        return;
-    }
-    const int first = a.sel.first, last = a.sel.last, want = a.sel.count - first - last, n = there - first - last;
-    for (int i = thread; i < first; i += 64 * W) out[i] = i;
-    for (int i = thread; i < last; i += 64 * W) out[a.sel.count - last + i] = there - last + i;
-    if (want == 0) return;
-
+    const int first = a.sel.first, want = a.sel.count - first - a.sel.last;
     constexpr int CHUNK = 64 * W * KEYS;
-    const bool one_chunk = n <= CHUNK;
     u64 key[KEYS];  // neighbouring pages'; 0 behind the last
     auto load = [&](int from) {
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
             const int k = from + thread * KEYS + i;
-            key[i] = k < n ? keys[k] : 0;
+            key[i] = 0;
+            if (k < n) key[i] = keys[k];
         }
     };
     auto each_chunk = [&](auto f) {
-        for (int from = 0; from < n; from += CHUNK) {
-            if (!one_chunk) load(from);
-            f(from);
-        }
+        if constexpr (ONE) f(0);
+        else
+            for (int from = 0; from < n; from += CHUNK) {
+                load(from);
+                f(from);
+            }
     };
-    load(0);
+    if constexpr (ONE) load(0);
     int turn = 0;
     // Two words of each wave to all.
     auto meet = [&](unsigned x, unsigned y, auto f) {
@@ -375,8 +415,8 @@ __device__ inline void choose(const SelectArgs &a, const u64 *keys, int there, i
 #pragma unroll
             for (int i = 0; i < KEYS; ++i) c += is(key[i]) ? 1u : 0u;
         });
-        meet(last_lane(sums_up_to(c)), 0, [&](int, unsigned x, unsigned) { all += x; });
-        return all;
+        meet(total(c), 0, [&](int, unsigned x, unsigned) { all += x; });
+        return (int)all;
     };
 
     // The score that `want` pages reach lies in [low, high].  Half way between as numbers, by their upper halves, which takes as many
@@ -384,41 +424,44 @@ __device__ inline void choose(const SelectArgs &a, const u64 *keys, int there, i
     unsigned highest = 0, lowest = 0;  // the latter's complement
     each_chunk([&](int) {
 #pragma unroll
-        for (int i = 0; i < KEYS; ++i)
-            if (key[i]) {
-                highest = max(highest, (unsigned)(key[i] >> 32));
-                lowest = max(lowest, ~(unsigned)(key[i] >> 32));
-            }
+        for (int i = 0; i < KEYS; ++i) {
+            const unsigned top = (unsigned)(key[i] >> 32);
+            highest = max(highest, top);
+            lowest = max(lowest, top ? ~top : 0u);
+        }
     });
     unsigned low = ~0u, high = 0;
     meet(largest(highest), largest(lowest), [&](int, unsigned x, unsigned y) {
         high = max(high, x);
         low = min(low, ~y);
     });
-    bool found = false;
-    for (int i = 0; i < 16 && !found && high - low > 1; ++i) {
+    int c = 0;
+    for (int i = 0; i < 16; ++i) {
+        asm("" : "+v"(low), "+v"(high));  // all the same, but kept from the scalar unit, which a vector instruction waits for
         // Of the numbers that these halves begin, the mean's; not a number, or none between them: half way as they are.
         const f64 mean = 0.5 * number_of((u64)low << 32) + 0.5 * number_of((u64)high << 32);
         unsigned middle = (unsigned)(key_of(mean) >> 32);
         if (!(middle > low && middle <= high)) middle = low + (high - low + 1) / 2;
-        const unsigned c = count([&](u64 k) { return (unsigned)(k >> 32) >= middle; });
-        if (c >= (unsigned)want) low = middle;
-        else high = middle - 1;
-        found = c == (unsigned)want;
+        c = count([&](u64 k) { return (unsigned)(k >> 32) >= middle; });
+        const bool enough = c >= want;
+        low = enough ? middle : low;
+        high = enough ? high : middle - 1;
+        if (__any(c == want || high <= low)) break;
     }
     u64 bar = (u64)low << 32;
-    if (!found) {
+    if (__any(c != want)) {
         const u64 top = (u64)high << 32 | 0xffffffffu, differ = bar ^ top;
         int bit = 63 - __builtin_clzll(differ);
         bar &= bit == 63 ? 0ull : ~0ull << (bit + 1);
         for (; bit >= 0; --bit) {
+            asm("" : "+v"(bar), "+v"(bit));
             const u64 higher = bar | 1ull << bit;
-            const unsigned c = count([&](u64 k) { return k >= higher; });
-            if (c >= (unsigned)want) bar = higher;
-            if (c == (unsigned)want) break;
+            c = count([&](u64 k) { return k >= higher; });
+            bar = c >= want ? higher : bar;
+            if (__any(c == want)) break;
         }
     }
-    const int above = (int)count([&](u64 k) { return k > bar; }), ties = want - above;
+    const int ties = want - count([&](u64 k) { return k > bar; });
 
     // In order: those above the bar, and of those at it the first.
     int taken = 0, tied = 0;  // before this chunk
@@ -431,14 +474,16 @@ __device__ inline void choose(const SelectArgs &a, const u64 *keys, int there, i
         }
         const unsigned gt_sum = sums_up_to(gt), eq_sum = sums_up_to(eq);
         int mine = taken + (int)(gt_sum - gt), mine_tied = tied + (int)(eq_sum - eq);
-        meet(last_lane(gt_sum), last_lane(eq_sum), [&](int w, unsigned x, unsigned y) {
-            taken += (int)x;
-            tied += (int)y;
-            if (W > 1 && w < wave) {
-                mine += (int)x;
-                mine_tied += (int)y;
-            }
-        });
+        if (!ONE || W > 1)
+            meet((unsigned)__builtin_amdgcn_readlane((int)gt_sum, 63), (unsigned)__builtin_amdgcn_readlane((int)eq_sum, 63), [&](int w, unsigned x, unsigned y) {
+                taken += (int)x;
+                tied += (int)y;
+                if (W > 1 && w < wave) {
+                    mine += (int)x;
+                    mine_tied += (int)y;
+                }
+            });
+        if (gt + eq == 0) return;
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
             const bool over = key[i] > bar, at = key[i] == bar;
@@ -447,6 +492,22 @@ __device__ inline void choose(const SelectArgs &a, const u64 *keys, int there, i
             mine_tied += at;
         }
     });
+}
+
+template <int W, int KEYS>
+__device__ inline void choose(const SelectArgs &a, const u64 *keys, int there, int32_t *out, Meeting<W> &m)
+{
+    const int thread = W == 1 ? threadIdx.x & 63 : threadIdx.x, first = a.sel.first, last = a.sel.last;
+    if (there <= a.sel.count) {  // all of them
+        for (int i = thread; i < a.sel.count; i += 64 * W) out[i] = i < there ? i : -1;
+        return;
+    }
+    for (int i = thread; i < first; i += 64 * W) out[i] = i;
+    for (int i = thread; i < last; i += 64 * W) out[a.sel.count - last + i] = there - last + i;
+    if (a.sel.count == first + last) return;
+    const int n = there - first - last;
+    if (n <= 64 * W * KEYS) choose_between<W, KEYS, true>(a, keys, n, out, m);
+    else choose_between<W, KEYS, false>(a, keys, n, out, m);
 }
 
 template <int W, int KEYS>
@@ -470,8 +531,9 @@ __global__ __launch_bounds__(64 * WAVES) void select_kernel(SelectArgs a)
     const int b = a.by_heads.of(pair), kv = pair - b * a.c.kv_heads;
     const int first_query = tile * a.at_once, queries = min(a.at_once, a.q.queries - first_query);
     int len = 0;
+    __shared__ u32x4 rows[WAVES][PAGES * D / 8];
     score_pages<D, BF, FEW>(
-        a, b, kv, first_query, queries,
+        a, b, kv, first_query, queries, rows[wave],
         [&]() {
             len = length_of(a, b, threadIdx.x == 0 && kv == 0 && tile == 0);
             const int there = pages_up_to(a, len, first_query + queries - 1);
@@ -486,11 +548,11 @@ __global__ __launch_bounds__(64 * WAVES) void select_kernel(SelectArgs a)
     }
 }
 
-// Keys that a block has in LDS: two blocks of a compute unit at once.
-constexpr int MOST_KEYS = 8192;
+// Keys that a block has in LDS beside its waves' rows.
+constexpr int MOST_KEYS = 4096;
 
 // Waves of a block that does both, by the tiles of a row.
-int select_waves(const rec_query &q) { return q.table_width > 16 * PAGES ? 16 : 8; }
+int select_waves(const rec_query &q) { return q.table_width > 4 * PAGES ? 8 : 4; }
 
 SelectArgs args_of(const Cache &c, const rec_query &q)
 {
@@ -554,8 +616,8 @@ hipError_t scored_as(const SelectArgs &a, hipStream_t s)
     if (a.walks == 0) {
         const dim3 grid((unsigned)((long long)a.q.batch * a.c.kv_heads * a.query_tiles));
         const size_t lds = sizeof(u64) * a.at_once * std::max(a.q.table_width, 1);
-        if (select_waves(a.q) == 16) hipLaunchKernelGGL((select_kernel<D, BF, FEW, 16>), grid, dim3(1024), lds, s, a);
-        else hipLaunchKernelGGL((select_kernel<D, BF, FEW, 8>), grid, dim3(512), lds, s, a);
+        if (select_waves(a.q) == 8) hipLaunchKernelGGL((select_kernel<D, BF, FEW, 8>), grid, dim3(512), lds, s, a);
+        else hipLaunchKernelGGL((select_kernel<D, BF, FEW, 4>), grid, dim3(256), lds, s, a);
     } else {
         hipLaunchKernelGGL((score_kernel<D, BF, FEW>), dim3((unsigned)score_blocks(a)), dim3(THREADS), 0, s, a);
     }
