@@ -1,7 +1,7 @@
 // Which pages of a long history a query attends to: mean keys of pages, their scores, and the highest of them.
 //
-// means_kernel: a lane has 32 columns of a token at a time, one scale's, and adds up its tokens'; lanes meet by
-// exchanges that halve the columns of each.  Bound by the keys' bytes.
+// means_kernel: a lane has 32 columns of a token at a time, one scale's, and adds up its tokens'; lanes of different rows of 16 meet by
+// swaps, which leave each a half of its columns, those of a row by rotations.  Bound by the keys' bytes.
 //
 // score_pages(): products of queries and means, in 64 bits on the matrix instructions (16 x 16 x 4): which of two pages
 // comes first must not hang on the order of a sum.  Operands are bf16 or fp16 numbers, so that their products are exact.
@@ -29,15 +29,14 @@ constexpr int THREADS = 256;
 // Lanes of a page's head.
 __host__ __device__ inline int lanes_of(int page_shift, int d) { return (d / BLOCK) << page_shift < 64 ? (d / BLOCK) << page_shift : 64; }
 
-template <int FMT, int D>
-__global__ __launch_bounds__(THREADS) void means_kernel(Cache c, const int32_t *which, int pages, unsigned *means)
+template <int FMT, int D, int LANES>
+__global__ __launch_bounds__(THREADS) void means_kernel(Cache c, const int32_t *which, int pages, Divider by_heads, u32x4 *means)
 {
-    constexpr int BLOCKS = D / BLOCK, CB = code_bytes<FMT>(D), WORDS = FMT == REC_MX4 ? 4 : 8;
-    const int lane = threadIdx.x & 63, lanes = lanes_of(c.page_shift, D), in_item = lane & (lanes - 1);
-    const int block = in_item % BLOCKS, first = in_item / BLOCKS, step = lanes / BLOCKS;
-    const long long item = ((long long)blockIdx.x * (THREADS / 64) + (threadIdx.x >> 6)) * (64 / lanes) + lane / lanes;
-    const long long entry = item / c.kv_heads;
-    const int head = (int)(item - entry * c.kv_heads);
+    constexpr int BLOCKS = D / BLOCK, CB = code_bytes<FMT>(D), WORDS = FMT == REC_MX4 ? 4 : 8, step = LANES / BLOCKS;
+    const int lane = threadIdx.x & 63, in_item = lane % LANES, block = in_item % BLOCKS, first = in_item / BLOCKS;
+    const int wave = (int)blockIdx.x * (THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int item = wave * (64 / LANES) + (LANES == 64 ? 0 : lane / LANES);  // below 2^28, as the launch has fewer than 2^32 threads
+    const int entry = by_heads.of(item), head = item - entry * c.kv_heads;
     long long page = -1;
     if (entry < pages) {
         page = which[entry];
@@ -60,7 +59,7 @@ __global__ __launch_bounds__(THREADS) void means_kernel(Cache c, const int32_t *
             const float scale = scale_of(group[2 * GROUP * CB + (t & 15) * BLOCKS + block]) * share;
             u32x4 w[WORDS / 4];
 #pragma unroll
-            for (int i = 0; i < WORDS / 4; ++i) w[i] = *reinterpret_cast<const u32x4 *>(codes + 16 * i);
+            for (int i = 0; i < WORDS / 4; ++i) w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes + 16 * i));
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) {
                 const unsigned word = w[i / 4][i % 4];
@@ -80,29 +79,51 @@ __global__ __launch_bounds__(THREADS) void means_kernel(Cache c, const int32_t *
             }
         }
     }
-    // Lanes of the same columns, BLOCKS apart: with each exchange a lane keeps half of its columns, down to two.
+    // Sums of two columns: of one in even rows of 16 lanes, or in the lower half, of the other in odd ones or in the upper.
+    auto two = [](float x, float y, auto half) {
+        const unsigned a = __builtin_bit_cast(unsigned, x), b = __builtin_bit_cast(unsigned, y);
+        if constexpr (half()) {
+            const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+            return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+        } else {
+            const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+            return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+        }
+    };
+    constexpr int AFTER_32 = LANES == 64 ? 16 : 32, COLUMNS = LANES == 16 ? 32 : AFTER_32 / 2;  // of a lane
     int column = 0;
+    if constexpr (LANES == 64) {
+        column += lane & 32 ? 16 : 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int half = 16 >> k;
-        const bool upper = first >> k & 1;
-        column += upper ? half : 0;
-#pragma unroll
-        for (int i = 0; i < half; ++i) {
-            const float keep = upper ? sum[half + i] : sum[i], give = upper ? sum[i] : sum[half + i];
-            sum[i] = keep + __shfl_xor(give, BLOCKS << k);
-        }
+        for (int i = 0; i < 16; ++i) sum[i] = two(sum[i], sum[i + 16], std::true_type());
     }
+    if constexpr (LANES >= 32) {
+        column += lane & 16 ? COLUMNS : 0;
 #pragma unroll
-    for (int k = 4; k < 6; ++k)
-        if (BLOCKS << k < lanes) {
-            const float x = __shfl_xor(sum[0], BLOCKS << k), y = __shfl_xor(sum[1], BLOCKS << k);
-            sum[0] += x;
-            sum[1] += y;
+        for (int i = 0; i < COLUMNS; ++i) sum[i] = two(sum[i], sum[i + COLUMNS], std::false_type());
+    }
+    auto rotated = [](float x, auto by) {
+        return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + by(), 0xf, 0xf, false));
+    };
+#pragma unroll
+    for (int i = 0; i < COLUMNS; ++i) {
+        sum[i] = rotated(sum[i], std::integral_constant<int, 8>());
+        sum[i] = rotated(sum[i], std::integral_constant<int, 4>());
+        if constexpr (BLOCKS <= 2) sum[i] = rotated(sum[i], std::integral_constant<int, 2>());
+        if constexpr (BLOCKS == 1) sum[i] = rotated(sum[i], std::integral_constant<int, 1>());
+    }
+    if (page >= 0 && lane % 16 < BLOCKS) {
+        u32x4 *to = means + ((page * c.kv_heads + head) * D + block * BLOCK + column) / 8;
+#pragma unroll
+        for (int i = 0; i < COLUMNS; i += 8) {
+            u32x4 w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bf16x2 mean = {(__bf16)sum[i + 2 * k], (__bf16)sum[i + 2 * k + 1]};
+                w[k] = __builtin_bit_cast(unsigned, mean);
+            }
+            to[i / 8] = w;
         }
-    if (page >= 0 && first < 16) {
-        const bf16x2 mean = {(__bf16)sum[0], (__bf16)sum[1]};
-        means[((page * c.kv_heads + head) * D + block * BLOCK + column) / 2] = __builtin_bit_cast(unsigned, mean);
     }
 }
 
@@ -599,15 +620,31 @@ long long means_blocks(const Cache &c, int d, int pages)
     return ((long long)pages * c.kv_heads + per_block - 1) / per_block;
 }
 
+template <int FMT, int D>
+hipError_t means_as(const Cache &c, const int32_t *which, int pages, void *means, hipStream_t s)
+{
+    const dim3 grid((unsigned)means_blocks(c, D, pages)), block(THREADS);
+    u32x4 *to = static_cast<u32x4 *>(means);
+    const int lanes = lanes_of(c.page_shift, D);
+    const Divider by_heads(c.kv_heads);
+    if constexpr (D == 32)
+        if (lanes == 16) {
+            hipLaunchKernelGGL((means_kernel<FMT, D, 16>), grid, block, 0, s, c, which, pages, by_heads, to);
+            return hipGetLastError();
+        }
+    if constexpr (D <= 64)
+        if (lanes == 32) {
+            hipLaunchKernelGGL((means_kernel<FMT, D, 32>), grid, block, 0, s, c, which, pages, by_heads, to);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((means_kernel<FMT, D, 64>), grid, block, 0, s, c, which, pages, by_heads, to);
+    return hipGetLastError();
+}
+
 template <int FMT>
 hipError_t means_of(const Cache &c, int d, const int32_t *which, int pages, void *means, hipStream_t s)
 {
-    const dim3 grid((unsigned)means_blocks(c, d, pages)), block(THREADS);
-    unsigned *to = static_cast<unsigned *>(means);
-    if (d == 32) hipLaunchKernelGGL((means_kernel<FMT, 32>), grid, block, 0, s, c, which, pages, to);
-    else if (d == 64) hipLaunchKernelGGL((means_kernel<FMT, 64>), grid, block, 0, s, c, which, pages, to);
-    else hipLaunchKernelGGL((means_kernel<FMT, 128>), grid, block, 0, s, c, which, pages, to);
-    return hipGetLastError();
+    return d == 32 ? means_as<FMT, 32>(c, which, pages, means, s) : d == 64 ? means_as<FMT, 64>(c, which, pages, means, s) : means_as<FMT, 128>(c, which, pages, means, s);
 }
 
 template <int D, bool BF, bool FEW>
