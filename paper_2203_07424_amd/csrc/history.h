@@ -102,6 +102,8 @@ hipError_t launch_chosen(const Cache &c, int format, int d, const rec_query &q, 
 struct Parts {
     float *o, *ml;
 };
+// Of a row whose parts are joined; of those, parts of what stands before its history.
+constexpr int MOST_PARTS = 64, MOST_BEFORE = 32;
 int own_parts(const Cache &c, int format, int d, const rec_query &q);
 // Histories behind `before` parts: results if own_parts() is 1, else that many parts more.
 hipError_t launch_behind(const Cache &c, int format, int d, const rec_query &q, const Parts &parts, int before, hipStream_t s);

@@ -399,7 +399,8 @@ struct Plan {
     bool join = true;  // parts become results
 };
 
-Plan plan_of(const Cache &c, int format, int d, const rec_query &q)
+// `most` is of parts.
+Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int most = MOST_PARTS)
 {
     Plan p;
     p.per = q.heads / c.kv_heads;
@@ -428,7 +429,7 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q)
     // Where pairs alone take all places, parts of eight tiles a wave, up to four, for the longest of ragged
     // histories (1600 pairs up to 8000 long 51 -> 43 us; all alike 171 -> 178).
     const long long room = 4ll * waves_of(format, d, q.dtype == REC_BF16, 1) * CUS / (pairs * p.waves);
-    const long long parts = room > 1 ? std::min({room, tiles / (2 * p.waves), 64ll}) : p.waves == 4 ? std::min(tiles / (8 * p.waves), 4ll) : 1;
+    const long long parts = room > 1 ? std::min({room, tiles / (2 * p.waves), (long long)most}) : p.waves == 4 ? std::min(tiles / (8 * p.waves), 4ll) : 1;
     p.splits = (int)std::max(1ll, parts);
     return p;
 }
@@ -491,11 +492,11 @@ long long threads_of(const Cache &c, const rec_query &q, const Plan &p) { return
 
 }  // namespace
 
-int own_parts(const Cache &c, int format, int d, const rec_query &q) { return plan_of(c, format, d, q).splits; }
+int own_parts(const Cache &c, int format, int d, const rec_query &q) { return plan_of(c, format, d, q, MOST_PARTS - MOST_BEFORE).splits; }
 
 hipError_t launch_behind(const Cache &c, int format, int d, const rec_query &q, const Parts &parts, int before, hipStream_t s)
 {
-    Plan p = plan_of(c, format, d, q);
+    Plan p = plan_of(c, format, d, q, MOST_PARTS - MOST_BEFORE);
     p.join = false;
     const long long at = before * p.rows;
     AttendArgs a = args_of(c, d, q, p, parts.o + at * d);

@@ -372,16 +372,17 @@ __global__ __launch_bounds__(256) void combine_kernel(const float *part_o, const
     using T = std::conditional_t<BF, __bf16, _Float16>;
     typedef T tx4 __attribute__((ext_vector_type(4)));
     constexpr int LANES = D / 4, GROUPS = 256 / LANES;
-    __shared__ float weight[64];
+    static_assert(MOST_PARTS == 64, "a wave has a lane for each part's weight");
+    __shared__ float weight[MOST_PARTS];
     __shared__ f32x4 sums[GROUPS][LANES];
     const long long row = blockIdx.x;
     const int col = threadIdx.x % LANES, group = threadIdx.x / LANES, lane = threadIdx.x & 63;
     f32x2 ml = {neg_inf(), 0.0f};
     if (lane < splits) ml = part_ml[lane * rows + row];
     // The parts' sums are on their way while their weights are worked out.
-    f32x4 part[64 / GROUPS];
+    f32x4 part[MOST_PARTS / GROUPS];
 #pragma unroll
-    for (int i = 0; i < 64 / GROUPS; ++i) {
+    for (int i = 0; i < MOST_PARTS / GROUPS; ++i) {
         part[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         if (group + i * GROUPS < splits) part[i] = *reinterpret_cast<const f32x4 *>(part_o + ((group + i * GROUPS) * rows + row) * D + 4 * col);
     }
@@ -396,7 +397,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const float *part_o, const
     __syncthreads();
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < 64 / GROUPS; ++i)
+    for (int i = 0; i < MOST_PARTS / GROUPS; ++i)
         if (group + i * GROUPS < splits) x += part[i] * weight[group + i * GROUPS];
     sums[group][col] = x;
     __syncthreads();

@@ -16,7 +16,6 @@ namespace hist {
 namespace {
 
 constexpr int CUS = 256;
-constexpr int MOST_PARTS = 32;  // of the prefix
 
 struct SharedArgs {
     Cache c;
@@ -609,7 +608,7 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int prefix_w
     const long long tiles = (((long long)prefix_width << c.page_shift) + TILE - 1) / TILE, waves = p.wide ? GROUPS : 4, at_once = p.wide ? CUS : 2 * CUS;
     long long best = 0;
     p.splits = 1;
-    for (int s = 1; s <= MOST_PARTS; ++s) {
+    for (int s = 1; s <= MOST_BEFORE; ++s) {
         const long long each = (tiles + s - 1) / s, turns = (each + waves - 1) / waves, cost = (p.blocks * (long long)s + at_once - 1) / at_once * (turns + 6);
         if (s == 1 || cost < best) {
             best = cost;

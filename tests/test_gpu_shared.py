@@ -89,6 +89,13 @@ def test_long_own_parts(b):
     O.assert_close(s.attend(q), *s.expect(q, 0.125, False))
 
 
+def test_most_parts(b):
+    """A row whose long prefix and long history are both divided into as many parts as there may be."""
+    s = Shared(b, 20000, [33000], 1, 32, "mx4", 128)
+    q = torch.randn(1, 1, 1, 32, generator=gen(100)).to(BF).cuda()
+    O.assert_close(s.attend(q, scale=0.2), *s.expect(q, 0.2, False))
+
+
 def test_nothing_in_front_or_behind(b):
     """A prefix of no tokens, of no pages, histories without pages: as attend(), or the prefix alone."""
     s = Shared(b, 0, [5, 0, 90], 2, 64, "mx4", 32)

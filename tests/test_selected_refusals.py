@@ -95,6 +95,16 @@ def test_shared_prefixes(b):
     assert b.rec_history_attend_shared_workspace_bytes(h, q, 4) > 0
 
 
+@pytest.mark.parametrize("width", [1, 400, 4000, 40000])
+@pytest.mark.parametrize("prefix", [1, 400, 4000, 40000])
+def test_shared_prefixes_and_long_histories_come_in_64_parts_at_most(b, prefix, width):
+    """What joins the parts of a row has room for 64; each takes the row's sums in 32 bits and two words more."""
+    for per in (1, 64):
+        q = query(b, batch=1, queries=1, heads=2 * per, table_width=width)
+        parts, odd = divmod(b.rec_history_attend_shared_workspace_bytes(cache(b), q, prefix), 2 * per * (64 * 4 + 8))
+        assert not odd and 1 <= parts <= 64
+
+
 def test_means(b):
     call = lambda h=cache(b), which=PTR, n=3, means=PTR: b._lib.rec_history_summarise(ref(h), which, n, means, None)  # noqa: E731
     assert call(n=0, which=None, means=None) == b.REC_OK
