@@ -234,6 +234,10 @@ __device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first
     const int heads = min(a.per, 16), rows = queries * heads, row_tiles = (a.per + 15) / 16;
     const int row = min(column, rows - 1), query = row / heads;
     const char *mine = static_cast<const char *>(a.q.dev_q) + 2 * (b * a.q.batch_stride + (first_query + query) * a.q.query_stride + 8 * g);
+    auto element = [](u32x4 w, int k, bool bf) -> f64 {
+        if (bf) return (f64) __builtin_bit_cast(float, k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+        return (f64) __builtin_bit_cast(f16x8, w)[k];
+    };
     u32x4 x[N / 8];
     auto load_rows = [&](int t) {
         const char *q = mine + 2 * (kv * a.per + min(16 * t + row - query * heads, a.per - 1)) * a.q.head_stride;
@@ -241,6 +245,17 @@ __device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first
         for (int i = 0; i < N / 8; ++i) x[i] = *reinterpret_cast<const u32x4 *>(q + 64 * i);
     };
     load_rows(0);
+    // Rows in 64 bits once, where registers for that do not cost a block its place (16 histories of 512 pages, 4 rows of 128 columns:
+    // 15.7 -> 14.1 us; 2048 blocks of 16 rows of 64: 45 -> 51): a tile's conversions take as long as its products.
+    constexpr bool ONCE = D == 32 || FEW;
+    f64 y[N];
+    auto convert_rows = [&]() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            y[i] = element(x[i / 8], i % 8, BF);
+            asm volatile("" : "+v"(y[i]));  // else it is converted where it is used
+        }
+    };
 
     const Walk w = walk();
     const int32_t *table = a.q.dev_pages_of + b * a.q.table_stride;
@@ -283,17 +298,16 @@ __device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
-    auto element = [](u32x4 w, int k, bool bf) -> f64 {
-        if (bf) return (f64) __builtin_bit_cast(float, k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
-        return (f64) __builtin_bit_cast(f16x8, w)[k];
-    };
     // known: bit i, page i of the tile is one.
     auto score = [&](const u32x4 (&raw)[N / 8], int n, unsigned known) {
         f64 best[PER_LANE];
 #pragma unroll
         for (int r = 0; r < PER_LANE; ++r) best[r] = -__builtin_inf();
         for (int t = 0; t < row_tiles; ++t) {
-            if (row_tiles > 1) load_rows(t);
+            if (row_tiles > 1) {
+                load_rows(t);
+                if constexpr (ONCE) convert_rows();
+            }
             // Two sums, which do not wait for each other.
             std::conditional_t<FEW, f64, f64x4> even = {}, odd = {};
 #pragma unroll
@@ -301,15 +315,16 @@ __device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first
                 u32x4 p = raw[i / 8], q = x[i / 8];
                 if constexpr (D == 128) {  // converted where they are used: all at once they would take 128 registers
                     if (i % 8 == 0) __builtin_amdgcn_sched_barrier(0);
-                    asm volatile("" : "+v"(p), "+v"(q));
+                    if constexpr (ONCE) asm volatile("" : "+v"(p));
+                    else asm volatile("" : "+v"(p), "+v"(q));
                 }
-                const f64 m = element(p, i % 8, true), m1 = element(p, i % 8 + 1, true), y = element(q, i % 8, BF), y1 = element(q, i % 8 + 1, BF);
+                const f64 m = element(p, i % 8, true), m1 = element(p, i % 8 + 1, true);
                 if constexpr (FEW) {
-                    even = __builtin_amdgcn_mfma_f64_4x4x4f64(m, y, even, 0, 0, 0);
-                    odd = __builtin_amdgcn_mfma_f64_4x4x4f64(m1, y1, odd, 0, 0, 0);
+                    even = __builtin_amdgcn_mfma_f64_4x4x4f64(m, ONCE ? y[i] : element(q, i % 8, BF), even, 0, 0, 0);
+                    odd = __builtin_amdgcn_mfma_f64_4x4x4f64(m1, ONCE ? y[i + 1] : element(q, i % 8 + 1, BF), odd, 0, 0, 0);
                 } else {
-                    even = __builtin_amdgcn_mfma_f64_16x16x4f64(m, y, even, 0, 0, 0);
-                    odd = __builtin_amdgcn_mfma_f64_16x16x4f64(m1, y1, odd, 0, 0, 0);
+                    even = __builtin_amdgcn_mfma_f64_16x16x4f64(m, ONCE ? y[i] : element(q, i % 8, BF), even, 0, 0, 0);
+                    odd = __builtin_amdgcn_mfma_f64_16x16x4f64(m1, ONCE ? y[i + 1] : element(q, i % 8 + 1, BF), odd, 0, 0, 0);
                 }
             }
             // A product that is NaN counts for nothing.
@@ -337,6 +352,7 @@ __device__ inline void score_pages(const SelectArgs &a, int b, int kv, int first
         }
     };
     int pages = look_up(w.n);
+    if constexpr (ONCE) convert_rows();
     for (int n = w.n; n < w.end; n += BATCH * w.step) {
         load_means(pages);
         const u64 known = __ballot(pages >= 0);
@@ -682,7 +698,7 @@ hipError_t launch_means(const Cache &c, int format, int d, const int32_t *which,
 long long select_threads(const Cache &c, const rec_query &q)
 {
     const SelectArgs a = args_of(c, q);
-    return a.walks ? std::max(score_blocks(a) * THREADS, (long long)q.batch * q.queries * c.kv_heads * 256)
+    return a.walks ? std::max(score_blocks(a) * THREADS, (long long)q.batch * q.queries * c.kv_heads * 1024)
                    : (long long)q.batch * c.kv_heads * a.query_tiles * 64 * select_waves(q);
 }
 
@@ -702,8 +718,11 @@ hipError_t launch_select(const Cache &c, int d, const rec_query &q, const Select
     }
     a.by_query_tiles = Divider(q.queries);
     const dim3 grid((unsigned)((long long)q.batch * q.queries * c.kv_heads));
-    if (q.table_width <= 512) hipLaunchKernelGGL((choose_kernel<1, 8>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((choose_kernel<4, 8>), grid, dim3(256), 0, s, a);
+    // All of a row's keys in lanes, up to 16384: 1500 pages 10.7 us with 4 waves of 8 keys a lane, 11.8 with 8, 18.0 with 16 of 16;
+    // 4096 pages 44 (read again for each count), 17.6 and 24.8; 16384 pages 104, 98 and 29.7.
+    if (q.table_width <= 2048) hipLaunchKernelGGL((choose_kernel<4, 8>), grid, dim3(256), 0, s, a);
+    else if (q.table_width <= 4096) hipLaunchKernelGGL((choose_kernel<8, 8>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((choose_kernel<16, 16>), grid, dim3(1024), 0, s, a);
     return hipGetLastError();
 }
 

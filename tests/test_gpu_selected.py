@@ -139,9 +139,9 @@ def test_choice(b, exact, d, kv, per, queries, page_tokens, dtype):
 
 
 @pytest.mark.parametrize("exact", [False, True])
-@pytest.mark.parametrize("lengths,kv", [([16 * 511, 16 * 513], 2), ([16 * 1500 + 5, 16 * 700], 1), ([16 * 5000, 3], 1), ([16 * 1000, 16 * 600], 2), ([16 * 9000], 1)])
+@pytest.mark.parametrize("lengths,kv", [([16 * 511, 16 * 513], 2), ([16 * 1500 + 5, 16 * 700], 1), ([16 * 5000, 3], 1), ([16 * 1000, 16 * 600], 2), ([16 * 9000], 1), ([16 * 3000 + 1, 16 * 2500], 2), ([16 * 17000], 1)])
 def test_choice_among_many(b, exact, lengths, kv):
-    """A row's scores in LDS and in memory, for one wave and for four, at once and in several goes."""
+    """A row's scores in LDS and in memory, for one wave to sixteen, at once and in several goes."""
     s = Choices(b, lengths, kv, 32, 16, 31, exact)
     q = numbers((len(lengths), 1, kv * 2, 32), 32, exact).to(BF)
     for count, first, last in ((3, 1, 1), (40, 1, 2), (500, 0, 1), (5, 2, 3), (1400, 1, 1)):
