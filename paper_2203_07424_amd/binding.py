@@ -899,9 +899,11 @@ class HistoryCache:
         call = "rec_history_select"
         query, shapes = self._query(call, q, pages_of, lengths, 0, 1.0, candidates)
         self._means(call, means)
+        if not 0 <= first <= count < 1 << 31 or not 0 < last <= count:
+            raise ValueError(f"{call}: first is at least 0, last at least 1, count at least both")
         shape = (shapes[0], shapes[1], self.kv_heads, count) if q.dim() == 4 else (shapes[0], self.kv_heads, count)
         if out is None:
-            out = torch.empty(shape, dtype=_I32, device=self.device) if count > 0 else means
+            out = torch.empty(shape, dtype=_I32, device=self.device)
         elif out.shape != shape or out.dtype is not _I32 or out.get_device() != self._index or not out.is_contiguous():
             raise ValueError(f"{call}: out must be a contiguous int32 {list(shape)} on {self.device}")
         workspace, at, need = self._workspace(_lib.rec_history_select_workspace_bytes, ("select", shapes, count), query, count)

@@ -391,3 +391,51 @@ def test_strided_queries_and_empty_calls(b):
     assert none.shape == (0, 3, 2, 2) and s.cache.attend_selected(q[:0], none, table[:0], s.len_t[:0]).shape == (0, 3, 4, 64)
     nothing = s.cache.select(q, means, table[:, :0], torch.zeros_like(s.len_t), 3)
     assert (nothing == -1).all() and not s.cache.attend_selected(q, nothing, table[:, :0], torch.zeros_like(s.len_t)).any()
+
+
+def test_pages_behind_the_first_4_gib(b):
+    """Pages and means at offsets beyond 32 bits: the same calls on the same contents at the start of a small cache."""
+    pages, kv, d, page = 2 ** 31 // (8 * 128) + 64, 8, 128, 16
+    near, far = (b.HistoryCache(n, page, kv, d, "mx4") for n in (64, pages))
+    x = torch.randn(2, 40 * page, kv, d, generator=gen(97))
+    at = torch.randperm(40, generator=gen(98))
+    lengths = torch.tensor([17 * page + 5, 23 * page - 2], dtype=torch.int32).cuda()
+    q = torch.randn(2, 3, 16, d, generator=gen(99)).to(BF).cuda()
+    results = []
+    for cache, shift in ((near, 24), (far, pages - 40)):
+        slots = ((shift + at)[:, None] * page + torch.arange(page)).flatten().cuda()
+        cache.write(x[0].cuda(), x[1].cuda(), slots)
+        means = torch.empty(len(cache.pages), kv, d, dtype=BF, device="cuda")
+        cache.summarise((shift + at).int().cuda(), means)
+        table = torch.full((2, 23), -1, dtype=torch.int32)
+        table[0, :18], table[1] = (shift + at[:18]).int(), (shift + at[17:]).int()
+        table[0, 17] = shift + int(at[39])
+        table = table.cuda()
+        chosen = cache.select(q, means, table, lengths, 6)
+        results.append((means[(shift + at).tolist()], chosen, cache.attend_selected(q, chosen, table, lengths),
+                        cache.attend_shared(q, table[0, :7].contiguous(), lengths[:1] - 11 * page, table[:, 7:].contiguous(), lengths - 7 * page)))
+        assert cache.check()[0] == b.REC_OK
+    for one, other in zip(*results):
+        assert torch.equal(one, other)
+    assert (results[0][1][:, :, :, 1:5] > 0).all() and results[0][2].isfinite().all() and results[0][3].isfinite().all()
+
+
+def test_choice_in_one_launch_of_long_rows(b):
+    """As many pages as a block has room for beside its waves' means, and one more."""
+    kv, d, histories, total = 2, 128, 128, 5000
+    means = torch.randn(total, kv, d, generator=gen(101)).to(BF).cuda()
+    cache = b.HistoryCache(total, 16, kv, d, "mx4")
+    for width in (4096, 4097):
+        table = torch.stack([torch.randperm(total, generator=gen(102 + i))[:width] for i in range(histories)]).int().cuda()
+        lengths = torch.randint(16 * 4000, 16 * 4096, (histories,), generator=gen(103)).int()
+        lengths[0] = 16 * width
+        q = torch.randn(histories, 2, d, generator=gen(104)).to(BF).cuda()
+        got = cache.select(q, means, table, lengths.cuda(), 9, first=1, last=2)
+        scores = torch.stack([means[:, h].double() @ q[:, h].double().t() for h in range(kv)], 1)       # [page, head, history]
+        for i, n in enumerate(lengths.tolist()):
+            there = -(-n // 16)
+            mine = scores[table[i, :there].long(), :, i]
+            for h in range(kv):
+                best = mine[1:there - 2, h].topk(6).indices + 1
+                assert got[i, h].tolist() == [0, *sorted(best.tolist()), there - 2, there - 1]
+    assert cache.check()[0] == b.REC_OK

@@ -143,6 +143,10 @@ def test_python_refuses_tensors_that_do_not_fit(b, monkeypatch):
                     getattr(h, name)(*args)
     with pytest.raises(ValueError):
         h.select(*good["select"], out=chosen.long())
+    for counts in (dict(count=0), dict(count=-1), dict(count=1 << 31), dict(count=(1 << 32) + 4), dict(first=-1), dict(first=5), dict(first=1 << 32),
+                   dict(last=0), dict(last=5), dict(last=(1 << 32) + 1)):
+        with pytest.raises(ValueError):
+            h.select(*good["select"][:4], **{"count": 4, **counts})
     monkeypatch.undo()
     monkeypatch.setattr(b, "_lib", None)
     for name in ("attend_selected", "attend_shared"):
