@@ -123,8 +123,8 @@ struct Select {
     int32_t *chosen;
     unsigned long long *keys;  // a score's, as whole numbers of the same order: [batch * queries * kv_heads][table_width]
 };
-long long select_threads(const Cache &c, const rec_query &q);
-size_t select_workspace(const Cache &c, const rec_query &q, int count);
+long long select_threads(const Cache &c, int d, const rec_query &q);
+size_t select_workspace(const Cache &c, int d, const rec_query &q, int count);
 hipError_t launch_select(const Cache &c, int d, const rec_query &q, const Select &sel, hipStream_t s);
 long long window_blocks(const rec_window &w);  // of 256 threads
 hipError_t launch_window(const rec_window &w, hipStream_t s);

@@ -89,7 +89,7 @@ rec_status check_select(const rec_history *h, const rec_query *q, int32_t count)
     const rec_status st = check_unmasked(h, q);
     if (st != REC_OK) return st;
     if (count < 1) return REC_ERR_ARG;
-    return rec::hist::select_threads(cache_of(h), *q) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
+    return rec::hist::select_threads(cache_of(h), h->head_dim, *q) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
 }
 
 rec_status check_chosen(const rec_history *h, const rec_query *q, int32_t count)
@@ -214,7 +214,7 @@ rec_status rec_history_summarise(const rec_history *h, const int32_t *dev_which,
 
 size_t rec_history_select_workspace_bytes(const rec_history *h, const rec_query *q, int32_t count)
 {
-    return check_select(h, q, count) != REC_OK ? 0 : rec::hist::select_workspace(cache_of(h), *q, count);
+    return check_select(h, q, count) != REC_OK ? 0 : rec::hist::select_workspace(cache_of(h), h->head_dim, *q, count);
 }
 
 rec_status rec_history_select(const rec_history *h, const rec_query *q, const void *dev_means, int32_t count, int32_t first,
@@ -226,7 +226,7 @@ rec_status rec_history_select(const rec_history *h, const rec_query *q, const vo
     if (q->batch == 0 || q->queries == 0) return REC_OK;
     if (!query_fits(q) || !aligned(dev_means) || !dev_chosen || !words_fit(dev_chosen, 4)) return REC_ERR_ARG;
     const Cache c = cache_of(h);
-    if (!workspace_fits(rec::hist::select_workspace(c, *q, count), dev_workspace, workspace_bytes)) return REC_ERR_ARG;
+    if (!workspace_fits(rec::hist::select_workspace(c, h->head_dim, *q, count), dev_workspace, workspace_bytes)) return REC_ERR_ARG;
     const rec::hist::Select sel = {dev_means, count, first, last, dev_chosen, static_cast<unsigned long long *>(dev_workspace)};
     return status_of(rec::hist::launch_select(c, h->head_dim, *q, sel, static_cast<hipStream_t>(stream)));
 }

@@ -543,8 +543,8 @@ __device__ inline void choose(const SelectArgs &a, const u64 *keys, int there, i
     for (int i = thread; i < last; i += 64 * W) out[a.sel.count - last + i] = there - last + i;
     if (a.sel.count == first + last) return;
     const int n = there - first - last;
-    if (n <= 64 * W * KEYS) choose_between<W, KEYS, true>(a, keys, n, out, m);
-    else choose_between<W, KEYS, false>(a, keys, n, out, m);
+    if (W == 1 || n <= 64 * W * KEYS) choose_between<W, KEYS, true>(a, keys, n, out, m);
+    else if constexpr (W > 1) choose_between<W, KEYS, false>(a, keys, n, out, m);
 }
 
 template <int W, int KEYS>
@@ -557,6 +557,9 @@ __global__ __launch_bounds__(64 * W) void choose_kernel(SelectArgs a)
     const int len = length_of(a, b, threadIdx.x == 0 && kv == 0 && query == 0);
     choose<W, KEYS>(a, a.sel.keys + row * a.q.table_width + a.sel.first, pages_up_to(a, len, query), a.sel.chosen + row * a.sel.count, m);
 }
+
+// Keys that a block has in LDS beside its waves' rows, and that a wave has in its lanes.
+constexpr int MOST_KEYS = 4096, WAVE_KEYS = 512;
 
 // Both in one launch, where the scores of a block's queries fit LDS: all waves score, then each chooses for a query.
 template <int D, bool BF, bool FEW, int WAVES>
@@ -581,17 +584,14 @@ __global__ __launch_bounds__(64 * WAVES) void select_kernel(SelectArgs a)
     Meeting<1> none;
     for (int i = wave; i < queries; i += WAVES) {
         const long long row = ((long long)b * a.q.queries + first_query + i) * a.c.kv_heads + kv;
-        choose<1, 8>(a, keys + i * a.q.table_width + a.sel.first, pages_up_to(a, len, first_query + i), a.sel.chosen + row * a.sel.count, none);
+        choose<1, WAVE_KEYS / 64>(a, keys + i * a.q.table_width + a.sel.first, pages_up_to(a, len, first_query + i), a.sel.chosen + row * a.sel.count, none);
     }
 }
-
-// Keys that a block has in LDS beside its waves' rows.
-constexpr int MOST_KEYS = 4096;
 
 // Waves of a block that does both, by the tiles of a row.
 int select_waves(const rec_query &q) { return q.table_width > 4 * PAGES ? 8 : 4; }
 
-SelectArgs args_of(const Cache &c, const rec_query &q)
+SelectArgs args_of(const Cache &c, int d, const rec_query &q)
 {
     SelectArgs a;
     a.c = c;
@@ -603,12 +603,14 @@ SelectArgs args_of(const Cache &c, const rec_query &q)
         a.query_tiles = (q.queries + a.at_once - 1) / a.at_once;
         return (long long)q.batch * c.kv_heads * a.query_tiles;  // blocks, or rows of waves
     };
-    // In one launch where a row's pages fit, and where not many tiles are a wave's or blocks are enough for all compute units.
     a.walks = 0;
     a.each = 0;
-    if (q.table_width <= MOST_KEYS) {
-        const long long blocks = with(MOST_KEYS / std::max(q.table_width, 1));
-        if (tiles <= 8 * select_waves(q) || blocks >= 256) {
+    // In one launch where a wave has all of a row's keys in its lanes and the block's tiles do not take longer than a second launch (4 histories,
+    // 2 kv heads of 64, 4 rows: 512 pages 8.7 us in one, 9.2 in two, 1024 pages 19 and 10; 8 rows of 128: 256 pages 14.4 and 12.8, 512 pages
+    // 22 and 12.7; 256 such histories: 256 pages 27 and 32, 512 pages 47 and 48).
+    if (q.table_width <= WAVE_KEYS) {
+        with(MOST_KEYS / std::max(q.table_width, 1));
+        if (tiles * (d / 32) * (a.at_once * a.per <= 4 ? 1 : 2) <= 128) {
             a.by_walks = Divider(1);
             a.by_query_tiles = Divider(std::max(a.query_tiles, 1));
             a.by_heads = Divider(c.kv_heads);
@@ -695,22 +697,22 @@ hipError_t launch_means(const Cache &c, int format, int d, const int32_t *which,
     return format == REC_MX4 ? means_of<REC_MX4>(c, d, which, pages, means, s) : means_of<REC_MX8>(c, d, which, pages, means, s);
 }
 
-long long select_threads(const Cache &c, const rec_query &q)
+long long select_threads(const Cache &c, int d, const rec_query &q)
 {
-    const SelectArgs a = args_of(c, q);
+    const SelectArgs a = args_of(c, d, q);
     return a.walks ? std::max(score_blocks(a) * THREADS, (long long)q.batch * q.queries * c.kv_heads * 1024)
                    : (long long)q.batch * c.kv_heads * a.query_tiles * 64 * select_waves(q);
 }
 
-size_t select_workspace(const Cache &c, const rec_query &q, int count)
+size_t select_workspace(const Cache &c, int d, const rec_query &q, int count)
 {
-    if (q.table_width <= count || args_of(c, q).walks == 0) return 0;
+    if (q.table_width <= count || args_of(c, d, q).walks == 0) return 0;
     return (size_t)q.batch * q.queries * c.kv_heads * (size_t)q.table_width * sizeof(u64);
 }
 
 hipError_t launch_select(const Cache &c, int d, const rec_query &q, const Select &sel, hipStream_t s)
 {
-    SelectArgs a = args_of(c, q);
+    SelectArgs a = args_of(c, d, q);
     a.sel = sel;
     if (a.walks == 0 || (q.table_width > sel.count && sel.count > sel.first + sel.last)) {
         const hipError_t e = d == 32 ? scored_of<32>(a, s) : d == 64 ? scored_of<64>(a, s) : scored_of<128>(a, s);

@@ -599,13 +599,17 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int prefix_w
     p.rows = (long long)q.batch * q.queries * q.heads;
     const bool bf = q.dtype == REC_BF16;
     const long long of_head = p.rows / c.kv_heads;
-    p.wide = of_head > 2 * ROWS;
+    const long long tiles = (((long long)prefix_width << c.page_shift) + TILE - 1) / TILE;
+    // A wide block has a row's tile done in 0.08 to 0.13 us of a compute unit (head_dim 32 to 128), a narrow one in 0.17 to 0.25, but takes 7 us more
+    // to start and end.  Rows of two heads of 64, mx4: 1024 before 16000 tokens 37 us narrow, 38 wide, 2048 65 and 49; 4096 before 2000
+    // 27 and 30, 8192 48 and 45; 8192 before 300 29 and 33, 16384 50 and 47.
+    p.wide = (of_head + ROWS - 1) / ROWS * c.kv_heads * (tiles + 12) > 30000;
     const int per_block = p.wide ? row_tiles_of(d, bf) * ROW_WAVES * ROWS : ROWS;
     p.blocks = (int)((of_head + per_block - 1) / per_block * c.kv_heads);
     p.own = own_parts(c, format, d, q);
     // Parts of the prefix: as many as end soonest, at what a block's start and end cost beside its tiles, where so many
     // blocks work at once.
-    const long long tiles = (((long long)prefix_width << c.page_shift) + TILE - 1) / TILE, waves = p.wide ? GROUPS : 4, at_once = p.wide ? CUS : 2 * CUS;
+    const long long waves = p.wide ? GROUPS : 4, at_once = p.wide ? CUS : 2 * CUS;
     long long best = 0;
     p.splits = 1;
     for (int s = 1; s <= MOST_BEFORE; ++s) {

@@ -420,14 +420,14 @@ def test_pages_behind_the_first_4_gib(b):
     assert (results[0][1][:, :, :, 1:5] > 0).all() and results[0][2].isfinite().all() and results[0][3].isfinite().all()
 
 
-def test_choice_in_one_launch_of_long_rows(b):
-    """As many pages as a block has room for beside its waves' means, and one more."""
+def test_choice_of_many_histories(b):
+    """Many histories of as many pages as a wave has keys for, of one more, and of thousands."""
     kv, d, histories, total = 2, 128, 128, 5000
     means = torch.randn(total, kv, d, generator=gen(101)).to(BF).cuda()
     cache = b.HistoryCache(total, 16, kv, d, "mx4")
-    for width in (4096, 4097):
+    for width in (512, 513, 4096):
         table = torch.stack([torch.randperm(total, generator=gen(102 + i))[:width] for i in range(histories)]).int().cuda()
-        lengths = torch.randint(16 * 4000, 16 * 4096, (histories,), generator=gen(103)).int()
+        lengths = torch.randint(8 * width, 16 * width, (histories,), generator=gen(103)).int()
         lengths[0] = 16 * width
         q = torch.randn(histories, 2, d, generator=gen(104)).to(BF).cuda()
         got = cache.select(q, means, table, lengths.cuda(), 9, first=1, last=2)

@@ -68,7 +68,8 @@ def test_choice(b):
         assert call(**kw) == b.REC_ERR_ARG, kw
     assert b.rec_history_select_workspace_bytes(h, q, 4) == 3 * 2 * 9000 * 8       # queries, kv heads, pages, a word each
     assert b.rec_history_select_workspace_bytes(h, q, 9000) == 0                   # all pages are chosen
-    assert b.rec_history_select_workspace_bytes(h, query(b, table_width=1000), 4) == 0      # a row's scores fit LDS
+    assert b.rec_history_select_workspace_bytes(h, query(b, table_width=512), 4) == 0       # a wave has a row's scores
+    assert b.rec_history_select_workspace_bytes(h, query(b, table_width=513), 4) == 3 * 2 * 513 * 8
     assert b.rec_history_select_workspace_bytes(h, q, 0) == 0
 
 
