@@ -3,7 +3,9 @@
 // The products are those of history_attend.hip: a wave has 16 rows, here the heads of one query and kv head, and walks over 64 of the
 // chosen tokens at a time.  Where a page lies takes two trips to memory, so a wave looks up 64 pages at once, one a lane, and asks
 // lanes for them.  Two tiles are on their way in registers: lists are short, and with one a tile took a trip to memory
-// (1024 queries with 8 rows each, up to 768 tokens: 23 us).  All rows stand at one position, so that a tile's tokens are seen by all or none.
+// (1024 queries, 2 kv heads of 64 with 4 rows each, mx8, up to 768 tokens: 22 us, issue-bound: 350 vector instructions
+// a tile, of which a SIMD has two waves, while most histories are shorter; 16 histories of 2048 chosen tokens, 8 kv heads of 128, mx4: 14 us,
+// 3.7 TB/s).  All rows stand at one position, so that a tile's tokens are seen by all or none.
 #include <algorithm>
 
 #include "history_attend_body.h"
@@ -276,9 +278,11 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int count)
     p.waves = p.splits = 1;
     const long long blocks = p.pairs * p.row_tiles, tiles = (((long long)count << c.page_shift) + TILE - 1) / TILE, room = 4ll * CUS * waves_of(format, d, q.dtype == REC_BF16);
     if (blocks == 0) return p;
-    // As many waves of a block as are all at work at once, then parts in blocks of their own, of two tiles a wave at least.
+    // As many waves of a block as are all at work at once (8 pairs of query and kv head with 256 tokens: 4.2 us with four
+    // waves, 5.8 with one; 2560 pairs with 384: 15.7 with one, 16.5 with two, which take turns), then parts in blocks of their own, of two tiles a
+    // wave at least (2 pairs with 8192 tokens: 10.2 us in 8 parts, 24.9 in one; 64 with 4096: 10.4 and 15.3).
     while (p.waves < 8 && 2 * p.waves <= tiles && 2 * p.waves * blocks <= room) p.waves *= 2;
-    // Two parts are not worth their joining.
+    // Two parts take as long as one, and a launch and a workspace more (16 histories of 2048 tokens, 8 kv heads of 128: 13.8 us).
     const long long parts = std::min({room / (blocks * p.waves), tiles / (2 * p.waves), 64ll});
     p.splits = parts > 2 ? (int)parts : 1;
     return p;

@@ -4,6 +4,8 @@
 // wide_kernel: a block has 128 rows of a kv head or more, four waves of RT tiles of 16, and two such groups of waves, which
 // have every other tile of keys and meet in LDS in the end.  The four waves of a group share a tile's values: each makes a
 // quarter of them into bf16, in the order of the operands, in LDS, while the tile before is multiplied.  Keys go into the products as they are stored.
+// Bound by matrix instructions and exponentials, which the two groups' halves of a turn overlap in part: 1024 rows of each of 8 kv heads of 128, mx4, before
+// 8192 tokens 46 us, 750 TFLOP/s of the plain products.
 // narrow_kernel: one tile of 16 rows, whose keys four waves share.
 //
 // What that leaves are parts of the rows' sums; attend_kernel joins them with what each history holds of its own.
@@ -608,7 +610,7 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int prefix_w
     p.blocks = (int)((of_head + per_block - 1) / per_block * c.kv_heads);
     p.own = own_parts(c, format, d, q);
     // Parts of the prefix: as many as end soonest, at what a block's start and end cost beside its tiles, where so many
-    // blocks work at once.
+    // blocks work at once (two narrow ones of a compute unit; planned for four, 1024 rows of 2 heads of 128 before 2000 tokens take 28 us, so 20).
     const long long waves = p.wide ? GROUPS : 4, at_once = p.wide ? CUS : 2 * CUS;
     long long best = 0;
     p.splits = 1;

@@ -5,7 +5,8 @@
 // heads of the same token, whose sines and cosines a lane works out once.  Angles are reduced to turns in 64 bits, so
 // that positions may be times in seconds.
 //
-// Bound by memory: every number is read once and written once.
+// Bound by memory: every number is read once and written once, past the caches.  65536 events of 40 heads of 128, bf16: 231 us, 5.8 TB/s
+// (weights in registers, one row of a lane at a time and through the caches: 331); 81920 of 8 heads of 32, fp32: 39 us, 4.3 TB/s; 256 events: 4.2 us.
 #include "history.h"
 
 namespace rec {
@@ -205,7 +206,8 @@ struct Deal {
 
 Deal deal_of(const rec_turn &t)
 {
-    // As few as leave no lane idle, as sines are then worked out least often, unless there are few waves.
+    // As few as leave no lane idle, as sines are then worked out least often, unless there are few waves: 4096 events of 10 heads of 64 5.6 us,
+    // 7.5 with all rows of a token beside each other, 9.6 with one; 81920 of 8 of 32 29.6, 29.5 and 44.9.
     const int rows = rows_of(t), all = t.heads + t.kv_heads;
     const auto waves = [&](int shift) { return (t.tokens + (rows >> shift) - 1) / (rows >> shift); };
     int shift = 0;
