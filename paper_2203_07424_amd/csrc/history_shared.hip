@@ -495,7 +495,7 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
         page_next = page_of(n + 2 * GROUPS, 16 * g);
         k_next = page_of(n + 2 * GROUPS, 16 * (c >> 2));
         if (!whole) {
-            if (page_now != -1 && (unsigned)page_now >= pages && c == 0)
+            if ((unsigned)page_now >= pages && n < end && n * TILE + 16 * g < len && c == 0)
                 report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)a.q.batch * (unsigned)a.q.table_width + (unsigned)((n * TILE + 16 * g) >> shift));
 #pragma unroll
             for (int t = 0; t < RT; ++t)

@@ -147,6 +147,9 @@ def test_reports(b, wide):
     got = s.attend(q)
     O.assert_close(got, *s.expect(q, 0.125, False, hidden=range(96, 128)))
     assert s.cache.check() == (b.REC_ERR_INDEX_RANGE, 2 * s.own.shape[1] + 3, b.REC_FAULT_PAGE)
+    s.prefix[3] = -1                    # as attend() has it: no page where the length says that there is one
+    O.assert_close(s.attend(q), *s.expect(q, 0.125, False, hidden=range(96, 128)))
+    assert s.cache.check() == (b.REC_ERR_INDEX_RANGE, 2 * s.own.shape[1] + 3, b.REC_FAULT_PAGE)
     s.prefix[3] = s.table[0, 3]
     s.prefix_len[0] = 32 * len(s.prefix) + 1
     s.attend(q)
