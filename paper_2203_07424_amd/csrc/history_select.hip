@@ -633,6 +633,10 @@ SelectArgs args_of(const Cache &c, int d, const rec_query &q)
     return a;
 }
 
+// Waves that choose for a row, so that all of its keys are in lanes, up to 16384: 1500 pages 10.7 us with 4 waves of 8 keys a lane, 11.8 with 8, 18.0 with
+// 16 of 16; 4096 pages 44 (read again for each count), 17.6 and 24.8; 16384 pages 104, 98 and 29.7.
+int choose_waves(const rec_query &q) { return q.table_width <= 4 * 8 * 64 ? 4 : q.table_width <= 8 * 8 * 64 ? 8 : 16; }
+
 long long score_blocks(const SelectArgs &a)
 {
     return ((long long)a.q.batch * a.c.kv_heads * a.query_tiles * a.walks + THREADS / 64 - 1) / (THREADS / 64);  // none in one launch
@@ -706,7 +710,7 @@ hipError_t launch_means(const Cache &c, int format, int d, const int32_t *which,
 long long select_threads(const Cache &c, int d, const rec_query &q)
 {
     const SelectArgs a = args_of(c, d, q);
-    return a.walks ? std::max(score_blocks(a) * THREADS, (long long)q.batch * q.queries * c.kv_heads * 1024)
+    return a.walks ? std::max(score_blocks(a) * THREADS, (long long)q.batch * q.queries * c.kv_heads * 64 * choose_waves(q))
                    : (long long)q.batch * c.kv_heads * a.query_tiles * 64 * select_waves(q);
 }
 
@@ -726,10 +730,9 @@ hipError_t launch_select(const Cache &c, int d, const rec_query &q, const Select
     }
     a.by_query_tiles = Divider(q.queries);
     const dim3 grid((unsigned)((long long)q.batch * q.queries * c.kv_heads));
-    // All of a row's keys in lanes, up to 16384: 1500 pages 10.7 us with 4 waves of 8 keys a lane, 11.8 with 8, 18.0 with 16 of 16;
-    // 4096 pages 44 (read again for each count), 17.6 and 24.8; 16384 pages 104, 98 and 29.7.
-    if (q.table_width <= 2048) hipLaunchKernelGGL((choose_kernel<4, 8>), grid, dim3(256), 0, s, a);
-    else if (q.table_width <= 4096) hipLaunchKernelGGL((choose_kernel<8, 8>), grid, dim3(512), 0, s, a);
+    const int waves = choose_waves(q);
+    if (waves == 4) hipLaunchKernelGGL((choose_kernel<4, 8>), grid, dim3(256), 0, s, a);
+    else if (waves == 8) hipLaunchKernelGGL((choose_kernel<8, 8>), grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL((choose_kernel<16, 16>), grid, dim3(1024), 0, s, a);
     return hipGetLastError();
 }

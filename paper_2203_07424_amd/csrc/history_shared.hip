@@ -614,7 +614,7 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int prefix_w
     const long long waves = p.wide ? GROUPS : 4, at_once = p.wide ? CUS : 2 * CUS;
     long long best = 0;
     p.splits = 1;
-    for (int s = 1; s <= MOST_BEFORE; ++s) {
+    for (int s = 1; s <= std::clamp<long long>(tiles, 1, MOST_BEFORE); ++s) {
         const long long each = (tiles + s - 1) / s, turns = (each + waves - 1) / waves, cost = (p.blocks * (long long)s + at_once - 1) / at_once * (turns + 6);
         if (s == 1 || cost < best) {
             best = cost;
