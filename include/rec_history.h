@@ -228,7 +228,8 @@ REC_API rec_status rec_history_attend_selected(const rec_history *h, const rec_q
  * same tokens, *dev_prefix_length (int32, on the device) of them in the pages dev_prefix_pages, int32 [prefix_width]; q describes what
  * each has behind them, its pages, its length and its queries.  A query sees the whole prefix and, of its own history, what it
  * would see by itself; one that stands before its own history's first token sees nothing, but for candidates, which then see
- * the prefix.  The prefix is read once for many queries.  window and sinks are 0.
+ * the prefix.  Where there is much to read, the prefix is read once for
+ * many queries.  window and sinks are 0.
  * Device faults: as there; of the prefix REC_FAULT_LENGTH with position batch, REC_FAULT_PAGE with position
  * batch * table_width + column.  Errors as there; REC_ERR_ARG: prefix_width < 0, dev_prefix_pages (where prefix_width > 0) or
  * dev_prefix_length null or misaligned; REC_ERR_OVERFLOW: prefix_width * page_tokens > 2^31 - 1024.

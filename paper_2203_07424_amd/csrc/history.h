@@ -102,16 +102,21 @@ hipError_t launch_chosen(const Cache &c, int format, int d, const rec_query &q, 
 struct Parts {
     float *o, *ml;
 };
-// Of a row whose parts are joined; of those, parts of what stands before its history.
-constexpr int MOST_PARTS = 64, MOST_BEFORE = 32;
-int own_parts(const Cache &c, int format, int d, const rec_query &q);
-// Histories behind `before` parts: results if own_parts() is 1, else that many parts more.
-hipError_t launch_behind(const Cache &c, int format, int d, const rec_query &q, const Parts &parts, int before, hipStream_t s);
 struct Prefix {
     const int32_t *pages;
     int width;
     const int32_t *length;
 };
+// A prefix and histories one behind the other, in one launch: tiles that its waves walk over, and the call.
+long long joined_work(const Cache &c, const rec_query &q, int prefix_width);
+long long joined_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
+size_t joined_workspace(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
+hipError_t launch_joined(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s);
+// Of a row whose parts are joined; of those, parts of what stands before its history.
+constexpr int MOST_PARTS = 64, MOST_BEFORE = 32;
+int own_parts(const Cache &c, int format, int d, const rec_query &q);
+// Histories behind `before` parts: results if own_parts() is 1, else that many parts more.
+hipError_t launch_behind(const Cache &c, int format, int d, const rec_query &q, const Parts &parts, int before, hipStream_t s);
 long long shared_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
 size_t shared_workspace(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
 hipError_t launch_shared(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s);

@@ -41,13 +41,13 @@ namespace {
 
 constexpr int CUS = 256;
 
-// What a launch attends to: histories, or histories behind a prefix.
-enum { WHOLE, BEHIND };
+// What a launch attends to: histories, histories behind the sums of a prefix, or a prefix and histories one behind the other.
+enum { WHOLE, BEHIND, JOINED };
 
 // Waves that a SIMD holds at once; the compiler gives a wave at most its share of registers.
 __host__ __device__ constexpr int waves_of(int format, int d, bool bf, int heads, int kind = WHOLE)
 {
-    if (kind == BEHIND && d == 32 && format == REC_MX8 && heads == 1) return 3;  // a row's parts besides
+    if (kind != WHOLE && d == 32 && format == REC_MX8 && heads == 1) return 3;  // a row's parts, or a prefix, besides
     if (heads > 1) return d == 32 && format == REC_MX4 ? 3 : 2;
     return d == 128 ? (format == REC_MX4 && bf ? 3 : 2) : d == 64 ? (format == REC_MX4 && bf ? 4 : 3) : 4;
 }
@@ -68,6 +68,7 @@ struct AttendArgs {
     int before;            // parts of it
     const float *before_o;
     const f32x2 *before_ml;
+    Prefix prefix;
 };
 
 // Joins a row's sums x, of some columns, its weights' sum l and its maximum's exponent m with those of `parts` parts, in their order.
@@ -120,11 +121,25 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
         if (threadIdx.x == 0 && first_kv == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)b);
         len = len < 0 ? 0 : most_tokens;
     }
+    // Tokens of the prefix, and where a history's first one stands behind it: at the next group of 16, as a group is in one page.
+    int prefix = 0, own = 0;
+    if constexpr (KIND == JOINED) {
+        const int most = a.prefix.width << shift;
+        prefix = *a.prefix.length;
+        if (prefix < 0 || prefix > most) {
+            if (blockIdx.x == 0 && threadIdx.x == 0) report(a.c.fault, REC_FAULT_LENGTH, (unsigned long long)a.q.batch);
+            prefix = prefix < 0 ? 0 : most;
+        }
+        own = (prefix + GROUP - 1) & -GROUP;
+    }
     // Positions of this wave's rows: of its first, its last, and this lane's; -1 sees nothing.
     const int first_row = row_tile * ROWS, last_row = min(first_row + SLOT, a.rows) - 1, row = min(first_row + r, last_row);
     const bool real = first_row + r <= last_row;
     const bool together = a.q.candidates != 0;
-    auto position = [&](int row) { return together ? len - 1 : max(len - a.q.queries + a.by_per.of(row), -1); };
+    auto position = [&](int row) {
+        const int p = together ? len - 1 : max(len - a.q.queries + a.by_per.of(row), -1);
+        return KIND == JOINED && (p >= 0 || together) ? own + p : p;
+    };
     const int p_lo = position(first_row), p_hi = position(last_row), pos = position(row);
     const int window = a.q.window == 0 ? 0x7fffffff : a.q.window, sinks = a.q.sinks;
 
@@ -164,11 +179,13 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
         // The page of a group's first token, or -1.
         auto page_of = [&](int token) {
             int page = -1;
-            if (token < len) page = table[token >> shift];
+            if (KIND == JOINED && token < own) page = a.prefix.pages[token >> shift];
+            else if (token - own < len) page = table[(token - own) >> shift];
             return page;
         };
         auto group_at = [&](int page, int token) {
             const bool ok = (unsigned)page < pages;  // else some group that is there: its tokens count for nothing
+            if (KIND == JOINED && token >= own) token -= own;
             const unsigned in_page = ok ? (unsigned)((token >> 4) & (groups - 1)) * group_bytes<FMT>(D) : 0u;
             return first_page + ((unsigned long long)(ok ? (unsigned)page : 0u) * page_bytes + in_page);
         };
@@ -205,7 +222,8 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
 
             // Groups come with their page or not at all.
             const bool there = (unsigned)v_page < pages;
-            const bool whole = key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there);
+            const bool whole = key + TILE - 1 <= p_lo && (key > p_hi - window || key + TILE <= sinks) && __all(there) &&
+                               !(KIND == JOINED && key < own && key + TILE > prefix);
             unsigned nan = 0;  // bit 4 h + b: row c sees a NaN in block b of head h's values
             if (!whole) {
                 // Bit t: row c sees token t of group g; some row does.
@@ -214,9 +232,14 @@ __global__ __launch_bounds__(64 * W, waves_of(FMT, D, BF, HEADS, KIND)) void att
                 auto before = [&](int at) { return below(max(at - first, -1) - window + 1); };
                 unsigned seen = upto(pos) & (~before(pos) | below(sinks - first));
                 unsigned used = upto(p_hi) & (~before(p_lo) | below(sinks - first));
+                if (KIND == JOINED && first < own) {  // nothing stands between the prefix's end and the history
+                    seen &= below(prefix - first);
+                    used &= below(prefix - first);
+                }
                 if (!there) {
                     if (used && c == 0)
-                        report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)b * (unsigned)a.q.table_width + (unsigned)(first >> shift));
+                        report(a.c.fault, REC_FAULT_PAGE, (unsigned long long)(KIND == JOINED && first < own ? a.q.batch : b) * (unsigned)a.q.table_width +
+                                                              (unsigned)((KIND == JOINED && first >= own ? first - own : first) >> shift));
                     seen = used = 0;
                 }
                 saw |= seen;
@@ -438,7 +461,7 @@ template <int FMT, int D, bool BF, int KIND>
 hipError_t attend_as(const AttendArgs &a, const Plan &p, hipStream_t s)
 {
     const dim3 grid((unsigned)((long long)a.q.batch * a.c.kv_heads / p.heads * p.row_tiles * p.splits));
-    if constexpr (D <= 64)
+    if constexpr (D <= 64 && KIND != JOINED)
         if (p.heads == 2) {
             hipLaunchKernelGGL((attend_kernel<FMT, D, BF, 1, 2, KIND>), grid, dim3(64), 0, s, a);
             return hipGetLastError();
@@ -456,6 +479,7 @@ template <int FMT, int D>
 hipError_t attend_of(const AttendArgs &a, const Plan &p, hipStream_t s)
 {
     const bool bf = a.q.dtype == REC_BF16;
+    if (a.prefix.length) return bf ? attend_as<FMT, D, true, JOINED>(a, p, s) : attend_as<FMT, D, false, JOINED>(a, p, s);
     if (a.before) return bf ? attend_as<FMT, D, true, BEHIND>(a, p, s) : attend_as<FMT, D, false, BEHIND>(a, p, s);
     return bf ? attend_as<FMT, D, true, WHOLE>(a, p, s) : attend_as<FMT, D, false, WHOLE>(a, p, s);
 }
@@ -483,6 +507,7 @@ AttendArgs args_of(const Cache &c, int d, const rec_query &q, const Plan &p, voi
     a.part_ml = reinterpret_cast<f32x2 *>(a.part_o + (p.splits > 1 ? p.splits * p.rows * d : 0));
     a.parted = p.splits > 1;
     a.before = 0;
+    a.prefix = {nullptr, 0, nullptr};
     return a;
 }
 
@@ -491,6 +516,45 @@ size_t workspace_of(const Plan &p, int d) { return p.splits == 1 ? 0 : (size_t)p
 long long threads_of(const Cache &c, const rec_query &q, const Plan &p) { return (long long)q.batch * c.kv_heads * p.row_tiles * p.splits * 64 * p.waves; }
 
 }  // namespace
+
+// A call whose histories have the prefix's pages before their own, for plans only.
+rec_query joined_query(const rec_query &q, int prefix_width)
+{
+    rec_query j = q;
+    j.table_width += prefix_width + 1;
+    return j;
+}
+
+long long joined_work(const Cache &c, const rec_query &q, int prefix_width)
+{
+    const long long rows = (long long)q.queries * (q.heads / c.kv_heads);
+    return q.batch * (long long)c.kv_heads * ((rows + ROWS - 1) / ROWS) * ((((long long)q.table_width + prefix_width + 1) << c.page_shift) / TILE + 1);
+}
+
+Plan joined_plan(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
+{
+    Plan p = plan_of(c, format, d, joined_query(q, prefix_width));
+    p.heads = 1;
+    return p;
+}
+
+long long joined_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
+{
+    return threads_of(c, q, joined_plan(c, format, d, q, prefix_width));
+}
+
+size_t joined_workspace(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
+{
+    return workspace_of(joined_plan(c, format, d, q, prefix_width), d);
+}
+
+hipError_t launch_joined(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s)
+{
+    const Plan p = joined_plan(c, format, d, q, prefix.width);
+    AttendArgs a = args_of(c, d, q, p, workspace);
+    a.prefix = prefix;
+    return attend_any(a, p, format, d, s);
+}
 
 int own_parts(const Cache &c, int format, int d, const rec_query &q) { return plan_of(c, format, d, q, MOST_PARTS - MOST_BEFORE).splits; }
 

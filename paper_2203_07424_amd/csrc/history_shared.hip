@@ -8,7 +8,8 @@
 // 8192 tokens 46 us, 750 TFLOP/s of the plain products.
 // narrow_kernel: one tile of 16 rows, whose keys four waves share.
 //
-// What that leaves are parts of the rows' sums; attend_kernel joins them with what each history holds of its own.
+// What that leaves are parts of the rows' sums; attend_kernel joins them with what each history holds of its own.  Where there is little to
+// read, attend_kernel walks over the prefix and the history by itself.
 #include <algorithm>
 
 #include "history_attend_body.h"
@@ -646,8 +647,14 @@ hipError_t shared_of(const SharedArgs &a, const Plan &p, int format, hipStream_t
 
 }  // namespace
 
+// Few tiles in all: each history reads the prefix for itself, in one launch.  4 kv heads of 64, mx8, fp16, 20 events behind a prefix: 8 histories
+// behind 400 tokens 6.5 us so, 10.5 in two launches, 128 (4096 tiles) 8.6 and 11.4, 32 behind 4000 (8192 tiles) 16.0 and 13.2, 128 behind 1000
+// (8704) 14.4 and 11.4.
+bool joined(const Cache &c, const rec_query &q, int prefix_width) { return joined_work(c, q, prefix_width) <= 4096; }
+
 long long shared_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
 {
+    if (joined(c, q, prefix_width)) return joined_threads(c, format, d, q, prefix_width);
     const Plan p = plan_of(c, format, d, q, prefix_width);
     return std::max((long long)p.blocks * p.splits * 64 * ROW_WAVES * GROUPS, p.own == 1 ? 0 : p.rows * 256);
 }
@@ -655,12 +662,14 @@ long long shared_threads(const Cache &c, int format, int d, const rec_query &q, 
 size_t shared_workspace(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
 {
     if (q.batch == 0 || q.queries == 0) return 0;
+    if (joined(c, q, prefix_width)) return joined_workspace(c, format, d, q, prefix_width);
     const Plan p = plan_of(c, format, d, q, prefix_width);
     return (size_t)(p.splits + (p.own == 1 ? 0 : p.own)) * (size_t)p.rows * ((size_t)d * sizeof(float) + sizeof(f32x2));
 }
 
 hipError_t launch_shared(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s)
 {
+    if (joined(c, q, prefix.width)) return launch_joined(c, format, d, q, prefix, workspace, s);
     const Plan p = plan_of(c, format, d, q, prefix.width);
     SharedArgs a;
     a.c = c;
