@@ -58,7 +58,9 @@ EXPORTS = ("rec_create", "rec_destroy", "rec_workspace_bytes", "rec_bind_workspa
            "rec_probe_plan_joined", "rec_probe_plan_pooling", "rec_probe_dense_copy",
            "rec_history_bytes", "rec_history_write", "rec_history_read", "rec_history_attend_workspace_bytes",
            "rec_history_attend", "rec_history_summarise", "rec_history_select_workspace_bytes", "rec_history_select",
-           "rec_history_attend_selected_workspace_bytes", "rec_history_attend_selected", "rec_history_attend_shared_workspace_bytes", "rec_history_attend_shared", "rec_window_attend", "rec_rotate_heads", "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
+           "rec_history_attend_selected_workspace_bytes", "rec_history_attend_selected",
+           "rec_history_attend_shared_workspace_bytes", "rec_history_attend_shared", "rec_window_attend", "rec_rotate_heads",
+           "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
 
 
 class rec_config(C.Structure):
@@ -906,7 +908,10 @@ class HistoryCache:
             out = torch.empty(shape, dtype=_I32, device=self.device)
         elif out.shape != shape or out.dtype is not _I32 or out.get_device() != self._index or not out.is_contiguous():
             raise ValueError(f"{call}: out must be a contiguous int32 {list(shape)} on {self.device}")
-        workspace, at, need = self._workspace(_lib.rec_history_select_workspace_bytes, ("select", shapes, count), query, count)
+        key = ("select", shapes, count)
+        at, need = None, self._workspaces.get(key)
+        if need != 0:
+            workspace, at, need = self._workspace(_lib.rec_history_select_workspace_bytes, key, query, count)
         st = _lib.rec_history_select(self._ref, query, means.data_ptr(), count, first, last, out.data_ptr(), at, need,
                                      _stream_on(self._index, call))
         if st:
@@ -924,7 +929,10 @@ class HistoryCache:
         shape = (shapes[0], shapes[1], self.kv_heads, count) if q.dim() == 4 else (shapes[0], self.kv_heads, count)
         if chosen.shape != shape or chosen.dtype is not _I32 or chosen.get_device() != self._index or not chosen.is_contiguous():
             raise ValueError(f"{call}: chosen must be a contiguous int32 {list(shape[:-1])} and a count on {self.device}")
-        workspace, at, need = self._workspace(_lib.rec_history_attend_selected_workspace_bytes, ("selected", shapes, count), query, count)
+        key = ("selected", shapes, count)
+        at, need = None, self._workspaces.get(key)
+        if need != 0:
+            workspace, at, need = self._workspace(_lib.rec_history_attend_selected_workspace_bytes, key, query, count)
         st = _lib.rec_history_attend_selected(self._ref, query, chosen.data_ptr(), count, at, need, _stream_on(self._index, call))
         if st:
             self._ok(st, call)
@@ -944,7 +952,10 @@ class HistoryCache:
         if prefix_length.numel() != 1 or prefix_length.dtype is not _I32 or prefix_length.get_device() != index:
             raise ValueError(f"{call}: prefix_length must be one int32 on {self.device}")
         width = prefix_pages.shape[0]
-        workspace, at, need = self._workspace(_lib.rec_history_attend_shared_workspace_bytes, ("shared", shapes, width), query, width)
+        key = ("shared", shapes, width)
+        at, need = None, self._workspaces.get(key)
+        if need != 0:
+            workspace, at, need = self._workspace(_lib.rec_history_attend_shared_workspace_bytes, key, query, width)
         st = _lib.rec_history_attend_shared(self._ref, query, prefix_pages.data_ptr(), width, prefix_length.data_ptr(), at, need,
                                             _stream_on(index, call))
         if st:
