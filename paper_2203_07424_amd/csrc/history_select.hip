@@ -624,8 +624,8 @@ SelectArgs args_of(const Cache &c, int d, const rec_query &q)
         }
     }
     const long long rows = with(16);
-    // A tile a wave where there are few rows; several where that would be more waves than work at once.
-    a.each = (int)std::max(1ll, (rows * tiles + 8191) / 8192);
+    // A tile a wave where there are few rows; several where that would be more waves than work at once, and all of a row's at most.
+    a.each = (int)std::clamp((rows * tiles + 8191) / 8192, 1ll, std::max((long long)tiles, 1ll));
     a.walks = std::max((tiles + a.each - 1) / a.each, 1);
     a.by_walks = Divider(a.walks);
     a.by_query_tiles = Divider(std::max(a.query_tiles, 1));

@@ -73,6 +73,20 @@ def test_choice(b):
     assert b.rec_history_select_workspace_bytes(h, q, 0) == 0
 
 
+@pytest.mark.parametrize("batch", [1, 8192, 1 << 20, 1 << 22, (1 << 22) + 9, 1 << 23, (1 << 23) + 5, 1 << 24, 1 << 30])
+@pytest.mark.parametrize("width", [513, 5000, 1 << 20, (1 << 26) - 1, 1 << 26])
+def test_choices_of_any_size_have_an_answer(b, batch, width):
+    """Tiles of all rows may be 2^45 and more: what a wave has of them is a row's at most.  A wave or block chooses for a row of scores, 8 bytes a page."""
+    h, q = cache(b, kv_heads=1, page_tokens=16, num_pages=100), query(b, batch=batch, queries=1, heads=1, table_width=width)
+    call = b._lib.rec_history_select(C.byref(h), C.byref(q), PTR, 4, 1, 1, PTR, None, 0, None)
+    need = b.rec_history_select_workspace_bytes(h, q, 4)
+    threads = 64 * batch * (4 if width <= 2048 else 8 if width <= 4096 else 16)
+    if threads < 1 << 32:
+        assert need == 8 * batch * width and call == b.REC_ERR_ARG       # no workspace
+    else:
+        assert need == 0 and call == b.REC_ERR_OVERFLOW
+
+
 def test_chosen_pages(b):
     h, q = cache(b), query(b)
     call = lambda chosen=PTR, count=4: b._lib.rec_history_attend_selected(C.byref(h), C.byref(q), chosen, count, PTR, 1 << 40, None)  # noqa: E731
