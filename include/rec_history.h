@@ -205,7 +205,8 @@ REC_API rec_status rec_history_summarise(const rec_history *h, const int32_t *de
  *   q              as for rec_history_attend(); dev_out and scale are not looked at, window and sinks are 0
  *   count          >= first + last, first >= 0, last >= 1
  * Device faults: REC_FAULT_LENGTH, REC_FAULT_PAGE as there.
- * REC_ERR_ARG: null, misaligned, bad counts, a workspace too small; REC_ERR_SHAPE, REC_ERR_OVERFLOW as there.
+ * REC_ERR_ARG: null, misaligned, bad counts, a workspace too small; REC_ERR_SHAPE, REC_ERR_OVERFLOW as there, and
+ * REC_ERR_OVERFLOW: count > 2^31 - 1024.
  */
 REC_API size_t rec_history_select_workspace_bytes(const rec_history *h, const rec_query *q, int32_t count);
 REC_API rec_status rec_history_select(const rec_history *h, const rec_query *q, const void *dev_means, int32_t count, int32_t first,

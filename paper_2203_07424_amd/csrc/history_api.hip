@@ -89,6 +89,7 @@ rec_status check_select(const rec_history *h, const rec_query *q, int32_t count)
     const rec_status st = check_unmasked(h, q);
     if (st != REC_OK) return st;
     if (count < 1) return REC_ERR_ARG;
+    if (count > MOST_TOKENS) return REC_ERR_OVERFLOW;  // entries are counted a block of up to 1024 threads past the last one
     return rec::hist::select_threads(cache_of(h), h->head_dim, *q) > MOST_THREADS ? REC_ERR_OVERFLOW : REC_OK;
 }
 

@@ -87,6 +87,17 @@ def test_choices_of_any_size_have_an_answer(b, batch, width):
         assert need == 0 and call == b.REC_ERR_OVERFLOW
 
 
+@pytest.mark.parametrize("width", [2, 600, 9000])
+def test_counts_that_a_block_steps_past(b, width):
+    """A thread's next entry is up to 1024 behind its last: behind 2^31 - 1024 it does not fit 32 bits, and would be stored in front of the results."""
+    h, q = cache(b), query(b, table_width=width)
+    call = lambda count: b._lib.rec_history_select(C.byref(h), C.byref(q), None, count, 1, 1, PTR, PTR, 1 << 40, None)  # noqa: E731
+    for count in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 31 - 1023):
+        assert call(count) == b.REC_ERR_OVERFLOW and b.rec_history_select_workspace_bytes(h, q, count) == 0, count
+    assert call(2 ** 31 - 1024) == b.REC_ERR_ARG       # no means
+    assert max(range(1023, 2 ** 31 - 1024, 1024)) + 1024 < 2 ** 31
+
+
 def test_chosen_pages(b):
     h, q = cache(b), query(b)
     call = lambda chosen=PTR, count=4: b._lib.rec_history_attend_selected(C.byref(h), C.byref(q), chosen, count, PTR, 1 << 40, None)  # noqa: E731
