@@ -282,14 +282,15 @@ REC_API rec_status rec_window_attend(const rec_window *w, void *stream);
  *   q, k           [tokens][heads][head_dim], [tokens][kv_heads][head_dim] of dtype (REC_F32, REC_F16, REC_BF16);
  *                  one of heads and kv_heads may be 0, and its rows and weight null
  *   q_out, k_out   the same shapes and type, rows that do not overlap; they may be q and k themselves
- *                  (the same address and strides) and may not overlap them otherwise
+ *                  (the same address and strides) and may not overlap them, or each other, otherwise.  Rows that lie between
+ *                  another argument's have its token stride and, unless what each has of a token lies apart, its head stride
  *   head_dim       32, 64 or 128
  *   dev_positions  int32 or, wide = 1, int64 [tokens], of either sign
  *   dev_frequencies  double [pairs], radians a position; pairs a multiple of 8, at most head_dim / 2
  *   dev_q_weight, dev_k_weight   float [head_dim], 16-byte aligned, or null: those rows are not normalised
  *   eps            >= 0
  * Squares are summed in fp32, or in 64 bits where that would overflow or vanish; angles are worked out in 64 bits.
- * REC_ERR_ARG: null, misaligned, bad enum, negative counts or eps, rows of q_out or k_out that overlap;
+ * REC_ERR_ARG: null, misaligned, bad enum, negative counts or eps, rows of q_out or k_out that overlap each other or q and k;
  * REC_ERR_SHAPE: head_dim or pairs; REC_ERR_OVERFLOW: more than 2^20 heads, or more threads
  * than a launch can have (2^32; a wave has 2 to 32 rows).
  */

@@ -1010,7 +1010,8 @@ def rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     q: [tokens, heads, head_dim], k: [tokens, kv_heads, head_dim], fp32, fp16 or bf16, any token and head strides; either may be None.
     positions: int32 or int64 [tokens]; frequencies: float64 [pairs], radians a position, pairs a multiple of 8 (0: no rotation).
     q_weight, k_weight: fp32 [head_dim], or None: those rows are only rotated.  interleaved: columns 2 i and 2 i + 1 are a pair,
-    else i and i + pairs.  Results are contiguous, or go to q_out and k_out, which may be q and k.  No backward pass, as in HistoryCache."""
+    else i and i + pairs.  Results are contiguous, or go to q_out and k_out, which may be q and k, but not overlap them or each other otherwise.
+    No backward pass, as in HistoryCache."""
     like = q if q is not None else k
     dtype = None if like is None else like.dtype
     code, index = (None, -1) if dtype is None else (_DTYPE_CODES.get(dtype), like.get_device())

@@ -145,6 +145,50 @@ bool rows_apart(const rec_rows &r, int64_t tokens, int64_t heads, int64_t d)
     return (n_near == 1 || near >= d) && (n_far == 1 || (far >= d && (n_near == 1 || (far - d) / near >= n_near - 1)));
 }
 
+// Rows [tokens][heads][d] of `size` bytes an element.
+struct Place {
+    const rec_rows *r;
+    int64_t heads;
+};
+
+// Whether the rows x of a result and those of another argument have no element in common.  `own`: y is what x is made of, so that they may be the
+// same rows: each is read before it is written.  Exact where both lie in address ranges of their own, which is nearly always so, have the same strides, or have
+// their shares of a token beside each other; other rows between each other's count as overlapping.
+bool places_apart(const Place &x, const Place &y, bool own, int64_t tokens, int64_t d, int size)
+{
+    typedef __int128 wide;  // products of strides and counts
+    struct Span {
+        wide from, to;
+    };
+    const auto span_of = [&](const Place &p, int64_t n) {  // of n tokens, in bytes
+        const wide t = (wide)p.r->token_stride * (n - 1), h = (wide)p.r->head_stride * (p.heads - 1);
+        const wide from = reinterpret_cast<uintptr_t>(p.r->dev);
+        return Span{from + ((t < 0 ? t : 0) + (h < 0 ? h : 0)) * size, from + ((t > 0 ? t : 0) + (h > 0 ? h : 0) + d) * size};
+    };
+    const Span a = span_of(x, tokens), b = span_of(y, tokens);
+    if (a.to <= b.from || b.to <= a.from) return true;
+    const bool same_tokens = tokens == 1 || x.r->token_stride == y.r->token_stride;
+    const bool same_heads = (x.heads == 1 && y.heads == 1) || x.r->head_stride == y.r->head_stride;
+    if (own && same_tokens && same_heads && x.r->dev == y.r->dev) return true;
+    if (!same_tokens) return false;
+    const wide by_token = (wide)x.r->token_stride * size, step = by_token < 0 ? -by_token : by_token;  // not 0, of several tokens: rows_apart()
+    if (tokens > 1) {
+        // What x and y have of a token, repeated a step further each time.
+        const Span p = span_of(x, 1), q = span_of(y, 1);
+        const wide ahead = ((q.from - p.from) % step + step) % step;
+        if (p.to - p.from <= ahead && ahead + (q.to - q.from) <= step) return true;
+    }
+    if (!same_heads) return false;
+    // On the same grid: y's rows are `i` heads and any number of tokens from x's.
+    const wide off = (wide) reinterpret_cast<uintptr_t>(y.r->dev) - (wide) reinterpret_cast<uintptr_t>(x.r->dev), bytes = (wide)d * size;
+    for (int64_t i = 1 - x.heads; i < y.heads; ++i) {
+        wide left = off + i * ((wide)x.r->head_stride * size);
+        if (tokens > 1) left -= std::clamp<wide>((left < 0 ? left - step / 2 : left + step / 2) / step, 1 - tokens, tokens - 1) * step;
+        if (left < bytes && -left < bytes) return false;
+    }
+    return true;
+}
+
 rec_status status_of(hipError_t e) { return e == hipSuccess ? REC_OK : REC_ERR_DEVICE; }
 
 }  // namespace
@@ -299,6 +343,11 @@ rec_status rec_rotate_heads(const rec_turn *t, void *stream)
     const int size = t->dtype == REC_F32 ? 4 : 2;
     if (t->heads && (!rows_fit(t->q, size) || !rows_fit(t->q_out, size) || !rows_apart(t->q_out, t->tokens, t->heads, t->head_dim))) return REC_ERR_ARG;
     if (t->kv_heads && (!rows_fit(t->k, size) || !rows_fit(t->k_out, size) || !rows_apart(t->k_out, t->tokens, t->kv_heads, t->head_dim))) return REC_ERR_ARG;
+    const Place q = {&t->q, t->heads}, k = {&t->k, t->kv_heads}, q_out = {&t->q_out, t->heads}, k_out = {&t->k_out, t->kv_heads};
+    const auto apart = [&](const Place &x, const Place &y, bool own) {
+        return !x.heads || !y.heads || places_apart(x, y, own, t->tokens, t->head_dim, size);
+    };
+    if (!apart(q_out, q, true) || !apart(k_out, k, true) || !apart(q_out, k, false) || !apart(k_out, q, false) || !apart(q_out, k_out, false)) return REC_ERR_ARG;
     if (t->pairs && (!t->dev_positions || !words_fit(t->dev_positions, t->wide ? 8 : 4) || !t->dev_frequencies || !words_fit(t->dev_frequencies, 8)))
         return REC_ERR_ARG;
     if ((t->dev_q_weight && !aligned(t->dev_q_weight)) || (t->dev_k_weight && !aligned(t->dev_k_weight))) return REC_ERR_ARG;

@@ -91,3 +91,73 @@ def test_python_refuses_tensors_that_do_not_fit(b, monkeypatch):
         a.update(kw)
         with pytest.raises(ValueError):
             b.rotate_heads(a.pop("q"), a.pop("k"), a.pop("positions"), a.pop("frequencies"), **a)
+
+
+def bytes_of(r, tokens, heads, d, size):
+    """Sets of 16-byte pieces that a rec_rows names."""
+    return {(r.dev + size * (t * r.token_stride + h * r.head_stride)) // 16 + i for t in range(tokens) for h in range(heads) for i in range(d * size // 16)}
+
+
+def places(tokens, heads, kv, d, size):
+    """Ways to lay q, k, q_out and k_out out, as (q, k, q_out, k_out) of (offset in elements, token stride, head stride)."""
+    far, all_ = 1 << 20, heads + 2 * kv
+    row = all_ * d                                              # a projection's output: queries, keys, values of a token
+    slices = ((0, row, d), (heads * d, row, d))
+    apart = ((2 * far, heads * d, d), (3 * far, kv * d, d))
+    yield *slices, *apart
+    yield *slices, *slices                                      # in place
+    yield *slices, slices[0], apart[1]
+    yield *slices, slices[1], slices[0]                         # each in the other's
+    yield *slices, slices[0], slices[0]
+    yield *slices, ((heads + kv) * d, row, d), apart[1]         # among the values
+    yield slices[0], slices[0], slices[0], apart[1]             # q is k, and gets its result first
+    yield slices[0], slices[0], *apart
+    by_three = ((0, 3 * heads * d, 3 * d), (d, 3 * heads * d, 3 * d))           # q, k and v of a head beside each other
+    yield *by_three, *by_three
+    yield *by_three, by_three[0], (2 * d, 3 * heads * d, 3 * d)
+    yield *by_three, *reversed(by_three)
+    by_head = ((0, d, tokens * d), (heads * tokens * d, d, tokens * d))         # heads before tokens
+    yield *by_head, *by_head
+    yield *by_head, by_head[0], (d, d, tokens * d)
+    woven = ((0, 2 * d, 2 * tokens * d), (d, 2 * d, 2 * tokens * d))            # the same, q's tokens between k's
+    yield *woven, *woven
+    for shift in (16 // size, d, row, -row, heads * d - 16 // size, row * (tokens - 1), row * tokens, -row * tokens):
+        yield slices[0], apart[1], (shift, row, d), (4 * far, kv * d, d)        # a result that lies a little further than q
+        yield apart[0], slices[0], (shift, row, d), (5 * far, kv * d, d)
+        yield *apart, (0, row, d), (shift, row, d)
+        yield *apart, (0, -row, d), (shift, -row, d)
+        yield *apart, (0, row, -d), (shift, row, -d)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls that are not refused would run")
+@pytest.mark.parametrize("tokens,heads,kv", [(1, 1, 1), (1, 3, 2), (2, 1, 1), (5, 4, 2), (7, 2, 2), (4, 1, 3), (9, 6, 1)])
+@pytest.mark.parametrize("dtype,size,d", [(2, 2, 64), (0, 4, 32)])
+def test_results_over_other_rows(b, tokens, heads, kv, dtype, size, d):
+    """A result may be what it is made of, and nothing else that the call reads or writes: which was there first would be left to chance."""
+    refused = allowed = 0
+    for place in places(tokens, heads, kv, d, size):
+        names, counts = ("q", "k", "q_out", "k_out"), (heads, kv, heads, kv)
+        rows = {n: b.rec_rows((1 << 30) + size * at, token, head) for n, (at, token, head) in zip(names, place)}
+        t = turn(b, tokens=tokens, heads=heads, kv_heads=kv, head_dim=d, pairs=0, dtype=dtype)
+        for n in names:
+            setattr(t, n, rows[n])
+        held = {n: bytes_of(rows[n], tokens, c, d, size) for n, c in zip(names, counts)}
+        clash = any(len(held[o]) < tokens * counts[names.index(o)] * d * size // 16 for o in ("q_out", "k_out")) or bool(held["q_out"] & held["k_out"])
+        for o in ("q_out", "k_out"):
+            for i in ("q", "k"):
+                same = o[0] == i and rows[o].dev == rows[i].dev and (tokens == 1 or rows[o].token_stride == rows[i].token_stride) and \
+                    (counts[names.index(o)] == 1 or rows[o].head_stride == rows[i].head_stride)
+                clash |= not same and bool(held[o] & held[i])
+        got = b._lib.rec_rotate_heads(C.byref(t), None)
+        assert got == (b.REC_ERR_ARG if clash else b.REC_ERR_DEVICE), (place, clash)      # no device: further than its checks
+        refused, allowed = refused + clash, allowed + (not clash)
+    assert refused > 5 and allowed > 5
+
+
+def test_results_between_rows_of_other_strides(b):
+    """Where that cannot be told from the strides alone, rows between each other's count as overlapping."""
+    base = dict(q=dict(dev=PTR), k=dict(dev=PTR + (1 << 24)), k_out=dict(dev=PTR + (1 << 25)))
+    for bad in (dict(dev=PTR, token_stride=512), dict(dev=PTR + 128, token_stride=512, head_stride=128)):
+        assert call(b, **base, q_out=bad) == b.REC_ERR_ARG, bad
+    huge = 1 << 60                      # spans that do not fit 64 bits
+    assert call(b, **base, q_out=dict(dev=PTR, token_stride=huge, head_stride=huge >> 3)) == b.REC_ERR_ARG
