@@ -1040,6 +1040,8 @@ def rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
         raise ValueError(f"rec_rotate_heads: positions must be a contiguous int32 or int64 [{tokens}] on {like.device}")
     if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or frequencies.get_device() != index or not frequencies.is_contiguous():
         raise ValueError(f"rec_rotate_heads: frequencies must be a contiguous float64 vector on {like.device}")
+    if frequencies.requires_grad:
+        _no_backward("rec_rotate_heads")
     st = _lib.rec_rotate_heads(
         _TURN.pack(*q_at, *k_at, *q_to, *k_to, code, heads, kv_heads, dim, tokens, positions.data_ptr(), at is _I64,
                    frequencies.numel(), frequencies.data_ptr(), 1 if interleaved else 0, eps, q_w, k_w), _stream_on(index, "rec_rotate_heads"))

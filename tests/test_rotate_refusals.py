@@ -161,3 +161,13 @@ def test_results_between_rows_of_other_strides(b):
         assert call(b, **base, q_out=bad) == b.REC_ERR_ARG, bad
     huge = 1 << 60                      # spans that do not fit 64 bits
     assert call(b, **base, q_out=dict(dev=PTR, token_stride=huge, head_stride=huge >> 3)) == b.REC_ERR_ARG
+
+
+def test_frequencies_that_require_grad(b, monkeypatch):
+    """As queries, keys and weights do: their gradients would be lost without a word."""
+    monkeypatch.setattr(b, "_lib", None)
+    x, f, at = on(torch.zeros(10, 2, 64)), on(torch.zeros(32, dtype=torch.float64, requires_grad=True)), on(torch.zeros(10, dtype=torch.int32))
+    with pytest.raises(ValueError, match="backward"):
+        b.rotate_heads(x, x, at, f)
+    with torch.no_grad(), pytest.raises(AttributeError):        # no library: further than the checks
+        b.rotate_heads(x, x, at, f)
