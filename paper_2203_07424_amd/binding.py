@@ -809,6 +809,8 @@ class HistoryCache:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != index or not out.is_contiguous():
             raise ValueError("rec_history_attend: out must be contiguous and of q's shape, type and device")
+        elif out.requires_grad:
+            _no_backward("rec_history_attend")
         width = pages_of.shape[1]
         query = _QUERY.pack(q.data_ptr(), out.data_ptr(), by_batch, by_query, by_head, code, batch, queries, heads, pages_of.data_ptr(),
                             pages_of.stride(0), width, lengths.data_ptr(), dim ** -0.5 if scale is None else scale, window, sinks,
@@ -890,6 +892,8 @@ class HistoryCache:
             return torch.empty_like(q, memory_format=torch.contiguous_format)
         if out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != self._index or not out.is_contiguous():
             raise ValueError(f"{call}: out must be contiguous and of q's shape, type and device")
+        if out.requires_grad:
+            _no_backward(call)
         return out
 
     def select(self, q: torch.Tensor, means: torch.Tensor, pages_of: torch.Tensor, lengths: torch.Tensor, count: int, first: int = 1,

@@ -186,3 +186,18 @@ def test_python_refuses_tensors_that_do_not_fit(b, monkeypatch):
         with pytest.raises(ValueError):
             h.summarise(which, m)
     assert isinstance(q, OnDevice)
+
+
+@pytest.mark.parametrize("name", ["attend", "attend_selected", "attend_shared"])
+def test_results_that_require_grad(b, monkeypatch, name):
+    """What autograd knows of such a tensor would be of what it held before."""
+    monkeypatch.setattr(b, "_lib", None)
+    h = object.__new__(b.HistoryCache)
+    h._index, h.head_dim, h.kv_heads, h.device, h._workspaces = 0, 64, 2, "cuda:0", {}
+    q, out = (on(torch.zeros(3, 2, 4, 64, dtype=torch.bfloat16, requires_grad=r)) for r in (False, True))
+    table, n, chosen, prefix, one = (on(torch.zeros(s, dtype=torch.int32)) for s in ((3, 5), (3,), (3, 2, 2, 4), (7,), (1,)))
+    args = dict(attend=(q, table, n), attend_selected=(q, chosen, table, n), attend_shared=(q, prefix, one, table, n))[name]
+    with pytest.raises(ValueError, match="backward"):
+        getattr(h, name)(*args, out=out)
+    with torch.no_grad(), pytest.raises(AttributeError):        # no library: further than the checks
+        getattr(h, name)(*args, out=out)
