@@ -12,6 +12,7 @@ import struct
 from typing import List, Optional, Sequence, Tuple
 
 import torch  # loads the HIP runtime the library binds to
+from torch.autograd import forward_ad
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 # REC_MI355X_LIBRARY: another build of the same library (the host-instrumented
@@ -703,6 +704,13 @@ def _no_backward(call: str) -> None:
         raise ValueError(f"{call} has no backward pass: detach its inputs, or call it under torch.no_grad()")
 
 
+def _no_tangent(call: str, *tensors: Optional[torch.Tensor]) -> None:
+    """While a level of forward-mode differentiation is open: tensors with a tangent are refused, which a result would lose unseen.
+    Grad mode has no part in those."""
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError(f"{call} has no derivatives: unpack its dual tensors")
+
+
 class HistoryCache:
     """Keys and values of user histories in 4 or 8 bits a number (include/rec_history.h), and
     attention over them.
@@ -710,7 +718,7 @@ class HistoryCache:
     The pages are one uint8 tensor, the cache's own or the caller's (`pages`, of
     [num_pages, kv_heads, page_tokens / 16, bytes of a group]); which page holds what is the
     caller's bookkeeping.  Calls go to the current stream and only enqueue.  They serve: there is no
-    backward pass, and inputs that require grad are refused unless grad mode is off."""
+    backward pass, and inputs that require grad are refused unless grad mode is off, those with a tangent always."""
 
     def __init__(self, num_pages: int, page_tokens: int, kv_heads: int, head_dim: int, fmt: str = "mx4",
                  device: str = "cuda:0", pages: Optional[torch.Tensor] = None):
@@ -757,6 +765,8 @@ class HistoryCache:
         slots: int64 [tokens], page * page_tokens + place, -1 for a row to leave out."""
         if k.requires_grad or v.requires_grad:
             _no_backward("rec_history_write")
+        if forward_ad._current_level >= 0:
+            _no_tangent("rec_history_write", k, v)
         n = self._slots("rec_history_write", slots)
         code = _DTYPE_CODES.get(k.dtype)
         if code is None:
@@ -788,6 +798,8 @@ class HistoryCache:
         int32 [batch].  scale: 1 / sqrt(head_dim) if None.  Returns attention outputs of q's shape, contiguous."""
         if q.requires_grad:
             _no_backward("rec_history_attend")
+        if forward_ad._current_level >= 0:
+            _no_tangent("rec_history_attend", q, out)
         index, code = self._index, _ATTEND_CODES.get(q.dtype)
         if q.dim() == 4:
             batch, queries, heads, dim = q.shape
@@ -844,6 +856,8 @@ class HistoryCache:
     def _means(self, call: str, means: torch.Tensor) -> None:
         if means.requires_grad:
             _no_backward(call)
+        if forward_ad._current_level >= 0:
+            _no_tangent(call, means)
         if means.shape != self._means_shape or means.dtype is not torch.bfloat16 or means.get_device() != self._index or not means.is_contiguous():
             raise ValueError(f"{call}: means must be a contiguous bfloat16 {list(self._means_shape)} on {self.device}")
 
@@ -852,6 +866,8 @@ class HistoryCache:
         """A query without window and sinks as rec_query, and the shapes that decide its workspace."""
         if q.requires_grad:
             _no_backward(call)
+        if forward_ad._current_level >= 0:
+            _no_tangent(call, q)
         index, code = self._index, _ATTEND_CODES.get(q.dtype)
         if q.dim() == 4:
             batch, queries, heads, dim = q.shape
@@ -894,6 +910,8 @@ class HistoryCache:
             raise ValueError(f"{call}: out must be contiguous and of q's shape, type and device")
         if out.requires_grad:
             _no_backward(call)
+        if forward_ad._current_level >= 0:
+            _no_tangent(call, out)
         return out
 
     def select(self, q: torch.Tensor, means: torch.Tensor, pages_of: torch.Tensor, lengths: torch.Tensor, count: int, first: int = 1,
@@ -979,6 +997,8 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: to
     fault: int64 [REC_FAULT_WORDS], contiguous, all -1, for rec_history_check(), or None.  No backward pass, as in HistoryCache."""
     if q.requires_grad or k.requires_grad or v.requires_grad:
         _no_backward("rec_window_attend")
+    if forward_ad._current_level >= 0:
+        _no_tangent("rec_window_attend", q, k, v)
     code, index = _ATTEND_CODES.get(q.dtype), q.get_device()
     if code is None or index < 0 or q.dim() != 3 or k.dim() != 3 or k.shape != v.shape:
         raise ValueError("rec_window_attend: q must be [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim] on a device, "
@@ -1046,6 +1066,8 @@ def rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
         raise ValueError(f"rec_rotate_heads: frequencies must be a contiguous float64 vector on {like.device}")
     if frequencies.requires_grad:
         _no_backward("rec_rotate_heads")
+    if forward_ad._current_level >= 0:
+        _no_tangent("rec_rotate_heads", q, k, frequencies, q_weight, k_weight, q_out, k_out)
     st = _lib.rec_rotate_heads(
         _TURN.pack(*q_at, *k_at, *q_to, *k_to, code, heads, kv_heads, dim, tokens, positions.data_ptr(), at is _I64,
                    frequencies.numel(), frequencies.data_ptr(), 1 if interleaved else 0, eps, q_w, k_w), _stream_on(index, "rec_rotate_heads"))

@@ -118,3 +118,38 @@ def test_tensors_that_require_grad_are_refused(b):
             with torch.no_grad(), pytest.raises(ValueError) as e:      # what the call says next: not on a device
                 call(*args)
             assert "backward" not in str(e.value)
+
+
+@pytest.mark.parametrize("which", ["write", "attend", "window", "means", "select", "attend_selected", "attend_shared", "rotate"])
+def test_tensors_with_a_tangent_are_refused(b, monkeypatch, which):
+    """Forward-mode differentiation: a dual tensor does not require grad, and is one under torch.no_grad() too."""
+    from torch.autograd import forward_ad
+    monkeypatch.setattr(b, "_lib", None)
+
+    class Here(torch.Tensor):
+        def get_device(self):
+            return 0
+
+    on = lambda x: x.as_subclass(Here)  # noqa: E731
+    h = object.__new__(b.HistoryCache)
+    h._index, h.head_dim, h.kv_heads, h.device, h._means_shape, h._workspaces = 0, 64, 2, "cuda:0", (6, 2, 64), {}
+    bf = dict(dtype=torch.bfloat16)
+    q, out, means, k = (on(torch.zeros(s, **bf)) for s in ((3, 2, 4, 64), (3, 2, 4, 64), (6, 2, 64), (3, 2, 64)))
+    table, n, chosen, prefix, one = (on(torch.zeros(s, dtype=torch.int32)) for s in ((3, 5), (3,), (3, 2, 2, 4), (7,), (1,)))
+    w, f = on(torch.ones(64)), on(torch.zeros(32, dtype=torch.float64))
+    call, args = dict(write=(lambda x, y: h.write(x, y, n.long()), (k, k)), attend=(lambda x, o: h.attend(x, table, n, out=o), (q, out)),
+                      window=(lambda x, y, z: b.attend_window(x, y, z, n), (k, k, k)), means=(lambda m: h.summarise(n, m), (means,)),
+                      select=(lambda x, m: h.select(x, m, table, n, 4, out=chosen), (q, means)),
+                      attend_selected=(lambda x, o: h.attend_selected(x, chosen, table, n, out=o), (q, out)),
+                      attend_shared=(lambda x, o: h.attend_shared(x, prefix, one, table, n, out=o), (q, out)),
+                      rotate=(lambda x, y, e, v, z, o, p: b.rotate_heads(x, y, n, e, v, z, q_out=o, k_out=p), (k, k, f, w, w, k, k)))[which]
+    with forward_ad.dual_level():
+        for i, x in enumerate(args):
+            dual = on(forward_ad.make_dual(x.as_subclass(torch.Tensor), torch.ones(x.shape, dtype=x.dtype)))
+            assert forward_ad.unpack_dual(dual).tangent is not None and not dual.requires_grad
+            with torch.no_grad(), pytest.raises(ValueError, match="derivative"):
+                call(*args[:i], dual, *args[i + 1:])
+        with pytest.raises(AttributeError):                     # no library: further than the checks
+            call(*args)
+    with pytest.raises(AttributeError):
+        call(*args)
