@@ -240,6 +240,20 @@ __host__ __device__ constexpr int row_tiles_of(int d, bool bf)
 }
 constexpr int ROW_WAVES = 4, GROUPS = 2;  // of a block
 
+// The block of 32 columns of which wave w of a group makes half h of a tile's values, or -1: each is made once.
+__host__ __device__ constexpr int block_made(int d, int w, int h) { return d == 128 ? w : (w & 1) == h && w / 2 < d / BLOCK ? w / 2 : -1; }
+constexpr bool each_made_once(int d)
+{
+    for (int i = 0; i < d / BLOCK; ++i)
+        for (int h = 0; h < 2; ++h) {
+            int by = 0;
+            for (int w = 0; w < ROW_WAVES; ++w) by += block_made(d, w, h) == i ? 1 : 0;
+            if (by != 1) return false;
+        }
+    return true;
+}
+static_assert(each_made_once(32) && each_made_once(64) && each_made_once(128), "two waves would store to one place");
+
 // This lane's codes and scales of one block of 32 columns of a tile's values.
 template <int FMT, int D>
 __device__ inline void load_block(Tile<FMT, 32> &t, const unsigned char *vg, int b, int c)
@@ -361,12 +375,15 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
     // Bit t: token t of this lane's group of tile n is seen.
     auto seen_of = [&](int n, int page) { return (unsigned)page < pages ? below(len - n * TILE - 16 * g) : 0u; };
 
-    // What this wave makes of a tile's values: both halves of a block of 32 columns, one of them, or nothing.
-    const int block = D == 128 ? part_of_rows : D == 64 ? part_of_rows >> 1 : 0;
+    // What this wave makes of a tile's values: both halves of a block of 32 columns, one of them, or (of one block) nothing.
+    const int first_half = block_made(D, part_of_rows, 0), second_half = block_made(D, part_of_rows, 1), block = max(first_half, second_half);
     u32x4 *const values = lds + group * 2 * VALUES;
     Tile<FMT, 32> made;
-    auto load_made = [&](int n, int page) { load_block<FMT, D>(made, group_at(page, n * TILE + 16 * g), block, c); };
+    auto load_made = [&](int n, int page) {
+        if (block >= 0) load_block<FMT, D>(made, group_at(page, n * TILE + 16 * g), block, c);
+    };
     auto make = [&](unsigned seen, bool whole, int buffer) {
+        if (block < 0) return;
         if (!whole) hide<FMT>(made, seen);
         u32x4 *to = values + buffer * VALUES + block * 4 * 64 + lane;
         auto half = [&](auto h) {
@@ -375,8 +392,8 @@ __global__ __launch_bounds__(64 * ROW_WAVES * GROUPS, 2) void wide_kernel(Shared
             to[(2 * h()) * 64] = lo;
             to[(2 * h() + 1) * 64] = hi;
         };
-        if (D == 128 || (part_of_rows & 1) == 0) half(std::integral_constant<int, 0>());
-        if (D == 128 || (part_of_rows & 1) == 1) half(std::integral_constant<int, 1>());
+        if (first_half >= 0) half(std::integral_constant<int, 0>());
+        if (second_half >= 0) half(std::integral_constant<int, 1>());
     };
 
     int n = begin + group;
