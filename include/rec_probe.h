@@ -110,6 +110,19 @@ REC_API rec_status rec_probe_dense_copy(int32_t rows, int32_t columns, int32_t p
  * Errors as there; REC_ERR_ARG on a null form. */
 REC_API rec_status rec_probe_history_form(const rec_history *h, const rec_query *q, int32_t *form);
 
+/* What rec_history_select() would run: form[0] launches (where scores have to be in memory, one for them and one for the choice), form[1] rows that a
+ * wave scores at once, form[2] waves that a row's choice takes. */
+REC_API rec_status rec_probe_select_form(const rec_history *h, const rec_query *q, int32_t count, int32_t *form);
+
+/* form[0] of rec_probe_shared_form(). */
+enum {
+    REC_SHARED_JOINED = 0, /* each history reads the prefix by itself */
+    REC_SHARED_NARROW = 1, /* the prefix in a launch of its own, in blocks of 16 rows ... */
+    REC_SHARED_WIDE = 2    /* ... of 64 rows and more */
+};
+/* What rec_history_attend_shared() would run: form[1] parts of the prefix, form[2] of the histories behind it (REC_SHARED_JOINED: 0, and of both). */
+REC_API rec_status rec_probe_shared_form(const rec_history *h, const rec_query *q, int32_t prefix_width, int32_t *form);
+
 /* The end of rec_history_check() (rec_history.h): words of a fault record become all ones where they
  * still are what was read before, seen[] (host memory, as many words as a record has).  REC_ERR_ARG: null, misaligned. */
 REC_API rec_status rec_probe_clear_faults(uint64_t *dev_fault, const uint64_t *seen, void *stream);

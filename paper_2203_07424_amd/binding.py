@@ -35,6 +35,7 @@ REC_STATIC_SCRATCH_BYTES = 64 << 20
 REC_STATIC_MAX_TABLES = 64
 REC_F32, REC_F16, REC_BF16 = 0, 1, 2
 REC_MX4, REC_MX8 = 0, 1
+REC_SHARED_JOINED, REC_SHARED_NARROW, REC_SHARED_WIDE = 0, 1, 2
 REC_FAULT_LENGTH, REC_FAULT_SLOT, REC_FAULT_PAGE, REC_FAULT_VALUE, REC_FAULT_WORDS = 0, 1, 2, 3, 4
 REC_BOTTOM, REC_TOP = 0, 1          # REC_TOP + k: tower k of the Predict-FC
 REC_INTERACT_DOT, REC_INTERACT_CONCAT = 0, 1
@@ -61,7 +62,7 @@ EXPORTS = ("rec_create", "rec_destroy", "rec_workspace_bytes", "rec_bind_workspa
            "rec_history_attend", "rec_history_summarise", "rec_history_select_workspace_bytes", "rec_history_select",
            "rec_history_attend_selected_workspace_bytes", "rec_history_attend_selected",
            "rec_history_attend_shared_workspace_bytes", "rec_history_attend_shared", "rec_window_attend", "rec_rotate_heads",
-           "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form")
+           "rec_history_check", "rec_probe_clear_faults", "rec_probe_history_form", "rec_probe_select_form", "rec_probe_shared_form")
 
 
 class rec_config(C.Structure):
@@ -197,6 +198,8 @@ _lib.rec_history_check.restype = C.c_int
 _lib.rec_history_check.argtypes = [_vp, _vp, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
 _lib.rec_probe_history_form.restype = C.c_int
 _lib.rec_probe_history_form.argtypes = [_vp, _vp, C.POINTER(C.c_int32)]
+for _probe in (_lib.rec_probe_select_form, _lib.rec_probe_shared_form):
+    _probe.restype, _probe.argtypes = C.c_int, [_vp, _vp, C.c_int32, C.POINTER(C.c_int32)]
 _lib.rec_probe_clear_faults.restype = C.c_int
 _lib.rec_probe_clear_faults.argtypes = [_vp, C.POINTER(C.c_uint64), _vp]
 # The same layouts for one packing call, a quarter of the time of setting a structure's fields.
@@ -471,6 +474,20 @@ def rec_probe_history_form(h: rec_history, q: rec_query) -> Tuple[int, int, int,
     """(status, waves of a block, parts of a history, kv heads of a wave)."""
     form = (C.c_int32 * 3)()
     st = _lib.rec_probe_history_form(C.byref(h), C.byref(q), form)
+    return (st, *form)
+
+
+def rec_probe_select_form(h: rec_history, q: rec_query, count: int) -> Tuple[int, int, int, int]:
+    """(status, launches, rows that a wave scores at once, waves of a choice)."""
+    form = (C.c_int32 * 3)()
+    st = _lib.rec_probe_select_form(C.byref(h), C.byref(q), count, form)
+    return (st, *form)
+
+
+def rec_probe_shared_form(h: rec_history, q: rec_query, prefix_width: int) -> Tuple[int, int, int, int]:
+    """(status, REC_SHARED_*, parts of the prefix, parts of the histories)."""
+    form = (C.c_int32 * 3)()
+    st = _lib.rec_probe_shared_form(C.byref(h), C.byref(q), prefix_width, form)
     return (st, *form)
 
 

@@ -111,6 +111,7 @@ struct Prefix {
 long long joined_work(const Cache &c, const rec_query &q, int prefix_width);
 long long joined_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
 size_t joined_workspace(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
+int joined_parts(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
 hipError_t launch_joined(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s);
 // Of a row whose parts are joined; of those, parts of what stands before its history.
 constexpr int MOST_PARTS = 64, MOST_BEFORE = 32;
@@ -119,6 +120,7 @@ int own_parts(const Cache &c, int format, int d, const rec_query &q);
 hipError_t launch_behind(const Cache &c, int format, int d, const rec_query &q, const Parts &parts, int before, hipStream_t s);
 long long shared_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
 size_t shared_workspace(const Cache &c, int format, int d, const rec_query &q, int prefix_width);
+void shared_form(const Cache &c, int format, int d, const rec_query &q, int prefix_width, int32_t (&form)[3]);
 hipError_t launch_shared(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s);
 hipError_t launch_means(const Cache &c, int format, int d, const int32_t *which, int pages, void *means, hipStream_t s);
 long long means_threads(const Cache &c, int d, int pages);
@@ -130,6 +132,7 @@ struct Select {
 };
 long long select_threads(const Cache &c, int d, const rec_query &q);
 size_t select_workspace(const Cache &c, int d, const rec_query &q, int count);
+void select_form(const Cache &c, int d, const rec_query &q, int count, int32_t (&form)[3]);
 hipError_t launch_select(const Cache &c, int d, const rec_query &q, const Select &sel, hipStream_t s);
 long long window_blocks(const rec_window &w);  // of 256 threads
 hipError_t launch_window(const rec_window &w, hipStream_t s);

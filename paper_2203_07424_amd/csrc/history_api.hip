@@ -386,6 +386,28 @@ rec_status rec_probe_history_form(const rec_history *h, const rec_query *q, int3
     return REC_OK;
 }
 
+rec_status rec_probe_select_form(const rec_history *h, const rec_query *q, int32_t count, int32_t *form)
+{
+    if (!form) return REC_ERR_ARG;
+    const rec_status st = check_select(h, q, count);
+    if (st != REC_OK) return st;
+    int32_t f[3];
+    rec::hist::select_form(cache_of(h), h->head_dim, *q, count, f);
+    for (int i = 0; i < 3; ++i) form[i] = f[i];
+    return REC_OK;
+}
+
+rec_status rec_probe_shared_form(const rec_history *h, const rec_query *q, int32_t prefix_width, int32_t *form)
+{
+    if (!form) return REC_ERR_ARG;
+    const rec_status st = check_shared(h, q, prefix_width);
+    if (st != REC_OK) return st;
+    int32_t f[3];
+    rec::hist::shared_form(cache_of(h), h->format, h->head_dim, *q, prefix_width, f);
+    for (int i = 0; i < 3; ++i) form[i] = f[i];
+    return REC_OK;
+}
+
 rec_status rec_probe_clear_faults(uint64_t *dev_fault, const uint64_t *seen, void *stream)
 {
     if (!dev_fault || !words_fit(dev_fault, 8) || !seen) return REC_ERR_ARG;

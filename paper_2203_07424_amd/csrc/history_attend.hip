@@ -548,6 +548,8 @@ size_t joined_workspace(const Cache &c, int format, int d, const rec_query &q, i
     return workspace_of(joined_plan(c, format, d, q, prefix_width), d);
 }
 
+int joined_parts(const Cache &c, int format, int d, const rec_query &q, int prefix_width) { return joined_plan(c, format, d, q, prefix_width).splits; }
+
 hipError_t launch_joined(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s)
 {
     const Plan p = joined_plan(c, format, d, q, prefix.width);

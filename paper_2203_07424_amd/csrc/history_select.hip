@@ -720,6 +720,14 @@ size_t select_workspace(const Cache &c, int d, const rec_query &q, int count)
     return (size_t)q.batch * q.queries * c.kv_heads * (size_t)q.table_width * sizeof(u64);
 }
 
+void select_form(const Cache &c, int d, const rec_query &q, int count, int32_t (&form)[3])
+{
+    const SelectArgs a = args_of(c, d, q);
+    form[0] = a.walks == 0 || q.table_width <= count ? 1 : 2;
+    form[1] = a.at_once * std::min(a.per, 16);
+    form[2] = a.walks == 0 ? 1 : choose_waves(q);
+}
+
 hipError_t launch_select(const Cache &c, int d, const rec_query &q, const Select &sel, hipStream_t s)
 {
     SelectArgs a = args_of(c, d, q);

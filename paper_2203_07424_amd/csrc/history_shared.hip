@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "history_attend_body.h"
+#include "rec_probe.h"
 
 namespace rec {
 namespace hist {
@@ -682,6 +683,20 @@ size_t shared_workspace(const Cache &c, int format, int d, const rec_query &q, i
     if (joined(c, q, prefix_width)) return joined_workspace(c, format, d, q, prefix_width);
     const Plan p = plan_of(c, format, d, q, prefix_width);
     return (size_t)(p.splits + (p.own == 1 ? 0 : p.own)) * (size_t)p.rows * ((size_t)d * sizeof(float) + sizeof(f32x2));
+}
+
+void shared_form(const Cache &c, int format, int d, const rec_query &q, int prefix_width, int32_t (&form)[3])
+{
+    if (q.batch == 0 || q.queries == 0 || joined(c, q, prefix_width)) {
+        form[0] = REC_SHARED_JOINED;
+        form[1] = 0;
+        form[2] = joined_parts(c, format, d, q, prefix_width);
+        return;
+    }
+    const Plan p = plan_of(c, format, d, q, prefix_width);
+    form[0] = p.wide ? REC_SHARED_WIDE : REC_SHARED_NARROW;
+    form[1] = p.splits;
+    form[2] = p.own;
 }
 
 hipError_t launch_shared(const Cache &c, int format, int d, const rec_query &q, const Prefix &prefix, void *workspace, hipStream_t s)
