@@ -423,7 +423,7 @@ struct Plan {
 };
 
 // `most` is of parts.
-Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int most = MOST_PARTS)
+Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int kind = WHOLE, int most = MOST_PARTS)
 {
     Plan p;
     p.per = q.heads / c.kv_heads;
@@ -448,10 +448,11 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int most = M
     // then cost it no more than for one.
     if (d <= 64 && p.waves == 1 && pairs >= 16 * CUS) p.heads = rows <= ROWS / 2 && c.kv_heads % 2 == 0 ? 2 : 1;
     // Long histories of few pairs: as many parts as are all at work at once (a part too many waits
-    // for a place and then reads alone: 4 parts of 256 pairs in 3 places 221 us, 3 parts 199), of two tiles a wave at least.
+    // for a place and then reads alone: 4 parts of 256 pairs in 3 places 221 us, 3 parts 199; 400 pairs of 1000 tokens behind 4000, of 32 columns in
+    // mx8, two parts 21.2, one 19.7), of two tiles a wave at least.
     // Where pairs alone take all places, parts of eight tiles a wave, up to four, for the longest of ragged
     // histories (1600 pairs up to 8000 long 51 -> 43 us; all alike 171 -> 178).
-    const long long room = 4ll * waves_of(format, d, q.dtype == REC_BF16, 1) * CUS / (pairs * p.waves);
+    const long long room = 4ll * waves_of(format, d, q.dtype == REC_BF16, 1, kind) * CUS / (pairs * p.waves);
     const long long parts = room > 1 ? std::min({room, tiles / (2 * p.waves), (long long)most}) : p.waves == 4 ? std::min(tiles / (8 * p.waves), 4ll) : 1;
     p.splits = (int)std::max(1ll, parts);
     return p;
@@ -533,7 +534,7 @@ long long joined_work(const Cache &c, const rec_query &q, int prefix_width)
 
 Plan joined_plan(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
 {
-    Plan p = plan_of(c, format, d, joined_query(q, prefix_width));
+    Plan p = plan_of(c, format, d, joined_query(q, prefix_width), JOINED);
     p.heads = 1;
     return p;
 }
@@ -558,11 +559,11 @@ hipError_t launch_joined(const Cache &c, int format, int d, const rec_query &q, 
     return attend_any(a, p, format, d, s);
 }
 
-int own_parts(const Cache &c, int format, int d, const rec_query &q) { return plan_of(c, format, d, q, MOST_PARTS - MOST_BEFORE).splits; }
+int own_parts(const Cache &c, int format, int d, const rec_query &q) { return plan_of(c, format, d, q, BEHIND, MOST_PARTS - MOST_BEFORE).splits; }
 
 hipError_t launch_behind(const Cache &c, int format, int d, const rec_query &q, const Parts &parts, int before, hipStream_t s)
 {
-    Plan p = plan_of(c, format, d, q, MOST_PARTS - MOST_BEFORE);
+    Plan p = plan_of(c, format, d, q, BEHIND, MOST_PARTS - MOST_BEFORE);
     p.join = false;
     const long long at = before * p.rows;
     AttendArgs a = args_of(c, d, q, p, parts.o + at * d);

@@ -60,6 +60,15 @@ def test_forms_behind_a_prefix(b):
     assert shared(b, 0, 1, 1, 2, 64, "mx4", bf, 32, 500, 1) == shared(b, 4, 0, 1, 2, 64, "mx4", bf, 32, 500, 1) == (joined, 0, 1)
 
 
+@pytest.mark.parametrize("dtype", ["REC_BF16", "REC_F16"])
+def test_parts_behind_a_prefix_are_all_at_work_at_once(b, dtype):
+    """Four waves a history, head and part; a SIMD of 1024 holds three of the kernel behind a prefix, at 32 columns in mx8, else as many as without one."""
+    for fmt, places in (("mx8", 3), ("mx4", 4)):
+        for batch, own in ((64, 4000), (100, 1000), (150, 2000), (16, 8000)):
+            form, _, parts = shared(b, batch, 1, 2, 4, 32, fmt, getattr(b, dtype), 32, 8000 // 32, own // 32)
+            assert form == b.REC_SHARED_NARROW and parts == max(1, min(places * 1024 // (batch * 4 * 4), -(-own // 64) // 8)), (fmt, batch, parts)
+
+
 def test_refused_calls_have_no_form(b):
     h = cache(b)
     for probe in (b.rec_probe_select_form, b.rec_probe_shared_form):
