@@ -292,7 +292,7 @@ REC_API rec_status rec_window_attend(const rec_window *w, void *stream);
  * Squares are summed in fp32, or in 64 bits where that would overflow or vanish; angles are worked out in 64 bits.
  * REC_ERR_ARG: null, misaligned, bad enum, negative counts or eps, rows of q_out or k_out that overlap each other or q and k;
  * REC_ERR_SHAPE: head_dim or pairs; REC_ERR_OVERFLOW: more than 2^20 heads, or more threads
- * than a launch can have (2^32; a wave has 2 to 32 rows).
+ * than a launch can have (2^32; a wave has 4 to 32 rows).
  */
 typedef struct {
     rec_rows q, k, q_out, k_out;

@@ -2,10 +2,12 @@
 //
 // The products are those of history_attend.hip: a wave has 16 rows, here the heads of one query and kv head, and walks over 64 of the
 // chosen tokens at a time.  Where a page lies takes two trips to memory, so a wave looks up 64 pages at once, one a lane, and asks
-// lanes for them.  Two tiles are on their way in registers: lists are short, and with one a tile took a trip to memory
-// (1024 queries, 2 kv heads of 64 with 4 rows each, mx8, up to 768 tokens: 22 us, issue-bound: 350 vector instructions
-// a tile, of which a SIMD has two waves, while most histories are shorter; 16 histories of 2048 chosen tokens, 8 kv heads of 128, mx4: 14 us,
-// 3.7 TB/s).  All rows stand at one position, so that a tile's tokens are seen by all or none.
+// lanes for them.  Two tiles are on their way in registers: lists are short, and with one a tile took a trip to memory.
+// All rows stand at one position, so that a tile's tokens are seen by all or none.
+//
+// 1024 queries, 2 kv heads of 64 with 4 rows each, mx8, up to 768 tokens: 22.6 us, bound by the longest lists: a wave has one list, of 5 tiles
+// on average, a quarter of them of 12, which it walks over one behind the other (350 vector instructions a tile are 6 us of a SIMD in all).
+// 16 histories of 2048 chosen tokens, 8 kv heads of 128, mx4: 35.7 MB in 14 us, 2.5 TB/s: 128 blocks of eight waves, on half of the compute units.
 #include <algorithm>
 
 #include "history_attend_body.h"

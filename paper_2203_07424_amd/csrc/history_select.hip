@@ -2,7 +2,7 @@
 //
 // means_kernel: a lane has 32 columns of a token at a time, one scale's, and adds up its tokens'; lanes of different rows of 16 meet by
 // swaps, which leave each a half of its columns, those of a row by rotations.  Bound by the keys' bytes: 8192 pages of 64 tokens,
-// 8 heads of 128, mx4 62 us, 4.9 TB/s, with columns halved by shuffles, through the caches and with a page looked up a lane 79.
+// 8 heads of 128, mx4 62 us, 4.9 TB/s, with columns halved by shuffles, through the caches and with a page looked up a lane 79; mx8 124 us, 4.6 TB/s.
 //
 // score_pages(): products of queries and means, in 64 bits on the matrix instructions (16 x 16 x 4): which of two pages
 // comes first must not hang on the order of a sum.  Operands are bf16 or fp16 numbers, so that their products are exact.
@@ -13,7 +13,8 @@
 // numbers it lies in and counting over all lanes.
 //
 // In one launch, 16 histories of 512 pages, 8 kv heads of 128 with 4 rows each: 14 us, of which 1.5 are the length and the pages one behind the
-// other, 7 the scores (two waves of a SIMD, 4 tiles each), 3.5 the choice (8 counts of 470 cycles); 256 x 4 queries of 47 pages: 8.5 us.
+// other, 7 the scores (two waves of a SIMD, 4 tiles each, on half of the compute units: 128 blocks), 3.5 the choice (8 counts of 470 cycles); 256 x 4
+// queries of 47 pages: 8.5 us.  In two launches, 16 histories of 4096 pages as above: 134 MB of means in 48 us, 2.8 TB/s.
 #include <algorithm>
 
 #include "history.h"
@@ -613,7 +614,9 @@ SelectArgs args_of(const Cache &c, int d, const rec_query &q)
     a.each = 0;
     // In one launch where a wave has all of a row's keys in its lanes and the block's tiles do not take longer than a second launch (4 histories,
     // 2 kv heads of 64, 4 rows: 512 pages 8.7 us in one, 9.2 in two, 1024 pages 19 and 10; 8 rows of 128: 256 pages 14.4 and 12.8, 512 pages
-    // 22 and 12.7; 256 such histories: 256 pages 27 and 32, 512 pages 47 and 48).
+    // 22 and 12.7; 256 such histories: 256 pages 27 and 32, 512 pages 47 and 48.  8 kv heads of 128: 4 histories of 4 rows, 300 pages 10.8 and 11.4, 512
+    // 14.9 and 14.4, 16 histories 11.4 and 16.2, 14.0 and 18.1, 64 histories 21 and 25, 26 and 34; 16 of 8 rows, 256 pages 15.6 and 15.8, 384 19.0 and 16.7,
+    // 64 of them 26 and 32, 34 and 37).
     if (q.table_width <= WAVE_KEYS) {
         with(MOST_KEYS / std::max(q.table_width, 1));
         if (tiles * (d / 32) * (a.at_once * a.per <= 4 ? 1 : 2) <= 128) {

@@ -5,7 +5,8 @@
 // have every other tile of keys and meet in LDS in the end.  The four waves of a group share a tile's values: each makes a
 // quarter of them into bf16, in the order of the operands, in LDS, while the tile before is multiplied.  Keys go into the products as they are stored.
 // Bound by matrix instructions and exponentials, which the two groups' halves of a turn overlap in part: 1024 rows of each of 8 kv heads of 128, mx4, before
-// 8192 tokens 46 us, 750 TFLOP/s of the plain products.
+// 8192 tokens 46 us, 750 TFLOP/s of the plain products.  (With the launch behind it 59 us in bf16, mx8 too, and 79 in fp16, 81 in mx8: twice the weights' products, half
+// as many row tiles.)
 // narrow_kernel: one tile of 16 rows, whose keys four waves share.
 //
 // What that leaves are parts of the rows' sums; attend_kernel joins them with what each history holds of its own.  Where there is little to
@@ -629,7 +630,8 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int prefix_w
     p.blocks = (int)((of_head + per_block - 1) / per_block * c.kv_heads);
     p.own = own_parts(c, format, d, q);
     // Parts of the prefix: as many as end soonest, at what a block's start and end cost beside its tiles, where so many
-    // blocks work at once (two narrow ones of a compute unit; planned for four, 1024 rows of 2 heads of 128 before 2000 tokens take 28 us, so 20).
+    // blocks work at once (two narrow ones of a compute unit: of 128 columns a SIMD's registers hold two waves; planned for four, 1024 rows of 2 heads
+    // of 128 before 2000 tokens take 28 us, so 20).
     const long long waves = p.wide ? GROUPS : 4, at_once = p.wide ? CUS : 2 * CUS;
     long long best = 0;
     p.splits = 1;
@@ -667,7 +669,9 @@ hipError_t shared_of(const SharedArgs &a, const Plan &p, int format, hipStream_t
 
 // Few tiles in all: each history reads the prefix for itself, in one launch.  4 kv heads of 64, mx8, fp16, 20 events behind a prefix: 8 histories
 // behind 400 tokens 6.5 us so, 10.5 in two launches, 128 (4096 tiles) 8.6 and 11.4, 32 behind 4000 (8192 tiles) 16.0 and 13.2, 128 behind 1000
-// (8704) 14.4 and 11.4.
+// (8704) 14.4 and 11.4.  4 kv heads of 32, mx4, bf16: 128 behind 300 (3584 tiles) 6.8 and 9.5, 500 (5120) 7.5 and 9.6, 1000 (9216) 12.9 and 9.6; 32 behind
+// 2000 (4352) 10.1 both ways; of 128, mx8, fp16: 12.3 and 13.6, 14.0 and 14.7, 20.1 and 15.0, 16.1 and 15.8; of 128, mx4, bf16: 9.9 and 12.5, 11.1 and 13.0,
+// 15.6 and 13.9, 13.4 and 15.6.
 bool joined(const Cache &c, const rec_query &q, int prefix_width) { return joined_work(c, q, prefix_width) <= 4096; }
 
 long long shared_threads(const Cache &c, int format, int d, const rec_query &q, int prefix_width)
