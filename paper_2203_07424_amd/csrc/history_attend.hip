@@ -437,7 +437,7 @@ Plan plan_of(const Cache &c, int format, int d, const rec_query &q, int kind = W
     long long tiles = (((long long)q.table_width << c.page_shift) + TILE - 1) / TILE;
     if (q.window) {
         const long long apart = q.candidates ? 0 : std::min<long long>(q.queries - 1, (ROWS - 1) / p.per + 1);
-        tiles = std::min(tiles, (q.window + apart + TILE - 2) / TILE + 1 + (q.sinks + TILE - 1ll) / TILE);
+        tiles = std::min(tiles, (q.window + apart + TILE - 2) / TILE + 1 + ((long long)q.sinks + TILE - 1) / TILE);
     }
     // Several waves for a history where there are few pairs, and where the longest may be much longer than most:
     // a wave that has it alone works on when all others are done.  64-wide mx4, 4 kv heads, lengths up to 2000,

@@ -47,6 +47,13 @@ def test_forms(b):
     assert form(b, 0, 1, 4, 2, 64, "mx4", bf, 32, 70) == form(b, 5, 1, 4, 2, 64, "mx4", bf, 32, 0) == (1, 1, 1)
 
 
+@pytest.mark.parametrize("sinks", [2 ** 31 - 1, 2 ** 31 - 64, 2 ** 31 - 65, 1 << 20])
+def test_as_many_first_events_as_there_are(b, sinks):
+    """All of a history is seen, whatever the window: as without one."""
+    for batch, width in ((1, 512), (32, 512), (1024, 8), (1100, 150)):
+        assert form(b, batch, 1, 4, 2, 64, "mx4", b.REC_BF16, 64, width, window=100, sinks=sinks) == form(b, batch, 1, 4, 2, 64, "mx4", b.REC_BF16, 64, width)
+
+
 def test_a_divided_history_needs_its_workspace(b):
     h, q = cache(b, num_pages=100000), query(b, batch=1, table_width=2000)
     need = b.rec_history_attend_workspace_bytes(h, q)
