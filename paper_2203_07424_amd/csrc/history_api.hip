@@ -322,7 +322,7 @@ rec_status rec_window_attend(const rec_window *w, void *stream)
         return REC_ERR_ARG;
     if (!head_dim_fits(w->head_dim) || w->heads % w->kv_heads) return REC_ERR_SHAPE;
     if (w->tokens > MOST_TOKENS || w->tokens * w->heads >= 1ll << 31) return REC_ERR_OVERFLOW;
-    if (rec::hist::window_blocks(*w) * 256 > MOST_THREADS || !tiles_fit(w->k) || !tiles_fit(w->v)) return REC_ERR_OVERFLOW;
+    if (rec::hist::window_blocks(*w) > MOST_THREADS / 256 || !tiles_fit(w->k) || !tiles_fit(w->v)) return REC_ERR_OVERFLOW;
     if (w->tokens == 0 || w->batch == 0) return REC_OK;
     if (!rows_fit(w->q, 2) || !rows_fit(w->k, 2) || !rows_fit(w->v, 2) || !aligned(w->dev_out) || !w->dev_offsets ||
         !words_fit(w->dev_offsets, 4) || !words_fit(w->dev_fault, 8))

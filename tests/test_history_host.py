@@ -103,6 +103,14 @@ def test_more_rows_than_a_launch_has_threads_for(b, kv_heads):
         assert b._lib.rec_history_read(C.byref(h), PTR, n, b.REC_F32, PTR, PTR, None) == b.REC_ERR_OVERFLOW, n
 
 
+@pytest.mark.parametrize("batch", [1 << 25, 1 << 26, (1 << 26) + 1, 1 << 27, (1 << 31) - 1])
+def test_more_histories_than_a_launch_has_blocks_for(b, batch):
+    """2^56 blocks of 256 threads are 2^64: refused as well, not as few as what is left of that in 64 bits."""
+    from test_history_refusals import window
+    w = window(b, batch=batch, tokens=1, heads=1 << 30, kv_heads=1 << 30)
+    assert b._lib.rec_window_attend(C.byref(w), None) == b.REC_ERR_OVERFLOW
+
+
 def test_tensors_that_require_grad_are_refused(b):
     """There is no backward pass, and a result without one would lose gradients without a word."""
     x = torch.zeros(10, 2, 64, dtype=torch.float16)
