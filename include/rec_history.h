@@ -283,7 +283,7 @@ REC_API rec_status rec_window_attend(const rec_window *w, void *stream);
  *                  one of heads and kv_heads may be 0, and its rows and weight null
  *   q_out, k_out   the same shapes and type, rows that do not overlap; they may be q and k themselves
  *                  (the same address and strides) and may not overlap them, or each other, otherwise.  Rows that lie between
- *                  another argument's have its token stride and, unless what each has of a token lies apart, its head stride
+ *                  another argument's have its token stride, or one row for all tokens (stride 0)
  *   head_dim       32, 64 or 128
  *   dev_positions  int32 or, wide = 1, int64 [tokens], of either sign
  *   dev_frequencies  double [pairs], radians a position; pairs a multiple of 8, at most head_dim / 2

@@ -152,8 +152,8 @@ struct Place {
 };
 
 // Whether the rows x of a result and those of another argument have no element in common.  `own`: y is what x is made of, so that they may be the
-// same rows: each is read before it is written.  Exact where both lie in address ranges of their own, which is nearly always so, have the same strides, or have
-// their shares of a token beside each other; other rows between each other's count as overlapping.
+// same rows: each is read before it is written.  Rows between each other's of several tokens that are as many, but not as far apart, count as overlapping; so do
+// more than 2^20 pairs of heads that lie between each other.
 bool places_apart(const Place &x, const Place &y, bool own, int64_t tokens, int64_t d, int size)
 {
     typedef __int128 wide;  // products of strides and counts
@@ -168,24 +168,37 @@ bool places_apart(const Place &x, const Place &y, bool own, int64_t tokens, int6
     const Span a = span_of(x, tokens), b = span_of(y, tokens);
     if (a.to <= b.from || b.to <= a.from) return true;
     const bool same_tokens = tokens == 1 || x.r->token_stride == y.r->token_stride;
-    const bool same_heads = (x.heads == 1 && y.heads == 1) || x.r->head_stride == y.r->head_stride;
-    if (own && same_tokens && same_heads && x.r->dev == y.r->dev) return true;
-    if (!same_tokens) return false;
-    const wide by_token = (wide)x.r->token_stride * size, step = by_token < 0 ? -by_token : by_token;  // not 0, of several tokens: rows_apart()
+    if (own && same_tokens && x.r->dev == y.r->dev && (x.heads == 1 || x.r->head_stride == y.r->head_stride)) return true;
+    // One row for all tokens or heads: y's only, as a result's would overlap (rows_apart()).
+    const int64_t y_tokens = y.r->token_stride == 0 ? 1 : tokens, y_heads = y.r->head_stride == 0 ? 1 : y.heads;
+    if (!same_tokens && y_tokens > 1) return false;
+    const wide by_token = (wide)x.r->token_stride * size, step = by_token < 0 ? -by_token : by_token;  // not 0, of several tokens
     if (tokens > 1) {
         // What x and y have of a token, repeated a step further each time.
         const Span p = span_of(x, 1), q = span_of(y, 1);
         const wide ahead = ((q.from - p.from) % step + step) % step;
         if (p.to - p.from <= ahead && ahead + (q.to - q.from) <= step) return true;
     }
-    if (!same_heads) return false;
-    // On the same grid: y's rows are `i` heads and any number of tokens from x's.
-    const wide off = (wide) reinterpret_cast<uintptr_t>(y.r->dev) - (wide) reinterpret_cast<uintptr_t>(x.r->dev), bytes = (wide)d * size;
-    for (int64_t i = 1 - x.heads; i < y.heads; ++i) {
-        wide left = off + i * ((wide)x.r->head_stride * size);
-        if (tokens > 1) left -= std::clamp<wide>((left < 0 ? left - step / 2 : left + step / 2) / step, 1 - tokens, tokens - 1) * step;
-        if (left < bytes && -left < bytes) return false;
+    const wide bytes = (wide)d * size;
+    // Whether a row of y, `at` bytes behind one of x in their first tokens, meets it in others: with y's n tokens behind x's.
+    const auto meet = [&](wide at) {
+        if (tokens > 1) {
+            const wide last = tokens - 1, least = by_token < 0 ? -last : 1 - (wide)y_tokens, most = by_token < 0 ? (wide)y_tokens - 1 : last;
+            at -= std::clamp<wide>((at < 0 ? at - step / 2 : at + step / 2) / step, least, most) * step;
+        }
+        return at < bytes && -at < bytes;
+    };
+    const wide off = (wide) reinterpret_cast<uintptr_t>(y.r->dev) - (wide) reinterpret_cast<uintptr_t>(x.r->dev);
+    const wide x_head = (wide)x.r->head_stride * size, y_head = (wide)y.r->head_stride * size;
+    if (x.heads == 1 || y_heads == 1 || x_head == y_head) {  // the same for heads as far apart
+        for (int64_t i = 1 - x.heads; i < y_heads; ++i)
+            if (meet(off + i * (x.heads == 1 ? y_head : x_head))) return false;
+        return true;
     }
+    if (x.heads * y_heads > 1 << 20) return false;
+    for (int64_t i = 0; i < x.heads; ++i)
+        for (int64_t j = 0; j < y_heads; ++j)
+            if (meet(off + j * y_head - i * x_head)) return false;
     return true;
 }
 

@@ -121,6 +121,17 @@ def places(tokens, heads, kv, d, size):
     yield *by_head, by_head[0], (d, d, tokens * d)
     woven = ((0, 2 * d, 2 * tokens * d), (d, 2 * d, 2 * tokens * d))            # the same, q's tokens between k's
     yield *woven, *woven
+    one = (heads * d, 0, d)                                                     # one token's keys for all, a projection's; one head's for all
+    yield slices[0], one, slices[0], apart[1]
+    yield slices[0], (d, 0, d), slices[0], apart[1]
+    yield slices[0], (row * (tokens - 1) + heads * d, 0, 0), slices[0], apart[1]
+    yield slices[0], (heads * d, row, 0), slices[0], apart[1]
+    yield slices[0], (0, row, 0), slices[0], apart[1]
+    for first in (0, d, 2 * d, 3 * d):                                          # heads two apart, three apart, and towards each other
+        yield *apart, (0, 40 * d, 2 * d), (first, 40 * d, 3 * d)
+        yield *apart, (0, -40 * d, 2 * d), (first, -40 * d, 3 * d)
+        yield *apart, (0, 40 * d, 2 * d), (first + 8 * d, 40 * d, -2 * d)
+        yield *apart, (0, 2 * d, 4 * tokens * d), (first, 2 * d, 6 * tokens * d)
     for shift in (16 // size, d, row, -row, heads * d - 16 // size, row * (tokens - 1), row * tokens, -row * tokens):
         yield slices[0], apart[1], (shift, row, d), (4 * far, kv * d, d)        # a result that lies a little further than q
         yield apart[0], slices[0], (shift, row, d), (5 * far, kv * d, d)
@@ -157,8 +168,11 @@ def test_results_over_other_rows(b, tokens, heads, kv, dtype, size, d):
 def test_results_between_rows_of_other_strides(b):
     """Where that cannot be told from the strides alone, rows between each other's count as overlapping."""
     base = dict(q=dict(dev=PTR), k=dict(dev=PTR + (1 << 24)), k_out=dict(dev=PTR + (1 << 25)))
-    for bad in (dict(dev=PTR, token_stride=512), dict(dev=PTR + 128, token_stride=512, head_stride=128)):
+    for bad in (dict(dev=PTR, token_stride=512), dict(dev=PTR + 128, token_stride=512, head_stride=128), dict(dev=PTR + (1 << 24), token_stride=320)):
         assert call(b, **base, q_out=bad) == b.REC_ERR_ARG, bad
+    # as many pairs of heads as would take long to compare
+    assert call(b, **{**base, "k_out": dict(dev=PTR + (1 << 30), token_stride=1 << 20, head_stride=192)}, heads=1 << 11, kv_heads=1 << 11,
+                q_out=dict(dev=PTR + (1 << 30) + 128, token_stride=1 << 20, head_stride=128)) == b.REC_ERR_ARG
     huge = 1 << 60                      # spans that do not fit 64 bits
     assert call(b, **base, q_out=dict(dev=PTR, token_stride=huge, head_stride=huge >> 3)) == b.REC_ERR_ARG
 
